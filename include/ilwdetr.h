@@ -3,7 +3,8 @@
  *
  * Every entry point computes one integer operator of "Enabling Fully Integer-Only Inference for
  * Lightweight Detection Transformers" exactly (bit for bit) as the paper defines it; the
- * passages are cited beside each declaration.  All arithmetic on the device is integer.
+ * passages are cited beside each declaration.  All arithmetic on the device is integer, but for the
+ * microscaled 4-bit products and the mixture-of-experts routing around them (the last two sections).
  *
  * Conventions (apply to every call unless a declaration says otherwise)
  *   - Pointers to tensors are DEVICE pointers owned by the caller; the library never frees or
@@ -62,7 +63,8 @@ const char *ilwdetr_version(void);
 const char *ilwdetr_last_error(void);
 /* Synchronises `stream`, then reads and clears the device status word of the current device:
  * ILW_OK, ILW_ERR_TIMEOUT if a kernel gave up a bounded wait since the last read, or
- * ILW_ERR_INVALID_ARG if ilwdetr_gather_rows met an index outside its source since then. */
+ * ILW_ERR_INVALID_ARG if ilwdetr_gather_rows, ilwdetr_mx_quantize or ilwdetr_moe_combine met an index
+ * outside its source since then. */
 int ilwdetr_device_status(ilw_stream_t stream);
 
 /* Constrained Shiftmax parameters (Algorithm 2 inputs; Sec. 3.3.2).
@@ -459,6 +461,86 @@ int ilwdetr_gather_rows(const void *src, int64_t src_ld, int64_t src_rows, const
  * row idx[b n + i] of source b, i < n; idx int32 [batches, n]. */
 int ilwdetr_gather_rows_batched(const void *src, int64_t src_ld, int64_t src_rows, const int32_t *idx, int64_t n,
                                 int64_t batches, int64_t row_bytes, void *dst, int64_t dst_ld, ilw_stream_t stream);
+
+/* ------------------------------------------------------------------ microscaled 4-bit (MXFP4) */
+
+/* Linear layers below 8 bits.  These entry points stand beside the paper's integer path, not on it: their arithmetic is
+ * floating point (E2M1 codes with E8M0 block scales, the OCP Microscaling Formats 1.0), which is what the tensor
+ * cores of this chip multiply below 8 bits.
+ *
+ * An MXFP4 matrix [rows, K] is two byte arrays:
+ *   codes   rows of ceil(K / 32) * 16 bytes, two E2M1 codes a byte, the lower nibble first; past K: zero codes
+ *   scales  rows of ceil(K / 32) E8M0 bytes, one for 32 consecutive values: b stands for 2^(b - 127), 255 for NaN
+ * Row strides (bytes) and base addresses of both are multiples of 16; ilwdetr_mx_quantize also zeroes each scale
+ * row up to the next multiple of 16 bytes. */
+
+/* Element forms of the float tensors around them (8: int8). */
+#define ILW_FP32 232
+#define ILW_FP16 216
+#define ILW_BF16 217
+
+/* Rows to MXFP4.  Row i of the result is row gather[i] of X (gather NULL: row i).
+ *   scale byte of a block = clamp(floor(log2 max|x|) - 2, -127, 127) + 127, 0 if all are zero, 255 if any is not finite
+ *   code = x / 2^(b - 127) rounded to the nearest of 0, .5, 1, 1.5, 2, 3, 4, 6 (ties to the even code), saturating
+ * X [x_rows, ldx] in x_form (8, ILW_FP32, ILW_FP16, ILW_BF16), aligned to its elements, ldx >= K; gather int32
+ * [rows] device: -1 gives a row of zeros, any other index outside [0, x_rows) does too and is reported by the next
+ * ilwdetr_device_status.  K >= 1. */
+int ilwdetr_mx_quantize(const void *X, int32_t x_form, int64_t ldx, int64_t x_rows, const int32_t *gather, int64_t rows,
+                        int32_t K, uint8_t *codes, int64_t ldc, uint8_t *scales, int64_t lds, ilw_stream_t stream);
+/* MXFP4 back to values, rounded to y_form (exact in fp32, and in bf16; fp16 overflows to infinity past 65504). */
+int ilwdetr_mx_dequantize(const uint8_t *codes, int64_t ldc, const uint8_t *scales, int64_t lds, int64_t rows, int32_t K,
+                          void *Y, int32_t y_form, int64_t ldy, ilw_stream_t stream);
+
+/* Activations of a product's result z, computed in fp32:
+ *   GELU       z (1 + erf(z / sqrt 2)) / 2
+ *   SILU_GATE  rows 2j and 2j + 1 of W are a gate and what it gates: y[., j] = z[., 2j] / (1 + exp(-z[., 2j])) z[., 2j+1]
+ *              (N even, N / 2 output columns) */
+enum { ILW_ACT_NONE = 0, ILW_ACT_GELU = 1, ILW_ACT_SILU_GATE = 2 };
+
+/* Y = act(A W^T + bias) of MXFP4 matrices A [M, K] and W [N, K], or of the W [experts, N, K] of each group of rows:
+ * row r uses expert e where offsets[e] <= r < offsets[e + 1]; rows of no expert are written as zeros.
+ *   a_ldc, a_lds, w_ldc, w_lds   bytes between rows of codes and scales
+ *   w_codes_stride, w_scales_stride  bytes between experts (multiples of 16; ignored for one expert without offsets)
+ *   bias     fp32 [experts, N] device, or NULL
+ *   offsets  int32 [experts + 1] device, not decreasing, within [0, M]; or NULL (experts = 1: every row).  They are
+ *            read on the device; ones out of order or range give wrong rows but no access outside the tensors
+ *   y_form   ILW_FP32, ILW_FP16, ILW_BF16; Y aligned to its elements, ldy in elements
+ * Products and block scales are exact, sums are fp32, the result is rounded once.  1 <= experts <= 1024, M < 2^31. */
+typedef struct {
+    uint32_t struct_size;
+    const uint8_t *a_codes; int64_t a_ldc;
+    const uint8_t *a_scales; int64_t a_lds;
+    const uint8_t *w_codes; int64_t w_ldc, w_codes_stride;
+    const uint8_t *w_scales; int64_t w_lds, w_scales_stride;
+    const float *bias;
+    const int32_t *offsets;
+    int64_t M;
+    int32_t N, K, experts, act, y_form;
+    void *Y; int64_t ldy;
+} ilw_mx_gemm_t;
+int ilwdetr_mx_gemm(const ilw_mx_gemm_t *p, ilw_stream_t stream);
+
+/* ------------------------------------------------------------------ mixture of experts */
+
+/* Routing of T tokens to k of E experts each (1 <= k <= min(E, 16), E <= 512):
+ *   expert[t, j]  the experts of the k largest logits of row t in decreasing order, equal ones by index; -inf and
+ *                 NaN are never taken: a row with fewer others ends in expert -1, weight 0, slot -1
+ *   weight[t, j]  their softmax: over the row's chosen logits (renormalize != 0) or over all of its logits
+ *   slot[t, j]    the entry's place in the order by expert, and by token within an expert
+ *   offsets[e]    the number of entries of experts before e (offsets[E]: of all)
+ *   source[s]     the token at place s; -1 past the last
+ * logits [T, ld] in `form` (ILW_FP32, ILW_FP16, ILW_BF16).  weight fp32, the rest int32: [T, k], offsets [E + 1], source
+ * [T k].  workspace: ilwdetr_moe_route_workspace_bytes, 4-byte aligned. */
+size_t ilwdetr_moe_route_workspace_bytes(int32_t T, int32_t E);
+int ilwdetr_moe_route(const void *logits, int32_t form, int64_t ld, int32_t T, int32_t E, int32_t k, int32_t renormalize,
+                      int32_t *expert, float *weight, int32_t *offsets, int32_t *source, int32_t *slot, void *workspace,
+                      size_t workspace_bytes, ilw_stream_t stream);
+/* out[t] = (res[t] +) sum_j weight[t, j] Y[slot[t, j]], added in fp32 in the order of j, rounded once.  A slot of -1 adds
+ * nothing; any other outside [0, rows) neither, and is reported by the next ilwdetr_device_status.  Y [rows, ldy], res
+ * [T, ldr] (or NULL) and out [T, ldo] in `form`; out may be res; 1 <= k. */
+int ilwdetr_moe_combine(const void *Y, int32_t form, int64_t ldy, int64_t rows, const int32_t *slot, const float *weight,
+                        int32_t T, int32_t k, int32_t N, const void *res, int64_t ldr, void *out, int64_t ldo,
+                        ilw_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -1,4 +1,4 @@
-"""GB300 (sm_103a) integer-only I-LW-DETR forward path.
+"""GB300 (sm_103a) integer-only I-LW-DETR forward path, and microscaled 4-bit linear layers and experts beside it (mx.py).
 
 Python names mirror the C-ABI of ``include/ilwdetr.h`` (``libilwdetr.so`` in this directory).
 This module only marshals arguments: torch tensors provide device memory and the current CUDA
@@ -18,6 +18,8 @@ __all__ = [
     "requant", "resample_nearest", "DecoderWeights", "decoder_workspace_bytes", "decoder_layer_forward",
     "Projector", "Detector", "int_sigmoid", "requant_sigmoid", "gemm_relu", "relu_i8", "topk", "gather_rows", "gather_rows_batched", "DetectionHead", "TwoStage",
     "QueryPos", "BoxRefine", "ivit_shiftgelu",
+    "MxTensor", "Routing", "mx_empty", "mx_quantize", "mx_dequantize", "mx_linear", "mx_grouped_linear", "moe_route", "moe_combine",
+    "gate_rows", "MxExperts",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -161,6 +163,12 @@ SIGNATURES = {
     "ilwdetr_decoder_workspace_bytes": ([_I32, _I32, _I64, _I32, _I32, _I32, _I32, _I32], C.c_size_t),
     "ilwdetr_decoder_layer_forward": ([C.POINTER(DecoderParamsT), _VP, _VP, _VP, C.POINTER(_I32), _I32, _VP,
                                        _I32, _I32, _VP, _VP, C.c_size_t, _VP], C.c_int),
+    "ilwdetr_mx_quantize": ([_VP, _I32, _I64, _I64, _VP, _I64, _I32, _VP, _I64, _VP, _I64, _VP], C.c_int),
+    "ilwdetr_mx_dequantize": ([_VP, _I64, _VP, _I64, _I64, _I32, _VP, _I32, _I64, _VP], C.c_int),
+    "ilwdetr_mx_gemm": ([_VP, _VP], C.c_int),
+    "ilwdetr_moe_route_workspace_bytes": ([_I32, _I32], C.c_size_t),
+    "ilwdetr_moe_route": ([_VP, _I32, _I64, _I32, _I32, _I32, _I32, _VP, _VP, _VP, _VP, _VP, _VP, C.c_size_t, _VP], C.c_int),
+    "ilwdetr_moe_combine": ([_VP, _I32, _I64, _I64, _VP, _VP, _I32, _I32, _I32, _VP, _I64, _VP, _I64, _VP], C.c_int),
 }
 
 
@@ -941,3 +949,9 @@ def ivit_shiftgelu(X, gelu: dict, out=None):
     _check(lib().ilwdetr_ivit_shiftgelu(_ptr(X), X.stride(0), rows, L, _ptr(out), out.stride(0), C.byref(g), _stream()),
            "ivit_shiftgelu")
     return out
+
+
+# the microscaled 4-bit and mixture-of-experts operators (they use the helpers above)
+from .mx import (  # noqa: E402
+    MxExperts, MxTensor, Routing, gate_rows, moe_combine, moe_route, mx_dequantize, mx_empty, mx_grouped_linear, mx_linear, mx_quantize,
+)

@@ -1,0 +1,472 @@
+"""Microscaled 4-bit and mixture-of-experts operators on the GPU against plain restatements in 64 bits.
+
+Quantisation, its inverse, expert choice and order are exact.  Products: every code product and block scale is exact and
+sums are fp32, so whatever the order and even if each addition truncates, |error| <= (K + 8) 2^-23 sum_k |a_k w_k| before
+the activation; the activations here have a slope of at most 1.13 (GELU) and take at most 8 further roundings, and the
+output is rounded once to its type."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+EPS = {torch.float32: 2.0**-24, torch.float16: 2.0**-11, torch.bfloat16: 2.0**-8}  # half an ulp, relative
+LEVELS = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6])
+
+
+@pytest.fixture(scope="module")
+def ilw():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    import paper_2607_24981_gb300 as m
+    from paper_2607_24981_gb300 import build
+
+    build.build()
+    m.lib()
+    return m
+
+
+# ---------------------------------------------------------------------------- restatements
+def ref_quantize(x):
+    """Codes [R, blocks * 32] and scale bytes [R, blocks] of float64 x [R, K]."""
+    R, K = x.shape
+    nb = -(-K // 32)
+    v = np.zeros((R, nb * 32))
+    v[:, :K] = x
+    neg = np.zeros(v.shape, bool)
+    neg[:, :K] = np.signbit(x)
+    v = v.reshape(R, nb, 32)
+    amax = np.abs(v).max(2)
+    byte = np.full(amax.shape, 255)
+    fine = np.isfinite(amax)
+    exponent = np.frexp(np.where(fine, amax, 1))[1] - 1
+    byte[fine] = (np.clip(exponent - 2, -127, 127) + 127)[fine]
+    byte[amax == 0] = 0
+    with np.errstate(invalid="ignore"):
+        y = np.abs(v) / np.ldexp(1.0, byte - 127)[:, :, None]
+    d = np.abs(np.minimum(np.where(np.isfinite(y), y, 0), 6.0)[..., None] - LEVELS)
+    d[..., 1::2] += 1e-9  # ties go to the even code (no distance of these inputs is within 1e-9 of another but a tie)
+    code = d.argmin(-1).reshape(R, -1) + 8 * neg
+    code[np.repeat(byte == 255, 32, axis=1)] = 0
+    return code, byte
+
+
+def ref_values(codes, scales, k):
+    """Float64 values of uint8 codes [.., R, 16 nb] and scales (numpy)."""
+    nib = np.stack([codes & 15, codes >> 4], -1).reshape(*codes.shape[:-1], -1)
+    v = LEVELS[nib & 7] * np.where(nib & 8, -1.0, 1.0)
+    s = np.ldexp(1.0, scales.astype(np.int64) - 127)
+    s[scales == 255] = np.nan
+    return (v * np.repeat(s, 32, axis=-1)[..., : v.shape[-1]])[..., :k]
+
+
+def ref_act(z, act):
+    from math import erf
+
+    if act == "gelu":
+        return 0.5 * z * (1 + np.vectorize(erf)(z / np.sqrt(2)))
+    if act == "silu_gate":
+        g, u = z[:, 0::2], z[:, 1::2]
+        return g / (1 + np.exp(-g)) * u
+    return z
+
+
+def host(m):
+    return m.codes.cpu().numpy(), m.scales.cpu().numpy()
+
+
+def packed(ilw, x):
+    """x float64 numpy [.., R, K] as an MxTensor made on the host."""
+    R, K = x.shape[-2:]
+    code, byte = ref_quantize(x.reshape(-1, K))
+    nb = byte.shape[1]
+    codes = (code[:, 0::2] | code[:, 1::2] << 4).astype(np.uint8)
+    scales = np.full((codes.shape[0], -(-nb // 16) * 16), 255, np.uint8)  # bytes past the row's blocks are not read
+    scales[:, :nb] = byte
+    lead = x.shape[:-1]
+    return ilw.MxTensor(torch.from_numpy(codes.reshape(*lead, -1)).cuda(), torch.from_numpy(scales.reshape(*lead, -1)).cuda(), K)
+
+
+def check_product(got, a, w, bias, act, dtype):
+    """got [M, n] against the 64-bit product of values a [M, K], w [N, K]; the bound of the module's docstring."""
+    z, mass = a @ w.T, np.abs(a) @ np.abs(w).T
+    if bias is not None:
+        z, mass = z + bias, mass + np.abs(bias)
+    tol = (a.shape[1] + 8) * 2.0**-23 * mass
+    want = ref_act(z, act)
+    if act == "silu_gate":
+        g, u = z[:, 0::2], z[:, 1::2]
+        s = 1 / (1 + np.exp(-g))
+        tol = 1.1 * tol[:, 0::2] * (np.abs(u) + tol[:, 1::2]) + np.abs(g * s) * tol[:, 1::2] + 8 * 2.0**-24 * np.abs(want)
+    elif act == "gelu":
+        tol = 1.13 * tol + 8 * 2.0**-24 * np.abs(z)
+    tol = tol + EPS[dtype] * (np.abs(want) + tol) + (2.0**-25 if dtype == torch.float16 else 0.0)  # (a subnormal's half ulp)
+    err = np.abs(got.double().cpu().numpy() - want)
+    assert got.dtype == dtype and got.shape == want.shape
+    assert (err <= tol).all(), f"{(err > tol).sum()} of {err.size} outside, worst {np.max(err / tol):.3g} times the bound"
+
+
+def values(rng, R, K):
+    """Rows of very different sizes, a few of them zero."""
+    x = rng.standard_normal((R, K)) * np.exp2(rng.integers(-6, 7, (R, 1)))
+    x[rng.random(R) < 0.1] = 0
+    return x
+
+
+# ---------------------------------------------------------------------------- quantisation
+FORMS = [torch.float32, torch.float16, torch.bfloat16, torch.int8]
+
+
+@pytest.mark.parametrize("dtype", FORMS)
+@pytest.mark.parametrize("R,K", [(1, 1), (3, 31), (2, 32), (5, 33), (4, 264), (7, 257), (2, 2051), (130, 520)])
+def test_quantize_matches_64_bits(ilw, dtype, R, K):
+    rng = np.random.default_rng(R * 1000 + K)
+    x = torch.from_numpy(values(rng, R, K) * 4).clamp(-127, 127)
+    x = (x.round() if dtype == torch.int8 else x).to(dtype).cuda()
+    m = ilw.mx_quantize(x)
+    code, byte = ref_quantize(x.double().cpu().numpy())
+    codes, scales = host(m)
+    assert (codes == (code[:, 0::2] | code[:, 1::2] << 4)).all()
+    assert (scales[:, : byte.shape[1]] == byte).all() and (scales[:, byte.shape[1]:] == 0).all()
+    for out in (torch.float32, torch.float16, torch.bfloat16):
+        want = torch.from_numpy(ref_values(codes, scales, K)).to(out).cuda()
+        assert torch.equal(ilw.mx_dequantize(m, out), want)
+
+
+def test_quantize_special_values(ilw):
+    """Ties, powers of two, subnormals, the largest values, signed zeros, infinities and NaN."""
+    rows = [np.zeros(64), np.full(64, -0.0), np.tile(LEVELS, 8), np.tile([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 7.0], 8),
+            -np.tile([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0], 8) * 2.0**-40, np.full(64, 3.4028234e38), np.full(64, 2.0**-149),
+            np.exp2(np.arange(64) - 140.0), np.exp2(-np.arange(64.0)), np.r_[np.inf, np.ones(63)], np.r_[np.ones(40), np.nan, np.ones(23)],
+            np.r_[np.full(32, -np.inf), np.ones(32)], np.full(64, 2.0**-126), np.full(64, 1.5 * 2.0**-127)]
+    x = torch.from_numpy(np.stack(rows)).float()
+    m = ilw.mx_quantize(x.cuda())
+    code, byte = ref_quantize(x.double().numpy())
+    codes, scales = host(m)
+    assert (scales[:, :2] == byte).all()
+    assert (codes == (code[:, 0::2] | code[:, 1::2] << 4)).all()
+    back = ilw.mx_dequantize(m).cpu().numpy()
+    assert np.isnan(back[9, :32]).all() and np.isfinite(back[9, 32:]).all() and np.isnan(back[10, 32:]).all()
+    assert np.array_equal(back, ref_values(codes, scales, 64).astype(np.float32), equal_nan=True)
+
+
+def test_quantize_gathers_rows(ilw):
+    rng = np.random.default_rng(3)
+    x = torch.from_numpy(values(rng, 50, 300)).float().cuda()
+    at = torch.from_numpy(rng.integers(-1, 50, 77).astype(np.int32)).cuda()
+    m, whole = ilw.mx_quantize(x, gather=at), ilw.mx_quantize(x)
+    rows = at.long()
+    assert torch.equal(m.codes, torch.where(rows[:, None] < 0, 0, whole.codes[rows]))
+    assert torch.equal(m.scales, torch.where(rows[:, None] < 0, 0, whole.scales[rows]))
+    ilw.device_status()
+    bad = torch.tensor([0, 50, -2, 49], dtype=torch.int32, device="cuda")
+    m = ilw.mx_quantize(x, gather=bad)
+    assert (m.codes[1:3] == 0).all() and (m.scales[1:3] == 0).all() and torch.equal(m.codes[3], whole.codes[49])
+    with pytest.raises(ilw.IlwError, match="index"):
+        ilw.device_status()
+    ilw.device_status()
+
+
+@pytest.mark.parametrize("dtype", FORMS)
+def test_quantize_rows_with_strides_and_offsets(ilw, dtype):
+    """Rows inside a wider tensor, starting off 16-byte boundaries; results into rows of a wider one, the rest untouched."""
+    rng = np.random.default_rng(4)
+    wide = torch.from_numpy(np.clip(values(rng, 9, 200), -127, 127)).to(dtype).cuda()
+    for lo, hi in ((3, 100), (16, 112), (1, 2)):
+        x = wide[:, lo:hi]
+        want = ilw.mx_quantize(x.contiguous())
+        assert all(torch.equal(p, q) for p, q in zip(ilw.mx_quantize(x)[:2], want[:2]))
+        n, s = want.codes.shape[1], want.scales.shape[1]
+        codes = torch.full((9, n + 32), 77, dtype=torch.uint8, device="cuda")
+        scales = torch.full((9, s + 16), 77, dtype=torch.uint8, device="cuda")
+        out = ilw.MxTensor(codes[:, 16: 16 + n], scales[:, :s], hi - lo)
+        ilw.mx_quantize(x, out=out)
+        assert torch.equal(out.codes, want.codes) and torch.equal(out.scales, want.scales)
+        assert (codes[:, :16] == 77).all() and (codes[:, 16 + n:] == 77).all() and (scales[:, s:] == 77).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+def test_dequantize_every_code_and_scale(ilw, dtype):
+    codes = np.tile(np.arange(256, dtype=np.uint8), (256, 1))
+    scales = np.tile(np.arange(256, dtype=np.uint8)[:, None], (1, 16))
+    m = ilw.MxTensor(torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda(), 512)
+    want = torch.from_numpy(ref_values(codes, scales, 512)).float().to(dtype)
+    got = ilw.mx_dequantize(m, dtype).cpu()
+    assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got[~got.isnan()], want[~want.isnan()])
+    out = torch.full((256, 520), 7.0, dtype=dtype, device="cuda")
+    for lo, k in ((1, 511), (8, 512), (0, 1)):  # rows off 16-byte boundaries, and odd widths
+        part = ilw.mx_dequantize(ilw.MxTensor(m.codes, m.scales, k), out=out[:, lo: lo + k]).cpu()
+        assert torch.equal(part.nan_to_num(3.0), want[:, :k].nan_to_num(3.0))
+        assert (out[:, :lo] == 7).all() and (out[:, lo + k:] == 7).all()
+        out.fill_(7)
+
+
+# ---------------------------------------------------------------------------- products
+@pytest.mark.parametrize("act,bias", [("none", False), ("none", True), ("gelu", True), ("silu_gate", False), ("silu_gate", True)])
+@pytest.mark.parametrize("M,N,K", [(1, 2, 1), (1, 128, 4096), (3, 130, 512), (16, 300, 33), (17, 128, 250), (33, 1000, 2048),
+                                   (224, 256, 768), (225, 126, 1100), (700, 514, 96)])
+def test_linear_matches_64_bits(ilw, M, N, K, act, bias):
+    rng = np.random.default_rng(M * 7 + N * 3 + K)
+    A, W = packed(ilw, values(rng, M, K)), packed(ilw, rng.standard_normal((N, K)) / np.sqrt(K))
+    b = rng.standard_normal(N).astype(np.float32) if bias else None
+    a, w = ref_values(*host(A), K), ref_values(*host(W), K)
+    for dtype in (torch.float32, torch.bfloat16):
+        got = ilw.mx_linear(A, W, None if b is None else torch.from_numpy(b).cuda(), act=act, out_dtype=dtype)
+        check_product(got, a, w, b, act, dtype)
+    ilw.device_status()
+
+
+@pytest.mark.parametrize("splits,K", [(2, 1024), (4, 2048 + 32), (8, 8192 + 300)])
+def test_linear_of_few_tiles(ilw, splits, K):
+    """One to three tiles, whose K is shared by several CTAs: the same bound, and the same bits on every run."""
+    rng = np.random.default_rng(K)
+    for M, N in ((1, 128), (5, 300), (200, 64)):
+        A, W = packed(ilw, values(rng, M, K)), packed(ilw, rng.standard_normal((N, K)) / np.sqrt(K))
+        a, w = ref_values(*host(A), K), ref_values(*host(W), K)
+        got = ilw.mx_linear(A, W, out_dtype=torch.float32)
+        check_product(got, a, w, None, "none", torch.float32)
+        assert all(torch.equal(got, ilw.mx_linear(A, W, out_dtype=torch.float32)) for _ in range(5))
+
+
+def test_linear_rows_with_strides(ilw):
+    """Operands inside wider byte arrays, a result inside a wider tensor, fp16."""
+    rng = np.random.default_rng(11)
+    M, N, K = 70, 90, 200
+    A, W = packed(ilw, values(rng, M, K)), packed(ilw, rng.standard_normal((N, K)) / np.sqrt(K))
+    want = ilw.mx_linear(A, W, out_dtype=torch.float16)
+    check_product(want, ref_values(*host(A), K), ref_values(*host(W), K), None, "none", torch.float16)
+
+    def spread(m):
+        c = torch.full((m.codes.shape[0], m.codes.shape[1] + 48), 0x77, dtype=torch.uint8, device="cuda")
+        s = torch.full((m.scales.shape[0], 64), 255, dtype=torch.uint8, device="cuda")
+        c[:, 32: 32 + m.codes.shape[1]] = m.codes
+        s[:, 16: 16 + m.scales.shape[1]] = m.scales
+        return ilw.MxTensor(c[:, 32: 32 + m.codes.shape[1]], s[:, 16: 16 + m.scales.shape[1]], m.k)
+
+    out = torch.full((M, N + 9), 5.0, dtype=torch.float16, device="cuda")
+    ilw.mx_linear(spread(A), spread(W), out=out[:, 3: 3 + N])
+    assert torch.equal(out[:, 3: 3 + N], want) and (out[:, :3] == 5).all() and (out[:, 3 + N:] == 5).all()
+
+
+def test_linear_scales_and_nan(ilw):
+    """Block scales far from one (their product near it), and NaN blocks: only their rows and columns are NaN."""
+    rng = np.random.default_rng(12)
+    M, N, K = 40, 140, 320
+    A, W = packed(ilw, values(rng, M, K)), packed(ilw, rng.standard_normal((N, K)))
+    A.scales[:, :10] += 100
+    W.scales[:, :10] -= 100
+    got = ilw.mx_linear(A, W, out_dtype=torch.float32)
+    check_product(got, ref_values(*host(A), K), ref_values(*host(W), K), None, "none", torch.float32)
+    A.scales[7, 3], W.scales[133, 9] = 255, 255
+    bad = ilw.mx_linear(A, W, out_dtype=torch.float32)
+    nan = torch.zeros(M, N, dtype=torch.bool, device="cuda")
+    nan[7], nan[:, 133] = True, True
+    assert torch.equal(bad.isnan(), nan) and torch.equal(bad[~nan], got[~nan])
+
+
+GROUPS = {
+    "one row each": [1] * 7, "empty ones": [0, 5, 0, 0, 33, 0], "one takes all": [0, 0, 300, 0], "odd": [17, 226, 1, 449, 15],
+    "none": [0, 0, 0], "many": [(7 * i) % 5 for i in range(200)],
+}
+
+
+@pytest.mark.parametrize("counts", GROUPS.values(), ids=GROUPS.keys())
+@pytest.mark.parametrize("N,K,act", [(130, 100, "none"), (256, 1536, "silu_gate"), (66, 544, "gelu")])
+def test_grouped_matches_64_bits(ilw, counts, N, K, act):
+    """Ragged groups between rows of no expert (before the first and after the last), which come out zero."""
+    rng = np.random.default_rng(N + K + len(counts))
+    E, head, tail = len(counts), 3, 5
+    off = head + np.r_[0, np.cumsum(counts)]
+    M = int(off[-1]) + tail
+    A, W = packed(ilw, values(rng, M, K)), packed(ilw, rng.standard_normal((E, N, K)) / np.sqrt(K))
+    b = rng.standard_normal((E, N)).astype(np.float32)
+    a, w = ref_values(*host(A), K), ref_values(*host(W), K)
+    for dtype in (torch.float32, torch.bfloat16):
+        got = ilw.mx_grouped_linear(A, W, torch.from_numpy(off.astype(np.int32)).cuda(), torch.from_numpy(b).cuda(), act=act, out_dtype=dtype)
+        assert (got[:head] == 0).all() and (got[off[-1]:] == 0).all()
+        for e in range(E):
+            if counts[e]:
+                check_product(got[off[e]: off[e + 1]], a[off[e]: off[e + 1]], w[e], b[e], act, dtype)
+    ilw.device_status()
+
+
+def test_grouped_survives_bad_offsets(ilw):
+    """Offsets out of order and range: no access outside the tensors (rows come out wrong, as documented), no error."""
+    rng = np.random.default_rng(5)
+    A, W = packed(ilw, values(rng, 64, 96)), packed(ilw, rng.standard_normal((4, 40, 96)))
+    for off in ([0, 1 << 30, 5, -7, 64], [-5, 70, 80, 90, 1 << 31 - 1], [60, 50, 40, 30, 20]):
+        out = torch.full((66, 40), 9.0, device="cuda")
+        ilw.mx_grouped_linear(A, W, torch.tensor(off, dtype=torch.int64).clamp(-(1 << 31), (1 << 31) - 1).int().cuda(), out=out[1:65])
+        torch.cuda.synchronize()
+        assert (out[0] == 9).all() and (out[65] == 9).all()
+    ilw.device_status()
+
+
+def test_products_follow_their_stream_and_graphs(ilw):
+    """A chain on a side stream, and the same chain replayed from a graph on new inputs."""
+    rng = np.random.default_rng(6)
+    W = packed(ilw, rng.standard_normal((200, 256)) / 16)
+    x = torch.from_numpy(rng.standard_normal((50, 256))).float().cuda()
+    want = ilw.mx_linear(ilw.mx_quantize(x), W)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = ilw.mx_linear(ilw.mx_quantize(x), W)
+    side.synchronize()
+    assert torch.equal(got, want)
+    g = ilw.Graphed(lambda: ilw.mx_linear(ilw.mx_quantize(x), W))
+    x.mul_(-3)
+    want = ilw.mx_linear(ilw.mx_quantize(x), W)
+    assert torch.equal(g.replay(), want)
+
+
+def test_product_gives_up_a_bounded_wait(ilw):
+    """A load that never comes: the kernel latches the status and returns, and the next call is right."""
+    rng = np.random.default_rng(7)
+    A, W = packed(ilw, values(rng, 300, 2048)), packed(ilw, rng.standard_normal((256, 2048)) / 45)
+    few = ilw.MxTensor(A.codes[:4], A.scales[:4], A.k)
+    want, want_few = ilw.mx_linear(A, W), ilw.mx_linear(few, W)
+    short = packed(ilw, values(rng, 300, 512)), packed(ilw, rng.standard_normal((256, 512)) / 22)
+    cases = ((A, W, want), (few, W, want_few), (*short, ilw.mx_linear(*short)))  # clusters on a tile, and one CTA (K = 512)
+    for m, W, w in cases:
+        assert ilw.lib().ilwdetr_debug_gemm_wait(1, 20_000_000) == 0  # (each CTA's second load)
+        try:
+            ilw.mx_linear(m, W)
+            with pytest.raises(ilw.IlwError, match="wait"):
+                ilw.device_status()
+        finally:
+            assert ilw.lib().ilwdetr_debug_gemm_wait(-1, 0) == 0
+        assert torch.equal(ilw.mx_linear(m, W), w)
+        ilw.device_status()
+
+
+# ---------------------------------------------------------------------------- routing and combination
+def ref_route(x, k, renormalize):
+    """float64 x [T, E] -> expert, weight, offsets, source, slot."""
+    T, E = x.shape
+    x = np.where(np.isnan(x), -np.inf, x)
+    expert, weight = np.full((T, k), -1), np.zeros((T, k))
+    for t in range(T):
+        order = np.argsort(-x[t], kind="stable")[:k]
+        order = order[x[t, order] > -np.inf]
+        if not len(order):
+            continue
+        p = np.exp(x[t] - x[t].max())
+        expert[t, : len(order)] = order
+        weight[t, : len(order)] = p[order] / (p[order].sum() if renormalize else p.sum())
+    entries = sorted((expert[t, j], t, j) for t in range(T) for j in range(k) if expert[t, j] >= 0)
+    offsets = np.searchsorted([e for e, _, _ in entries], np.arange(E + 1))
+    source, slot = np.full(T * k, -1), np.full((T, k), -1)
+    for s, (_, t, j) in enumerate(entries):
+        source[s], slot[t, j] = t, s
+    return expert, weight, offsets, source, slot
+
+
+@pytest.mark.parametrize("renormalize", [True, False])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("T,E,k", [(1, 1, 1), (1, 8, 2), (7, 33, 4), (33, 64, 8), (300, 129, 6), (1000, 512, 16), (5000, 16, 1), (40000, 5, 2)])
+def test_route_matches_64_bits(ilw, T, E, k, dtype, renormalize):
+    """Many equal logits (a coarse grid), masked experts, whole rows masked, NaN."""
+    rng = np.random.default_rng(T + E + k)
+    x = np.round(rng.standard_normal((T, E)) * 4) / 4
+    x[rng.random((T, E)) < 0.1] = -np.inf
+    x[rng.random((T, E)) < 0.02] = np.nan
+    x[rng.random(T) < 0.1] = -np.inf
+    wide = torch.from_numpy(np.pad(x, ((0, 0), (1, 2)))).to(dtype).cuda()
+    r = ilw.moe_route(wide[:, 1: 1 + E], k, renormalize)
+    expert, weight, offsets, source, slot = ref_route(x, k, renormalize)
+    for got, want in ((r.expert, expert), (r.offsets, offsets), (r.source, source), (r.slot, slot)):
+        assert np.array_equal(got.cpu().numpy(), want)
+    # exp's arguments are exact (a quarter grid); a sum of at most 512 terms and a quotient of fp32 exponentials of 2 ulp
+    assert (np.abs(r.weight.double().cpu().numpy() - weight) <= (E + 8) * 2.0**-23 * weight).all()
+
+
+def test_route_extremes(ilw):
+    big = float(np.float32(3.4028234e38))
+    x = torch.tensor([[big, -big, 0.0, -0.0], [-big, -big, -big, float("-inf")], [0.0, -0.0, -0.0, 0.0], [float("nan")] * 4,
+                      [float("inf"), 1.0, 2.0, 3.0]])
+    r = ilw.moe_route(x.cuda(), 3)
+    assert r.expert.tolist() == [[0, 2, 3], [0, 1, 2], [0, 1, 2], [-1, -1, -1], [0, 3, 2]]
+    w = r.weight.cpu()
+    assert w[0].tolist() == [1, 0, 0] and torch.allclose(w[1:3], torch.full((2, 3), 1 / 3)) and (w[3] == 0).all() and w[4].isnan().all()
+    empty = ilw.moe_route(torch.empty((0, 6), device="cuda"), 2)
+    assert empty.offsets.tolist() == [0] * 7 and empty.expert.shape == (0, 2)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("T,k,N", [(1, 1, 1), (5, 2, 33), (64, 8, 256), (300, 3, 1000), (17, 16, 40)])
+@pytest.mark.parametrize("residual", [False, True])
+def test_combine_matches_64_bits(ilw, T, k, N, dtype, residual):
+    rng = np.random.default_rng(T + k + N)
+    R = T * k + 3
+    Y = torch.from_numpy(rng.standard_normal((R, N + 8))).to(dtype).cuda()[:, 8:]
+    Y[T * k:] = float("nan")  # rows that no slot names
+    slot = rng.permutation(T * k).reshape(T, k).astype(np.int32)
+    slot[rng.random((T, k)) < 0.2] = -1
+    w = rng.random((T, k)).astype(np.float32)
+    res = torch.from_numpy(rng.standard_normal((T, N))).to(dtype).cuda() if residual else None
+    got = ilw.moe_combine(Y, torch.from_numpy(slot).cuda(), torch.from_numpy(w).cuda(), residual=res)
+    y = np.where(slot[..., None] < 0, 0, Y.double().cpu().numpy()[slot]) * w[..., None]
+    want, mass = y.sum(1), np.abs(y).sum(1)
+    if residual:
+        want, mass = want + res.double().cpu().numpy(), mass + np.abs(res.double().cpu().numpy())
+    tol = (k + 1) * 2.0**-24 * mass + EPS[dtype] * (np.abs(want) + (k + 1) * 2.0**-24 * mass) + (2.0**-25 if dtype == torch.float16 else 0)
+    assert got.dtype == dtype and (np.abs(got.double().cpu().numpy() - want) <= tol).all()
+    if residual:
+        ilw.moe_combine(Y, torch.from_numpy(slot).cuda(), torch.from_numpy(w).cuda(), residual=res, out=res)
+        assert torch.equal(res, got)
+
+
+def test_combine_reports_a_bad_slot(ilw):
+    Y = torch.ones((4, 8), device="cuda")
+    out = ilw.moe_combine(Y, torch.tensor([[0, 4], [-2, 1]], dtype=torch.int32, device="cuda"), torch.ones((2, 2), device="cuda"))
+    assert (out == 1).all()
+    with pytest.raises(ilw.IlwError, match="index"):
+        ilw.device_status()
+
+
+# ---------------------------------------------------------------------------- the feed-forward
+@pytest.mark.parametrize("act,dtype", [("silu_gate", torch.bfloat16), ("gelu", torch.float32), ("silu_gate", torch.float16)])
+@pytest.mark.parametrize("T", [0, 1, 37, 600])
+def test_experts_feed_forward(ilw, T, act, dtype):
+    """Each step against 64 bits on what the step before it gave (a rounding that falls the other way before the second
+    quantisation would otherwise be a whole code)."""
+    rng = np.random.default_rng(T)
+    E, d, F, top = 6, 192, 320, 2
+    F1 = 2 * F if act == "silu_gate" else F
+    w1 = torch.from_numpy(rng.standard_normal((E, F1, d)) / np.sqrt(d)).float().cuda()
+    w2 = torch.from_numpy(rng.standard_normal((E, d, F)) / np.sqrt(F)).float().cuda()
+    if act == "silu_gate":
+        assert torch.equal(ilw.gate_rows(w1[:, :F], w1[:, F:])[:, 1::2], w1[:, F:])
+        w1 = ilw.gate_rows(w1[:, :F], w1[:, F:])
+    b1 = torch.from_numpy(0.1 * rng.standard_normal((E, F1))).float().cuda()
+    ffn = ilw.MxExperts(w1, w2, top, act=act, b1=b1)
+    x = torch.from_numpy(rng.standard_normal((T, d))).to(dtype).cuda()
+    logits = torch.from_numpy(rng.standard_normal((T, E))).to(dtype).cuda()
+    logits[T // 2:, 1:] = float("-inf")  # half of the tokens have one expert left
+    got = ffn.forward(x, logits, residual=x)
+    assert got.dtype == dtype and got.shape == (T, d)
+    if not T:
+        return
+    r = ilw.moe_route(logits, top)
+    expert, weight, offsets, source, slot = ref_route(logits.double().cpu().numpy(), top, True)
+    assert np.array_equal(r.source.cpu().numpy(), source) and np.array_equal(r.offsets.cpu().numpy(), offsets)
+    a = ilw.mx_quantize(x, gather=r.source)
+    h = ilw.mx_grouped_linear(a, ffn.w1, r.offsets, bias=b1, act=act, out_dtype=dtype)
+    q = ilw.mx_quantize(h)
+    y = ilw.mx_grouped_linear(q, ffn.w2, r.offsets, out_dtype=dtype)
+    av, qv = ref_values(*host(a), d), ref_values(*host(q), F)
+    w1v, w2v = ref_values(*host(ffn.w1), d), ref_values(*host(ffn.w2), F)
+    xv = np.where(source[:, None] < 0, 0, x.double().cpu().numpy()[source])
+    assert np.array_equal(av, ref_values(*[p.astype(np.uint8) for p in _bytes(*ref_quantize(xv))], d))
+    for e in range(E):
+        s = slice(int(offsets[e]), int(offsets[e + 1]))
+        if s.stop > s.start:
+            check_product(h[s], av[s], w1v[e], b1[e].double().cpu().numpy(), act, dtype)
+            check_product(y[s], qv[s], w2v[e], None, "none", dtype)
+    assert torch.equal(got, ilw.moe_combine(y, r.slot, r.weight, residual=x))
+    ilw.device_status()
+
+
+def _bytes(code, byte):
+    return code[:, 0::2] | code[:, 1::2] << 4, byte

@@ -1,0 +1,138 @@
+"""Argument checks of the microscaled 4-bit and mixture-of-experts entry points: validate-only mode, so no kernel runs
+and the addresses are never used."""
+import ctypes
+
+import pytest
+
+V = ctypes.c_void_p(0x100000)
+
+
+@pytest.fixture
+def L():
+    from paper_2607_24981_gb300 import build
+
+    build.build()
+    import paper_2607_24981_gb300 as ilw
+
+    lib = ilw.lib()
+    assert lib.ilwdetr_validate_only(1) == 0
+    yield lib
+    lib.ilwdetr_validate_only(0)
+
+
+def refused(L, rc, code, text):
+    assert rc == code and text in L.ilwdetr_last_error(), (rc, L.ilwdetr_last_error())
+
+
+def test_quantize_checks(L):
+    def q(X=V, form=232, ldx=100, x_rows=8, gather=None, rows=8, K=100, codes=V, ldc=64, scales=V, lds=16):
+        return L.ilwdetr_mx_quantize(X, form, ldx, x_rows, gather, rows, K, codes, ldc, scales, lds, None)
+
+    assert q() == 0 and q(form=8) == 0 and q(form=216) == 0 and q(form=217, gather=V, rows=50) == 0
+    assert q(rows=0, X=None, codes=None, scales=None) == 0
+    assert q(X=None, x_rows=0, gather=V) == 0  # every index is then outside: rows of zeros
+    refused(L, q(form=16), -1, b"x_form")
+    refused(L, q(K=0), -1, b"sizes")
+    refused(L, q(ldx=99), -1, b"sizes")
+    refused(L, q(rows=9), -1, b"sizes")  # more rows than X has, without a gather
+    refused(L, q(X=None), -1, b"NULL")
+    refused(L, q(X=ctypes.c_void_p(0x100002)), -1, b"misaligned")
+    refused(L, q(codes=ctypes.c_void_p(0x100008)), -1, b"codes")
+    refused(L, q(ldc=48), -1, b"codes")
+    refused(L, q(ldc=72), -1, b"codes")
+    refused(L, q(lds=8), -1, b"scales")
+    refused(L, q(scales=None), -1, b"scales")
+
+
+def test_dequantize_checks(L):
+    def d(codes=V, ldc=64, scales=V, lds=16, rows=8, K=100, Y=V, form=217, ldy=100):
+        return L.ilwdetr_mx_dequantize(codes, ldc, scales, lds, rows, K, Y, form, ldy, None)
+
+    assert d() == 0 and d(rows=0, codes=None, scales=None, Y=None) == 0
+    refused(L, d(form=8), -1, b"y_form")
+    refused(L, d(ldy=99), -1, b"sizes")
+    refused(L, d(Y=ctypes.c_void_p(0x100001)), -1, b"misaligned")
+    refused(L, d(lds=0), -1, b"scales")
+    refused(L, d(rows=-1), -1, b"sizes")
+
+
+def test_gemm_checks(L):
+    from paper_2607_24981_gb300 import mx
+
+    def g(**over):
+        p = mx.MxGemmT(ctypes.sizeof(mx.MxGemmT), 0x100000, 128, 0x200000, 16, 0x300000, 128, 128 * 64, 0x400000, 16, 16 * 64, None, None,
+                       300, 64, 256, 1, 0, 217, 0x500000, 64)
+        for k, v in over.items():
+            setattr(p, k, v)
+        return L.ilwdetr_mx_gemm(ctypes.byref(p), None)
+
+    assert g() == 0 and g(M=0, Y=None, a_codes=None) == 0 and g(N=0) == 0
+    assert g(offsets=0x600000, experts=5, bias=0x700000) == 0
+    assert g(act=2, ldy=32) == 0  # a gated result has half the columns
+    refused(L, g(struct_size=8), -1, b"struct_size")
+    refused(L, L.ilwdetr_mx_gemm(None, None), -1, b"struct_size")
+    refused(L, g(act=3), -1, b"act")
+    refused(L, g(y_form=8), -1, b"y_form")
+    refused(L, g(K=0), -1, b"sizes")
+    refused(L, g(experts=2), -1, b"sizes")  # several experts need offsets
+    refused(L, g(act=2, N=63), -1, b"even")
+    refused(L, g(offsets=0x600000, experts=1025), -2, b"experts")
+    refused(L, g(K=(1 << 24) + 1), -2, b"2^24")
+    refused(L, g(M=(1 << 31) - 2048, N=1 << 20, ldy=1 << 20), -2, b"too large")
+    refused(L, g(a_codes=0x100008), -1, b"a_codes")
+    refused(L, g(a_ldc=112), -1, b"a_codes")
+    refused(L, g(w_scales=None), -1, b"w_scales")
+    refused(L, g(w_lds=24), -1, b"w_scales")
+    refused(L, g(offsets=0x600000, experts=5, w_codes_stride=0), -1, b"strides")
+    refused(L, g(offsets=0x600000, experts=5, w_scales_stride=1032), -1, b"strides")
+    refused(L, g(offsets=0x600002, experts=5), -1, b"misaligned")
+    refused(L, g(ldy=63), -1, b"Y")
+    refused(L, g(Y=0x500001), -1, b"Y")
+
+
+def test_route_and_combine_check(L):
+    def r(logits=V, form=217, ld=64, T=100, E=64, k=4, offsets=V, slot=V, ws=V, size=1 << 20):
+        return L.ilwdetr_moe_route(logits, form, ld, T, E, k, 1, V, V, offsets, V, slot, ws, size, None)
+
+    assert r() == 0 and r(T=0, logits=None, slot=None) == 0
+    assert L.ilwdetr_moe_route_workspace_bytes(0, 64) >= 4 * 64
+    refused(L, r(form=8), -1, b"form")
+    refused(L, r(k=0), -1, b"sizes")
+    refused(L, r(k=65), -1, b"sizes")
+    refused(L, r(ld=63), -1, b"sizes")
+    refused(L, r(E=513, ld=513), -2, b"512")
+    refused(L, r(k=17), -2, b"16")
+    refused(L, r(slot=None), -1, b"NULL")
+    refused(L, r(offsets=None), -1, b"offsets")
+    refused(L, r(logits=ctypes.c_void_p(0x100001)), -1, b"misaligned")
+    refused(L, r(size=16), -1, b"workspace")
+
+    def c(Y=V, form=232, ldy=32, rows=20, slot=V, T=10, k=2, N=32, res=None, ldr=0, out=V, ldo=32):
+        return L.ilwdetr_moe_combine(Y, form, ldy, rows, slot, V, T, k, N, res, ldr, out, ldo, None)
+
+    assert c() == 0 and c(res=V, ldr=32) == 0 and c(T=0, Y=None, slot=None, out=None) == 0 and c(Y=None, rows=0) == 0
+    refused(L, c(form=8), -1, b"form")
+    refused(L, c(k=0), -1, b"sizes")
+    refused(L, c(ldy=31), -1, b"sizes")
+    refused(L, c(res=V, ldr=31), -1, b"sizes")
+    refused(L, c(slot=None), -1, b"NULL")
+    refused(L, c(out=ctypes.c_void_p(0x100002)), -1, b"misaligned")
+
+
+def test_binding_refuses_what_it_cannot_pass_on():
+    """Checks of the binding itself, on CPU tensors: none reaches the library."""
+    torch = pytest.importorskip("torch")
+    import paper_2607_24981_gb300 as ilw
+
+    x = torch.zeros(4, 64)
+    m = ilw.MxTensor(torch.zeros(4, 32, dtype=torch.uint8), torch.zeros(4, 16, dtype=torch.uint8), 64)
+    for call in (lambda: ilw.mx_quantize(x), lambda: ilw.mx_dequantize(m), lambda: ilw.mx_linear(m, m), lambda: ilw.moe_route(x, 2),
+                 lambda: ilw.moe_combine(x, torch.zeros(2, 2, dtype=torch.int32), torch.zeros(2, 2))):
+        with pytest.raises(ilw.IlwError, match="GPU|CUDA"):
+            call()
+    with pytest.raises(ilw.IlwError, match="2 dimensions|dimensions, not 2"):
+        ilw.mx_quantize(torch.zeros(2, 2, 2))
+    with pytest.raises(ilw.IlwError, match="MXFP4"):
+        ilw.mx_linear(m._replace(k=65), m)
+    with pytest.raises(ilw.IlwError, match="GPU"):
+        ilw.mx_grouped_linear(m, m, torch.zeros(5, dtype=torch.int32))
