@@ -530,7 +530,8 @@ int ilwdetr_mx_gemm(const ilw_mx_gemm_t *p, ilw_stream_t stream);
  *   offsets[e]    the number of entries of experts before e (offsets[E]: of all)
  *   source[s]     the token at place s; -1 past the last
  * logits [T, ld] in `form` (ILW_FP32, ILW_FP16, ILW_BF16).  weight fp32, the rest int32: [T, k], offsets [E + 1], source
- * [T k].  workspace: ilwdetr_moe_route_workspace_bytes, 4-byte aligned. */
+ * [T k].  workspace: ilwdetr_moe_route_workspace_bytes (0 for a few hundred tokens: then it may be NULL), 4-byte
+ * aligned. */
 size_t ilwdetr_moe_route_workspace_bytes(int32_t T, int32_t E);
 int ilwdetr_moe_route(const void *logits, int32_t form, int64_t ld, int32_t T, int32_t E, int32_t k, int32_t renormalize,
                       int32_t *expert, float *weight, int32_t *offsets, int32_t *source, int32_t *slot, void *workspace,

@@ -6,7 +6,10 @@
 // rounded to the nearest code, ties to the even one, saturating at 6.  A block of zeros has scale byte 0, a
 // block with a value that is not finite the NaN byte 255.
 //
-// Both kernels move bytes and little else.  A warp takes 256 values of a row: each lane 8, four lanes a block.
+// Both move bytes and little else, so what counts is how many are in flight.  Rows on 16-byte boundaries: eight values a
+// thread and step, four steps in flight, four lanes a block.  Other rows: a warp takes 256 values of a row, one
+// after the other in memory, and hands them over through shared memory, so that its accesses stay whole lines
+// (eight values a lane in a row of its own would touch every line eight times).
 #include <algorithm>
 #include <cstdint>
 
@@ -20,34 +23,29 @@
 namespace ilw {
 namespace {
 
-constexpr int kWarps = 8;
+constexpr int kThreads = 256;
+constexpr int kSteps = 4;  // groups of eight values of a thread in flight
+
+// n / d for n < 2^31 (round-up reciprocal of Granlund and Montgomery, 1994)
+struct Divisor {
+    uint32_t d, m, s;
+    __device__ __forceinline__ uint32_t div(uint32_t n) const { return (__umulhi(n, m) + n) >> s; }
+};
+Divisor divisor(uint32_t d) {
+    uint32_t s = 0;
+    while (((uint64_t)1 << s) < d) ++s;
+    return {d, (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << s) - d)) / d + 1), s};
+}
 
 __device__ __forceinline__ float to_f(float v) { return v; }
 __device__ __forceinline__ float to_f(__half v) { return __half2float(v); }
 __device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ float to_f(int8_t v) { return (float)v; }
 
-// 8 consecutive values from x (n of them exist, the rest are 0); VEC: x is aligned to 8 values (16 bytes for 4-byte ones)
-template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const T *x, int n, float (&v)[8]) {
-    if (VEC && n >= 8) {
-        union {
-            uint32_t w[2 * sizeof(T)];
-            T t[8];
-        } u;
-        if constexpr (sizeof(T) == 1) {
-            *(uint2 *)u.w = *(const uint2 *)x;
-        } else {
-#pragma unroll
-            for (int i = 0; i < (int)sizeof(T) / 2; ++i) ((uint4 *)u.w)[i] = ((const uint4 *)x)[i];
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = to_f(u.t[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < n ? to_f(x[i]) : 0.0f;
-    }
-}
+// 8 values of T (16 or 32 bytes; 8 for int8) as loaded
+template <typename T> struct alignas(sizeof(T) == 1 ? 8 : 16) Eight {
+    T t[8];
+};
 
 // Two values to two codes of a byte, `lo` in the low nibble: nearest, ties to even, saturating.
 __device__ __forceinline__ uint32_t e2m1x2(float lo, float hi) {
@@ -60,45 +58,95 @@ __device__ __forceinline__ float scale_value(uint32_t b) {
     return __uint_as_float(b == 255 ? 0x7fc00000u : b == 0 ? 0x00400000u : b << 23);
 }
 
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(32 * kWarps) mx_quantize_kernel(const MxQuantParams p) {
+// Scale byte and codes of this lane's 8 values (four lanes a block, all of them here).
+__device__ __forceinline__ uint32_t encode8(const float (&v)[8], uint32_t &b) {
+    uint32_t m = 0;  // magnitudes as bits: in order, infinities and NaN on top
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+    // floor(log2 amax) - 2 + 127 is the biased exponent less 2, at least 0 (a subnormal's too)
+    const uint32_t e = m >> 23;
+    b = e == 255 ? 255u : e < 2 ? 0u : e - 2;
+    if (e == 255) return 0;
+    const float inv = __uint_as_float((254 - b) << 23);  // 2^(127 - b), b <= 252
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w |= e2m1x2(v[2 * i] * inv, v[2 * i + 1] * inv) << (8 * i);
+    return w;
+}
+
+// The row of X that row r takes; -1: a row of zeros.
+__device__ __forceinline__ int64_t source_row(const MxQuantParams &p, int64_t r) {
+    if (!p.gather) return r;
+    const int32_t s = p.gather[r];
+    if (s >= 0 && s < p.x_rows) return s;
+    if (s != -1 && p.status) atomicExch(p.status, kStatusBadIndex);
+    return -1;
+}
+
+// Rows of X on 16-byte boundaries, K a multiple of 8.  Step i of the grid: row i / per, values 8 (i % per) .. + 7, whole
+// blocks of four lanes.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) mx_quantize_kernel(const MxQuantParams p, Divisor per, uint32_t r0, uint32_t total) {
     grid_wait();
-    const int lane = threadIdx.x & 31;
-    const int32_t segs = (p.K + 255) / 256;
-    const int32_t blocks = (p.K + 31) / 32, pad = (blocks + 15) & ~15;
-    for (int64_t r = blockIdx.y; r < p.rows; r += gridDim.y) {
-        int64_t src = r;
-        if (p.gather) {
-            src = p.gather[r];
-            if (src < 0 || src >= p.x_rows) {
-                if (src != -1 && p.status && lane == 0) atomicExch(p.status, kStatusBadIndex);
-                src = -1;
-            }
-        }
-        for (int32_t seg = blockIdx.x * kWarps + (threadIdx.x >> 5); seg < segs; seg += gridDim.x * kWarps) {
-            const int32_t k = seg * 256 + lane * 8;
-            float v[8];
-            load8<T, VEC>((const T *)p.X + (src < 0 ? 0 : src) * p.ldx + k, src < 0 ? 0 : p.K - k, v);
-            uint32_t m = 0;  // magnitudes as bits: in order, infinities and NaN on top
+    const uint32_t base = blockIdx.x * (kThreads * kSteps) + threadIdx.x;
+    Eight<T> x[kSteps];
+    uint32_t row[kSteps], k[kSteps];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
-            m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-            m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-            // floor(log2 amax) - 2 + 127 is the biased exponent less 2, at least 0 (a subnormal's too)
-            const uint32_t e = m >> 23;
-            const uint32_t b = e == 255 ? 255u : e < 2 ? 0u : e - 2;
-            uint32_t w = 0;
-            if (e != 255) {
-                const float inv = __uint_as_float((254 - b) << 23);  // 2^(127 - b), b <= 252
+    for (int j = 0; j < kSteps; ++j) {
+        const uint32_t i = base + j * kThreads;
+        row[j] = per.div(i);
+        k[j] = (i - row[j] * per.d) * 8;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) w |= e2m1x2(v[2 * i] * inv, v[2 * i + 1] * inv) << (8 * i);
-            }
-            if (k < blocks * 32) *(uint32_t *)(p.codes + r * p.ldc + (k >> 1)) = w;
-            const int32_t blk = k >> 5;
-            if ((lane & 3) == 0 && blk < pad) p.scales[r * p.lds + blk] = (uint8_t)b;
-            if (seg == segs - 1 && seg * 8 + 8 + lane < pad) p.scales[r * p.lds + seg * 8 + 8 + lane] = 0;
+        for (int u = 0; u < 8; ++u) x[j].t[u] = T(0);
+        if (i < total && k[j] < (uint32_t)p.K) {
+            const int64_t src = source_row(p, (int64_t)r0 + row[j]);
+            if (src >= 0) x[j] = *(const Eight<T> *)((const T *)p.X + src * p.ldx + k[j]);
         }
     }
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j) {
+        float v[8];
+        uint32_t b;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = to_f(x[j].t[u]);
+        const uint32_t w = encode8(v, b);
+        if (base + j * kThreads >= total) continue;
+        const int64_t r = (int64_t)r0 + row[j];
+        const uint32_t blk = k[j] >> 5, lane4 = threadIdx.x & 3;
+        *(uint32_t *)(p.codes + r * p.ldc + (k[j] >> 1)) = w;
+        if (lane4 == 0) p.scales[r * p.lds + blk] = (uint8_t)b;
+        if (blk + 1 == per.d / 4)  // the row's last block: its lanes fill up the scale bytes
+            for (uint32_t z = blk + 1 + lane4; z <= (blk | 15); z += 4) p.scales[r * p.lds + z] = 0;
+    }
+}
+
+// Any rows: a warp takes 256 values of a row at a time.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) mx_quantize_any_kernel(const MxQuantParams p, Divisor segs, uint32_t r0, uint32_t total) {
+    __shared__ __align__(16) float stage[kThreads / 32][256];
+    grid_wait();
+    const int lane = threadIdx.x & 31;
+    float *mine = stage[threadIdx.x >> 5];
+    const uint32_t u = (blockIdx.x * kThreads + threadIdx.x) >> 5;
+    if (u >= total) return;
+    const uint32_t row = segs.div(u), k0 = (u - row * segs.d) * 256;
+    const int64_t r = (int64_t)r0 + row, src = source_row(p, r);
+    const uint32_t K = (uint32_t)p.K, blocks = (K + 31) / 32;
+    const T *x = (const T *)p.X + src * p.ldx + k0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) mine[32 * i + lane] = src >= 0 && k0 + 32 * i + lane < K ? to_f(x[32 * i + lane]) : 0.0f;
+    __syncwarp();
+    float v[8];
+    uint32_t b;
+    *(float4 *)v = *(const float4 *)(mine + 8 * lane);
+    *(float4 *)(v + 4) = *(const float4 *)(mine + 8 * lane + 4);
+    const uint32_t w = encode8(v, b), k = k0 + 8 * lane;
+    if (k < blocks * 32) *(uint32_t *)(p.codes + r * p.ldc + (k >> 1)) = w;
+    const uint32_t blk = k >> 5;
+    if ((k & 31) == 0 && blk < blocks) p.scales[r * p.lds + blk] = (uint8_t)b;
+    if (k0 + 256 >= K && lane < 15 && blocks + lane <= ((blocks - 1) | 15)) p.scales[r * p.lds + blocks + lane] = 0;  // (up to a multiple of 16)
 }
 
 // the two values of a byte of codes
@@ -113,56 +161,88 @@ template <> __device__ __forceinline__ float from_f<float>(float v) { return v; 
 template <> __device__ __forceinline__ __half from_f<__half>(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(32 * kWarps) mx_dequantize_kernel(const MxDequantParams p) {
+template <typename T>
+__global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(const MxDequantParams p, Divisor per, uint32_t r0, uint32_t total) {
     grid_wait();
-    const int lane = threadIdx.x & 31;
-    const int32_t segs = (p.K + 255) / 256;
-    for (int64_t r = blockIdx.y; r < p.rows; r += gridDim.y) {
-        for (int32_t seg = blockIdx.x * kWarps + (threadIdx.x >> 5); seg < segs; seg += gridDim.x * kWarps) {
-            const int32_t k = seg * 256 + lane * 8, n = p.K - k;
-            if (n <= 0) continue;
-            const uint32_t w = *(const uint32_t *)(p.codes + r * p.ldc + (k >> 1));
-            const float s = scale_value(p.scales[r * p.lds + (k >> 5)]);
-            T *y = (T *)p.Y + r * p.ldy + k;
-            union {
-                uint4 q[sizeof(T) / 2];
-                T t[8];
-            } u;
+    const uint32_t base = blockIdx.x * (kThreads * kSteps) + threadIdx.x;
+    uint32_t w[kSteps], b[kSteps], row[kSteps], k[kSteps];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 f = from_e2m1x2((w >> (8 * i)) & 255);
-                u.t[2 * i] = from_f<T>(f.x * s);
-                u.t[2 * i + 1] = from_f<T>(f.y * s);
-            }
-            if (VEC && n >= 8) {
-#pragma unroll
-                for (int i = 0; i < (int)sizeof(T) / 2; ++i) ((uint4 *)y)[i] = u.q[i];
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (i < n) y[i] = u.t[i];
-            }
+    for (int j = 0; j < kSteps; ++j) {
+        const uint32_t i = base + j * kThreads;
+        row[j] = per.div(i);
+        k[j] = (i - row[j] * per.d) * 8;
+        w[j] = b[j] = 0;
+        if (i < total) {
+            const int64_t r = (int64_t)r0 + row[j];
+            w[j] = *(const uint32_t *)(p.codes + r * p.ldc + (k[j] >> 1));
+            b[j] = p.scales[r * p.lds + (k[j] >> 5)];
         }
+    }
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j) {
+        if (base + j * kThreads >= total) continue;
+        const float s = scale_value(b[j]);
+        Eight<T> y;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const float2 f = from_e2m1x2((w[j] >> (8 * u)) & 255);
+            y.t[2 * u] = from_f<T>(f.x * s);
+            y.t[2 * u + 1] = from_f<T>(f.y * s);
+        }
+        *(Eight<T> *)((T *)p.Y + ((int64_t)r0 + row[j]) * p.ldy + k[j]) = y;
     }
 }
 
-dim3 row_grid(int64_t rows, int32_t K) {
-    const int32_t segs = (K + 255) / 256;
-    return dim3((unsigned)((segs + kWarps - 1) / kWarps), (unsigned)std::min<int64_t>(rows, 65535));
+template <typename T>
+__global__ void __launch_bounds__(kThreads) mx_dequantize_any_kernel(const MxDequantParams p, Divisor segs, uint32_t r0, uint32_t total) {
+    __shared__ __align__(16) float stage[kThreads / 32][256];
+    grid_wait();
+    const int lane = threadIdx.x & 31;
+    float *mine = stage[threadIdx.x >> 5];
+    const uint32_t u = (blockIdx.x * kThreads + threadIdx.x) >> 5;
+    if (u >= total) return;
+    const uint32_t row = segs.div(u), k0 = (u - row * segs.d) * 256, k = k0 + 8 * lane;
+    const int64_t r = (int64_t)r0 + row;
+    const uint32_t K = (uint32_t)p.K;
+    if (k < K) {
+        const uint32_t w = *(const uint32_t *)(p.codes + r * p.ldc + (k >> 1));
+        const float s = scale_value(p.scales[r * p.lds + (k >> 5)]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float2 f = from_e2m1x2((w >> (16 * i)) & 255), g = from_e2m1x2((w >> (16 * i + 8)) & 255);
+            ((float4 *)(mine + 8 * lane))[i] = make_float4(f.x * s, f.y * s, g.x * s, g.y * s);
+        }
+    }
+    __syncwarp();
+    T *y = (T *)p.Y + r * p.ldy + k0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (k0 + 32 * i + lane < K) y[32 * i + lane] = from_f<T>(mine[32 * i + lane]);
+}
+
+// Launches `kernel` over `rows` rows of `per` steps each, `step` of them a CTA, as often as 2^31 steps at a time take.
+template <typename P>
+cudaError_t over_rows(void (*kernel)(const P, Divisor, uint32_t, uint32_t), const P &p, int64_t rows, uint32_t per, uint32_t step, cudaStream_t s) {
+    const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 30) / per);
+    for (int64_t r0 = 0; r0 < rows; r0 += most) {
+        const uint32_t total = (uint32_t)(std::min(most, rows - r0) * per);
+        const cudaError_t e = launch_after(kernel, (total + step - 1) / step, kThreads, 0, s, p, divisor(per), (uint32_t)r0, total);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
 }
 
 template <typename T>
 cudaError_t quantize(const MxQuantParams &p, cudaStream_t s) {
-    const bool vec = (uintptr_t)p.X % 16 == 0 && p.ldx * (int64_t)sizeof(T) % 16 == 0;
-    if (vec) return launch_after(mx_quantize_kernel<T, true>, row_grid(p.rows, p.K), 32 * kWarps, 0, s, p);
-    return launch_after(mx_quantize_kernel<T, false>, row_grid(p.rows, p.K), 32 * kWarps, 0, s, p);
+    if ((uintptr_t)p.X % alignof(Eight<T>) == 0 && p.ldx * (int64_t)sizeof(T) % alignof(Eight<T>) == 0 && p.K % 8 == 0)
+        return over_rows(mx_quantize_kernel<T>, p, p.rows, (uint32_t)(p.K + 31) / 32 * 4, kThreads * kSteps, s);
+    return over_rows(mx_quantize_any_kernel<T>, p, p.rows, (uint32_t)(p.K + 255) / 256, kThreads / 32, s);
 }
 template <typename T>
 cudaError_t dequantize(const MxDequantParams &p, cudaStream_t s) {
-    const bool vec = (uintptr_t)p.Y % 16 == 0 && p.ldy * (int64_t)sizeof(T) % 16 == 0;
-    if (vec) return launch_after(mx_dequantize_kernel<T, true>, row_grid(p.rows, p.K), 32 * kWarps, 0, s, p);
-    return launch_after(mx_dequantize_kernel<T, false>, row_grid(p.rows, p.K), 32 * kWarps, 0, s, p);
+    if ((uintptr_t)p.Y % 16 == 0 && p.ldy * (int64_t)sizeof(T) % 16 == 0 && p.K % 8 == 0)
+        return over_rows(mx_dequantize_kernel<T>, p, p.rows, p.K / 8, kThreads * kSteps, s);
+    return over_rows(mx_dequantize_any_kernel<T>, p, p.rows, (uint32_t)(p.K + 255) / 256, kThreads / 32, s);
 }
 
 }  // namespace

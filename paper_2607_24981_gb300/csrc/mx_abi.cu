@@ -45,7 +45,7 @@ int ilwdetr_mx_quantize(const void *X, int32_t x_form, int64_t ldx, int64_t x_ro
                         int32_t K, uint8_t *codes, int64_t ldc, uint8_t *scales, int64_t lds, ilw_stream_t stream) {
     const int size = x_form == 8 ? 1 : form_size(x_form);
     if (!size) return fail(ILW_ERR_INVALID_ARG, "mx_quantize: x_form=%d", x_form);
-    if (K < 1 || K > INT32_MAX - 1024 || rows < 0 || x_rows < 0 || ldx < K || (!gather && rows > x_rows) || x_rows > INT32_MAX)
+    if (K < 1 || K > INT32_MAX - 1024 || rows < 0 || rows > INT32_MAX || x_rows < 0 || ldx < K || (!gather && rows > x_rows) || x_rows > INT32_MAX)
         return fail(ILW_ERR_INVALID_ARG, "mx_quantize: bad sizes rows=%lld x_rows=%lld K=%d", (long long)rows, (long long)x_rows, K);
     if (rows == 0) return ILW_OK;
     if ((!X && x_rows > 0) || !aligned(X, size) || !aligned(gather, 4))
@@ -60,7 +60,7 @@ int ilwdetr_mx_quantize(const void *X, int32_t x_form, int64_t ldx, int64_t x_ro
 int ilwdetr_mx_dequantize(const uint8_t *codes, int64_t ldc, const uint8_t *scales, int64_t lds, int64_t rows, int32_t K,
                           void *Y, int32_t y_form, int64_t ldy, ilw_stream_t stream) {
     if (!form_size(y_form)) return fail(ILW_ERR_INVALID_ARG, "mx_dequantize: y_form=%d", y_form);
-    if (K < 1 || K > INT32_MAX - 1024 || rows < 0 || ldy < K) return fail(ILW_ERR_INVALID_ARG, "mx_dequantize: bad sizes rows=%lld K=%d", (long long)rows, K);
+    if (K < 1 || K > INT32_MAX - 1024 || rows < 0 || rows > INT32_MAX || ldy < K) return fail(ILW_ERR_INVALID_ARG, "mx_dequantize: bad sizes rows=%lld K=%d", (long long)rows, K);
     if (rows == 0) return ILW_OK;
     if (!Y || !aligned(Y, form_size(y_form))) return fail(ILW_ERR_INVALID_ARG, "mx_dequantize: Y NULL or misaligned");
     ILW_TRY(mx_array("mx_dequantize", "codes", codes, ldc, code_bytes(K)));
@@ -122,8 +122,9 @@ int ilwdetr_moe_route(const void *logits, int32_t form, int64_t ld, int32_t T, i
     if (!offsets || !aligned(logits, form_size(form)) || !aligned(expert, 4) || !aligned(weight, 4) || !aligned(offsets, 4) ||
         !aligned(source, 4) || !aligned(slot, 4))
         return fail(ILW_ERR_INVALID_ARG, "moe_route: offsets NULL or a tensor misaligned");
-    if (!workspace || !aligned(workspace, 4) || workspace_bytes < ilw::moe_route_workspace(T, E))
-        return fail(ILW_ERR_INVALID_ARG, "moe_route: workspace NULL, misaligned or smaller than %zu bytes", ilw::moe_route_workspace(T, E));
+    const size_t need = ilw::moe_route_workspace(T, E);
+    if (need && (!workspace || !aligned(workspace, 4) || workspace_bytes < need))
+        return fail(ILW_ERR_INVALID_ARG, "moe_route: workspace NULL, misaligned or smaller than %zu bytes", need);
     if (ilw::validate_only()) return ILW_OK;
     const ilw::MoeRouteParams p{logits, form, ld, T, E, k, renormalize, expert, weight, offsets, source, slot, (int32_t *)workspace};
     return done(ilw::launch_moe_route(p, (cudaStream_t)stream), "moe_route");

@@ -1,0 +1,765 @@
+#pragma once
+// mx_gemm.cuh -- products of microscaled 4-bit (MXFP4) matrices on the 5th-generation tensor cores
+// (tcgen05.mma kind::mxf4, sm_103a): Y = act(A W^T + bias), for one weight or for one weight per expert
+// with ragged groups of rows.
+//
+//   z[m, n] = sum over blocks b of 2^(sa[m,b] + sw[n,b] - 254) sum_{k in b} a[m,k] w[n,k]  + bias[n]
+//
+// The tensor core multiplies the 4-bit codes and the block scales exactly and accumulates in fp32 in
+// tensor memory; activation and rounding to the output type happen once, in the epilogue.
+//
+// Tiles.  The rows of W take the 128 lanes of a tile and the rows of A (tokens) its columns: a tile is 128
+// outputs x up to 224 tokens, with the number of tokens set at run time in steps of 16.  So one kernel
+// serves a single token (the 128 rows of W stream past one 16-wide MMA), a ragged group of an expert
+// (the columns past its end are neither computed beyond the next 16 nor stored) and a long batch.
+//
+// Three forms.  ONE: a CTA a tile.  SPLIT, for few tiles: the K range of a tile is shared by the CTAs of a
+// cluster, whose partial sums meet in distributed shared memory and are added in a fixed order.  PAIR, for
+// many: two SMs share a tile of 256 outputs (cta_group::2), each with its own 128 rows of W and half of
+// the tokens.  One CTA's shared memory takes 45 KB of operands for each 256 of K of its tile and gives them to the
+// tensor core once, at 128 bytes a clock 700 clocks for MMAs of 450; in a pair it is 30 KB.
+//
+// Scales are stored row-major, 16 bytes of a row for 512 values of K.  Two warps bring them in by asynchronous copies
+// of 16 bytes (TMA boxes 16 bytes wide held up the loads of the codes behind them), a lane its own rows, and
+// write them, still in shared memory, in the order in which tcgen05.cp brings them to tensor memory (lane i,
+// column c: row 32 c + i; the four scales of 128 values of K to a word), so rows may start anywhere; the copies
+// and the MMAs that read them follow one another in the tensor pipe without a wait.
+//
+// One CTA per SM, 20 warps: TMA producer, MMA issuer, 2 scale warps, 16 epilogue warps (four on each scheduler: with
+// two, the activation's chains of latency set the time of a short K).  Two accumulators let a tile's epilogue overlap
+// the next tile's MMAs.  Tiles are dealt out in turn; with experts each CTA works out the list of tiles from
+// the offsets itself, so no count has to reach the host.
+//
+// Every mbarrier wait is bounded; on expiry the kernel latches the device status word, stops issuing
+// work, waits for its loads and MMAs in flight and frees its tensor memory.
+#include <climits>
+#include <cstdint>
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "attn_ptx.cuh"
+#include "ilwdetr.h"
+#include "ilw_kernels.h"
+#include "mx_kernels.h"
+
+namespace ilw {
+
+constexpr int kMxRowsW = 128;   // rows of W a CTA
+constexpr int kMxMaxTok = 224;  // tokens a tile
+constexpr int kMxMaxStages = 16, kMxMaxRaw = 6, kMxMaxScale = 4;
+constexpr int kMxEpiWarp0 = 4, kMxEpiWarps = 16, kMxThreads = 32 * (kMxEpiWarp0 + kMxEpiWarps);
+constexpr int kMxAtom = 512;    // bytes of the scales of 128 rows and 128 values of K
+constexpr int kMxPatch = 1024;  // bytes of shared memory in which an epilogue warp turns 2-byte results
+constexpr int kMxSmemLimit = 226 * 1024;  // dynamic; the barriers are static
+
+enum MxMode { MX_ONE = 0, MX_SPLIT = 1, MX_PAIR = 2 };
+
+struct MxExpert {
+    int32_t start, row, end, width;  // first token tile, its rows [row, end), rows a tile
+};
+
+struct MxParams {
+    CUtensorMap wc, ac;     // codes of W [E, N, .] and A [M, .]
+    const uint8_t *w_scales, *a_scales;
+    int64_t w_lds, w_scales_stride, a_lds;
+    int32_t nb;             // scale bytes of a row
+    const int32_t *offsets;
+    const float *bias;
+    void *Y;
+    int64_t ldy, M;
+    int32_t N, E;
+    int32_t nkb, nsb;       // K in blocks of 256 (a data stage) and 512 (a scale stage)
+    int32_t wtiles;         // tiles of rows of W (128, or 256 a pair)
+    uint32_t wdiv_m, wdiv_s;  // division by wtiles
+    int32_t nt;             // most tokens a tile, a multiple of 16 (a pair's: of 32)
+    int32_t abox;           // rows of A a TMA box
+    int32_t stages, raws, scales;  // ring sizes: data, scales as loaded (2 to kMxMaxRaw), scales as the tensor core takes them
+    int32_t stage_bytes, raw_bytes, scale_bytes;
+    int32_t wide;           // 2-byte rows of Y take 16-byte stores
+    int32_t splits;         // CTAs of a cluster that share a tile's K (SPLIT)
+    int32_t mode;
+    int32_t dbg_skip;
+    long long wait_cycles;
+    int *status;
+};
+
+template <typename T>
+cudaError_t launch_mx(const MxParams &p, int32_t act, int grid, size_t smem, cudaStream_t s);
+
+namespace {
+
+struct Tile {
+    int32_t e, row0, rows, n0;
+};
+
+// Bounded wait: false (after latching `code` and raising the abort flag) when it ran out, or when another role aborted.
+__device__ __forceinline__ bool wait_bar(uint32_t b, uint32_t parity, volatile int *abort, const MxParams &p, int code) {
+    if (bar_try(b, parity)) return true;
+    const long long t0 = clock64();
+    for (uint32_t i = 0;; ++i) {
+        if (bar_try(b, parity)) return true;
+        if ((i & 63) == 63) {
+            if (*abort) return false;
+            if (clock64() - t0 > p.wait_cycles) {
+                if (p.status) atomicExch(p.status, code);
+                *abort = 1;
+                return false;
+            }
+        }
+    }
+}
+// The same for a whole warp, one answer for all lanes (the tcgen05 instructions after it are warp-wide).
+__device__ __forceinline__ bool wait_warp(uint32_t b, uint32_t parity, volatile int *abort, const MxParams &p, int code) {
+    return __all_sync(0xffffffffu, wait_bar(b, parity, abort, p, code));
+}
+// This barrier's address in CTA `rank` of the cluster, and an arrival there.  What the arrivals of a pair order is read by the
+// tensor core alone, through the async proxy, to which its writers hand it themselves (TMA, or fence.proxy.async
+// after the stores); a release at cluster scope on top of that held each arrival up by some 1000 clocks.
+__device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void arrive_cluster(uint32_t addr) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void prefetch_map(const CUtensorMap *m) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)m) : "memory");
+}
+
+// A value that is the same in every lane, in a uniform register: the operands of TMA loads and MMAs are uniform
+// registers, and each one that has to be moved there at its instruction costs some 50 clocks (a lane alone in a
+// branch took 300 clocks a TMA load, which was the rate of every product).
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __reduce_max_sync(0xffffffffu, v); }
+// TMA loads and their barrier, by the lane with `issue` set, of a converged warp
+__device__ __forceinline__ void expect_if(uint32_t b, uint32_t bytes, uint32_t issue) {
+    asm volatile("{\n .reg .pred q;\n setp.ne.b32 q, %2, 0;\n @q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n}\n" ::"r"(b), "r"(bytes),
+                 "r"(issue)
+                 : "memory");
+}
+__device__ __forceinline__ void tma_2d_if(uint32_t dst, const CUtensorMap *m, int32_t x, int32_t y, uint32_t bar, uint32_t issue) {
+    asm volatile(
+        "{\n .reg .pred q;\n setp.ne.b32 q, %5, 0;\n"
+        " @q cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n}\n" ::"r"(dst),
+        "l"((uint64_t)m), "r"(x), "r"(y), "r"(bar), "r"(issue)
+        : "memory");
+}
+__device__ __forceinline__ void tma_3d_if(uint32_t dst, const CUtensorMap *m, int32_t x, int32_t y, int32_t z, uint32_t bar, uint32_t issue) {
+    asm volatile(
+        "{\n .reg .pred q;\n setp.ne.b32 q, %6, 0;\n"
+        " @q cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n}\n" ::"r"(dst),
+        "l"((uint64_t)m), "r"(x), "r"(y), "r"(z), "r"(bar), "r"(issue)
+        : "memory");
+}
+
+// Of a pair (PAIR) only the first CTA issues, for both.
+template <bool PAIR>
+__device__ __forceinline__ void mma_mx(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb,
+                                       uint32_t acc, uint32_t issue) {
+    if constexpr (PAIR)
+        asm volatile(
+            "{\n .reg .pred p, q;\n setp.ne.b32 p, %6, 0;\n setp.ne.b32 q, %7, 0;\n"
+            " @q tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}\n" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(acc), "r"(issue)
+            : "memory");
+    else
+        asm volatile(
+            "{\n .reg .pred p, q;\n setp.ne.b32 p, %6, 0;\n setp.ne.b32 q, %7, 0;\n"
+            " @q tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}\n" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(acc), "r"(issue)
+            : "memory");
+}
+// An arrival at `bar` (of a pair: in both CTAs, unless `local`) when the MMAs and copies issued so far have ended.
+template <bool PAIR>
+__device__ __forceinline__ void commit_if(uint32_t bar, uint32_t issue, bool local = false) {
+    if constexpr (PAIR) {
+        if (!local) {
+            asm volatile(
+                "{\n .reg .pred q;\n setp.ne.b32 q, %1, 0;\n"
+                " @q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %2;\n}\n" ::"r"(bar),
+                "r"(issue), "h"((uint16_t)3)
+                : "memory");
+            return;
+        }
+        asm volatile(
+            "{\n .reg .pred q;\n setp.ne.b32 q, %1, 0;\n"
+            " @q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(bar), "r"(issue)
+            : "memory");
+    } else {
+        asm volatile(
+            "{\n .reg .pred q;\n setp.ne.b32 q, %1, 0;\n"
+            " @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(bar), "r"(issue)
+            : "memory");
+    }
+}
+// Shared memory to tensor memory (of a pair: in both CTAs, each its own): 32 rows of 16 bytes to 4 columns of 32 lanes, the
+// same for each quarter of the lanes.
+template <bool PAIR>
+__device__ __forceinline__ void copy_scales(uint32_t t, uint32_t saddr, uint32_t issue) {
+    // rows of 16 bytes, eight of them (128 bytes) a core matrix, no swizzle
+    const uint64_t d = (uint64_t)((saddr >> 4) & 0x3FFFu) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
+    if constexpr (PAIR)
+        asm volatile(
+            "{\n .reg .pred q;\n setp.ne.b32 q, %2, 0;\n @q tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n}\n" ::"r"(t), "l"(d), "r"(issue)
+            : "memory");
+    else
+        asm volatile(
+            "{\n .reg .pred q;\n setp.ne.b32 q, %2, 0;\n @q tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n}\n" ::"r"(t), "l"(d), "r"(issue)
+            : "memory");
+}
+// Waits until no more than n of this thread's groups of asynchronous copies are in flight.
+__device__ __forceinline__ void copies_but(int n) {
+    switch (n) {
+        case 1: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
+        case 2: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
+        case 3: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
+        case 4: asm volatile("cp.async.wait_group 4;" ::: "memory"); break;
+        case 5: asm volatile("cp.async.wait_group 5;" ::: "memory"); break;
+        default: asm volatile("cp.async.wait_group 0;" ::: "memory");
+    }
+}
+__device__ __forceinline__ void lds128(uint32_t a, uint32_t (&v)[4]) {
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+                 : "r"(a)
+                 : "memory");
+}
+
+// Instruction descriptor of kind::mxf4: E2M1 operands (format 1), UE8M0 scales, M = m, N = n, both
+// operands K-major; `id` (0 or 2) is the byte of a scale word at which this MMA's two scales begin.
+__device__ __forceinline__ uint32_t idesc_mx(uint32_t m, uint32_t n, uint32_t id) {
+    return (id << 4) | (1u << 7) | (1u << 10) | ((n >> 3) << 17) | (1u << 23) | ((m >> 4) << 24) | (id << 29);
+}
+
+template <typename T> __device__ __forceinline__ T to_out(float v);
+template <> __device__ __forceinline__ float to_out<float>(float v) { return v; }
+template <> __device__ __forceinline__ __half to_out<__half>(float v) { return __float2half_rn(v); }
+template <> __device__ __forceinline__ __nv_bfloat16 to_out<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// (By a whole warp.) Tile t: the tile of W's rows runs fastest, so CTAs that run together share a token tile's rows.  tab: the
+// experts that have rows, n of them (n <= 1024: two probes of 32), and an end.
+template <int MODE>
+__device__ __forceinline__ Tile find_tile(const MxParams &p, const MxExpert *tab, const int32_t *id, int n, int32_t t, uint32_t rank) {
+    const int lane = threadIdx.x & 31;
+    const int32_t tt = (int32_t)((__umulhi((uint32_t)t, p.wdiv_m) + (uint32_t)t) >> p.wdiv_s);  // t / wtiles
+    int a = 0;  // the expert with start <= tt < the next one's
+    if (n > 32) a = 32 * (__popc(__ballot_sync(0xffffffffu, 32 * lane < n && tab[min(32 * lane, n)].start <= tt)) - 1);
+    a += __popc(__ballot_sync(0xffffffffu, a + lane < n && tab[min(a + lane, n)].start <= tt)) - 1;
+    const int4 x = *(const int4 *)(tab + a);
+    Tile r;
+    r.e = id[a];
+    r.row0 = x.y + (tt - x.x) * x.w;
+    r.rows = min(x.w, x.z - r.row0);
+    r.n0 = (t - tt * p.wtiles) * (MODE == MX_PAIR ? 2 * kMxRowsW : kMxRowsW) + (MODE == MX_PAIR ? rank * kMxRowsW : 0);
+    return r;
+}
+
+// Two floats at a time.
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 unpack2(uint64_t v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+// z (1 + erf(z / sqrt 2)) / 2 of two values, with erf by Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26
+// (absolute error at most 1.5e-7): about 10 operations a value.
+__device__ __forceinline__ void gelu2(float &a, float &b) {
+    const uint64_t z = pack2(a, b);
+    const float2 d = unpack2(fma2(pack2(fabsf(a), fabsf(b)), pack2(0.23164190f, 0.23164190f), pack2(1.0f, 1.0f)));  // 0.3275911 / sqrt 2
+    const uint64_t t = pack2(__fdividef(1.0f, d.x), __fdividef(1.0f, d.y));
+    uint64_t q = fma2(t, pack2(-1.061405429f, -1.061405429f), pack2(1.453152027f, 1.453152027f));  // (-erf's polynomial)
+    q = fma2(q, t, pack2(-1.421413741f, -1.421413741f));
+    q = fma2(q, t, pack2(0.284496736f, 0.284496736f));
+    q = fma2(q, t, pack2(-0.254829592f, -0.254829592f));
+    q = mul2(q, t);
+    const float2 x = unpack2(mul2(mul2(z, z), pack2(-0.72134752f, -0.72134752f)));  // -z^2 / 2 log2 e
+    const float2 e = unpack2(fma2(q, pack2(exp2_fast(x.x), exp2_fast(x.y)), pack2(1.0f, 1.0f)));  // erf |z / sqrt 2|
+    const uint64_t h = mul2(z, pack2(0.5f, 0.5f));
+    const float2 r = unpack2(fma2(h, pack2(copysignf(e.x, a), copysignf(e.y, b)), h));
+    a = r.x;
+    b = r.y;
+}
+__device__ __forceinline__ float silu_gate(float gate, float up) { return __fdividef(gate, 1.0f + __expf(-gate)) * up; }
+
+// One warp's 32 rows of W (this lane: row n) x 16 tokens (c0 .. c0 + 15 of the tile).  A lane holds one output of 16
+// tokens, so its own stores would be 2 bytes wide; where rows of Y allow it (`wide`), 2-byte results pass through
+// the warp's patch of shared memory [token][output] and leave in 16-byte pieces.
+template <int ACT, typename T>
+__device__ __forceinline__ void store_chunk(const MxParams &p, float (&v)[16], const Tile &t, int c0, int n, float bias, uint32_t patch,
+                                            int lane) {
+    const int left = t.rows - c0;
+    constexpr bool kGate = ACT == ILW_ACT_SILU_GATE;
+    constexpr int kCols = kGate ? 16 : 32, kVals = kGate ? 8 : 16;  // outputs of the warp's rows of W, results of a lane
+    if (p.bias) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] += bias;
+    }
+    if constexpr (kGate) {
+        // even lanes hold gates, odd lanes the rows they gate: each lane of a pair finishes every other token
+        const bool odd = lane & 1;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float other = __shfl_xor_sync(0xffffffffu, odd ? v[2 * i] : v[2 * i + 1], 1);
+            v[i] = silu_gate(odd ? other : v[2 * i], odd ? v[2 * i + 1] : other);
+        }
+    } else if constexpr (ACT == ILW_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) gelu2(v[2 * i], v[2 * i + 1]);
+    }
+    const int out0 = (kGate ? n >> 1 : n) - (kGate ? lane >> 1 : lane);  // first output of the warp
+    const int width = kGate ? p.N / 2 : p.N;
+    if constexpr (sizeof(T) == 2) {
+        if (p.wide) {
+            const uint32_t at = patch + (kGate ? (lane & 1) * 2 * kCols + (lane & ~1) : 2 * lane);
+#pragma unroll
+            for (int i = 0; i < kVals; ++i) {
+                const T h = to_out<T>(v[i]);
+                asm volatile("st.shared.b16 [%0], %1;" ::"r"(at + i * (kGate ? 4 * kCols : 2 * kCols)), "h"(*(const uint16_t *)&h) : "memory");
+            }
+            __syncwarp();
+            constexpr int kPieces = kCols / 8, kTokens = 32 / kPieces;  // pieces of a token, tokens at a time
+            const int piece = lane % kPieces, token = lane / kPieces;
+            T *y = (T *)p.Y + (int64_t)(t.row0 + c0 + token) * p.ldy + out0 + 8 * piece;
+            const bool in = out0 + 8 * piece < width;
+#pragma unroll
+            for (int i = 0; i < 16 / kTokens; ++i) {
+                uint32_t q[4];
+                lds128(patch + lane * 16 + i * 512, q);
+                if (in && token + i * kTokens < left) *(uint4 *)(y + (int64_t)i * kTokens * p.ldy) = make_uint4(q[0], q[1], q[2], q[3]);
+            }
+            __syncwarp();
+            return;
+        }
+    }
+    const int col = out0 + (kGate ? lane >> 1 : lane), first = kGate ? lane & 1 : 0;
+    T *y = (T *)p.Y + (int64_t)(t.row0 + c0 + first) * p.ldy + col;
+    const int64_t step = kGate ? 2 * p.ldy : p.ldy;
+#pragma unroll
+    for (int i = 0; i < kVals; ++i, y += step)
+        if ((kGate ? 2 * i + first : i) < left && col < width) *y = to_out<T>(v[i]);
+}
+
+template <int ACT, typename T, int MODE>
+__global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_constant__ MxParams p) {
+    constexpr bool SPLIT = MODE == MX_SPLIT, PAIR = MODE == MX_PAIR;
+    // tensor-memory columns: two accumulators, then two buffers of the scales of 256 values of K (2 x 4 columns of
+    // W's rows, 2 x 8 of A's)
+    constexpr int kScaleCol = 2 * kMxMaxTok, kScaleCols = 24;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t bars[3 * kMxMaxStages + 2 * kMxMaxScale + 5];
+    __shared__ uint32_t tmem_base;
+    __shared__ volatile int abort_flag;
+    __shared__ int32_t s_experts, s_head, s_tail;  // experts with rows; rows before the first and from the end of the last
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t data0 = (su32(smem_raw) + 1023) & ~1023u;
+    const uint32_t raw0 = data0 + p.stages * p.stage_bytes, scale0 = raw0 + p.raws * p.raw_bytes;
+    const uint32_t patch0 = scale0 + p.scales * p.scale_bytes;
+    MxExpert *tab = (MxExpert *)(smem_raw + (patch0 - su32(smem_raw)) + (p.wide ? kMxEpiWarps * kMxPatch : 0));
+    int32_t *tab_id = (int32_t *)(tab + p.E + 1);
+
+    uint32_t next_bar = su32(bars);
+    auto take = [&](int n) {
+        const uint32_t at = next_bar;
+        next_bar += 8 * n;
+        return at;
+    };
+    const uint32_t full = take(kMxMaxStages), empty = take(kMxMaxStages), pfull = take(kMxMaxStages);    // data; pfull: the other CTA's
+    const uint32_t sfull = take(kMxMaxScale), sempty = take(kMxMaxScale);                                // scales in order (a pair's: at the first CTA)
+    const uint32_t afull = take(2), aempty = take(2), drain = take(1);                                   // accumulators
+
+    const uint32_t rank = SPLIT ? blockIdx.x % p.splits : PAIR ? blockIdx.x & 1 : 0;
+    const bool leader = !PAIR || rank == 0;
+    if (threadIdx.x == 0) {
+        abort_flag = 0;
+        for (int i = 0; i < kMxMaxStages; ++i) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 1), bar_init(pfull + 8 * i, 1);
+        for (int i = 0; i < kMxMaxScale; ++i) bar_init(sfull + 8 * i, PAIR ? 4 : 2), bar_init(sempty + 8 * i, 1);
+        for (int i = 0; i < 2; ++i) bar_init(afull + 8 * i, 1), bar_init(aempty + 8 * i, PAIR ? 2 * kMxEpiWarps : kMxEpiWarps);
+        bar_init(drain, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (threadIdx.x == 32) {
+        prefetch_map(&p.wc);
+        prefetch_map(&p.ac);
+    }
+    if (warp == 3) {
+        if constexpr (PAIR) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(su32(&tmem_base)) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(su32(&tmem_base)) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        }
+    }
+    grid_wait();
+    // the list of tiles: the experts that have rows, in order.  Their ranges are held in order, apart and inside [0, M],
+    // whatever the offsets say.
+    if (warp == 2) {
+        const int32_t M = (int32_t)p.M;
+        int32_t sum = 0, count = 0, before = 0, head = M;  // of the experts before this round: tiles, those with rows, end of the last range
+        for (int e0 = 0; e0 < p.E; e0 += 32) {
+            const int e = e0 + lane;
+            int32_t l = 0, h = e < p.E ? M : 0;
+            if (p.offsets && e < p.E) {
+                l = max(0, min(p.offsets[e], M));
+                h = max(0, min(p.offsets[e + 1], M));
+            }
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int32_t y = __shfl_up_sync(0xffffffffu, h, d);
+                if (lane >= d) h = max(h, y);
+            }
+            h = max(h, before);
+            const int32_t prev = __shfl_up_sync(0xffffffffu, h, 1);
+            l = min(max(l, lane ? prev : before), h);
+            if (e0 == 0) head = __shfl_sync(0xffffffffu, l, 0);
+            before = __shfl_sync(0xffffffffu, h, 31);
+            const int32_t rows = e < p.E ? h - l : 0, tiles = (rows + p.nt - 1) / p.nt;
+            int32_t x = tiles;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int32_t y = __shfl_up_sync(0xffffffffu, x, d);
+                if (lane >= d) x += y;
+            }
+            const uint32_t with = __ballot_sync(0xffffffffu, rows > 0);
+            if (rows > 0) {  // equal tiles of at most nt, multiples of 16 (a pair's: of 32)
+                constexpr int kStep = PAIR ? 32 : 16;
+                const int i = count + __popc(with & ((1u << lane) - 1));
+                *(int4 *)(tab + i) = make_int4(sum + x - tiles, l, h, ((rows + tiles - 1) / tiles + kStep - 1) & ~(kStep - 1));
+                tab_id[i] = e;
+            }
+            sum += __shfl_sync(0xffffffffu, x, 31);
+            count += __popc(with);
+        }
+        if (lane == 0) {
+            tab[count].start = sum;
+            s_experts = count;
+            s_head = head;
+            s_tail = before;
+        }
+    }
+    fence_before();
+    if constexpr (PAIR) cluster_sync();
+    else __syncthreads();
+    fence_after();
+    const uint32_t tmem = uniform(tmem_base);
+    const int experts = s_experts;
+    const int32_t tiles = tab[experts].start * p.wtiles;
+    const int32_t group = SPLIT ? p.splits : PAIR ? 2 : 1;
+    const int32_t first = (int32_t)blockIdx.x / group, step = (int32_t)gridDim.x / group;
+    const int32_t sb_lo = SPLIT ? (int32_t)((int64_t)p.nsb * rank / p.splits) : 0;
+    const int32_t sb_hi = SPLIT ? (int32_t)((int64_t)p.nsb * (rank + 1) / p.splits) : p.nsb;
+    const int32_t kb_hi = min(2 * sb_hi, p.nkb);
+    const int atoms = 1 + (p.nt + 127) / 128;  // of W's rows, and of A's
+    auto tile_at = [&](int32_t t) { return find_tile<MODE>(p, tab, tab_id, experts, t, rank); };
+    auto mma_tokens = [&](const Tile &x) { return PAIR ? (x.rows + 31) & ~31 : (x.rows + 15) & ~15; };
+
+    // (SPLIT: a cluster has one tile at most, the host gives it as many clusters as there can be tiles)
+    if (warp == 0) {
+        const uint32_t one = elect_one();
+        uint32_t it = 0, s = 0, sp = 1;  // stages loaded, the place in the ring, the parity of a free one
+        bool ok = true;
+        for (int32_t t = first; ok && t < tiles; t += step) {
+            Tile x = tile_at(t);
+            x.e = uniform(x.e), x.row0 = uniform(x.row0), x.rows = uniform(x.rows);
+            // a pair's CTA loads its half of the tokens
+            const int part = PAIR ? mma_tokens(x) / 2 : x.rows, row = x.row0 + (PAIR ? (int)rank * part : 0);
+            const int loads = (part + p.abox - 1) / p.abox;
+            for (int32_t kb = 2 * sb_lo; kb < kb_hi; ++kb) {
+                ok = wait_warp(empty + 8 * s, sp, &abort_flag, p, kStatusTimeoutFree);
+                if (!ok) break;
+                const uint32_t d = data0 + s * p.stage_bytes, db = full + 8 * s;
+                if ((int32_t)it != p.dbg_skip) {
+                    expect_if(db, kMxRowsW * 128 + loads * p.abox * 128, one);
+                    tma_3d_if(d, &p.wc, kb * 128, x.n0, x.e, db, one);
+                    for (int i = 0; i < loads; ++i)
+                        tma_2d_if(d + kMxRowsW * 128 + i * p.abox * 128, &p.ac, kb * 128, row + i * p.abox, db, one);
+                }
+                ++it;
+                if (++s == (uint32_t)p.stages) s = 0, sp ^= 1;
+            }
+        }
+        if (lane == 0 && abort_flag) {  // the loads in flight end (bounded) before the CTA can exit
+            const long long t0 = clock64();
+            for (uint32_t i = it > (uint32_t)p.stages ? it - p.stages : 0; i < it; ++i)
+                while ((int32_t)i != p.dbg_skip && !bar_try(full + 8 * (i % p.stages), (i / p.stages) & 1) && clock64() - t0 < p.wait_cycles) {
+                }
+        }
+        __syncwarp();
+    } else if (warp == 1 && leader) {
+        const uint32_t one = elect_one();
+        uint32_t n = 0, s = 0, sp = 0, q = 0, qp = 0;
+        bool ok = true;
+        Tile x = {};
+        if (first < tiles) x = tile_at(first);
+        for (int32_t t = first; ok && t < tiles; t += step, ++n) {
+            const uint32_t acc = n & 1, d = tmem + acc * kMxMaxTok;
+            const uint32_t id = idesc_mx(PAIR ? 256 : 128, uniform(mma_tokens(x)), 0);
+            ok = wait_warp(aempty + 8 * acc, ((n >> 1) & 1) ^ 1, &abort_flag, p, kStatusTimeoutFree);
+            fence_after();
+            for (int32_t sb = sb_lo; ok && sb < sb_hi; ++sb) {
+                ok = wait_warp(sfull + 8 * q, qp, &abort_flag, p, kStatusTimeoutOperand);
+                for (int32_t kb = 2 * sb; ok && kb < min(2 * sb + 2, p.nkb); ++kb) {
+                    ok = wait_warp(full + 8 * s, sp, &abort_flag, p, kStatusTimeoutTma);
+                    if (PAIR) ok = ok && wait_warp(pfull + 8 * s, sp, &abort_flag, p, kStatusTimeoutTma);
+                    if (!ok) break;
+                    fence_after();
+                    const uint32_t sc = tmem + kScaleCol + (kb & 1) * kScaleCols;
+                    uint32_t src = scale0 + q * p.scale_bytes + (kb & 1) * 2 * kMxAtom * atoms;
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) {
+                        copy_scales<PAIR>(sc + 4 * w, src, one);
+                        copy_scales<PAIR>(sc + 8 + 8 * w, src + kMxAtom, one);
+                        if (atoms > 2) copy_scales<PAIR>(sc + 12 + 8 * w, src + 2 * kMxAtom, one);
+                        src += kMxAtom * atoms;
+                    }
+                    const uint64_t wd = desc_sw128(data0 + s * p.stage_bytes), ad = desc_sw128(data0 + s * p.stage_bytes + kMxRowsW * 128);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t w = j >> 1, sf = (j & 1) * 2;
+                        mma_mx<PAIR>(d, wd + 2 * j, ad + 2 * j, id | (sf << 4) | (sf << 29), sc + 4 * w, sc + 8 + 8 * w,
+                                     kb > 2 * sb_lo || j > 0, one);
+                    }
+                    commit_if<PAIR>(empty + 8 * s, one);
+                    if (++s == (uint32_t)p.stages) s = 0, sp ^= 1;
+                }
+                if (ok) commit_if<PAIR>(sempty + 8 * q, one);
+                if (++q == (uint32_t)p.scales) q = 0, qp ^= 1;
+            }
+            if (ok) commit_if<PAIR>(afull + 8 * acc, one);
+            if (t + step < tiles) x = tile_at(t + step);  // (while the MMAs run)
+        }
+        if (!ok) {  // the MMAs in flight end before tensor memory is freed
+            commit_if<PAIR>(drain, one, true);
+            const long long t0 = clock64();
+            while (!bar_try(drain, 0) && clock64() - t0 < p.wait_cycles) {
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        // a pair's second CTA tells the first what has arrived here
+        uint32_t s = 0, sp = 0;
+        bool ok = true;
+        for (int32_t t = first; ok && t < tiles; t += step)
+            for (int32_t kb = 2 * sb_lo; ok && kb < kb_hi; ++kb) {
+                ok = wait_warp(full + 8 * s, sp, &abort_flag, p, kStatusTimeoutTma);
+                if (ok && lane == 0) arrive_cluster(in_cta(pfull + 8 * s, 0));
+                if (++s == (uint32_t)p.stages) s = 0, sp ^= 1;
+            }
+        __syncwarp();
+    } else if (warp < kMxEpiWarp0) {
+        // scales to the tensor core's order; warp 2: W's rows, warp 3: the tokens, in one or two parts of 128.  A lane copies the
+        // 16 bytes of its rows 32 c + lane into the ring, raws - 1 stages ahead, and is the only one to read them there.
+        const uint32_t total = first < tiles ? (uint32_t)((tiles - first + step - 1) / step) * (uint32_t)(sb_hi - sb_lo) : 0;
+        const int part = warp - 2, parts = warp == 2 ? 1 : atoms - 1;
+        int32_t lt = first, lsb = sb_lo;  // the stage to load next
+        uint32_t lr = 0;
+        const uint8_t *base = nullptr;  // its rows: from `base` on, `pitch` apart, `rows` of them
+        int64_t pitch = 0;
+        int rows = 0;
+        auto begin = [&] {
+            if (lt >= tiles) return;
+            const Tile x = tile_at(lt);
+            base = warp == 2 ? p.w_scales + x.e * p.w_scales_stride + x.n0 * p.w_lds : p.a_scales + x.row0 * p.a_lds;
+            rows = warp == 2 ? p.N - x.n0 : x.rows;
+        };
+        pitch = warp == 2 ? p.w_lds : p.a_lds;
+        begin();
+        auto load = [&] {
+            if (lt < tiles) {
+                const uint32_t n = min(p.nb - 16 * lsb, 16);
+                const uint32_t dst = raw0 + lr * p.raw_bytes + part * kMxRowsW * 16 + lane * 16;
+                const uint8_t *src = base + 16 * lsb + lane * pitch;
+                const int last = warp == 2 ? 4 : (p.nt + 31) / 32;
+                for (int c = 0; c < last; ++c, src += 32 * pitch) {
+                    const bool in = 32 * c + lane < rows;
+                    cpa16(dst + c * 512, in ? src : base, in ? n : 0);
+                }
+                if (++lsb == sb_hi) {
+                    lsb = sb_lo;
+                    lt += step;
+                    begin();
+                }
+                if (++lr == (uint32_t)p.raws) lr = 0;
+            }
+            cpa_commit();
+        };
+        for (int i = 1; i < p.raws; ++i) load();
+        uint32_t r = 0, q = 0, qp = 1;
+        for (uint32_t st = 0; st < total; ++st) {
+            load();
+            copies_but(p.raws - 1);
+            const uint32_t src = raw0 + r * p.raw_bytes + part * kMxRowsW * 16 + lane * 16;
+            uint32_t w[2][4][4];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    w[i][c][0] = w[i][c][1] = w[i][c][2] = w[i][c][3] = 0;
+                    if (i < parts && (part == 0 || 128 * i + 32 * c < p.nt)) lds128(src + i * kMxRowsW * 16 + c * 512, w[i][c]);
+                }
+            if (!wait_warp(sempty + 8 * q, qp, &abort_flag, p, kStatusTimeoutFree)) break;
+            const uint32_t dst = scale0 + q * p.scale_bytes + part * kMxAtom + lane * 16;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (i < parts) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + i * kMxAtom + j * kMxAtom * atoms), "r"(w[i][0][j]),
+                                     "r"(w[i][1][j]), "r"(w[i][2][j]), "r"(w[i][3][j])
+                                     : "memory");
+                }
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                if constexpr (PAIR) arrive_cluster(in_cta(sfull + 8 * q, 0));
+                else bar_arrive(sfull + 8 * q);
+            }
+            if (++r == (uint32_t)p.raws) r = 0;
+            if (++q == (uint32_t)p.scales) q = 0, qp ^= 1;
+        }
+        copies_but(0);
+    } else {
+        const uint32_t quarter = (uint32_t)(warp & 3) << 21;  // lane field of the warp's 32 lanes
+        const int part = (warp - kMxEpiWarp0) >> 2, row = 32 * (warp & 3) + lane;
+        const uint32_t patch = patch0 + (warp - kMxEpiWarp0) * kMxPatch;
+        const uint32_t free0 = PAIR ? in_cta(aempty, 0) : aempty;
+        uint32_t n = 0;
+        Tile x = {};
+        if (first < tiles) x = tile_at(first);
+        for (int32_t t = first; t < tiles; t += step, ++n) {
+            const uint32_t acc = n & 1;
+            const int nn = x.n0 + row;
+            const float bias = !SPLIT && p.bias && nn < p.N ? p.bias[(int64_t)x.e * p.N + nn] : 0.0f;
+            if (!wait_warp(afull + 8 * acc, (n >> 1) & 1, &abort_flag, p, kStatusTimeoutMma)) break;
+            fence_after();
+            for (int c0 = 16 * part; c0 < x.rows; c0 += 64) {
+                uint32_t u[16];
+                tld<16>(tmem + quarter + acc * kMxMaxTok + c0, u);
+                twait<16>(u);
+                float v[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(u[i]);
+                if constexpr (SPLIT) {  // this CTA's part of the sums: [token][row of W] over the stages, which are all read
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(data0 + ((c0 + i) * kMxRowsW + row) * 4), "f"(v[i]) : "memory");
+                } else {
+                    store_chunk<ACT, T>(p, v, x, c0, nn, bias, patch, lane);
+                }
+            }
+            fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if constexpr (PAIR) arrive_cluster(free0 + 8 * acc);
+                else bar_arrive(aempty + 8 * acc);
+            }
+            if (t + step < tiles) x = tile_at(t + step);
+        }
+    }
+    if constexpr (SPLIT) {
+        __syncwarp();
+        cluster_sync();
+        if (first < tiles && !abort_flag && warp >= kMxEpiWarp0) {
+            // each CTA of the cluster finishes some chunks of 16 tokens x 32 rows of W
+            const Tile x = tile_at(first);
+            const int chunks = 4 * ((x.rows + 15) / 16), w = warp - kMxEpiWarp0;
+            for (int c = w + kMxEpiWarps * rank; c < chunks; c += kMxEpiWarps * p.splits) {
+                const int c0 = 16 * (c >> 2), row = 32 * (c & 3) + lane, nn = x.n0 + row;
+                const float bias = p.bias && nn < p.N ? p.bias[(int64_t)x.e * p.N + nn] : 0.0f;
+                float v[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+                for (int r = 0; r < p.splits; ++r) {
+                    const uint32_t at = in_cta(data0 + (c0 * kMxRowsW + row) * 4, r);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        float y;
+                        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(y) : "r"(at + i * kMxRowsW * 4) : "memory");
+                        v[i] += y;
+                    }
+                }
+                store_chunk<ACT, T>(p, v, x, c0, nn, bias, patch0 + w * kMxPatch, lane);
+            }
+        }
+    }
+    // rows of no expert are zero
+    if (p.offsets) {
+        const int64_t wide = ACT == ILW_ACT_SILU_GATE ? p.N / 2 : p.N;
+        const int64_t head = s_head, tail = s_tail, total = (head + p.M - tail) * wide;
+        for (int64_t i = blockIdx.x * (int64_t)kMxThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kMxThreads) {
+            const int64_t r = i / wide;
+            ((T *)p.Y)[(r < head ? r : r - head + tail) * p.ldy + (i - r * wide)] = to_out<T>(0.0f);
+        }
+    }
+    fence_before();
+    __syncwarp();
+    if constexpr (MODE != MX_ONE) cluster_sync();  // nothing of this CTA is read or signalled any more
+    else __syncthreads();
+    if (warp == 3) {
+        fence_after();
+        if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    }
+}
+
+template <int ACT, typename T, int MODE>
+cudaError_t launch_mode(const MxParams &p, int grid, size_t smem, cudaStream_t s) {
+    static SmemLimit limit;
+    cudaError_t e = raise_smem_limit(limit, (const void *)mx_gemm_kernel<ACT, T, MODE>, kMxSmemLimit);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = kMxThreads;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = MODE == MX_SPLIT ? p.splits : 2;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = MODE == MX_ONE ? 1 : 2;
+    e = cudaLaunchKernelEx(&cfg, mx_gemm_kernel<ACT, T, MODE>, p);
+    return e != cudaSuccess ? e : cudaGetLastError();
+}
+template <int ACT, typename T>
+cudaError_t launch_act(const MxParams &p, int grid, size_t smem, cudaStream_t s) {
+    if (p.mode == MX_SPLIT) return launch_mode<ACT, T, MX_SPLIT>(p, grid, smem, s);
+    if (p.mode == MX_PAIR) return launch_mode<ACT, T, MX_PAIR>(p, grid, smem, s);
+    return launch_mode<ACT, T, MX_ONE>(p, grid, smem, s);
+}
+
+}  // namespace
+
+template <typename T>
+cudaError_t launch_mx(const MxParams &p, int32_t act, int grid, size_t smem, cudaStream_t s) {
+    if (act == ILW_ACT_GELU) return launch_act<ILW_ACT_GELU, T>(p, grid, smem, s);
+    if (act == ILW_ACT_SILU_GATE) return launch_act<ILW_ACT_SILU_GATE, T>(p, grid, smem, s);
+    return launch_act<ILW_ACT_NONE, T>(p, grid, smem, s);
+}
+
+}  // namespace ilw

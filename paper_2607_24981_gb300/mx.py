@@ -5,10 +5,10 @@ run on the current CUDA stream, and nothing is computed here.
 """
 from __future__ import annotations
 
-import ctypes as C
+import struct
 from typing import NamedTuple
 
-from . import IlwError, _check, _ptr, _stream, lib
+from . import IlwError, _check, lib
 
 __all__ = ["MxTensor", "Routing", "mx_empty", "mx_quantize", "mx_dequantize", "mx_linear", "mx_grouped_linear", "moe_route", "moe_combine",
            "gate_rows", "MxExperts"]
@@ -17,16 +17,13 @@ FP32, FP16, BF16 = 232, 216, 217
 ACTS = {"none": 0, "gelu": 1, "silu_gate": 2}
 
 
-class MxGemmT(C.Structure):
-    _fields_ = [
-        ("struct_size", C.c_uint32),
-        ("a_codes", C.c_void_p), ("a_ldc", C.c_int64), ("a_scales", C.c_void_p), ("a_lds", C.c_int64),
-        ("w_codes", C.c_void_p), ("w_ldc", C.c_int64), ("w_codes_stride", C.c_int64),
-        ("w_scales", C.c_void_p), ("w_lds", C.c_int64), ("w_scales_stride", C.c_int64),
-        ("bias", C.c_void_p), ("offsets", C.c_void_p),
-        ("M", C.c_int64), ("N", C.c_int32), ("K", C.c_int32), ("experts", C.c_int32), ("act", C.c_int32), ("y_form", C.c_int32),
-        ("Y", C.c_void_p), ("ldy", C.c_int64),
-    ]
+# ilw_mx_gemm_t, in its natural alignment
+_GEMM = struct.Struct("@IPqPqPqqPqqPPqiiiiiPq")
+
+
+def gemm_struct(*fields) -> bytes:
+    """An ilw_mx_gemm_t of the given fields (all but struct_size)."""
+    return _GEMM.pack(_GEMM.size, *fields)
 
 
 class MxTensor(NamedTuple):
@@ -49,118 +46,141 @@ class Routing(NamedTuple):
     slot: object
 
 
-def _form(dtype) -> int:
-    import torch
-
-    forms = {torch.float32: FP32, torch.float16: FP16, torch.bfloat16: BF16}
-    if dtype not in forms:
-        raise IlwError(f"{dtype} is neither float32, float16 nor bfloat16")
-    return forms[dtype]
+# Calls of a few microseconds are common here, so each tensor's properties are read once, and torch's types are
+# looked up once (on first use: the package itself imports without torch).
+_T = None
 
 
-def _on(what, *tensors):
-    """Device tensors whose last dimension is contiguous."""
-    for t in tensors:
-        if t is not None and (not t.is_cuda or (t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1)):
-            raise IlwError(f"{what}: a tensor is not on the GPU, or its last dimension is not contiguous")
+class _Torch:
+    def __init__(self):
+        import torch
+
+        self.torch, self.empty = torch, torch.empty
+        self.u8, self.i32, self.f32, self.bf16 = torch.uint8, torch.int32, torch.float32, torch.bfloat16
+        self.form = {torch.float32: FP32, torch.float16: FP16, torch.bfloat16: BF16}
+        self.form_i8 = {**self.form, torch.int8: 8}
+        self.stream = torch._C._cuda_getCurrentRawStream
 
 
-def _row(t) -> int:
-    """Elements between rows (no or a single row may carry any stride: then at least what holds a row)."""
-    return t.stride(-2) if t.shape[-2] > 1 and t.numel() else max(t.stride(-2), t.shape[-1])
+def _torch() -> _Torch:
+    global _T
+    if _T is None:
+        _T = _Torch()
+    return _T
 
 
-def _ints(what, *tensors):
-    import torch
+def _float(T, what, t, forms=None):
+    """(form, rows, columns, elements between rows) of a float matrix on the GPU with contiguous rows.  No or a single row may
+    carry any stride: then at least what holds a row."""
+    form, shape, stride = (forms or T.form).get(t.dtype), t.shape, t.stride()
+    if form is None:
+        raise IlwError(f"{what}: {t.dtype} is none of {', '.join(str(d) for d in forms or T.form)}")
+    if len(shape) != 2:
+        raise IlwError(f"{what}: a tensor of {len(shape)} dimensions, not 2")
+    rows, cols = shape
+    if not t.is_cuda or (stride[1] != 1 and cols > 1 and rows > 0):
+        raise IlwError(f"{what}: a tensor is not on the GPU, or its rows are not contiguous")
+    return form, rows, cols, stride[0] if rows > 1 and cols > 0 else max(stride[0], cols)
 
-    for t in tensors:
-        if t is not None and (t.dtype != torch.int32 or not t.is_contiguous() or not t.is_cuda):
-            raise IlwError(f"{what}: indices, slots and offsets are contiguous int32 CUDA tensors")
+
+def _index(T, what, t):
+    if t.dtype is not T.i32 or not t.is_cuda or not t.is_contiguous():
+        raise IlwError(f"{what}: indices, slots and offsets are contiguous int32 CUDA tensors")
+    return t.data_ptr()
 
 
-def _parts(what, m: MxTensor, dims: int):
-    import torch
+def _weights(T, what, name, t, n):
+    if t.dtype is not T.f32 or not t.is_cuda or not t.is_contiguous() or t.numel() != n:
+        raise IlwError(f"{what}: {name} is a contiguous float32 CUDA tensor of {n} values")
+    return t.data_ptr()
 
-    nb = (m.k + 31) // 32
-    for t, width in ((m.codes, 16 * nb), (m.scales, nb)):
-        if t.dtype != torch.uint8 or t.dim() != dims or t.shape[-1] < width or t.shape[:-1] != m.codes.shape[:-1]:
-            raise IlwError(f"{what}: an MXFP4 tensor of k={m.k} has uint8 codes [..., {16 * nb}] and scales [..., >= {nb}] of {dims} dimensions")
-    _on(what, m.codes, m.scales)
+
+def _parts(T, what, m, dims):
+    """(shape, strides of codes, strides of scales) of an MXFP4 tensor."""
+    codes, scales, k = m
+    cs, ss, c, s = codes.shape, scales.shape, codes.stride(), scales.stride()
+    nb = (k + 31) >> 5
+    if codes.dtype is not T.u8 or scales.dtype is not T.u8 or len(cs) != dims or cs[-1] < 16 * nb or ss[-1] < nb or cs[:-1] != ss[:-1]:
+        raise IlwError(f"{what}: an MXFP4 tensor of k={k} has uint8 codes [..., {16 * nb}] and scales [..., >= {nb}] of {dims} dimensions")
+    if not codes.is_cuda or not scales.is_cuda or ((c[-1] != 1 or s[-1] != 1) and codes.numel()):
+        raise IlwError(f"{what}: codes or scales are not on the GPU, or their rows are not contiguous")
+    if cs[-2] <= 1 or not cs[-1]:  # (no or a single row may carry any stride)
+        c, s = (*c[:-2], max(c[-2], 16 * (-cs[-1] // -16)), 1), (*s[:-2], max(s[-2], 16 * (-ss[-1] // -16)), 1)
+    return cs, c, s
 
 
 def mx_empty(rows: int, k: int, device="cuda") -> MxTensor:
     """Room for ``rows`` rows of ``k`` values (uninitialised)."""
-    import torch
-
-    nb = (k + 31) // 32
-    return MxTensor(torch.empty((rows, 16 * nb), dtype=torch.uint8, device=device),
-                    torch.empty((rows, -(-nb // 16) * 16), dtype=torch.uint8, device=device), k)
+    T = _torch()
+    nb = (k + 31) >> 5
+    return MxTensor(T.empty((rows, 16 * nb), dtype=T.u8, device=device), T.empty((rows, (nb + 15) & ~15), dtype=T.u8, device=device), k)
 
 
 def mx_quantize(X, gather=None, out: MxTensor | None = None) -> MxTensor:
     """ilwdetr_mx_quantize: X [rows, K] (float32, float16, bfloat16 or int8), or its rows ``gather`` (int32; -1: a row of
     zeros), to MXFP4."""
-    import torch
-
-    if X.dim() != 2:
-        raise IlwError(f"mx_quantize: X has {X.dim()} dimensions, not 2")
-    _on("mx_quantize", X)
-    _ints("mx_quantize", gather)
-    form = 8 if X.dtype == torch.int8 else _form(X.dtype)
-    rows, K = (X.shape[0] if gather is None else gather.numel()), X.shape[1]
+    T = _torch()
+    form, x_rows, K, ldx = _float(T, "mx_quantize", X, T.form_i8)
+    rows, at = x_rows, None
+    if gather is not None:
+        rows, at = gather.numel(), _index(T, "mx_quantize", gather)
     if out is None:
         out = mx_empty(rows, K, X.device)
-    _parts("mx_quantize", out, 2)
-    if out.k != K or out.codes.shape[0] != rows:
-        raise IlwError(f"mx_quantize: out holds {out.codes.shape[0]} rows of {out.k}, not {rows} of {K}")
-    _check(lib().ilwdetr_mx_quantize(_ptr(X), form, _row(X), X.shape[0], _ptr(gather), rows, K, _ptr(out.codes), _row(out.codes),
-                                     _ptr(out.scales), _row(out.scales), _stream()), "mx_quantize")
+        nb = (K + 31) >> 5
+        ldc, lds = 16 * nb, (nb + 15) & ~15
+    else:
+        shape, c, s = _parts(T, "mx_quantize", out, 2)
+        ldc, lds = c[0], s[0]
+        if out.k != K or shape[0] != rows:
+            raise IlwError(f"mx_quantize: out holds {shape[0]} rows of {out.k}, not {rows} of {K}")
+    _check(lib().ilwdetr_mx_quantize(X.data_ptr(), form, ldx, x_rows, at, rows, K, out.codes.data_ptr(), ldc, out.scales.data_ptr(), lds,
+                                     T.stream(X.get_device())), "mx_quantize")
     return out
 
 
 def mx_dequantize(m: MxTensor, dtype=None, out=None):
     """ilwdetr_mx_dequantize: the values of an MXFP4 matrix, in float32 unless ``dtype`` says otherwise."""
-    import torch
-
-    _parts("mx_dequantize", m, 2)
+    T = _torch()
+    shape, c, s = _parts(T, "mx_dequantize", m, 2)
+    codes, scales, k = m
+    rows = shape[0]
     if out is None:
-        out = torch.empty((m.codes.shape[0], m.k), dtype=dtype or torch.float32, device=m.codes.device)
-    _on("mx_dequantize", out)
-    if tuple(out.shape) != (m.codes.shape[0], m.k):
-        raise IlwError(f"mx_dequantize: out is {tuple(out.shape)}, not {(m.codes.shape[0], m.k)}")
-    _check(lib().ilwdetr_mx_dequantize(_ptr(m.codes), _row(m.codes), _ptr(m.scales), _row(m.scales), m.codes.shape[0], m.k,
-                                       _ptr(out), _form(out.dtype), _row(out), _stream()), "mx_dequantize")
+        out = T.empty((rows, k), dtype=dtype or T.f32, device=codes.device)
+    form, r, n, ldy = _float(T, "mx_dequantize", out)
+    if r != rows or n != k:
+        raise IlwError(f"mx_dequantize: out is {(r, n)}, not {(rows, k)}")
+    _check(lib().ilwdetr_mx_dequantize(codes.data_ptr(), c[0], scales.data_ptr(), s[0], rows, k, out.data_ptr(), form, ldy,
+                                       T.stream(codes.get_device())), "mx_dequantize")
     return out
 
 
 def _gemm(what, A, W, offsets, bias, act, out_dtype, out):
-    import torch
-
-    _parts(what, A, 2)
-    _parts(what, W, 2 if offsets is None else 3)
-    _ints(what, offsets)
-    if act not in ACTS:
+    T = _torch()
+    (M, _), ac, as_ = _parts(T, what, A, 2)
+    code = ACTS.get(act)
+    if code is None:
         raise IlwError(f"{what}: act {act!r} is none of {', '.join(ACTS)}")
-    experts = 1 if offsets is None else W.codes.shape[0]
-    M, N = A.codes.shape[0], W.codes.shape[-2]
+    if offsets is None:
+        (N, _), wc, ws = _parts(T, what, W, 2)
+        experts, off, between = 1, None, (0, 0)
+    else:
+        (experts, N, _), wc, ws = _parts(T, what, W, 3)
+        off, between = _index(T, what, offsets), (wc[0], ws[0])
+        if offsets.numel() != experts + 1:
+            raise IlwError(f"{what}: {experts} experts need {experts + 1} offsets, not {offsets.numel()}")
     if A.k != W.k:
         raise IlwError(f"{what}: A has k={A.k}, W k={W.k}")
-    if offsets is not None and offsets.numel() != experts + 1:
-        raise IlwError(f"{what}: {experts} experts need {experts + 1} offsets, not {offsets.numel()}")
-    if bias is not None and (bias.dtype != torch.float32 or not bias.is_contiguous() or not bias.is_cuda or bias.numel() != experts * N):
-        raise IlwError(f"{what}: bias is a contiguous float32 tensor of {experts * N} values")
-    wide = N // 2 if act == "silu_gate" else N
+    wide = N // 2 if code == 2 else N
+    device = A.codes.get_device()
     if out is None:
-        out = torch.empty((M, wide), dtype=out_dtype or torch.bfloat16, device=A.codes.device)
-    _on(what, out)
-    if tuple(out.shape) != (M, wide):
-        raise IlwError(f"{what}: out is {tuple(out.shape)}, not {(M, wide)}")
-    between = (lambda t: t.stride(0)) if offsets is not None else (lambda t: 0)
-    desc = MxGemmT(C.sizeof(MxGemmT), A.codes.data_ptr(), _row(A.codes), A.scales.data_ptr(), _row(A.scales),
-                   W.codes.data_ptr(), _row(W.codes), between(W.codes), W.scales.data_ptr(), _row(W.scales), between(W.scales),
-                   None if bias is None else bias.data_ptr(), None if offsets is None else offsets.data_ptr(),
-                   M, N, A.k, experts, ACTS[act], _form(out.dtype), out.data_ptr(), _row(out))
-    _check(lib().ilwdetr_mx_gemm(C.byref(desc), _stream()), what)
+        out = T.empty((M, wide), dtype=out_dtype or T.bf16, device=A.codes.device)
+    form, r, n, ldy = _float(T, what, out)
+    if r != M or n != wide:
+        raise IlwError(f"{what}: out is {(r, n)}, not {(M, wide)}")
+    desc = gemm_struct(A.codes.data_ptr(), ac[0], A.scales.data_ptr(), as_[0], W.codes.data_ptr(), wc[-2], between[0], W.scales.data_ptr(),
+                       ws[-2], between[1], 0 if bias is None else _weights(T, what, "bias", bias, experts * N), off or 0, M, N, A.k, experts,
+                       code, form, out.data_ptr(), ldy)
+    _check(lib().ilwdetr_mx_gemm(desc, T.stream(device)), what)
     return out
 
 
@@ -174,48 +194,49 @@ def mx_linear(A: MxTensor, W: MxTensor, bias=None, act="none", out_dtype=None, o
 def mx_grouped_linear(A: MxTensor, W: MxTensor, offsets, bias=None, act="none", out_dtype=None, out=None):
     """ilwdetr_mx_gemm by expert: rows offsets[e] .. offsets[e + 1] - 1 of A times W[e] (W [E, N, K], bias [E, N]; offsets int32
     [E + 1] on the device).  Rows of no expert are zero."""
+    if offsets is None:
+        raise IlwError("mx_grouped_linear: offsets are needed")
     return _gemm("mx_grouped_linear", A, W, offsets, bias, act, out_dtype, out)
 
 
-def moe_route(logits, k: int, renormalize=True, workspace=None) -> Routing:
+def moe_route(logits, k: int, renormalize=True) -> Routing:
     """ilwdetr_moe_route: the k experts of each row of logits [T, E], their weights, and the rows' order by expert."""
-    import torch
-
-    if logits.dim() != 2:
-        raise IlwError(f"moe_route: logits have {logits.dim()} dimensions, not 2")
-    _on("moe_route", logits)
-    T, E = logits.shape
-    dev = logits.device
-    need = int(lib().ilwdetr_moe_route_workspace_bytes(T, E))
+    t = _torch()
+    form, T, E, ld = _float(t, "moe_route", logits)
+    dev, L = logits.device, lib()
     kk = max(k, 0)  # (the entry point refuses k < 1)
-    i32 = torch.empty(3 * T * kk + E + 1, dtype=torch.int32, device=dev)
-    expert, source, slot, offsets = i32.split([T * kk, T * kk, T * kk, E + 1])
-    r = Routing(expert.view(T, kk), torch.empty((T, kk), dtype=torch.float32, device=dev), offsets, source, slot.view(T, kk))
-    if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    _check(lib().ilwdetr_moe_route(_ptr(logits), _form(logits.dtype), _row(logits), T, E, k, int(bool(renormalize)), _ptr(r.expert),
-                                   _ptr(r.weight), _ptr(r.offsets), _ptr(r.source), _ptr(r.slot), _ptr(workspace),
-                                   workspace.numel() * workspace.element_size(), _stream()), "moe_route")
-    return r
+    need = L.ilwdetr_moe_route_workspace_bytes(T, E)
+    expert, slot = t.empty((T, kk), dtype=t.i32, device=dev), t.empty((T, kk), dtype=t.i32, device=dev)
+    source, offsets = t.empty((T * kk,), dtype=t.i32, device=dev), t.empty((E + 1,), dtype=t.i32, device=dev)
+    weight = t.empty((T, kk), dtype=t.f32, device=dev)
+    workspace = t.empty((need,), dtype=t.u8, device=dev) if need else None
+    _check(L.ilwdetr_moe_route(logits.data_ptr(), form, ld, T, E, k, 1 if renormalize else 0, expert.data_ptr(), weight.data_ptr(),
+                               offsets.data_ptr(), source.data_ptr(), slot.data_ptr(), workspace.data_ptr() if need else None, need,
+                               t.stream(logits.get_device())), "moe_route")
+    return Routing(expert, weight, offsets, source, slot)
 
 
 def moe_combine(Y, slot, weight, residual=None, out=None):
     """ilwdetr_moe_combine: out[t] = (residual[t] +) sum_j weight[t, j] Y[slot[t, j]], in Y's type."""
-    import torch
-
-    _on("moe_combine", Y, residual, out)
-    _ints("moe_combine", slot)
+    t = _torch()
+    form, rows, N, ldy = _float(t, "moe_combine", Y)
+    at = _index(t, "moe_combine", slot)
     T, k = slot.shape
-    if weight.dtype != torch.float32 or not weight.is_contiguous() or not weight.is_cuda or tuple(weight.shape) != (T, k):
-        raise IlwError(f"moe_combine: weight is a contiguous float32 tensor {(T, k)}")
-    N = Y.shape[1]
+    w = _weights(t, "moe_combine", "weight", weight, T * k)
     if out is None:
-        out = torch.empty((T, N), dtype=Y.dtype, device=Y.device)
-    for t in (residual, out):
-        if t is not None and (t.dtype != Y.dtype or tuple(t.shape) != (T, N)):
-            raise IlwError(f"moe_combine: residual and out are {Y.dtype} {(T, N)}")
-    _check(lib().ilwdetr_moe_combine(_ptr(Y), _form(Y.dtype), _row(Y), Y.shape[0], _ptr(slot), _ptr(weight), T, k, N, _ptr(residual),
-                                     0 if residual is None else _row(residual), _ptr(out), _row(out), _stream()), "moe_combine")
+        out, ldo = t.empty((T, N), dtype=Y.dtype, device=Y.device), N
+    else:
+        f, r, n, ldo = _float(t, "moe_combine", out)
+        if (f, r, n) != (form, T, N):
+            raise IlwError(f"moe_combine: out is {out.dtype} {(r, n)}, not {Y.dtype} {(T, N)}")
+    res, ldr = None, 0
+    if residual is not None:
+        f, r, n, ldr = _float(t, "moe_combine", residual)
+        res = residual.data_ptr()
+        if (f, r, n) != (form, T, N):
+            raise IlwError(f"moe_combine: residual is {residual.dtype} {(r, n)}, not {Y.dtype} {(T, N)}")
+    _check(lib().ilwdetr_moe_combine(Y.data_ptr(), form, ldy, rows, at, w, T, k, N, res, ldr, out.data_ptr(), ldo,
+                                     t.stream(Y.get_device())), "moe_combine")
     return out
 
 

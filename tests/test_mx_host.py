@@ -59,17 +59,17 @@ def test_dequantize_checks(L):
 def test_gemm_checks(L):
     from paper_2607_24981_gb300 import mx
 
-    def g(**over):
-        p = mx.MxGemmT(ctypes.sizeof(mx.MxGemmT), 0x100000, 128, 0x200000, 16, 0x300000, 128, 128 * 64, 0x400000, 16, 16 * 64, None, None,
-                       300, 64, 256, 1, 0, 217, 0x500000, 64)
-        for k, v in over.items():
-            setattr(p, k, v)
-        return L.ilwdetr_mx_gemm(ctypes.byref(p), None)
+    fields = dict(a_codes=0x100000, a_ldc=128, a_scales=0x200000, a_lds=16, w_codes=0x300000, w_ldc=128, w_codes_stride=128 * 64,
+                  w_scales=0x400000, w_lds=16, w_scales_stride=16 * 64, bias=0, offsets=0, M=300, N=64, K=256, experts=1, act=0, y_form=217,
+                  Y=0x500000, ldy=64)
 
-    assert g() == 0 and g(M=0, Y=None, a_codes=None) == 0 and g(N=0) == 0
+    def g(**over):
+        return L.ilwdetr_mx_gemm(mx.gemm_struct(*{**fields, **over}.values()), None)
+
+    assert g() == 0 and g(M=0, Y=0, a_codes=0) == 0 and g(N=0) == 0
     assert g(offsets=0x600000, experts=5, bias=0x700000) == 0
     assert g(act=2, ldy=32) == 0  # a gated result has half the columns
-    refused(L, g(struct_size=8), -1, b"struct_size")
+    refused(L, L.ilwdetr_mx_gemm(bytes(200), None), -1, b"struct_size")
     refused(L, L.ilwdetr_mx_gemm(None, None), -1, b"struct_size")
     refused(L, g(act=3), -1, b"act")
     refused(L, g(y_form=8), -1, b"y_form")
@@ -81,7 +81,7 @@ def test_gemm_checks(L):
     refused(L, g(M=(1 << 31) - 2048, N=1 << 20, ldy=1 << 20), -2, b"too large")
     refused(L, g(a_codes=0x100008), -1, b"a_codes")
     refused(L, g(a_ldc=112), -1, b"a_codes")
-    refused(L, g(w_scales=None), -1, b"w_scales")
+    refused(L, g(w_scales=0), -1, b"w_scales")
     refused(L, g(w_lds=24), -1, b"w_scales")
     refused(L, g(offsets=0x600000, experts=5, w_codes_stride=0), -1, b"strides")
     refused(L, g(offsets=0x600000, experts=5, w_scales_stride=1032), -1, b"strides")
@@ -91,11 +91,11 @@ def test_gemm_checks(L):
 
 
 def test_route_and_combine_check(L):
-    def r(logits=V, form=217, ld=64, T=100, E=64, k=4, offsets=V, slot=V, ws=V, size=1 << 20):
+    def r(logits=V, form=217, ld=64, T=5000, E=64, k=4, offsets=V, slot=V, ws=V, size=1 << 20):
         return L.ilwdetr_moe_route(logits, form, ld, T, E, k, 1, V, V, offsets, V, slot, ws, size, None)
 
     assert r() == 0 and r(T=0, logits=None, slot=None) == 0
-    assert L.ilwdetr_moe_route_workspace_bytes(0, 64) >= 4 * 64
+    assert r(T=16, ws=None, size=0) == 0 and L.ilwdetr_moe_route_workspace_bytes(16, 64) == 0  # one CTA needs none
     refused(L, r(form=8), -1, b"form")
     refused(L, r(k=0), -1, b"sizes")
     refused(L, r(k=65), -1, b"sizes")
