@@ -43,17 +43,38 @@ cudaError_t launch_mx_gemm(const MxGemmProblem &g, cudaStream_t s) {
     gemm_debug_wait(&p.dbg_skip, &p.wait_cycles);
     const int64_t sms = sm_count();
 
-    // Tokens a tile: as wide as the tokens (of an expert, twice the mean) fill, at most 224.
+    const int64_t out = g.act == ILW_ACT_SILU_GATE ? g.N / 2 : g.N;
+    p.wide = g.form != ILW_FP32 && out % 8 == 0 && (uintptr_t)g.Y % 16 == 0 && g.ldy % 8 == 0;
+    const int fixed = 1024 + (g.experts + 1) * (int)sizeof(MxExpert) + g.experts * 4 + (p.wide ? kMxEpiWarps * kMxPatch : 0);
+    auto bytes = [&] { return fixed + p.stages * p.stage_bytes + p.raws * p.raw_bytes + 2 * p.scale_bytes; };
+
+    // Tokens a tile: as wide as the tokens (of an expert, twice the mean) fill, at most 224, and what leaves room for four stages.
     const int64_t per = g.offsets ? (2 * g.M + g.experts - 1) / g.experts : g.M;
     p.nt = (int32_t)std::min<int64_t>(kMxMaxTok, (std::min(per, g.M) + 15) / 16 * 16);
     if (p.nt > 32) p.nt = (p.nt + 31) / 32 * 32;
-    auto token_tiles = [&] { return g.offsets ? std::min<int64_t>(g.M, g.M / p.nt + g.experts) : (g.M + p.nt - 1) / p.nt; };  // at most
-    // Pairs where they fill the chip with tiles wide enough to be bound by operands
-    const int64_t pair_tiles = token_tiles() * ((g.N + 2 * kMxRowsW - 1) / (2 * kMxRowsW));
-    p.mode = p.nt >= 64 && g.N > kMxRowsW && 2 * pair_tiles >= sms ? MX_PAIR : MX_ONE;
-    const int rows_w = p.mode == MX_PAIR ? 2 * kMxRowsW : kMxRowsW;
-    p.wtiles = (g.N + rows_w - 1) / rows_w;
-    const int64_t tiles = token_tiles() * p.wtiles;
+    int64_t tiles;
+    for (;; p.nt -= 32) {
+        const int64_t token_tiles = g.offsets ? std::min<int64_t>(g.M, g.M / p.nt + g.experts) : (g.M + p.nt - 1) / p.nt;  // at most
+        // Pairs where they fill the chip with tiles wide enough to be bound by operands
+        const int64_t pair_tiles = token_tiles * ((g.N + 2 * kMxRowsW - 1) / (2 * kMxRowsW));
+        p.mode = p.nt >= 64 && g.N > kMxRowsW && 2 * pair_tiles >= sms ? MX_PAIR : MX_ONE;
+        const int rows_w = p.mode == MX_PAIR ? 2 * kMxRowsW : kMxRowsW;
+        p.wtiles = (g.N + rows_w - 1) / rows_w;
+        tiles = token_tiles * p.wtiles;
+        const int32_t tokens = p.mode == MX_PAIR ? p.nt / 2 : p.nt;  // whose codes a CTA loads
+        p.abox = g.offsets ? 0 : tokens;
+        p.stage_bytes = kMxRowsW * 128 + tokens * 128;
+        p.raw_bytes = kMxRowsW * 16 + (p.nt + 31) / 32 * 512;
+        p.scale_bytes = 4 * kMxAtom * (1 + (p.nt + 127) / 128);
+        // rings: as many data stages as fit, the scales' loads as far ahead
+        p.raws = 4;
+        for (p.stages = kMxMaxStages; p.stages >= kMxMinStages && bytes() > kMxSmemLimit; --p.stages) {
+        }
+        p.raws = kMxMaxRaw;
+        if (bytes() > kMxSmemLimit) p.raws = 4;
+        if (p.stages >= kMxMinStages) break;
+        if (p.nt <= 32) return cudaErrorInvalidValue;
+    }
     if (tiles > INT32_MAX) return cudaErrorInvalidValue;
     // t / wtiles for t < 2^31 (round-up reciprocal of Granlund and Montgomery, 1994)
     while ((1ll << p.wdiv_s) < p.wtiles) ++p.wdiv_s;
@@ -64,32 +85,14 @@ cudaError_t launch_mx_gemm(const MxGemmProblem &g, cudaStream_t s) {
         while (p.splits < 8 && 2 * p.splits * tiles <= sms && 2 * p.splits <= p.nsb) p.splits *= 2;
     if (p.splits > 1) p.mode = MX_SPLIT;
 
-    const int32_t tokens = p.mode == MX_PAIR ? p.nt / 2 : p.nt;  // whose codes a CTA loads
-    p.abox = !g.offsets || tokens <= 32 ? tokens : tokens % 32 ? 16 : 32;
-    p.stage_bytes = kMxRowsW * 128 + tokens * 128;
-    p.raw_bytes = kMxRowsW * 16 + (p.nt + 31) / 32 * 512;
-    p.scale_bytes = 4 * kMxAtom * (1 + (p.nt + 127) / 128);
-    const int64_t out = g.act == ILW_ACT_SILU_GATE ? g.N / 2 : g.N;
-    p.wide = g.form != ILW_FP32 && out % 8 == 0 && (uintptr_t)g.Y % 16 == 0 && g.ldy % 8 == 0;
-    // rings: as many data stages as fit, the scales' loads as far ahead, two stages of scales in order, or three
-    const int fixed = 1024 + (g.experts + 1) * (int)sizeof(MxExpert) + g.experts * 4 + (p.wide ? kMxEpiWarps * kMxPatch : 0);
-    p.scales = 2;
-    auto bytes = [&] { return fixed + p.stages * p.stage_bytes + p.raws * p.raw_bytes + p.scales * p.scale_bytes; };
-    p.stages = kMxMaxStages;
-    for (;; --p.stages) {
-        p.raws = std::min(kMxMaxRaw, std::max(3, p.stages / 2 + 1));
-        if (bytes() <= kMxSmemLimit) break;
-        if (p.stages == 2) return cudaErrorInvalidValue;
-    }
-    ++p.scales;
-    if (bytes() > kMxSmemLimit) --p.scales;
-
     p.nb = (g.K + 31) / 32;
     p.w_scales = g.w_scales, p.w_lds = g.w_lds, p.w_scales_stride = g.w_scales_stride;
     p.a_scales = g.a_scales, p.a_lds = g.a_lds;
     if (!code_map(&p.wc, g.w_codes, 16 * p.nb, g.N, g.w_ldc, g.experts, g.w_codes_stride, kMxRowsW) ||
-        !code_map(&p.ac, g.a_codes, 16 * p.nb, g.M, g.a_ldc, 0, 0, p.abox))
+        !code_map(&p.ac[0], g.a_codes, 16 * p.nb, g.M, g.a_ldc, 0, 0, p.abox ? p.abox : 16))
         return cudaErrorInvalidValue;
+    for (int i = 1; i < 4 && !p.abox; ++i)
+        if (!code_map(&p.ac[i], g.a_codes, 16 * p.nb, g.M, g.a_ldc, 0, 0, 16 << i)) return cudaErrorInvalidValue;
     int grid = (int)std::min<int64_t>(tiles, sms);
     if (p.mode == MX_SPLIT) grid = (int)tiles * p.splits;
     if (p.mode == MX_PAIR) grid = 2 * (int)std::min<int64_t>(tiles, sms / 2);

@@ -19,16 +19,19 @@
 // the tokens.  One CTA's shared memory takes 45 KB of operands for each 256 of K of its tile and gives them to the
 // tensor core once, at 128 bytes a clock 700 clocks for MMAs of 450; in a pair it is 30 KB.
 //
-// Scales are stored row-major, 16 bytes of a row for 512 values of K.  Two warps bring them in by asynchronous copies
+// Scales are stored row-major, 16 bytes of a row for 512 values of K.  Two pairs of warps, in turn (one took 1400 clocks
+// for its chain of latencies, half as much again as the MMAs), bring them in by asynchronous copies
 // of 16 bytes (TMA boxes 16 bytes wide held up the loads of the codes behind them), a lane its own rows, and
 // write them, still in shared memory, in the order in which tcgen05.cp brings them to tensor memory (lane i,
 // column c: row 32 c + i; the four scales of 128 values of K to a word), so rows may start anywhere; the copies
 // and the MMAs that read them follow one another in the tensor pipe without a wait.
 //
-// One CTA per SM, 20 warps: TMA producer, MMA issuer, 2 scale warps, 16 epilogue warps (four on each scheduler: with
-// two, the activation's chains of latency set the time of a short K).  Two accumulators let a tile's epilogue overlap
-// the next tile's MMAs.  Tiles are dealt out in turn; with experts each CTA works out the list of tiles from
-// the offsets itself, so no count has to reach the host.
+// One CTA per SM, 23 warps: the loads of W and of A, the MMAs, 4 scale warps, 16 epilogue warps (four on each scheduler:
+// with two, the activation's chains of latency set the time of a short K).  A wait on a barrier takes a warp some
+// 100 clocks even when there is nothing to wait for, and 256 of K are 450 clocks of MMAs, so each of these roles waits
+// once in that time: everything that a block of K needs arrives at one barrier.  Two accumulators let a tile's
+// epilogue overlap the next tile's MMAs.  Tiles are dealt out in turn; with experts each CTA works out the list
+// of tiles from the offsets itself, so no count has to reach the host.
 //
 // Every mbarrier wait is bounded; on expiry the kernel latches the device status word, stops issuing
 // work, waits for its loads and MMAs in flight and frees its tensor memory.
@@ -47,8 +50,8 @@ namespace ilw {
 
 constexpr int kMxRowsW = 128;   // rows of W a CTA
 constexpr int kMxMaxTok = 224;  // tokens a tile
-constexpr int kMxMaxStages = 16, kMxMaxRaw = 6, kMxMaxScale = 4;
-constexpr int kMxEpiWarp0 = 4, kMxEpiWarps = 16, kMxThreads = 32 * (kMxEpiWarp0 + kMxEpiWarps);
+constexpr int kMxMaxStages = 16, kMxMinStages = 4, kMxMaxRaw = 6;
+constexpr int kMxEpiWarp0 = 7, kMxEpiWarps = 16, kMxThreads = 32 * (kMxEpiWarp0 + kMxEpiWarps);
 constexpr int kMxAtom = 512;    // bytes of the scales of 128 rows and 128 values of K
 constexpr int kMxPatch = 1024;  // bytes of shared memory in which an epilogue warp turns 2-byte results
 constexpr int kMxSmemLimit = 226 * 1024;  // dynamic; the barriers are static
@@ -60,7 +63,7 @@ struct MxExpert {
 };
 
 struct MxParams {
-    CUtensorMap wc, ac;     // codes of W [E, N, .] and A [M, .]
+    CUtensorMap wc, ac[4];  // codes of W [E, N, .]; of A [M, .] in boxes of abox rows, or of 16, 32, 64 and 128
     const uint8_t *w_scales, *a_scales;
     int64_t w_lds, w_scales_stride, a_lds;
     int32_t nb;             // scale bytes of a row
@@ -73,8 +76,8 @@ struct MxParams {
     int32_t wtiles;         // tiles of rows of W (128, or 256 a pair)
     uint32_t wdiv_m, wdiv_s;  // division by wtiles
     int32_t nt;             // most tokens a tile, a multiple of 16 (a pair's: of 32)
-    int32_t abox;           // rows of A a TMA box
-    int32_t stages, raws, scales;  // ring sizes: data, scales as loaded (2 to kMxMaxRaw), scales as the tensor core takes them
+    int32_t abox;           // rows of A a TMA box, one a stage; 0: as many boxes of 128 to 16 rows as its rows take
+    int32_t stages, raws;   // ring sizes: data, scales as loaded (4 or 6)
     int32_t stage_bytes, raw_bytes, scale_bytes;
     int32_t wide;           // 2-byte rows of Y take 16-byte stores
     int32_t splits;         // CTAs of a cluster that share a tile's K (SPLIT)
@@ -196,12 +199,14 @@ __device__ __forceinline__ void commit_if(uint32_t bar, uint32_t issue, bool loc
             : "memory");
     }
 }
+// Descriptor of scales in order: rows of 16 bytes, eight of them (128 bytes) a core matrix, no swizzle
+__device__ __forceinline__ uint64_t scale_desc(uint32_t saddr) {
+    return (uint64_t)((saddr >> 4) & 0x3FFFu) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
+}
 // Shared memory to tensor memory (of a pair: in both CTAs, each its own): 32 rows of 16 bytes to 4 columns of 32 lanes, the
 // same for each quarter of the lanes.
 template <bool PAIR>
-__device__ __forceinline__ void copy_scales(uint32_t t, uint32_t saddr, uint32_t issue) {
-    // rows of 16 bytes, eight of them (128 bytes) a core matrix, no swizzle
-    const uint64_t d = (uint64_t)((saddr >> 4) & 0x3FFFu) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
+__device__ __forceinline__ void copy_scales(uint32_t t, uint64_t d, uint32_t issue) {
     if constexpr (PAIR)
         asm volatile(
             "{\n .reg .pred q;\n setp.ne.b32 q, %2, 0;\n @q tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n}\n" ::"r"(t), "l"(d), "r"(issue)
@@ -369,14 +374,14 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
     // W's rows, 2 x 8 of A's)
     constexpr int kScaleCol = 2 * kMxMaxTok, kScaleCols = 24;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bars[3 * kMxMaxStages + 2 * kMxMaxScale + 5];
+    __shared__ uint64_t bars[3 * kMxMaxStages + 5];
     __shared__ uint32_t tmem_base;
     __shared__ volatile int abort_flag;
     __shared__ int32_t s_experts, s_head, s_tail;  // experts with rows; rows before the first and from the end of the last
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t data0 = (su32(smem_raw) + 1023) & ~1023u;
     const uint32_t raw0 = data0 + p.stages * p.stage_bytes, scale0 = raw0 + p.raws * p.raw_bytes;
-    const uint32_t patch0 = scale0 + p.scales * p.scale_bytes;
+    const uint32_t patch0 = scale0 + 2 * p.scale_bytes;
     MxExpert *tab = (MxExpert *)(smem_raw + (patch0 - su32(smem_raw)) + (p.wide ? kMxEpiWarps * kMxPatch : 0));
     int32_t *tab_id = (int32_t *)(tab + p.E + 1);
 
@@ -386,23 +391,27 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
         next_bar += 8 * n;
         return at;
     };
-    const uint32_t full = take(kMxMaxStages), empty = take(kMxMaxStages), pfull = take(kMxMaxStages);    // data; pfull: the other CTA's
-    const uint32_t sfull = take(kMxMaxScale), sempty = take(kMxMaxScale);                                // scales in order (a pair's: at the first CTA)
-    const uint32_t afull = take(2), aempty = take(2), drain = take(1);                                   // accumulators
+    // full: a block of K is there, codes and scales (a pair's, at the first CTA: in both); its own: this CTA's codes are, for
+    // the second CTA of a pair to pass on
+    const uint32_t full = take(kMxMaxStages), empty = take(kMxMaxStages), own = take(kMxMaxStages);
+    const uint32_t afull = take(2), aempty = take(2), drain = take(1);  // accumulators
 
     const uint32_t rank = SPLIT ? blockIdx.x % p.splits : PAIR ? blockIdx.x & 1 : 0;
     const bool leader = !PAIR || rank == 0;
     if (threadIdx.x == 0) {
         abort_flag = 0;
-        for (int i = 0; i < kMxMaxStages; ++i) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 1), bar_init(pfull + 8 * i, 1);
-        for (int i = 0; i < kMxMaxScale; ++i) bar_init(sfull + 8 * i, PAIR ? 4 : 2), bar_init(sempty + 8 * i, 1);
+        for (int i = 0; i < kMxMaxStages; ++i) {
+            bar_init(full + 8 * i, PAIR ? 2 + 1 + 4 : 2 + 2);  // loads, the second CTA's word, scale warps
+            bar_init(empty + 8 * i, 1);
+            bar_init(own + 8 * i, 2);
+        }
         for (int i = 0; i < 2; ++i) bar_init(afull + 8 * i, 1), bar_init(aempty + 8 * i, PAIR ? 2 * kMxEpiWarps : kMxEpiWarps);
         bar_init(drain, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (threadIdx.x == 32) {
         prefetch_map(&p.wc);
-        prefetch_map(&p.ac);
+        prefetch_map(&p.ac[0]);
     }
     if (warp == 3) {
         if constexpr (PAIR) {
@@ -477,8 +486,10 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
     auto mma_tokens = [&](const Tile &x) { return PAIR ? (x.rows + 31) & ~31 : (x.rows + 15) & ~15; };
 
     // (SPLIT: a cluster has one tile at most, the host gives it as many clusters as there can be tiles)
-    if (warp == 0) {
+    if (warp == 0 || warp == 4) {
+        // loads of the codes: warp 0 of W, warp 4 of A
         const uint32_t one = elect_one();
+        const uint32_t arrives = leader ? full : own;
         uint32_t it = 0, s = 0, sp = 1;  // stages loaded, the place in the ring, the parity of a free one
         bool ok = true;
         for (int32_t t = first; ok && t < tiles; t += step) {
@@ -486,31 +497,44 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
             x.e = uniform(x.e), x.row0 = uniform(x.row0), x.rows = uniform(x.rows);
             // a pair's CTA loads its half of the tokens
             const int part = PAIR ? mma_tokens(x) / 2 : x.rows, row = x.row0 + (PAIR ? (int)rank * part : 0);
-            const int loads = (part + p.abox - 1) / p.abox;
+            const int units = (part + 15) >> 4;
+            const uint32_t bytes = warp == 0 ? kMxRowsW * 128 : p.abox ? p.abox * 128 : units * 2048;
             for (int32_t kb = 2 * sb_lo; kb < kb_hi; ++kb) {
                 ok = wait_warp(empty + 8 * s, sp, &abort_flag, p, kStatusTimeoutFree);
                 if (!ok) break;
-                const uint32_t d = data0 + s * p.stage_bytes, db = full + 8 * s;
+                const uint32_t d = data0 + s * p.stage_bytes + (warp == 0 ? 0 : kMxRowsW * 128), db = arrives + 8 * s;
                 if ((int32_t)it != p.dbg_skip) {
-                    expect_if(db, kMxRowsW * 128 + loads * p.abox * 128, one);
-                    tma_3d_if(d, &p.wc, kb * 128, x.n0, x.e, db, one);
-                    for (int i = 0; i < loads; ++i)
-                        tma_2d_if(d + kMxRowsW * 128 + i * p.abox * 128, &p.ac, kb * 128, row + i * p.abox, db, one);
+                    expect_if(db, bytes, one);
+                    if (warp == 0) {
+                        tma_3d_if(d, &p.wc, kb * 128, x.n0, x.e, db, one);
+                    } else if (p.abox) {
+                        tma_2d_if(d, &p.ac[0], kb * 128, row, db, one);
+                    } else {
+                        int done = 0;  // (units of 16 rows)
+#pragma unroll
+                        for (int i = 3; i >= 0; --i)
+                            if (units & (1 << i)) {
+                                tma_2d_if(d + done * 2048, &p.ac[i], kb * 128, row + done * 16, db, one);
+                                done += 1 << i;
+                            }
+                    }
                 }
                 ++it;
                 if (++s == (uint32_t)p.stages) s = 0, sp ^= 1;
             }
         }
         if (lane == 0 && abort_flag) {  // the loads in flight end (bounded) before the CTA can exit
+            // (the barrier may miss other arrivals, so the limit is short: a load takes microseconds)
             const long long t0 = clock64();
             for (uint32_t i = it > (uint32_t)p.stages ? it - p.stages : 0; i < it; ++i)
-                while ((int32_t)i != p.dbg_skip && !bar_try(full + 8 * (i % p.stages), (i / p.stages) & 1) && clock64() - t0 < p.wait_cycles) {
+                while (!bar_try(arrives + 8 * (i % p.stages), (i / p.stages) & 1) && clock64() - t0 < 2000000) {
                 }
         }
         __syncwarp();
     } else if (warp == 1 && leader) {
         const uint32_t one = elect_one();
-        uint32_t n = 0, s = 0, sp = 0, q = 0, qp = 0;
+        uint32_t n = 0, s = 0, sp = 0, q = 0, at = 0;  // at: the stage's offset in units of 16 bytes, as descriptors hold it
+        const uint64_t desc0 = desc_sw128(data0), scales0 = scale_desc(scale0);
         bool ok = true;
         Tile x = {};
         if (first < tiles) x = tile_at(first);
@@ -519,35 +543,32 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
             const uint32_t id = idesc_mx(PAIR ? 256 : 128, uniform(mma_tokens(x)), 0);
             ok = wait_warp(aempty + 8 * acc, ((n >> 1) & 1) ^ 1, &abort_flag, p, kStatusTimeoutFree);
             fence_after();
-            for (int32_t sb = sb_lo; ok && sb < sb_hi; ++sb) {
-                ok = wait_warp(sfull + 8 * q, qp, &abort_flag, p, kStatusTimeoutOperand);
-                for (int32_t kb = 2 * sb; ok && kb < min(2 * sb + 2, p.nkb); ++kb) {
-                    ok = wait_warp(full + 8 * s, sp, &abort_flag, p, kStatusTimeoutTma);
-                    if (PAIR) ok = ok && wait_warp(pfull + 8 * s, sp, &abort_flag, p, kStatusTimeoutTma);
-                    if (!ok) break;
-                    fence_after();
-                    const uint32_t sc = tmem + kScaleCol + (kb & 1) * kScaleCols;
-                    uint32_t src = scale0 + q * p.scale_bytes + (kb & 1) * 2 * kMxAtom * atoms;
+            for (int32_t kb = 2 * sb_lo; ok && kb < kb_hi; ++kb) {
+                ok = wait_warp(full + 8 * s, sp, &abort_flag, p, kStatusTimeoutTma);
+                if (!ok) break;
+                fence_after();
+                const uint32_t sc = tmem + kScaleCol + (kb & 1) * kScaleCols;
+                uint64_t src = scales0 + ((q ? p.scale_bytes : 0) + (kb & 1) * 2 * kMxAtom * atoms) / 16;
 #pragma unroll
-                    for (int w = 0; w < 2; ++w) {
-                        copy_scales<PAIR>(sc + 4 * w, src, one);
-                        copy_scales<PAIR>(sc + 8 + 8 * w, src + kMxAtom, one);
-                        if (atoms > 2) copy_scales<PAIR>(sc + 12 + 8 * w, src + 2 * kMxAtom, one);
-                        src += kMxAtom * atoms;
-                    }
-                    const uint64_t wd = desc_sw128(data0 + s * p.stage_bytes), ad = desc_sw128(data0 + s * p.stage_bytes + kMxRowsW * 128);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const uint32_t w = j >> 1, sf = (j & 1) * 2;
-                        mma_mx<PAIR>(d, wd + 2 * j, ad + 2 * j, id | (sf << 4) | (sf << 29), sc + 4 * w, sc + 8 + 8 * w,
-                                     kb > 2 * sb_lo || j > 0, one);
-                    }
-                    commit_if<PAIR>(empty + 8 * s, one);
-                    if (++s == (uint32_t)p.stages) s = 0, sp ^= 1;
+                for (int w = 0; w < 2; ++w) {
+                    copy_scales<PAIR>(sc + 4 * w, src, one);
+                    copy_scales<PAIR>(sc + 8 + 8 * w, src + kMxAtom / 16, one);
+                    if (atoms > 2) copy_scales<PAIR>(sc + 12 + 8 * w, src + 2 * kMxAtom / 16, one);
+                    src += kMxAtom * atoms / 16;
                 }
-                if (ok) commit_if<PAIR>(sempty + 8 * q, one);
-                if (++q == (uint32_t)p.scales) q = 0, qp ^= 1;
+                const uint64_t wd = desc0 + at, ad = wd + kMxRowsW * 128 / 16;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t w = j >> 1, sf = (j & 1) * 2;
+                    mma_mx<PAIR>(d, wd + 2 * j, ad + 2 * j, id | (sf << 4) | (sf << 29), sc + 4 * w, sc + 8 + 8 * w,
+                                 kb > 2 * sb_lo || j > 0, one);
+                }
+                commit_if<PAIR>(empty + 8 * s, one);
+                at += p.stage_bytes / 16;
+                if (++s == (uint32_t)p.stages) s = 0, at = 0, sp ^= 1;
+                if (kb & 1) q ^= 1;
             }
+            if (p.nkb & 1 && kb_hi == p.nkb) q ^= 1;  // (a tile's last scale stage may hold one block)
             if (ok) commit_if<PAIR>(afull + 8 * acc, one);
             if (t + step < tiles) x = tile_at(t + step);  // (while the MMAs run)
         }
@@ -564,81 +585,98 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
         bool ok = true;
         for (int32_t t = first; ok && t < tiles; t += step)
             for (int32_t kb = 2 * sb_lo; ok && kb < kb_hi; ++kb) {
-                ok = wait_warp(full + 8 * s, sp, &abort_flag, p, kStatusTimeoutTma);
-                if (ok && lane == 0) arrive_cluster(in_cta(pfull + 8 * s, 0));
+                ok = wait_warp(own + 8 * s, sp, &abort_flag, p, kStatusTimeoutTma);
+                if (ok && lane == 0) arrive_cluster(in_cta(full + 8 * s, 0));
                 if (++s == (uint32_t)p.stages) s = 0, sp ^= 1;
             }
         __syncwarp();
     } else if (warp < kMxEpiWarp0) {
-        // scales to the tensor core's order; warp 2: W's rows, warp 3: the tokens, in one or two parts of 128.  A lane copies the
-        // 16 bytes of its rows 32 c + lane into the ring, raws - 1 stages ahead, and is the only one to read them there.
+        // scales to the tensor core's order; warps 2 and 5: W's rows, 3 and 6: the tokens, in one or two parts of 128; 2 and 3: even
+        // stages, 5 and 6: odd ones.  A lane copies the 16 bytes of its rows 32 c + lane into the ring, some stages ahead,
+        // and is the only one to read them there.
         const uint32_t total = first < tiles ? (uint32_t)((tiles - first + step - 1) / step) * (uint32_t)(sb_hi - sb_lo) : 0;
-        const int part = warp - 2, parts = warp == 2 ? 1 : atoms - 1;
+        const uint32_t turn = warp >= 5;
+        const int part = warp - (turn ? 5 : 2), parts = part == 0 ? 1 : atoms - 1, ahead = p.raws / 2 - 1;
+        const int64_t pitch = part == 0 ? p.w_lds : p.a_lds;
         int32_t lt = first, lsb = sb_lo;  // the stage to load next
-        uint32_t lr = 0;
+        uint32_t lr = turn;
         const uint8_t *base = nullptr;  // its rows: from `base` on, `pitch` apart, `rows` of them
-        int64_t pitch = 0;
         int rows = 0;
+        auto next = [&] {
+            if (++lsb < sb_hi) return false;
+            lsb = sb_lo;
+            lt += step;
+            return true;
+        };
         auto begin = [&] {
             if (lt >= tiles) return;
             const Tile x = tile_at(lt);
-            base = warp == 2 ? p.w_scales + x.e * p.w_scales_stride + x.n0 * p.w_lds : p.a_scales + x.row0 * p.a_lds;
-            rows = warp == 2 ? p.N - x.n0 : x.rows;
+            base = part == 0 ? p.w_scales + x.e * p.w_scales_stride + x.n0 * p.w_lds : p.a_scales + x.row0 * p.a_lds;
+            rows = part == 0 ? p.N - x.n0 : x.rows;
         };
-        pitch = warp == 2 ? p.w_lds : p.a_lds;
+        if (turn) next();
         begin();
         auto load = [&] {
             if (lt < tiles) {
                 const uint32_t n = min(p.nb - 16 * lsb, 16);
                 const uint32_t dst = raw0 + lr * p.raw_bytes + part * kMxRowsW * 16 + lane * 16;
                 const uint8_t *src = base + 16 * lsb + lane * pitch;
-                const int last = warp == 2 ? 4 : (p.nt + 31) / 32;
+                const int last = part == 0 ? 4 : (p.nt + 31) / 32;
                 for (int c = 0; c < last; ++c, src += 32 * pitch) {
                     const bool in = 32 * c + lane < rows;
                     cpa16(dst + c * 512, in ? src : base, in ? n : 0);
                 }
-                if (++lsb == sb_hi) {
-                    lsb = sb_lo;
-                    lt += step;
-                    begin();
-                }
-                if (++lr == (uint32_t)p.raws) lr = 0;
+                const bool another = next();
+                if (next() || another) begin();
+                if ((lr += 2) >= (uint32_t)p.raws) lr = turn;
             }
             cpa_commit();
         };
-        for (int i = 1; i < p.raws; ++i) load();
-        uint32_t r = 0, q = 0, qp = 1;
+        for (int i = 0; i < ahead; ++i) load();
+        // Two stages of scales in order: stage st takes the place of st - 2, free when the last MMAs that used it have ended, which
+        // frees their data stage too
+        uint32_t r = turn, s = 0, sp = 0, last = 0, lastp = 0;
+        int32_t sb = sb_lo;
         for (uint32_t st = 0; st < total; ++st) {
-            load();
-            copies_but(p.raws - 1);
-            const uint32_t src = raw0 + r * p.raw_bytes + part * kMxRowsW * 16 + lane * 16;
-            uint32_t w[2][4][4];
+            const int blocks = min(2, p.nkb - 2 * sb);
+            if (++sb == sb_hi) sb = sb_lo;
+            if ((st & 1) == turn) {
+                load();
+                copies_but(ahead);
+                const uint32_t src = raw0 + r * p.raw_bytes + part * kMxRowsW * 16 + lane * 16;
+                uint32_t w[2][4][4];
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+                for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    w[i][c][0] = w[i][c][1] = w[i][c][2] = w[i][c][3] = 0;
-                    if (i < parts && (part == 0 || 128 * i + 32 * c < p.nt)) lds128(src + i * kMxRowsW * 16 + c * 512, w[i][c]);
-                }
-            if (!wait_warp(sempty + 8 * q, qp, &abort_flag, p, kStatusTimeoutFree)) break;
-            const uint32_t dst = scale0 + q * p.scale_bytes + part * kMxAtom + lane * 16;
+                    for (int c = 0; c < 4; ++c) {
+                        w[i][c][0] = w[i][c][1] = w[i][c][2] = w[i][c][3] = 0;
+                        if (i < parts && (part == 0 || 128 * i + 32 * c < p.nt)) lds128(src + i * kMxRowsW * 16 + c * 512, w[i][c]);
+                    }
+                if (st >= 2 && !wait_warp(last, lastp, &abort_flag, p, kStatusTimeoutFree)) break;
+                const uint32_t dst = scale0 + turn * p.scale_bytes + part * kMxAtom + lane * 16;
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-                if (i < parts) {
+                for (int i = 0; i < 2; ++i)
+                    if (i < parts) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + i * kMxAtom + j * kMxAtom * atoms), "r"(w[i][0][j]),
-                                     "r"(w[i][1][j]), "r"(w[i][2][j]), "r"(w[i][3][j])
-                                     : "memory");
-                }
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) {
-                if constexpr (PAIR) arrive_cluster(in_cta(sfull + 8 * q, 0));
-                else bar_arrive(sfull + 8 * q);
+                        for (int j = 0; j < 4; ++j)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + i * kMxAtom + j * kMxAtom * atoms),
+                                         "r"(w[i][0][j]), "r"(w[i][1][j]), "r"(w[i][2][j]), "r"(w[i][3][j])
+                                         : "memory");
+                    }
+                fence_async_smem();
+                __syncwarp();
+                if ((r += 2) >= (uint32_t)p.raws) r = turn;
             }
-            if (++r == (uint32_t)p.raws) r = 0;
-            if (++q == (uint32_t)p.scales) q = 0, qp ^= 1;
+            for (int i = 0; i < blocks; ++i) {
+                if ((st & 1) == turn) {
+                    if (lane == 0) {
+                        if constexpr (PAIR) arrive_cluster(in_cta(full + 8 * s, 0));
+                        else bar_arrive(full + 8 * s);
+                    }
+                    last = empty + 8 * s, lastp = sp;
+                }
+                if (++s == (uint32_t)p.stages) s = 0, sp ^= 1;
+            }
         }
         copies_but(0);
     } else {
