@@ -53,7 +53,7 @@ constexpr int kMxMaxTok = 224;  // tokens a tile
 constexpr int kMxMaxStages = 16, kMxMinStages = 4, kMxMaxRaw = 6;
 constexpr int kMxEpiWarp0 = 7, kMxEpiWarps = 16, kMxThreads = 32 * (kMxEpiWarp0 + kMxEpiWarps);
 constexpr int kMxAtom = 512;    // bytes of the scales of 128 rows and 128 values of K
-constexpr int kMxPatch = 1024;  // bytes of shared memory in which an epilogue warp turns 2-byte results
+constexpr int kMxPatch = 512;   // bytes of shared memory in which an epilogue warp turns 2-byte results
 constexpr int kMxSmemLimit = 226 * 1024;  // dynamic; the barriers are static
 
 enum MxMode { MX_ONE = 0, MX_SPLIT = 1, MX_PAIR = 2 };
@@ -339,23 +339,23 @@ __device__ __forceinline__ void store_chunk(const MxParams &p, float (&v)[16], c
     if constexpr (sizeof(T) == 2) {
         if (p.wide) {
             const uint32_t at = patch + (kGate ? (lane & 1) * 2 * kCols + (lane & ~1) : 2 * lane);
-#pragma unroll
-            for (int i = 0; i < kVals; ++i) {
-                const T h = to_out<T>(v[i]);
-                asm volatile("st.shared.b16 [%0], %1;" ::"r"(at + i * (kGate ? 4 * kCols : 2 * kCols)), "h"(*(const uint16_t *)&h) : "memory");
-            }
-            __syncwarp();
-            constexpr int kPieces = kCols / 8, kTokens = 32 / kPieces;  // pieces of a token, tokens at a time
+            constexpr int kPieces = kCols / 8, kTokens = 32 / kPieces;  // pieces of a token, tokens the patch holds
             const int piece = lane % kPieces, token = lane / kPieces;
             T *y = (T *)p.Y + (int64_t)(t.row0 + c0 + token) * p.ldy + out0 + 8 * piece;
             const bool in = out0 + 8 * piece < width;
 #pragma unroll
-            for (int i = 0; i < 16 / kTokens; ++i) {
+            for (int h = 0; h < 16 / kTokens; ++h) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const T x = to_out<T>(v[8 * h + i]);
+                    asm volatile("st.shared.b16 [%0], %1;" ::"r"(at + i * (kGate ? 4 * kCols : 2 * kCols)), "h"(*(const uint16_t *)&x) : "memory");
+                }
+                __syncwarp();
                 uint32_t q[4];
-                lds128(patch + lane * 16 + i * 512, q);
-                if (in && token + i * kTokens < left) *(uint4 *)(y + (int64_t)i * kTokens * p.ldy) = make_uint4(q[0], q[1], q[2], q[3]);
+                lds128(patch + lane * 16, q);
+                if (in && token + h * kTokens < left) *(uint4 *)(y + (int64_t)h * kTokens * p.ldy) = make_uint4(q[0], q[1], q[2], q[3]);
+                __syncwarp();
             }
-            __syncwarp();
             return;
         }
     }
