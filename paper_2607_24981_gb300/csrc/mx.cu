@@ -6,8 +6,9 @@
 // rounded to the nearest code, ties to the even one, saturating at 6.  A block of zeros has scale byte 0, a
 // block with a value that is not finite the NaN byte 255.
 //
-// Both move bytes and little else, so what counts is how many are in flight.  Rows on 16-byte boundaries: eight values a
-// thread and step, four steps in flight, four lanes a block.  Other rows: a warp takes 256 values of a row, one
+// Both move bytes and little else, so what counts is how many are in flight and how few instructions go with them.  Rows on
+// 16-byte boundaries: sixteen values a thread and step to quantise (two lanes a block; magnitudes of 16-bit values are
+// compared two at a time), eight a thread back, several steps in flight.  Other rows: a warp takes 256 values of a row, one
 // after the other in memory, and hands them over through shared memory, so that its accesses stay whole lines
 // (eight values a lane in a row of its own would touch every line eight times).
 #include <algorithm>
@@ -24,7 +25,7 @@ namespace ilw {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kSteps = 4;  // groups of eight values of a thread in flight
+constexpr int kSteps = 4;  // groups of eight values of a thread in flight, on the way back
 
 // n / d for n < 2^31 (round-up reciprocal of Granlund and Montgomery, 1994)
 struct Divisor {
@@ -58,22 +59,56 @@ __device__ __forceinline__ float scale_value(uint32_t b) {
     return __uint_as_float(b == 255 ? 0x7fc00000u : b == 0 ? 0x00400000u : b << 23);
 }
 
-// Scale byte and codes of this lane's 8 values (four lanes a block, all of them here).
-__device__ __forceinline__ uint32_t encode8(const float (&v)[8], uint32_t &b) {
-    uint32_t m = 0;  // magnitudes as bits: in order, infinities and NaN on top
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
-    m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-    m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-    // floor(log2 amax) - 2 + 127 is the biased exponent less 2, at least 0 (a subnormal's too)
-    const uint32_t e = m >> 23;
-    b = e == 255 ? 255u : e < 2 ? 0u : e - 2;
-    if (e == 255) return 0;
-    const float inv = __uint_as_float((254 - b) << 23);  // 2^(127 - b), b <= 252
+// Scale byte of a block whose largest magnitude has the bits m (infinities and NaN are above all others), and the factor
+// 2^(127 - b) by which its values become codes: floor(log2 amax) - 2 + 127 is the biased exponent less 2, at least 0 (a
+// subnormal's too).
+__device__ __forceinline__ uint32_t scale_byte(uint32_t m, float &inv) {
+    const uint32_t e = m >> 23, b = e == 255 ? 255u : e < 2 ? 0u : e - 2;
+    inv = __uint_as_float((254 - min(b, 253u)) << 23);
+    return b;
+}
+__device__ __forceinline__ uint32_t codes8(const float (&v)[8], float inv) {
     uint32_t w = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) w |= e2m1x2(v[2 * i] * inv, v[2 * i + 1] * inv) << (8 * i);
     return w;
+}
+// Scale byte and codes of this lane's 8 values (four lanes a block, all of them here).
+__device__ __forceinline__ uint32_t encode8(const float (&v)[8], uint32_t &b) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+    float inv;
+    b = scale_byte(m, inv);
+    return b == 255 ? 0 : codes8(v, inv);
+}
+
+// The largest magnitude of 8 values, as the bits of a float.
+__device__ __forceinline__ uint32_t magnitude8(const Eight<float> &x) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x.t[i]) & 0x7fffffffu);
+    return m;
+}
+template <typename T>
+__device__ __forceinline__ uint32_t magnitude8_16bit(const Eight<T> &x) {
+    const uint32_t *w = (const uint32_t *)&x;
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
+    return max(m & 0xffffu, m >> 16);
+}
+__device__ __forceinline__ uint32_t magnitude8(const Eight<__nv_bfloat16> &x) { return magnitude8_16bit(x) << 16; }
+__device__ __forceinline__ uint32_t magnitude8(const Eight<__half> &x) {
+    return __float_as_uint(__half2float(__ushort_as_half((unsigned short)magnitude8_16bit(x)))) & 0x7fffffffu;
+}
+__device__ __forceinline__ uint32_t magnitude8(const Eight<int8_t> &x) {
+    int m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, abs((int)x.t[i]));
+    return __float_as_uint((float)m);
 }
 
 // The row of X that row r takes; -1: a row of zeros.
@@ -85,40 +120,51 @@ __device__ __forceinline__ int64_t source_row(const MxQuantParams &p, int64_t r)
     return -1;
 }
 
-// Rows of X on 16-byte boundaries, K a multiple of 8.  Step i of the grid: row i / per, values 8 (i % per) .. + 7, whole
-// blocks of four lanes.
+// Rows of X on 16-byte boundaries, K a multiple of 8.  Step i of the grid: row i / per, values 16 (i % per) .. + 15, two lanes a
+// block.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) mx_quantize_kernel(const MxQuantParams p, Divisor per, uint32_t r0, uint32_t total) {
+    constexpr int kSteps = 2;
     grid_wait();
     const uint32_t base = blockIdx.x * (kThreads * kSteps) + threadIdx.x;
-    Eight<T> x[kSteps];
+    Eight<T> x[kSteps][2];
     uint32_t row[kSteps], k[kSteps];
 #pragma unroll
     for (int j = 0; j < kSteps; ++j) {
         const uint32_t i = base + j * kThreads;
         row[j] = per.div(i);
-        k[j] = (i - row[j] * per.d) * 8;
+        k[j] = (i - row[j] * per.d) * 16;
 #pragma unroll
-        for (int u = 0; u < 8; ++u) x[j].t[u] = T(0);
+        for (int u = 0; u < 8; ++u) x[j][0].t[u] = x[j][1].t[u] = T(0);
         if (i < total && k[j] < (uint32_t)p.K) {
             const int64_t src = source_row(p, (int64_t)r0 + row[j]);
-            if (src >= 0) x[j] = *(const Eight<T> *)((const T *)p.X + src * p.ldx + k[j]);
+            if (src >= 0) {
+                const Eight<T> *at = (const Eight<T> *)((const T *)p.X + src * p.ldx + k[j]);
+                x[j][0] = at[0];
+                if (k[j] + 8 < (uint32_t)p.K) x[j][1] = at[1];
+            }
         }
     }
 #pragma unroll
     for (int j = 0; j < kSteps; ++j) {
-        float v[8];
-        uint32_t b;
-#pragma unroll
-        for (int u = 0; u < 8; ++u) v[u] = to_f(x[j].t[u]);
-        const uint32_t w = encode8(v, b);
+        uint32_t m = max(magnitude8(x[j][0]), magnitude8(x[j][1]));
+        m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
         if (base + j * kThreads >= total) continue;
+        float inv;
+        const uint32_t b = scale_byte(m, inv);
+        uint2 w = make_uint2(0, 0);
+        if (b != 255) {
+            float v[8], u[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = to_f(x[j][0].t[i]), u[i] = to_f(x[j][1].t[i]);
+            w = make_uint2(codes8(v, inv), codes8(u, inv));
+        }
         const int64_t r = (int64_t)r0 + row[j];
-        const uint32_t blk = k[j] >> 5, lane4 = threadIdx.x & 3;
-        *(uint32_t *)(p.codes + r * p.ldc + (k[j] >> 1)) = w;
-        if (lane4 == 0) p.scales[r * p.lds + blk] = (uint8_t)b;
-        if (blk + 1 == per.d / 4)  // the row's last block: its lanes fill up the scale bytes
-            for (uint32_t z = blk + 1 + lane4; z <= (blk | 15); z += 4) p.scales[r * p.lds + z] = 0;
+        const uint32_t blk = k[j] >> 5, half = threadIdx.x & 1;
+        *(uint2 *)(p.codes + r * p.ldc + (k[j] >> 1)) = w;
+        if (half == 0) p.scales[r * p.lds + blk] = (uint8_t)b;
+        if (blk + 1 == per.d / 2)  // the row's last block: its lanes fill up the scale bytes
+            for (uint32_t z = blk + 1 + half; z <= (blk | 15); z += 2) p.scales[r * p.lds + z] = 0;
     }
 }
 
@@ -235,7 +281,7 @@ cudaError_t over_rows(void (*kernel)(const P, Divisor, uint32_t, uint32_t), cons
 template <typename T>
 cudaError_t quantize(const MxQuantParams &p, cudaStream_t s) {
     if ((uintptr_t)p.X % alignof(Eight<T>) == 0 && p.ldx * (int64_t)sizeof(T) % alignof(Eight<T>) == 0 && p.K % 8 == 0)
-        return over_rows(mx_quantize_kernel<T>, p, p.rows, (uint32_t)(p.K + 31) / 32 * 4, kThreads * kSteps, s);
+        return over_rows(mx_quantize_kernel<T>, p, p.rows, (uint32_t)(p.K + 31) / 32 * 2, kThreads * 2, s);
     return over_rows(mx_quantize_any_kernel<T>, p, p.rows, (uint32_t)(p.K + 255) / 256, kThreads / 32, s);
 }
 template <typename T>
