@@ -116,6 +116,16 @@ __device__ __forceinline__ bool wait_bar(uint32_t b, uint32_t parity, volatile i
 __device__ __forceinline__ bool wait_warp(uint32_t b, uint32_t parity, volatile int *abort, const MxParams &p, int code) {
     return __all_sync(0xffffffffu, wait_bar(b, parity, abort, p, code));
 }
+// The same for a lane that issues loads or MMAs on its own, with the long way out of line: its loop then keeps the operands in
+// uniform registers and a wait with nothing to wait for costs next to nothing (a block of K: 225 clocks for 6 copies and 4
+// MMAs of 16 tokens, what they take; with a vote of the warp 395).
+__device__ __noinline__ bool wait_long(uint32_t b, uint32_t parity, volatile int *abort, const MxParams *p, int code) {
+    return wait_bar(b, parity, abort, *p, code);
+}
+__device__ __forceinline__ bool wait_lane(uint32_t b, uint32_t parity, volatile int *abort, const MxParams &p, int code) {
+    return bar_try(b, parity) || wait_long(b, parity, abort, &p, code);
+}
+
 // This barrier's address in CTA `rank` of the cluster, and an arrival there.  What the arrivals of a pair order is read by the
 // tensor core alone, through the async proxy, to which its writers hand it themselves (TMA, or fence.proxy.async
 // after the stores); a release at cluster scope on top of that held each arrival up by some 1000 clocks.
@@ -135,68 +145,37 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap *m) {
 }
 
 // A value that is the same in every lane, in a uniform register: the operands of TMA loads and MMAs are uniform
-// registers, and each one that has to be moved there at its instruction costs some 50 clocks (a lane alone in a
-// branch took 300 clocks a TMA load, which was the rate of every product).
+// registers, and each one that has to be moved there at its instruction costs some 50 clocks (with values that the
+// compiler could not know to be uniform a TMA load took 300 clocks, which was the rate of every product).
 __device__ __forceinline__ uint32_t uniform(uint32_t v) { return __reduce_max_sync(0xffffffffu, v); }
-// TMA loads and their barrier, by the lane with `issue` set, of a converged warp
-__device__ __forceinline__ void expect_if(uint32_t b, uint32_t bytes, uint32_t issue) {
-    asm volatile("{\n .reg .pred q;\n setp.ne.b32 q, %2, 0;\n @q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n}\n" ::"r"(b), "r"(bytes),
-                 "r"(issue)
-                 : "memory");
-}
-__device__ __forceinline__ void tma_2d_if(uint32_t dst, const CUtensorMap *m, int32_t x, int32_t y, uint32_t bar, uint32_t issue) {
-    asm volatile(
-        "{\n .reg .pred q;\n setp.ne.b32 q, %5, 0;\n"
-        " @q cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n}\n" ::"r"(dst),
-        "l"((uint64_t)m), "r"(x), "r"(y), "r"(bar), "r"(issue)
-        : "memory");
-}
-__device__ __forceinline__ void tma_3d_if(uint32_t dst, const CUtensorMap *m, int32_t x, int32_t y, int32_t z, uint32_t bar, uint32_t issue) {
-    asm volatile(
-        "{\n .reg .pred q;\n setp.ne.b32 q, %6, 0;\n"
-        " @q cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n}\n" ::"r"(dst),
-        "l"((uint64_t)m), "r"(x), "r"(y), "r"(z), "r"(bar), "r"(issue)
-        : "memory");
-}
-
-// Of a pair (PAIR) only the first CTA issues, for both.
+// Of a pair (PAIR) only the first CTA issues, for both.  All by one lane.
 template <bool PAIR>
-__device__ __forceinline__ void mma_mx(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb,
-                                       uint32_t acc, uint32_t issue) {
+__device__ __forceinline__ void mma_mx(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t acc) {
     if constexpr (PAIR)
         asm volatile(
-            "{\n .reg .pred p, q;\n setp.ne.b32 p, %6, 0;\n setp.ne.b32 q, %7, 0;\n"
-            " @q tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}\n" ::"r"(d),
-            "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(acc), "r"(issue)
+            "{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
+            " tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}\n" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(acc)
             : "memory");
     else
         asm volatile(
-            "{\n .reg .pred p, q;\n setp.ne.b32 p, %6, 0;\n setp.ne.b32 q, %7, 0;\n"
-            " @q tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}\n" ::"r"(d),
-            "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(acc), "r"(issue)
+            "{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
+            " tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}\n" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(acc)
             : "memory");
 }
 // An arrival at `bar` (of a pair: in both CTAs, unless `local`) when the MMAs and copies issued so far have ended.
 template <bool PAIR>
-__device__ __forceinline__ void commit_if(uint32_t bar, uint32_t issue, bool local = false) {
+__device__ __forceinline__ void commit_mma(uint32_t bar, bool local = false) {
     if constexpr (PAIR) {
-        if (!local) {
-            asm volatile(
-                "{\n .reg .pred q;\n setp.ne.b32 q, %1, 0;\n"
-                " @q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %2;\n}\n" ::"r"(bar),
-                "r"(issue), "h"((uint16_t)3)
-                : "memory");
-            return;
-        }
-        asm volatile(
-            "{\n .reg .pred q;\n setp.ne.b32 q, %1, 0;\n"
-            " @q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(bar), "r"(issue)
-            : "memory");
+        if (!local)
+            asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+                         "h"((uint16_t)3)
+                         : "memory");
+        else
+            asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
     } else {
-        asm volatile(
-            "{\n .reg .pred q;\n setp.ne.b32 q, %1, 0;\n"
-            " @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(bar), "r"(issue)
-            : "memory");
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
     }
 }
 // Descriptor of scales in order: rows of 16 bytes, eight of them (128 bytes) a core matrix, no swizzle
@@ -206,15 +185,9 @@ __device__ __forceinline__ uint64_t scale_desc(uint32_t saddr) {
 // Shared memory to tensor memory (of a pair: in both CTAs, each its own): 32 rows of 16 bytes to 4 columns of 32 lanes, the
 // same for each quarter of the lanes.
 template <bool PAIR>
-__device__ __forceinline__ void copy_scales(uint32_t t, uint64_t d, uint32_t issue) {
-    if constexpr (PAIR)
-        asm volatile(
-            "{\n .reg .pred q;\n setp.ne.b32 q, %2, 0;\n @q tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n}\n" ::"r"(t), "l"(d), "r"(issue)
-            : "memory");
-    else
-        asm volatile(
-            "{\n .reg .pred q;\n setp.ne.b32 q, %2, 0;\n @q tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n}\n" ::"r"(t), "l"(d), "r"(issue)
-            : "memory");
+__device__ __forceinline__ void copy_scales(uint32_t t, uint64_t d) {
+    if constexpr (PAIR) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(t), "l"(d) : "memory");
+    else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(t), "l"(d) : "memory");
 }
 // Waits until no more than n of this thread's groups of asynchronous copies are in flight.
 __device__ __forceinline__ void copies_but(int n) {
@@ -398,15 +371,18 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
 
     const uint32_t rank = SPLIT ? blockIdx.x % p.splits : PAIR ? blockIdx.x & 1 : 0;
     const bool leader = !PAIR || rank == 0;
-    if (threadIdx.x == 0) {
-        abort_flag = 0;
-        for (int i = 0; i < kMxMaxStages; ++i) {
-            bar_init(full + 8 * i, PAIR ? 2 + 1 + 4 : 2 + 2);  // loads, the second CTA's word, scale warps
-            bar_init(empty + 8 * i, 1);
-            bar_init(own + 8 * i, 2);
+    if (warp == 0) {
+        if (lane == 0) abort_flag = 0;
+        if (lane < kMxMaxStages) {
+            bar_init(full + 8 * lane, PAIR ? 2 + 1 + 4 : 2 + 2);  // loads, the second CTA's word, scale warps
+            bar_init(empty + 8 * lane, 1);
+            bar_init(own + 8 * lane, 2);
+        } else if (lane < kMxMaxStages + 2) {
+            bar_init(afull + 8 * (lane - kMxMaxStages), 1);
+            bar_init(aempty + 8 * (lane - kMxMaxStages), PAIR ? 2 * kMxEpiWarps : kMxEpiWarps);
+        } else if (lane == kMxMaxStages + 2) {
+            bar_init(drain, 1);
         }
-        for (int i = 0; i < 2; ++i) bar_init(afull + 8 * i, 1), bar_init(aempty + 8 * i, PAIR ? 2 * kMxEpiWarps : kMxEpiWarps);
-        bar_init(drain, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (threadIdx.x == 32) {
@@ -499,31 +475,36 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
             const int part = PAIR ? mma_tokens(x) / 2 : x.rows, row = x.row0 + (PAIR ? (int)rank * part : 0);
             const int units = (part + 15) >> 4;
             const uint32_t bytes = warp == 0 ? kMxRowsW * 128 : p.abox ? p.abox * 128 : units * 2048;
-            for (int32_t kb = 2 * sb_lo; kb < kb_hi; ++kb) {
-                ok = wait_warp(empty + 8 * s, sp, &abort_flag, p, kStatusTimeoutFree);
-                if (!ok) break;
-                const uint32_t d = data0 + s * p.stage_bytes + (warp == 0 ? 0 : kMxRowsW * 128), db = arrives + 8 * s;
-                if ((int32_t)it != p.dbg_skip) {
-                    expect_if(db, bytes, one);
-                    if (warp == 0) {
-                        tma_3d_if(d, &p.wc, kb * 128, x.n0, x.e, db, one);
-                    } else if (p.abox) {
-                        tma_2d_if(d, &p.ac[0], kb * 128, row, db, one);
-                    } else {
-                        int done = 0;  // (units of 16 rows)
-#pragma unroll
-                        for (int i = 3; i >= 0; --i)
-                            if (units & (1 << i)) {
-                                tma_2d_if(d + done * 2048, &p.ac[i], kb * 128, row + done * 16, db, one);
-                                done += 1 << i;
-                            }
+            if (one) {
+                for (int32_t kb = 2 * sb_lo; kb < kb_hi; ++kb) {
+                    if (!wait_lane(empty + 8 * s, sp, &abort_flag, p, kStatusTimeoutFree)) {
+                        ok = false;
+                        break;
                     }
+                    const uint32_t d = data0 + s * p.stage_bytes + (warp == 0 ? 0 : kMxRowsW * 128), db = arrives + 8 * s;
+                    if ((int32_t)it != p.dbg_skip) {
+                        bar_expect_tx(db, bytes);
+                        if (warp == 0) {
+                            tma_3d(d, &p.wc, kb * 128, x.n0, x.e, db);
+                        } else if (p.abox) {
+                            tma_2d(d, &p.ac[0], kb * 128, row, db);
+                        } else {
+                            int done = 0;  // (units of 16 rows)
+#pragma unroll
+                            for (int i = 3; i >= 0; --i)
+                                if (units & (1 << i)) {
+                                    tma_2d(d + done * 2048, &p.ac[i], kb * 128, row + done * 16, db);
+                                    done += 1 << i;
+                                }
+                        }
+                    }
+                    ++it;
+                    if (++s == (uint32_t)p.stages) s = 0, sp ^= 1;
                 }
-                ++it;
-                if (++s == (uint32_t)p.stages) s = 0, sp ^= 1;
             }
+            ok = __all_sync(0xffffffffu, ok);
         }
-        if (lane == 0 && abort_flag) {  // the loads in flight end (bounded) before the CTA can exit
+        if (one && abort_flag) {  // the loads in flight end (bounded) before the CTA can exit
             // (the barrier may miss other arrivals, so the limit is short: a load takes microseconds)
             const long long t0 = clock64();
             for (uint32_t i = it > (uint32_t)p.stages ? it - p.stages : 0; i < it; ++i)
@@ -533,8 +514,10 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
         __syncwarp();
     } else if (warp == 1 && leader) {
         const uint32_t one = elect_one();
-        uint32_t n = 0, s = 0, sp = 0, q = 0, at = 0;  // at: the stage's offset in units of 16 bytes, as descriptors hold it
+        uint32_t n = 0, s = 0, sp = 0, at = 0;  // at: the stage's offset in units of 16 bytes, as descriptors hold it
         const uint64_t desc0 = desc_sw128(data0), scales0 = scale_desc(scale0);
+        uint64_t scales = scales0;  // the stage of scales: one of two
+        const uint32_t scol = tmem + kScaleCol, half = 2 * kMxAtom * atoms / 16;
         bool ok = true;
         Tile x = {};
         if (first < tiles) x = tile_at(first);
@@ -542,38 +525,47 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
             const uint32_t acc = n & 1, d = tmem + acc * kMxMaxTok;
             const uint32_t id = idesc_mx(PAIR ? 256 : 128, uniform(mma_tokens(x)), 0);
             ok = wait_warp(aempty + 8 * acc, ((n >> 1) & 1) ^ 1, &abort_flag, p, kStatusTimeoutFree);
+            if (!ok) break;
             fence_after();
-            for (int32_t kb = 2 * sb_lo; ok && kb < kb_hi; ++kb) {
-                ok = wait_warp(full + 8 * s, sp, &abort_flag, p, kStatusTimeoutTma);
-                if (!ok) break;
+            // one block of 256 of K: its scales to the columns from sc on, then 4 MMAs of 64
+            auto block = [&](uint32_t sc, uint64_t src, bool add) {
+                if (!wait_lane(full + 8 * s, sp, &abort_flag, p, kStatusTimeoutTma)) return false;
                 fence_after();
-                const uint32_t sc = tmem + kScaleCol + (kb & 1) * kScaleCols;
-                uint64_t src = scales0 + ((q ? p.scale_bytes : 0) + (kb & 1) * 2 * kMxAtom * atoms) / 16;
 #pragma unroll
                 for (int w = 0; w < 2; ++w) {
-                    copy_scales<PAIR>(sc + 4 * w, src, one);
-                    copy_scales<PAIR>(sc + 8 + 8 * w, src + kMxAtom / 16, one);
-                    if (atoms > 2) copy_scales<PAIR>(sc + 12 + 8 * w, src + 2 * kMxAtom / 16, one);
+                    copy_scales<PAIR>(sc + 4 * w, src);
+                    copy_scales<PAIR>(sc + 8 + 8 * w, src + kMxAtom / 16);
+                    if (atoms > 2) copy_scales<PAIR>(sc + 12 + 8 * w, src + 2 * kMxAtom / 16);
                     src += kMxAtom * atoms / 16;
                 }
                 const uint64_t wd = desc0 + at, ad = wd + kMxRowsW * 128 / 16;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const uint32_t w = j >> 1, sf = (j & 1) * 2;
-                    mma_mx<PAIR>(d, wd + 2 * j, ad + 2 * j, id | (sf << 4) | (sf << 29), sc + 4 * w, sc + 8 + 8 * w,
-                                 kb > 2 * sb_lo || j > 0, one);
+                    mma_mx<PAIR>(d, wd + 2 * j, ad + 2 * j, id | (sf << 4) | (sf << 29), sc + 4 * w, sc + 8 + 8 * w, add || j > 0);
                 }
-                commit_if<PAIR>(empty + 8 * s, one);
+                commit_mma<PAIR>(empty + 8 * s);
                 at += p.stage_bytes / 16;
                 if (++s == (uint32_t)p.stages) s = 0, at = 0, sp ^= 1;
-                if (kb & 1) q ^= 1;
+                return true;
+            };
+            if (one) {
+                for (int32_t kb = 2 * sb_lo; kb < kb_hi; kb += 2) {  // a stage of scales: two blocks, the last one may be alone
+                    ok = block(scol, scales, kb > 2 * sb_lo);
+                    if (!ok) break;
+                    if (kb + 1 < kb_hi) {
+                        ok = block(scol + kScaleCols, scales + half, true);
+                        if (!ok) break;
+                    }
+                    scales = scales == scales0 ? scales0 + p.scale_bytes / 16 : scales0;
+                }
+                if (ok) commit_mma<PAIR>(afull + 8 * acc);
             }
-            if (p.nkb & 1 && kb_hi == p.nkb) q ^= 1;  // (a tile's last scale stage may hold one block)
-            if (ok) commit_if<PAIR>(afull + 8 * acc, one);
+            ok = __all_sync(0xffffffffu, ok);
             if (t + step < tiles) x = tile_at(t + step);  // (while the MMAs run)
         }
-        if (!ok) {  // the MMAs in flight end before tensor memory is freed
-            commit_if<PAIR>(drain, one, true);
+        if (!ok && one) {  // the MMAs in flight end before tensor memory is freed
+            commit_mma<PAIR>(drain, true);
             const long long t0 = clock64();
             while (!bar_try(drain, 0) && clock64() - t0 < p.wait_cycles) {
             }
@@ -721,25 +713,37 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
         __syncwarp();
         cluster_sync();
         if (first < tiles && !abort_flag && warp >= kMxEpiWarp0) {
-            // each CTA of the cluster finishes some chunks of 16 tokens x 32 rows of W
+            // each warp of the cluster finishes the 32 rows of W of a quarter for four tokens at a time
             const Tile x = tile_at(first);
-            const int chunks = 4 * ((x.rows + 15) / 16), w = warp - kMxEpiWarp0;
-            for (int c = w + kMxEpiWarps * rank; c < chunks; c += kMxEpiWarps * p.splits) {
-                const int c0 = 16 * (c >> 2), row = 32 * (c & 3) + lane, nn = x.n0 + row;
+            const int w = warp - kMxEpiWarp0, units = 4 * ((x.rows + 3) / 4);
+            for (int u = w + kMxEpiWarps * rank; u < units; u += kMxEpiWarps * p.splits) {
+                const int c0 = u & ~3, row = 32 * (u & 3) + lane, nn = x.n0 + row;
                 const float bias = p.bias && nn < p.N ? p.bias[(int64_t)x.e * p.N + nn] : 0.0f;
-                float v[16];
+                float v[8][4], z[4];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) v[i] = 0.0f;
-                for (int r = 0; r < p.splits; ++r) {
-                    const uint32_t at = in_cta(data0 + (c0 * kMxRowsW + row) * 4, r);
+                for (int r = 0; r < 8; ++r)
+                    if (r < p.splits) {
+                        const uint32_t at = in_cta(data0 + (c0 * kMxRowsW + row) * 4, r);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        float y;
-                        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(y) : "r"(at + i * kMxRowsW * 4) : "memory");
-                        v[i] += y;
+                        for (int i = 0; i < 4; ++i)
+                            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[r][i]) : "r"(at + i * kMxRowsW * 4) : "memory");
                     }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    z[i] = v[0][i];
+#pragma unroll
+                    for (int r = 1; r < 8; ++r)
+                        if (r < p.splits) z[i] += v[r][i];
+                    z[i] += bias;
                 }
-                store_chunk<ACT, T>(p, v, x, c0, nn, bias, patch0 + w * kMxPatch, lane);
+                constexpr bool kGate = ACT == ILW_ACT_SILU_GATE;
+                const int width = kGate ? p.N / 2 : p.N, col = kGate ? nn >> 1 : nn;
+                if constexpr (ACT == ILW_ACT_GELU) gelu2(z[0], z[1]), gelu2(z[2], z[3]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (kGate) z[i] = silu_gate(z[i], __shfl_down_sync(0xffffffffu, z[i], 1));  // (even lanes: gate, odd: gated)
+                    if (c0 + i < x.rows && col < width && !(kGate && lane & 1)) ((T *)p.Y)[(int64_t)(x.row0 + c0 + i) * p.ldy + col] = to_out<T>(z[i]);
+                }
             }
         }
     }

@@ -329,7 +329,7 @@ def test_product_gives_up_a_bounded_wait(ilw):
     short = packed(ilw, values(rng, 300, 512)), packed(ilw, rng.standard_normal((256, 512)) / 22)
     cases = ((A, W, want), (few, W, want_few), (*short, ilw.mx_linear(*short)))  # clusters on a tile, and one CTA (K = 512)
     for m, W, w in cases:
-        assert ilw.lib().ilwdetr_debug_gemm_wait(1, 20_000_000) == 0  # (each CTA's second load)
+        assert ilw.lib().ilwdetr_debug_gemm_wait(0, 20_000_000) == 0  # (each CTA's first load)
         try:
             ilw.mx_linear(m, W)
             with pytest.raises(ilw.IlwError, match="wait"):
