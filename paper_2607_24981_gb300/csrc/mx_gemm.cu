@@ -46,7 +46,7 @@ cudaError_t launch_mx_gemm(const MxGemmProblem &g, cudaStream_t s) {
     const int64_t out = g.act == ILW_ACT_SILU_GATE ? g.N / 2 : g.N;
     p.wide = g.form != ILW_FP32 && out % 8 == 0 && (uintptr_t)g.Y % 16 == 0 && g.ldy % 8 == 0;
     const int fixed = 1024 + (g.experts + 1) * (int)sizeof(MxExpert) + g.experts * 4 + (p.wide ? kMxEpiWarps * kMxPatch : 0);
-    auto bytes = [&] { return fixed + p.stages * p.stage_bytes + p.raws * p.raw_bytes + 2 * p.scale_bytes; };
+    auto bytes = [&] { return fixed + p.stages * p.stage_bytes + kMxScaleSets * p.raw_bytes + 2 * p.scale_bytes; };
 
     // Tokens a tile: as wide as the tokens (of an expert, twice the mean) fill, at most 224, and what leaves room for four stages.
     const int64_t per = g.offsets ? (2 * g.M + g.experts - 1) / g.experts : g.M;
@@ -66,12 +66,9 @@ cudaError_t launch_mx_gemm(const MxGemmProblem &g, cudaStream_t s) {
         p.stage_bytes = kMxRowsW * 128 + tokens * 128;
         p.raw_bytes = kMxRowsW * 16 + (p.nt + 31) / 32 * 512;
         p.scale_bytes = 4 * kMxAtom * (1 + (p.nt + 127) / 128);
-        // rings: as many data stages as fit, the scales' loads as far ahead
-        p.raws = 4;
+        // as many stages as fit
         for (p.stages = kMxMaxStages; p.stages >= kMxMinStages && bytes() > kMxSmemLimit; --p.stages) {
         }
-        p.raws = kMxMaxRaw;
-        if (bytes() > kMxSmemLimit) p.raws = 4;
         if (p.stages >= kMxMinStages) break;
         if (p.nt <= 32) return cudaErrorInvalidValue;
     }

@@ -19,14 +19,14 @@
 // the tokens.  One CTA's shared memory takes 45 KB of operands for each 256 of K of its tile and gives them to the
 // tensor core once, at 128 bytes a clock 700 clocks for MMAs of 450; in a pair it is 30 KB.
 //
-// Scales are stored row-major, 16 bytes of a row for 512 values of K.  Two pairs of warps, in turn (one took 1400 clocks
-// for its chain of latencies, half as much again as the MMAs), bring them in by asynchronous copies
-// of 16 bytes (TMA boxes 16 bytes wide held up the loads of the codes behind them), a lane its own rows, and
+// Scales are stored row-major, 16 bytes of a row for 512 values of K.  Four pairs of warps take turns (a turn is a chain of
+// latencies of some 2000 clocks, the MMAs of 512 values are done in 900) to bring them in by asynchronous copies
+// of 16 bytes (TMA boxes 16 bytes wide held up the loads of the codes behind them), a lane its own rows, and to
 // write them, still in shared memory, in the order in which tcgen05.cp brings them to tensor memory (lane i,
 // column c: row 32 c + i; the four scales of 128 values of K to a word), so rows may start anywhere; the copies
 // and the MMAs that read them follow one another in the tensor pipe without a wait.
 //
-// One CTA per SM, 23 warps: the loads of W and of A, the MMAs, 4 scale warps, 16 epilogue warps (four on each scheduler:
+// One CTA per SM, 27 warps: the loads of W and of A, the MMAs, 8 scale warps, 16 epilogue warps (four on each scheduler:
 // with two, the activation's chains of latency set the time of a short K).  A wait on a barrier takes a warp some
 // 100 clocks even when there is nothing to wait for, and 256 of K are 450 clocks of MMAs, so each of these roles waits
 // once in that time: everything that a block of K needs arrives at one barrier.  Two accumulators let a tile's
@@ -50,8 +50,9 @@ namespace ilw {
 
 constexpr int kMxRowsW = 128;   // rows of W a CTA
 constexpr int kMxMaxTok = 224;  // tokens a tile
-constexpr int kMxMaxStages = 16, kMxMinStages = 4, kMxMaxRaw = 6;
-constexpr int kMxEpiWarp0 = 7, kMxEpiWarps = 16, kMxThreads = 32 * (kMxEpiWarp0 + kMxEpiWarps);
+constexpr int kMxMaxStages = 16, kMxMinStages = 4;
+constexpr int kMxScaleWarp0 = 3, kMxScaleSets = 4;  // pairs of scale warps
+constexpr int kMxEpiWarp0 = kMxScaleWarp0 + 2 * kMxScaleSets, kMxEpiWarps = 16, kMxThreads = 32 * (kMxEpiWarp0 + kMxEpiWarps);
 constexpr int kMxAtom = 512;    // bytes of the scales of 128 rows and 128 values of K
 constexpr int kMxPatch = 512;   // bytes of shared memory in which an epilogue warp turns 2-byte results
 constexpr int kMxSmemLimit = 226 * 1024;  // dynamic; the barriers are static
@@ -77,7 +78,7 @@ struct MxParams {
     uint32_t wdiv_m, wdiv_s;  // division by wtiles
     int32_t nt;             // most tokens a tile, a multiple of 16 (a pair's: of 32)
     int32_t abox;           // rows of A a TMA box, one a stage; 0: as many boxes of 128 to 16 rows as its rows take
-    int32_t stages, raws;   // ring sizes: data, scales as loaded (4 or 6)
+    int32_t stages;         // stages of codes
     int32_t stage_bytes, raw_bytes, scale_bytes;
     int32_t wide;           // 2-byte rows of Y take 16-byte stores
     int32_t splits;         // CTAs of a cluster that share a tile's K (SPLIT)
@@ -188,17 +189,6 @@ template <bool PAIR>
 __device__ __forceinline__ void copy_scales(uint32_t t, uint64_t d) {
     if constexpr (PAIR) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(t), "l"(d) : "memory");
     else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(t), "l"(d) : "memory");
-}
-// Waits until no more than n of this thread's groups of asynchronous copies are in flight.
-__device__ __forceinline__ void copies_but(int n) {
-    switch (n) {
-        case 1: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
-        case 2: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
-        case 3: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
-        case 4: asm volatile("cp.async.wait_group 4;" ::: "memory"); break;
-        case 5: asm volatile("cp.async.wait_group 5;" ::: "memory"); break;
-        default: asm volatile("cp.async.wait_group 0;" ::: "memory");
-    }
 }
 __device__ __forceinline__ void lds128(uint32_t a, uint32_t (&v)[4]) {
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
@@ -347,13 +337,13 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
     // W's rows, 2 x 8 of A's)
     constexpr int kScaleCol = 2 * kMxMaxTok, kScaleCols = 24;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bars[3 * kMxMaxStages + 5];
+    __shared__ uint64_t bars[3 * kMxMaxStages + kMxScaleSets + 5];
     __shared__ uint32_t tmem_base;
     __shared__ volatile int abort_flag;
     __shared__ int32_t s_experts, s_head, s_tail;  // experts with rows; rows before the first and from the end of the last
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t data0 = (su32(smem_raw) + 1023) & ~1023u;
-    const uint32_t raw0 = data0 + p.stages * p.stage_bytes, scale0 = raw0 + p.raws * p.raw_bytes;
+    const uint32_t raw0 = data0 + p.stages * p.stage_bytes, scale0 = raw0 + kMxScaleSets * p.raw_bytes;
     const uint32_t patch0 = scale0 + 2 * p.scale_bytes;
     MxExpert *tab = (MxExpert *)(smem_raw + (patch0 - su32(smem_raw)) + (p.wide ? kMxEpiWarps * kMxPatch : 0));
     int32_t *tab_id = (int32_t *)(tab + p.E + 1);
@@ -367,6 +357,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
     // full: a block of K is there, codes and scales (a pair's, at the first CTA: in both); its own: this CTA's codes are, for
     // the second CTA of a pair to pass on
     const uint32_t full = take(kMxMaxStages), empty = take(kMxMaxStages), own = take(kMxMaxStages);
+    const uint32_t sfree = take(kMxScaleSets);                          // a place for the scales of a pair's next turn
     const uint32_t afull = take(2), aempty = take(2), drain = take(1);  // accumulators
 
     const uint32_t rank = SPLIT ? blockIdx.x % p.splits : PAIR ? blockIdx.x & 1 : 0;
@@ -382,6 +373,8 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
             bar_init(aempty + 8 * (lane - kMxMaxStages), PAIR ? 2 * kMxEpiWarps : kMxEpiWarps);
         } else if (lane == kMxMaxStages + 2) {
             bar_init(drain, 1);
+        } else if (lane < kMxMaxStages + 3 + kMxScaleSets) {
+            bar_init(sfree + 8 * (lane - kMxMaxStages - 3), 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -462,8 +455,8 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
     auto mma_tokens = [&](const Tile &x) { return PAIR ? (x.rows + 31) & ~31 : (x.rows + 15) & ~15; };
 
     // (SPLIT: a cluster has one tile at most, the host gives it as many clusters as there can be tiles)
-    if (warp == 0 || warp == 4) {
-        // loads of the codes: warp 0 of W, warp 4 of A
+    if (warp == 0 || warp == 2) {
+        // loads of the codes: warp 0 of W, warp 2 of A
         const uint32_t one = elect_one();
         const uint32_t arrives = leader ? full : own;
         uint32_t it = 0, s = 0, sp = 1;  // stages loaded, the place in the ring, the parity of a free one
@@ -514,7 +507,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
         __syncwarp();
     } else if (warp == 1 && leader) {
         const uint32_t one = elect_one();
-        uint32_t n = 0, s = 0, sp = 0, at = 0;  // at: the stage's offset in units of 16 bytes, as descriptors hold it
+        uint32_t n = 0, s = 0, sp = 0, st = 0, at = 0;  // at: the stage's offset in units of 16 bytes, as descriptors hold it
         const uint64_t desc0 = desc_sw128(data0), scales0 = scale_desc(scale0);
         uint64_t scales = scales0;  // the stage of scales: one of two
         const uint32_t scol = tmem + kScaleCol, half = 2 * kMxAtom * atoms / 16;
@@ -558,6 +551,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
                         if (!ok) break;
                     }
                     scales = scales == scales0 ? scales0 + p.scale_bytes / 16 : scales0;
+                    commit_mma<PAIR>(sfree + 8 * ((st++ + 2) % kMxScaleSets));  // (the turn after the next takes the place of these scales)
                 }
                 if (ok) commit_mma<PAIR>(afull + 8 * acc);
             }
@@ -583,22 +577,22 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
             }
         __syncwarp();
     } else if (warp < kMxEpiWarp0) {
-        // scales to the tensor core's order; warps 2 and 5: W's rows, 3 and 6: the tokens, in one or two parts of 128; 2 and 3: even
-        // stages, 5 and 6: odd ones.  A lane copies the 16 bytes of its rows 32 c + lane into the ring, some stages ahead,
-        // and is the only one to read them there.
+        // scales to the tensor core's order, a stage of 512 values of K a turn; the first warp of a pair: W's rows, the second: the
+        // tokens, in one or two parts of 128.  A lane copies the 16 bytes of its rows 32 c + lane into the pair's place when it is
+        // done with a turn's, and is the only one to read them there.
         const uint32_t total = first < tiles ? (uint32_t)((tiles - first + step - 1) / step) * (uint32_t)(sb_hi - sb_lo) : 0;
-        const uint32_t turn = warp >= 5;
-        const int part = warp - (turn ? 5 : 2), parts = part == 0 ? 1 : atoms - 1, ahead = p.raws / 2 - 1;
+        const uint32_t turn = (warp - kMxScaleWarp0) >> 1;
+        const int part = (warp - kMxScaleWarp0) & 1, parts = part == 0 ? 1 : atoms - 1;
         const int64_t pitch = part == 0 ? p.w_lds : p.a_lds;
+        const uint32_t raw = raw0 + turn * p.raw_bytes + part * kMxRowsW * 16 + lane * 16;
         int32_t lt = first, lsb = sb_lo;  // the stage to load next
-        uint32_t lr = turn;
-        const uint8_t *base = nullptr;  // its rows: from `base` on, `pitch` apart, `rows` of them
+        const uint8_t *base = nullptr;    // its rows: from `base` on, `pitch` apart, `rows` of them
         int rows = 0;
-        auto next = [&] {
-            if (++lsb < sb_hi) return false;
-            lsb = sb_lo;
-            lt += step;
-            return true;
+        auto skip = [&](int n) {  // n stages on; whether that is another tile
+            lsb += n;
+            bool another = false;
+            while (lsb >= sb_hi) lsb -= sb_hi - sb_lo, lt += step, another = true;
+            return another;
         };
         auto begin = [&] {
             if (lt >= tiles) return;
@@ -606,46 +600,45 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
             base = part == 0 ? p.w_scales + x.e * p.w_scales_stride + x.n0 * p.w_lds : p.a_scales + x.row0 * p.a_lds;
             rows = part == 0 ? p.N - x.n0 : x.rows;
         };
-        if (turn) next();
-        begin();
         auto load = [&] {
-            if (lt < tiles) {
-                const uint32_t n = min(p.nb - 16 * lsb, 16);
-                const uint32_t dst = raw0 + lr * p.raw_bytes + part * kMxRowsW * 16 + lane * 16;
-                const uint8_t *src = base + 16 * lsb + lane * pitch;
-                const int last = part == 0 ? 4 : (p.nt + 31) / 32;
-                for (int c = 0; c < last; ++c, src += 32 * pitch) {
-                    const bool in = 32 * c + lane < rows;
-                    cpa16(dst + c * 512, in ? src : base, in ? n : 0);
-                }
-                const bool another = next();
-                if (next() || another) begin();
-                if ((lr += 2) >= (uint32_t)p.raws) lr = turn;
+            if (lt >= tiles) return;
+            const uint32_t n = min(p.nb - 16 * lsb, 16);
+            const uint8_t *src = base + 16 * lsb + lane * pitch;
+            const int last = part == 0 ? 4 : (p.nt + 31) / 32;
+            for (int c = 0; c < last; ++c, src += 32 * pitch) {
+                const bool in = 32 * c + lane < rows;
+                cpa16(raw + c * 512, in ? src : base, in ? n : 0);
             }
-            cpa_commit();
+            if (skip(kMxScaleSets)) begin();
         };
-        for (int i = 0; i < ahead; ++i) load();
-        // Two stages of scales in order: stage st takes the place of st - 2, free when the last MMAs that used it have ended, which
-        // frees their data stage too
-        uint32_t r = turn, s = 0, sp = 0, last = 0, lastp = 0;
+        skip(turn);
+        begin();
+        load();
+        // Two stages of scales in order: stage st takes the place of st - 2, whose MMAs then complete a phase of this pair's barrier:
+        // one a turn, and none before the last has been seen, for the MMAs of st need what is written here
+        uint32_t s = 0, fp = 0;
         int32_t sb = sb_lo;
         for (uint32_t st = 0; st < total; ++st) {
             const int blocks = min(2, p.nkb - 2 * sb);
             if (++sb == sb_hi) sb = sb_lo;
-            if ((st & 1) == turn) {
-                load();
-                copies_but(ahead);
-                const uint32_t src = raw0 + r * p.raw_bytes + part * kMxRowsW * 16 + lane * 16;
-                uint32_t w[2][4][4];
+            const bool mine = st % kMxScaleSets == turn;
+            uint32_t w[2][4][4];
+            if (mine) {
+                asm volatile("cp.async.wait_all;" ::: "memory");
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         w[i][c][0] = w[i][c][1] = w[i][c][2] = w[i][c][3] = 0;
-                        if (i < parts && (part == 0 || 128 * i + 32 * c < p.nt)) lds128(src + i * kMxRowsW * 16 + c * 512, w[i][c]);
+                        if (i < parts && (part == 0 || 128 * i + 32 * c < p.nt)) lds128(raw + i * kMxRowsW * 16 + c * 512, w[i][c]);
                     }
-                if (st >= 2 && !wait_warp(last, lastp, &abort_flag, p, kStatusTimeoutFree)) break;
-                const uint32_t dst = scale0 + turn * p.scale_bytes + part * kMxAtom + lane * 16;
+            }
+            if (mine && st >= 2) {
+                if (!wait_warp(sfree + 8 * turn, fp, &abort_flag, p, kStatusTimeoutFree)) break;
+                fp ^= 1;
+            }
+            if (mine) {
+                const uint32_t dst = scale0 + (st & 1) * p.scale_bytes + part * kMxAtom + lane * 16;
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
                     if (i < parts) {
@@ -657,20 +650,17 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
                     }
                 fence_async_smem();
                 __syncwarp();
-                if ((r += 2) >= (uint32_t)p.raws) r = turn;
             }
             for (int i = 0; i < blocks; ++i) {
-                if ((st & 1) == turn) {
-                    if (lane == 0) {
-                        if constexpr (PAIR) arrive_cluster(in_cta(full + 8 * s, 0));
-                        else bar_arrive(full + 8 * s);
-                    }
-                    last = empty + 8 * s, lastp = sp;
+                if (mine && lane == 0) {
+                    if constexpr (PAIR) arrive_cluster(in_cta(full + 8 * s, 0));
+                    else bar_arrive(full + 8 * s);
                 }
-                if (++s == (uint32_t)p.stages) s = 0, sp ^= 1;
+                if (++s == (uint32_t)p.stages) s = 0;
             }
+            if (mine) load();  // (what it overwrites has gone into the stores above)
         }
-        copies_but(0);
+        asm volatile("cp.async.wait_all;" ::: "memory");
     } else {
         const uint32_t quarter = (uint32_t)(warp & 3) << 21;  // lane field of the warp's 32 lanes
         const int part = (warp - kMxEpiWarp0) >> 2, row = 32 * (warp & 3) + lane;

@@ -228,6 +228,36 @@ def test_linear_of_few_tiles(ilw, splits, K):
         assert all(torch.equal(got, ilw.mx_linear(A, W, out_dtype=torch.float32)) for _ in range(5))
 
 
+@pytest.mark.parametrize("act,K", [("none", 32), ("none", 1300), ("gelu", 2100), ("silu_gate", 4096)])
+def test_linear_of_many_tiles(ilw, act, K):
+    """As many tiles as two SMs share each (256 outputs, up to 224 tokens), over one to eight stages of scales; the same bits again."""
+    rng = np.random.default_rng(K)
+    M, N = 3001, 1700
+    A, W = packed(ilw, values(rng, M, K)), packed(ilw, rng.standard_normal((N, K)) / np.sqrt(K))
+    a, w = ref_values(*host(A), K), ref_values(*host(W), K)
+    for dtype in (torch.float32, torch.bfloat16):
+        got = ilw.mx_linear(A, W, act=act, out_dtype=dtype)
+        check_product(got, a, w, None, act, dtype)
+        assert all(torch.equal(got, ilw.mx_linear(A, W, act=act, out_dtype=dtype)) for _ in range(3))
+    ilw.device_status()
+
+
+@pytest.mark.parametrize("K,act", [(200, "none"), (1600, "silu_gate")])
+def test_grouped_of_many_tiles(ilw, K, act):
+    """Long ragged groups, whose tiles two SMs share."""
+    rng = np.random.default_rng(K)
+    counts, N = [700, 0, 1, 333, 1024, 225, 95], 2304
+    off = np.r_[0, np.cumsum(counts)]
+    A, W = packed(ilw, values(rng, int(off[-1]), K)), packed(ilw, rng.standard_normal((len(counts), N, K)) / np.sqrt(K))
+    a, w = ref_values(*host(A), K), ref_values(*host(W), K)
+    for dtype in (torch.float32, torch.bfloat16):
+        got = ilw.mx_grouped_linear(A, W, torch.from_numpy(off.astype(np.int32)).cuda(), act=act, out_dtype=dtype)
+        for e in range(len(counts)):
+            if counts[e]:
+                check_product(got[off[e]: off[e + 1]], a[off[e]: off[e + 1]], w[e], None, act, dtype)
+    ilw.device_status()
+
+
 def test_linear_rows_with_strides(ilw):
     """Operands inside wider byte arrays, a result inside a wider tensor, fp16."""
     rng = np.random.default_rng(11)
