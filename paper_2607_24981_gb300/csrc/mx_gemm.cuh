@@ -26,12 +26,14 @@
 // column c: row 32 c + i; the four scales of 128 values of K to a word), so rows may start anywhere; the copies
 // and the MMAs that read them follow one another in the tensor pipe without a wait.
 //
-// One CTA per SM, 27 warps: the loads of W and of A, the MMAs, 8 scale warps, 16 epilogue warps (four on each scheduler:
+// One CTA per SM, 28 warps: the loads of W and of A, the MMAs, 8 scale warps, 16 epilogue warps (four on each scheduler:
 // with two, the activation's chains of latency set the time of a short K).  A wait on a barrier takes a warp some
 // 100 clocks even when there is nothing to wait for, and 256 of K are 450 clocks of MMAs, so each of these roles waits
 // once in that time: everything that a block of K needs arrives at one barrier.  Two accumulators let a tile's
 // epilogue overlap the next tile's MMAs.  Tiles are dealt out in turn; with experts each CTA works out the list
-// of tiles from the offsets itself, so no count has to reach the host.
+// of experts that have rows from the offsets itself, so no count has to reach the host, and the last warp finds each tile's
+// rows ahead of the others (a role that did so itself lost some 2000 clocks a tile: code that runs once a tile is never
+// in the instruction caches that so many roles share).
 //
 // Every mbarrier wait is bounded; on expiry the kernel latches the device status word, stops issuing
 // work, waits for its loads and MMAs in flight and frees its tensor memory.
@@ -52,7 +54,9 @@ constexpr int kMxRowsW = 128;   // rows of W a CTA
 constexpr int kMxMaxTok = 224;  // tokens a tile
 constexpr int kMxMaxStages = 16, kMxMinStages = 4;
 constexpr int kMxScaleWarp0 = 3, kMxScaleSets = 4;  // pairs of scale warps
-constexpr int kMxEpiWarp0 = kMxScaleWarp0 + 2 * kMxScaleSets, kMxEpiWarps = 16, kMxThreads = 32 * (kMxEpiWarp0 + kMxEpiWarps);
+constexpr int kMxEpiWarp0 = kMxScaleWarp0 + 2 * kMxScaleSets, kMxEpiWarps = 16, kMxTileWarp = kMxEpiWarp0 + kMxEpiWarps;
+constexpr int kMxThreads = 32 * (kMxTileWarp + 1);
+constexpr int kMxTiles = 16;    // tiles found ahead
 constexpr int kMxAtom = 512;    // bytes of the scales of 128 rows and 128 values of K
 constexpr int kMxPatch = 512;   // bytes of shared memory in which an epilogue warp turns 2-byte results
 constexpr int kMxSmemLimit = 226 * 1024;  // dynamic; the barriers are static
@@ -337,7 +341,8 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
     // W's rows, 2 x 8 of A's)
     constexpr int kScaleCol = 2 * kMxMaxTok, kScaleCols = 24;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bars[3 * kMxMaxStages + kMxScaleSets + 5];
+    __shared__ uint64_t bars[3 * kMxMaxStages + kMxScaleSets + 2 * kMxTiles + 5];
+    __shared__ int4 tile_ring[kMxTiles];
     __shared__ uint32_t tmem_base;
     __shared__ volatile int abort_flag;
     __shared__ int32_t s_experts, s_head, s_tail;  // experts with rows; rows before the first and from the end of the last
@@ -358,6 +363,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
     // the second CTA of a pair to pass on
     const uint32_t full = take(kMxMaxStages), empty = take(kMxMaxStages), own = take(kMxMaxStages);
     const uint32_t sfree = take(kMxScaleSets);                          // a place for the scales of a pair's next turn
+    const uint32_t tfull = take(kMxTiles), tfree = take(kMxTiles);      // tiles found, and read by every warp
     const uint32_t afull = take(2), aempty = take(2), drain = take(1);  // accumulators
 
     const uint32_t rank = SPLIT ? blockIdx.x % p.splits : PAIR ? blockIdx.x & 1 : 0;
@@ -368,6 +374,8 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
             bar_init(full + 8 * lane, PAIR ? 2 + 1 + 4 : 2 + 2);  // loads, the second CTA's word, scale warps
             bar_init(empty + 8 * lane, 1);
             bar_init(own + 8 * lane, 2);
+            bar_init(tfull + 8 * lane, 1);
+            bar_init(tfree + 8 * lane, kMxTileWarp);
         } else if (lane < kMxMaxStages + 2) {
             bar_init(afull + 8 * (lane - kMxMaxStages), 1);
             bar_init(aempty + 8 * (lane - kMxMaxStages), PAIR ? 2 * kMxEpiWarps : kMxEpiWarps);
@@ -451,7 +459,19 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
     const int32_t sb_hi = SPLIT ? (int32_t)((int64_t)p.nsb * (rank + 1) / p.splits) : p.nsb;
     const int32_t kb_hi = min(2 * sb_hi, p.nkb);
     const int atoms = 1 + (p.nt + 127) / 128;  // of W's rows, and of A's
-    auto tile_at = [&](int32_t t) { return find_tile<MODE>(p, tab, tab_id, experts, t, rank); };
+    // the next tile of this CTA, as the last warp has found it (by a whole warp; false when a wait ran out)
+    uint32_t tiles_read = 0;
+    auto next_tile = [&](Tile &x) {
+        const uint32_t i = tiles_read % kMxTiles;
+        if (!wait_warp(tfull + 8 * i, (tiles_read / kMxTiles) & 1, &abort_flag, p, kStatusTimeoutOperand)) return false;
+        const int4 v = tile_ring[i];
+        x = Tile{v.x, v.y, v.z, v.w};
+        __syncwarp();
+        if (lane == 0) bar_arrive(tfree + 8 * i);
+        ++tiles_read;
+        return true;
+    };
+    Tile x = {};  // (an epilogue warp's)
     auto mma_tokens = [&](const Tile &x) { return PAIR ? (x.rows + 31) & ~31 : (x.rows + 15) & ~15; };
 
     // (SPLIT: a cluster has one tile at most, the host gives it as many clusters as there can be tiles)
@@ -461,9 +481,11 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
         const uint32_t arrives = leader ? full : own;
         uint32_t it = 0, s = 0, sp = 1;  // stages loaded, the place in the ring, the parity of a free one
         bool ok = true;
-        for (int32_t t = first; ok && t < tiles; t += step) {
-            Tile x = tile_at(t);
-            x.e = uniform(x.e), x.row0 = uniform(x.row0), x.rows = uniform(x.rows);
+        for (int32_t t = first; t < tiles; t += step) {
+            Tile x;
+            ok = ok && next_tile(x);
+            if (!ok) break;
+            x.e = uniform(x.e), x.row0 = uniform(x.row0), x.rows = uniform(x.rows), x.n0 = uniform(x.n0);
             // a pair's CTA loads its half of the tokens
             const int part = PAIR ? mma_tokens(x) / 2 : x.rows, row = x.row0 + (PAIR ? (int)rank * part : 0);
             const int units = (part + 15) >> 4;
@@ -512,9 +534,10 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
         uint64_t scales = scales0;  // the stage of scales: one of two
         const uint32_t scol = tmem + kScaleCol, half = 2 * kMxAtom * atoms / 16;
         bool ok = true;
-        Tile x = {};
-        if (first < tiles) x = tile_at(first);
         for (int32_t t = first; ok && t < tiles; t += step, ++n) {
+            Tile x;
+            ok = next_tile(x);
+            if (!ok) break;
             const uint32_t acc = n & 1, d = tmem + acc * kMxMaxTok;
             const uint32_t id = idesc_mx(PAIR ? 256 : 128, uniform(mma_tokens(x)), 0);
             ok = wait_warp(aempty + 8 * acc, ((n >> 1) & 1) ^ 1, &abort_flag, p, kStatusTimeoutFree);
@@ -556,7 +579,6 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
                 if (ok) commit_mma<PAIR>(afull + 8 * acc);
             }
             ok = __all_sync(0xffffffffu, ok);
-            if (t + step < tiles) x = tile_at(t + step);  // (while the MMAs run)
         }
         if (!ok && one) {  // the MMAs in flight end before tensor memory is freed
             commit_mma<PAIR>(drain, true);
@@ -569,12 +591,15 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
         // a pair's second CTA tells the first what has arrived here
         uint32_t s = 0, sp = 0;
         bool ok = true;
-        for (int32_t t = first; ok && t < tiles; t += step)
+        for (int32_t t = first; ok && t < tiles; t += step) {
+            Tile x;
+            ok = next_tile(x);  // (read like everyone's, so that its place can be filled again)
             for (int32_t kb = 2 * sb_lo; ok && kb < kb_hi; ++kb) {
                 ok = wait_warp(own + 8 * s, sp, &abort_flag, p, kStatusTimeoutTma);
                 if (ok && lane == 0) arrive_cluster(in_cta(full + 8 * s, 0));
                 if (++s == (uint32_t)p.stages) s = 0, sp ^= 1;
             }
+        }
         __syncwarp();
     } else if (warp < kMxEpiWarp0) {
         // scales to the tensor core's order, a stage of 512 values of K a turn; the first warp of a pair: W's rows, the second: the
@@ -588,20 +613,23 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
         int32_t lt = first, lsb = sb_lo;  // the stage to load next
         const uint8_t *base = nullptr;    // its rows: from `base` on, `pitch` apart, `rows` of them
         int rows = 0;
-        auto skip = [&](int n) {  // n stages on; whether that is another tile
-            lsb += n;
-            bool another = false;
-            while (lsb >= sb_hi) lsb -= sb_hi - sb_lo, lt += step, another = true;
-            return another;
-        };
+        bool ok = true;
         auto begin = [&] {
-            if (lt >= tiles) return;
-            const Tile x = tile_at(lt);
+            Tile x;
+            if (lt >= tiles || !(ok = ok && next_tile(x))) return;
             base = part == 0 ? p.w_scales + x.e * p.w_scales_stride + x.n0 * p.w_lds : p.a_scales + x.row0 * p.a_lds;
             rows = part == 0 ? p.N - x.n0 : x.rows;
         };
+        auto skip = [&](int n) {  // n stages on
+            lsb += n;
+            while (lsb >= sb_hi) {
+                lsb -= sb_hi - sb_lo;
+                lt += step;
+                begin();
+            }
+        };
         auto load = [&] {
-            if (lt >= tiles) return;
+            if (lt >= tiles || !ok) return;
             const uint32_t n = min(p.nb - 16 * lsb, 16);
             const uint8_t *src = base + 16 * lsb + lane * pitch;
             const int last = part == 0 ? 4 : (p.nt + 31) / 32;
@@ -609,16 +637,16 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
                 const bool in = 32 * c + lane < rows;
                 cpa16(raw + c * 512, in ? src : base, in ? n : 0);
             }
-            if (skip(kMxScaleSets)) begin();
+            skip(kMxScaleSets);
         };
-        skip(turn);
         begin();
+        skip(turn);
         load();
         // Two stages of scales in order: stage st takes the place of st - 2, whose MMAs then complete a phase of this pair's barrier:
         // one a turn, and none before the last has been seen, for the MMAs of st need what is written here
         uint32_t s = 0, fp = 0;
         int32_t sb = sb_lo;
-        for (uint32_t st = 0; st < total; ++st) {
+        for (uint32_t st = 0; ok && st < total; ++st) {
             const int blocks = min(2, p.nkb - 2 * sb);
             if (++sb == sb_hi) sb = sb_lo;
             const bool mine = st % kMxScaleSets == turn;
@@ -634,7 +662,8 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
                     }
             }
             if (mine && st >= 2) {
-                if (!wait_warp(sfree + 8 * turn, fp, &abort_flag, p, kStatusTimeoutFree)) break;
+                ok = wait_warp(sfree + 8 * turn, fp, &abort_flag, p, kStatusTimeoutFree);
+                if (!ok) break;
                 fp ^= 1;
             }
             if (mine) {
@@ -661,15 +690,14 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
             if (mine) load();  // (what it overwrites has gone into the stores above)
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
-    } else {
+    } else if (warp < kMxTileWarp) {
         const uint32_t quarter = (uint32_t)(warp & 3) << 21;  // lane field of the warp's 32 lanes
         const int part = (warp - kMxEpiWarp0) >> 2, row = 32 * (warp & 3) + lane;
         const uint32_t patch = patch0 + (warp - kMxEpiWarp0) * kMxPatch;
         const uint32_t free0 = PAIR ? in_cta(aempty, 0) : aempty;
         uint32_t n = 0;
-        Tile x = {};
-        if (first < tiles) x = tile_at(first);
         for (int32_t t = first; t < tiles; t += step, ++n) {
+            if (!next_tile(x)) break;
             const uint32_t acc = n & 1;
             const int nn = x.n0 + row;
             const float bias = !SPLIT && p.bias && nn < p.N ? p.bias[(int64_t)x.e * p.N + nn] : 0.0f;
@@ -696,15 +724,26 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
                 if constexpr (PAIR) arrive_cluster(free0 + 8 * acc);
                 else bar_arrive(aempty + 8 * acc);
             }
-            if (t + step < tiles) x = tile_at(t + step);
+        }
+    } else {
+        // the tiles of this CTA, one after the other
+        uint32_t n = 0;
+        for (int32_t t = first; t < tiles; t += step, ++n) {
+            const uint32_t i = n % kMxTiles;
+            if (!wait_warp(tfree + 8 * i, ((n / kMxTiles) & 1) ^ 1, &abort_flag, p, kStatusTimeoutFree)) break;
+            const Tile x = find_tile<MODE>(p, tab, tab_id, experts, t, rank);
+            if (lane == 0) {
+                tile_ring[i] = make_int4(x.e, x.row0, x.rows, x.n0);
+                bar_arrive(tfull + 8 * i);
+            }
+            __syncwarp();
         }
     }
     if constexpr (SPLIT) {
         __syncwarp();
         cluster_sync();
-        if (first < tiles && !abort_flag && warp >= kMxEpiWarp0) {
+        if (first < tiles && !abort_flag && warp >= kMxEpiWarp0 && warp < kMxTileWarp) {
             // each warp of the cluster finishes the 32 rows of W of a quarter for four tokens at a time
-            const Tile x = tile_at(first);
             const int w = warp - kMxEpiWarp0, units = 4 * ((x.rows + 3) / 4);
             for (int u = w + kMxEpiWarps * rank; u < units; u += kMxEpiWarps * p.splits) {
                 const int c0 = u & ~3, row = 32 * (u & 3) + lane, nn = x.n0 + row;
