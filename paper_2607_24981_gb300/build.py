@@ -1,6 +1,7 @@
 """Build libilwdetr.so (the C-ABI of include/ilwdetr.h) for sm_103a with nvcc, in-tree.
 
-Each translation unit is compiled in parallel; the shared library is written next to this file.
+Each translation unit is compiled in parallel; the shared library is written next to this file, and beside it
+_mxbind.so, the Python binding of the operators in mx.py (host code against torch's headers).
 """
 from __future__ import annotations
 
@@ -15,6 +16,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libilwdetr.so")
+BIND_SRC, BIND = os.path.join(CSRC, "mx_bind.cpp"), os.path.join(HERE, "_mxbind.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC, "--expt-relaxed-constexpr"]
@@ -38,6 +40,29 @@ def _stale(out: str, deps: list[str]) -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def build_binding(verbose: bool = False) -> str:
+    """_mxbind.so: one host translation unit, linked with torch's own libraries."""
+    import sysconfig
+
+    import torch
+
+    base = torch.__path__[0]
+    cuda = os.path.dirname(os.path.dirname(nvcc()))
+    tmp = BIND + ".tmp%d" % os.getpid()
+    cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-Wall", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI]
+    for d in (sysconfig.get_paths()["include"], os.path.join(base, "include"), os.path.join(cuda, "include")):
+        cmd += ["-isystem", d]
+    cmd += ["-I", os.path.join(ROOT, "include"), BIND_SRC, "-o", tmp, "-L", os.path.join(base, "lib"), "-Wl,-rpath," + os.path.join(base, "lib"),
+            "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+    if verbose:
+        print(" ".join(cmd), file=sys.stderr)
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"g++ failed on {os.path.basename(BIND_SRC)}:\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, BIND)
+    return r.stderr
+
+
 def build(force: bool = False, verbose: bool = False, extra: list[str] | None = None) -> str:
     os.makedirs(OBJ, exist_ok=True)
     headers = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".h", ".cuh"))]
@@ -56,10 +81,14 @@ def build(force: bool = False, verbose: bool = False, extra: list[str] | None = 
             raise RuntimeError(f"nvcc failed on {os.path.basename(s)}:\n{r.stdout}\n{r.stderr}")
         return r.stderr
 
-    with cf.ThreadPoolExecutor(max_workers=min(8, max(1, len(todo)))) as ex:
+    bind = force or _stale(BIND, [BIND_SRC, os.path.join(ROOT, "include", "ilwdetr.h")])
+    with cf.ThreadPoolExecutor(max_workers=min(9, 1 + len(todo))) as ex:
+        binding = ex.submit(build_binding, verbose) if bind else None
         for msg in ex.map(compile_one, todo):
             if verbose and msg:
                 print(msg, file=sys.stderr)
+        if binding:
+            binding.result()
     if force or todo or _stale(LIB, objs):
         tmp = LIB + ".tmp%d" % os.getpid()
         cmd = [nvcc()] + ARCH + ["-shared", "-Xcompiler", "-fPIC", "-o", tmp] + objs

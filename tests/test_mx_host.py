@@ -136,3 +136,14 @@ def test_binding_refuses_what_it_cannot_pass_on():
         ilw.mx_linear(m._replace(k=65), m)
     with pytest.raises(ilw.IlwError, match="GPU"):
         ilw.mx_grouped_linear(m, m, torch.zeros(5, dtype=torch.int32))
+
+
+def test_binding_fails_loudly_without_its_library(monkeypatch):
+    """With _mxbind.so absent a call raises instead of computing anything elsewhere."""
+    torch = pytest.importorskip("torch")
+    from paper_2607_24981_gb300 import IlwError, mx
+
+    monkeypatch.setattr(mx, "_bound", None)
+    monkeypatch.setattr(mx, "BIND_PATH", mx.BIND_PATH + ".absent")
+    with pytest.raises(IlwError, match="missing"):
+        mx.moe_route(torch.zeros(2, 4), 1)
