@@ -251,26 +251,29 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
-__device__ __forceinline__ float exp2_fast(float x) {
+__device__ __forceinline__ float rcp_fast(float x) {
     float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-// z (1 + erf(z / sqrt 2)) / 2 of two values, with erf by Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26
-// (absolute error at most 1.5e-7): about 10 operations a value.
+// z (1 + erf(z / sqrt 2)) / 2 of two values, with erf |x| = 1 - (1 + a1 |x| + ... + a6 |x|^6)^-16 by Abramowitz and Stegun, Handbook
+// of Mathematical Functions, 7.1.28 (absolute error at most 3e-7): two operations of the special-function unit for the
+// two values.  (With 7.1.26, an exponential and a reciprocal each, that unit was the epilogue's time.)
 __device__ __forceinline__ void gelu2(float &a, float &b) {
-    const uint64_t z = pack2(a, b);
-    const float2 d = unpack2(fma2(pack2(fabsf(a), fabsf(b)), pack2(0.23164190f, 0.23164190f), pack2(1.0f, 1.0f)));  // 0.3275911 / sqrt 2
-    const uint64_t t = pack2(__fdividef(1.0f, d.x), __fdividef(1.0f, d.y));
-    uint64_t q = fma2(t, pack2(-1.061405429f, -1.061405429f), pack2(1.453152027f, 1.453152027f));  // (-erf's polynomial)
-    q = fma2(q, t, pack2(-1.421413741f, -1.421413741f));
-    q = fma2(q, t, pack2(0.284496736f, 0.284496736f));
-    q = fma2(q, t, pack2(-0.254829592f, -0.254829592f));
-    q = mul2(q, t);
-    const float2 x = unpack2(mul2(mul2(z, z), pack2(-0.72134752f, -0.72134752f)));  // -z^2 / 2 log2 e
-    const float2 e = unpack2(fma2(q, pack2(exp2_fast(x.x), exp2_fast(x.y)), pack2(1.0f, 1.0f)));  // erf |z / sqrt 2|
+    const uint64_t z = pack2(a, b), x = pack2(fabsf(a), fabsf(b));
+    // the coefficients a_i / 2^(i/2): x here is |z|, not |z| / sqrt 2
+    uint64_t q = fma2(x, pack2(5.3829750e-6f, 5.3829750e-6f), pack2(4.8890637e-5f, 4.8890637e-5f));
+    q = fma2(q, x, pack2(3.8003575e-5f, 3.8003575e-5f));
+    q = fma2(q, x, pack2(3.2776263e-3f, 3.2776263e-3f));
+    q = fma2(q, x, pack2(2.1141006e-2f, 2.1141006e-2f));
+    q = fma2(q, x, pack2(4.9867347e-2f, 4.9867347e-2f));
+    q = fma2(q, x, pack2(1.0f, 1.0f));
+    q = mul2(q, q);
+    q = mul2(q, q);
+    q = mul2(q, q);
+    const float2 d = unpack2(mul2(q, q));
     const uint64_t h = mul2(z, pack2(0.5f, 0.5f));
-    const float2 r = unpack2(fma2(h, pack2(copysignf(e.x, a), copysignf(e.y, b)), h));
+    const float2 r = unpack2(fma2(h, pack2(copysignf(1.0f - rcp_fast(d.x), a), copysignf(1.0f - rcp_fast(d.y), b)), h));
     a = r.x;
     b = r.y;
 }
@@ -368,6 +371,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
 
     const uint32_t rank = SPLIT ? blockIdx.x % p.splits : PAIR ? blockIdx.x & 1 : 0;
     const bool leader = !PAIR || rank == 0;
+    const int32_t group = SPLIT ? p.splits : PAIR ? 2 : 1, first = (int32_t)blockIdx.x / group;
     if (warp == 0) {
         if (lane == 0) abort_flag = 0;
         if (lane < kMxMaxStages) {
@@ -445,6 +449,11 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
             s_head = head;
             s_tail = before;
         }
+        __syncwarp();
+        if (first < sum * p.wtiles) {  // the first tile at once; the others follow from the last warp
+            const Tile y = find_tile<MODE>(p, tab, tab_id, count, first, rank);
+            if (lane == 0) tile_ring[0] = make_int4(y.e, y.row0, y.rows, y.n0);
+        }
     }
     fence_before();
     if constexpr (PAIR) cluster_sync();
@@ -453,8 +462,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
     const uint32_t tmem = uniform(tmem_base);
     const int experts = s_experts;
     const int32_t tiles = tab[experts].start * p.wtiles;
-    const int32_t group = SPLIT ? p.splits : PAIR ? 2 : 1;
-    const int32_t first = (int32_t)blockIdx.x / group, step = (int32_t)gridDim.x / group;
+    const int32_t step = (int32_t)gridDim.x / group;
     const int32_t sb_lo = SPLIT ? (int32_t)((int64_t)p.nsb * rank / p.splits) : 0;
     const int32_t sb_hi = SPLIT ? (int32_t)((int64_t)p.nsb * (rank + 1) / p.splits) : p.nsb;
     const int32_t kb_hi = min(2 * sb_hi, p.nkb);
@@ -463,7 +471,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
     uint32_t tiles_read = 0;
     auto next_tile = [&](Tile &x) {
         const uint32_t i = tiles_read % kMxTiles;
-        if (!wait_warp(tfull + 8 * i, (tiles_read / kMxTiles) & 1, &abort_flag, p, kStatusTimeoutOperand)) return false;
+        if (tiles_read > 0 && !wait_warp(tfull + 8 * i, (tiles_read / kMxTiles) & 1, &abort_flag, p, kStatusTimeoutOperand)) return false;
         const int4 v = tile_ring[i];
         x = Tile{v.x, v.y, v.z, v.w};
         __syncwarp();
@@ -637,7 +645,6 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
                 const bool in = 32 * c + lane < rows;
                 cpa16(raw + c * 512, in ? src : base, in ? n : 0);
             }
-            skip(kMxScaleSets);
         };
         begin();
         skip(turn);
@@ -687,7 +694,10 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
                 }
                 if (++s == (uint32_t)p.stages) s = 0;
             }
-            if (mine) load();  // (what it overwrites has gone into the stores above)
+            if (mine) {  // (what is overwritten has gone into the stores above)
+                skip(kMxScaleSets);
+                load();
+            }
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
     } else if (warp < kMxTileWarp) {
@@ -696,13 +706,21 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
         const uint32_t patch = patch0 + (warp - kMxEpiWarp0) * kMxPatch;
         const uint32_t free0 = PAIR ? in_cta(aempty, 0) : aempty;
         uint32_t n = 0;
+        auto bias_of = [&](const Tile &y) {
+            const int nn = y.n0 + row;
+            return !SPLIT && p.bias && nn < p.N ? p.bias[(int64_t)y.e * p.N + nn] : 0.0f;
+        };
+        Tile next = {};  // (read, with its bias, while a tile is stored)
+        float next_bias = 0.0f;
+        if (first < tiles && next_tile(next)) next_bias = bias_of(next);
         for (int32_t t = first; t < tiles; t += step, ++n) {
-            if (!next_tile(x)) break;
             const uint32_t acc = n & 1;
+            x = next;
+            const float bias = next_bias;
             const int nn = x.n0 + row;
-            const float bias = !SPLIT && p.bias && nn < p.N ? p.bias[(int64_t)x.e * p.N + nn] : 0.0f;
             if (!wait_warp(afull + 8 * acc, (n >> 1) & 1, &abort_flag, p, kStatusTimeoutMma)) break;
             fence_after();
+            if (t + step < tiles && next_tile(next)) next_bias = bias_of(next);
             for (int c0 = 16 * part; c0 < x.rows; c0 += 64) {
                 uint32_t u[16];
                 tld<16>(tmem + quarter + acc * kMxMaxTok + c0, u);
@@ -730,12 +748,12 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
         uint32_t n = 0;
         for (int32_t t = first; t < tiles; t += step, ++n) {
             const uint32_t i = n % kMxTiles;
-            if (!wait_warp(tfree + 8 * i, ((n / kMxTiles) & 1) ^ 1, &abort_flag, p, kStatusTimeoutFree)) break;
-            const Tile x = find_tile<MODE>(p, tab, tab_id, experts, t, rank);
-            if (lane == 0) {
-                tile_ring[i] = make_int4(x.e, x.row0, x.rows, x.n0);
-                bar_arrive(tfull + 8 * i);
+            if (n >= kMxTiles && !wait_warp(tfree + 8 * i, (n / kMxTiles - 1) & 1, &abort_flag, p, kStatusTimeoutFree)) break;
+            if (n > 0) {
+                const Tile y = find_tile<MODE>(p, tab, tab_id, experts, t, rank);
+                if (lane == 0) tile_ring[i] = make_int4(y.e, y.row0, y.rows, y.n0);
             }
+            if (lane == 0) bar_arrive(tfull + 8 * i);
             __syncwarp();
         }
     }
