@@ -470,6 +470,11 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
     // the next tile of this CTA, as the last warp has found it (by a whole warp; false when a wait ran out)
     uint32_t tiles_read = 0;
     auto next_tile = [&](Tile &x) {
+        if constexpr (SPLIT) {  // (the only one)
+            const int4 v = tile_ring[0];
+            x = Tile{v.x, v.y, v.z, v.w};
+            return true;
+        }
         const uint32_t i = tiles_read % kMxTiles;
         if (tiles_read > 0 && !wait_warp(tfull + 8 * i, (tiles_read / kMxTiles) & 1, &abort_flag, p, kStatusTimeoutOperand)) return false;
         const int4 v = tile_ring[i];
@@ -743,7 +748,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
                 else bar_arrive(aempty + 8 * acc);
             }
         }
-    } else {
+    } else if constexpr (!SPLIT) {
         // the tiles of this CTA, one after the other
         uint32_t n = 0;
         for (int32_t t = first; t < tiles; t += step, ++n) {
