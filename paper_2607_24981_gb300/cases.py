@@ -21,6 +21,9 @@ launches of a few tens of microseconds).  Cases:
   gelu_2p28     SD-ShiftGELU over 2^28 int32 values
   ln_192 / ln_384
                 I-LayerNorm over 2^20 int32 rows of dim 192 / 384
+  mx_experts    a mixture-of-experts feed-forward on MXFP4 weights (routing, gathered rows to MXFP4, two products by
+                expert with a SiLU gate, weighted join onto the residual): 8 images x 1600 tokens of 384, two of 8
+                experts of 1536; --batch gives the images
 """
 from __future__ import annotations
 
@@ -115,6 +118,13 @@ def build(case: str, batch: int = 0):
         ts = ilw.TwoStage(synth.two_stage_params(9, d=d, C=80))
         mem = _dev(synth.uniform_int(9, "case.ts.mem", (B * S, d), -127, 127, np.int8))
         return (lambda: ts.forward(mem, B, S, K)), {"tokens": B * S}
+    if case == "mx_experts":
+        T, d, F, E = (batch or 8) * 1600, 384, 1536, 8
+        gen = torch.Generator(device="cuda").manual_seed(10)
+        normal = lambda *n: torch.randn(*n, generator=gen, device="cuda")  # noqa: E731
+        ffn = ilw.MxExperts(ilw.gate_rows(normal(E, F, d), normal(E, F, d)) / d**0.5, normal(E, d, F) / F**0.5, top=2)
+        x, router = normal(T, d).bfloat16(), normal(d, E) / d**0.5
+        return (lambda: ffn.forward(x, x.float() @ router, residual=x)), {"flops": 2.0 * T * 2 * 3 * d * F}
     raise SystemExit(f"unknown case {case}")
 
 

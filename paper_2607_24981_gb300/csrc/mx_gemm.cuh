@@ -51,7 +51,7 @@
 namespace ilw {
 
 constexpr int kMxRowsW = 128;   // rows of W a CTA
-constexpr int kMxMaxTok = 224;  // tokens a tile
+constexpr int kMxMaxTok = 224;  // tokens a tile; a multiple of 32, as tiles of pairs are
 constexpr int kMxMaxStages = 16, kMxMinStages = 4;
 constexpr int kMxScaleWarp0 = 3, kMxScaleSets = 4;  // pairs of scale warps
 constexpr int kMxEpiWarp0 = kMxScaleWarp0 + 2 * kMxScaleSets, kMxEpiWarps = 16, kMxTileWarp = kMxEpiWarp0 + kMxEpiWarps;
@@ -648,7 +648,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
             const int last = part == 0 ? 4 : (p.nt + 31) / 32;
             for (int c = 0; c < last; ++c, src += 32 * pitch) {
                 const bool in = 32 * c + lane < rows;
-                cpa16(raw + c * 512, in ? src : base, in ? n : 0);
+                cpa16(raw + c * 512, in ? src : p.a_scales, in ? n : 0);  // (of a row past the end nothing is read: zeros)
             }
         };
         begin();
