@@ -125,6 +125,15 @@ Mx mx(PyObject *o, int dims, const char *what) {
 
 ilw_stream_t stream_of(const at::Tensor &t) { return c10::cuda::getCurrentCUDAStream(t.get_device()).stream(); }
 at::Tensor room(at::IntArrayRef size, at::ScalarType type, const at::Tensor &like) { return at::empty(size, at::TensorOptions().dtype(type).device(like.device())); }
+// Several results in one allocation (an allocation is a good part of a short call): the tensor of `size` and `type` that begins
+// `bytes` into `whole`, `bytes` a multiple of its element size.
+at::Tensor part_of(const at::Tensor &whole, int64_t bytes, at::IntArrayRef size, at::ScalarType type) {
+    const caffe2::TypeMeta meta = c10::scalarTypeToTypeMeta(type);
+    at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::TensorImpl::VIEW, c10::Storage(whole.storage()), whole.key_set(), meta);
+    t.unsafeGetTensorImpl()->set_storage_offset(bytes / (int64_t)meta.itemsize());
+    t.unsafeGetTensorImpl()->set_sizes_contiguous(size);
+    return t;
+}
 PyObject *wrap(const at::Tensor &t) { return THPVariable_Wrap(t); }
 // The dtype argument, or what it stands for when it is None.
 at::ScalarType dtype_or(PyObject *o, at::ScalarType otherwise, const char *what) {
@@ -160,9 +169,11 @@ PyObject *quantize(PyObject *const *a) {
               what);
         return Py_NewRef(a[2]);
     }
-    const at::Tensor codes = room({rows, 16 * nb}, at::kByte, X), scales = room({rows, (nb + 15) / 16 * 16}, at::kByte, X);
+    const int64_t pad = (nb + 15) / 16 * 16;
+    const at::Tensor both = room({rows * (16 * nb + pad)}, at::kByte, X), codes = part_of(both, 0, {rows, 16 * nb}, at::kByte),
+                     scales = part_of(both, rows * 16 * nb, {rows, pad}, at::kByte);
     check(lib.quantize(x.data, x.form, x.ld, x.rows, at, rows, (int32_t)std::min<int64_t>(x.cols, INT32_MAX), (uint8_t *)codes.data_ptr(), 16 * nb,
-                       (uint8_t *)scales.data_ptr(), (nb + 15) / 16 * 16, stream_of(X)),
+                       (uint8_t *)scales.data_ptr(), pad, stream_of(X)),
           what);
     return Py_BuildValue("(NNL)", wrap(codes), wrap(scales), (long long)x.cols);
 }
@@ -217,12 +228,13 @@ PyObject *route(PyObject *const *a) {
     if (m.rows > INT32_MAX || m.cols > INT32_MAX || k > INT32_MAX || k < INT32_MIN) fail("%s: more than 2^31 tokens or experts", what);
     const int32_t T = (int32_t)m.rows, E = (int32_t)m.cols;
     const size_t bytes = lib.route_bytes(T, E);
-    const at::Tensor expert = room({T, kk}, at::kInt, x), slot = room({T, kk}, at::kInt, x), source = room({T * kk}, at::kInt, x),
-                     offsets = room({(int64_t)E + 1}, at::kInt, x), weight = room({T, kk}, at::kFloat, x);
-    at::Tensor workspace;
-    if (bytes) workspace = room({(int64_t)bytes}, at::kByte, x);
+    const int64_t n = T * kk, words = 4 * n + E + 1;  // expert, weight, source, slot, offsets, then the workspace
+    const at::Tensor all = room({4 * words + (int64_t)bytes}, at::kByte, x);
+    const at::Tensor expert = part_of(all, 0, {T, kk}, at::kInt), weight = part_of(all, 4 * n, {T, kk}, at::kFloat),
+                     source = part_of(all, 8 * n, {n}, at::kInt), slot = part_of(all, 12 * n, {T, kk}, at::kInt),
+                     offsets = part_of(all, 16 * n, {(int64_t)E + 1}, at::kInt);
     check(lib.route(m.data, m.form, m.ld, T, E, (int32_t)k, PyObject_IsTrue(a[2]), (int32_t *)expert.data_ptr(), (float *)weight.data_ptr(),
-                    (int32_t *)offsets.data_ptr(), (int32_t *)source.data_ptr(), (int32_t *)slot.data_ptr(), bytes ? workspace.data_ptr() : nullptr, bytes,
+                    (int32_t *)offsets.data_ptr(), (int32_t *)source.data_ptr(), (int32_t *)slot.data_ptr(), bytes ? (char *)all.data_ptr() + 4 * words : nullptr, bytes,
                     stream_of(x)),
           what);
     return Py_BuildValue("(NNNNN)", wrap(expert), wrap(weight), wrap(offsets), wrap(source), wrap(slot));
