@@ -386,9 +386,7 @@ cudaError_t route(const MoeRouteParams &p, cudaStream_t s) {
     const int32_t chunks = (int32_t)((p.T + (int64_t)kChunk - 1) / kChunk);
     e = launch_after(route_select_kernel<T, S>, chunks * kSelectCtas, select_tokens(S) * kSelectLanes, select_smem(p.E, p.k), s, p, wide);
     if (e != cudaSuccess) return e;
-    static SmemLimit place;
-    e = raise_smem_limit(place, (const void *)route_place_kernel<W>, 2 * kGroups * S * (W + 1) * 4);
-    if (e != cudaSuccess) return e;
+    static_assert(2 * kGroups * S * (W + 1) * 4 + 3 * kRouteMaxExperts * 4 + 16 <= 48 * 1024, "route_place_kernel: no limit raised");
     return launch_after(route_place_kernel<W>, chunks, kPlaceThreads, (size_t)2 * p.E * (W + 1) * 4, s, p, chunks);
 }
 template <typename T>

@@ -411,6 +411,13 @@ def test_route_matches_64_bits(ilw, T, E, k, dtype, renormalize):
     assert (np.abs(r.weight.double().cpu().numpy() - weight) <= (E + 8) * 2.0**-23 * weight).all()
 
 
+def test_route_of_many_experts_after_few(ilw):
+    x = torch.randn(600, 256, device="cuda")
+    first = ilw.moe_route(x, 3)
+    ilw.moe_route(torch.randn(600, 8, device="cuda"), 3)
+    assert all(torch.equal(a, b) for a, b in zip(ilw.moe_route(x, 3), first))
+
+
 def test_route_extremes(ilw):
     big = float(np.float32(3.4028234e38))
     x = torch.tensor([[big, -big, 0.0, -0.0], [-big, -big, -big, float("-inf")], [0.0, -0.0, -0.0, 0.0], [float("nan")] * 4,
