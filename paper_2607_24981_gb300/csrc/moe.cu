@@ -39,7 +39,9 @@ constexpr int kSelectLanes = 2, kSelectCtas = 8;
 __host__ __device__ constexpr int select_tokens(int S) { return S >= 32 ? 32 : 64; }
 __host__ __device__ constexpr int chunk_tokens(int S) { return select_tokens(S) * kSelectCtas; }
 constexpr int kPlaceThreads = 1024;
-constexpr int kOneTokens = 256, kOneSmem = 200 * 1024;  // what one CTA takes alone
+// What one CTA takes alone (one kernel and two, in us: 16 tokens of 64 experts 3.6 and 7.6, 256 of 64 7.1 and 8.1, 128 of 256 11.1 and
+// 12.1, 224 of 128 10.6 and 10.4, 256 of 128 11.6 and 10.7)
+constexpr int kOneTokens = 256, kOneLogits = 32 * 1024 - 4096, kOneSmem = 200 * 1024;
 constexpr int kGroups = 16;
 
 // Experts a group (4, 8, 16 or 32), and words between the rows of the tokens' logits in shared memory: 16 groups, filled up with
@@ -367,7 +369,7 @@ size_t one_smem(int32_t T, int32_t E, int32_t k) {
     const size_t tokens = (std::max(T, 1) + 7) / 8 * 8;
     return ((size_t)2 * E * (kOneTokens / 32 + 1) + tokens * (2 * k + row_words(E))) * 4;
 }
-bool route_in_one(int32_t T, int32_t E) { return T <= kOneTokens && one_smem(T, E, kRouteMaxTop) <= kOneSmem; }
+bool route_in_one(int32_t T, int32_t E) { return T <= kOneTokens && (int64_t)T * E <= kOneLogits && one_smem(T, E, kRouteMaxTop) <= kOneSmem; }
 
 template <typename T, int S>
 cudaError_t route(const MoeRouteParams &p, cudaStream_t s) {

@@ -44,25 +44,29 @@ cudaError_t launch_mx_gemm(const MxGemmProblem &g, cudaStream_t s) {
     const int64_t sms = sm_count();
 
     const int64_t out = g.act == ILW_ACT_SILU_GATE ? g.N / 2 : g.N;
-    p.wide = g.form != ILW_FP32 && out % 8 == 0 && (uintptr_t)g.Y % 16 == 0 && g.ldy % 8 == 0;
+    p.wide = g.act != ILW_ACT_NONE && g.form != ILW_FP32 && out % 8 == 0 && (uintptr_t)g.Y % 16 == 0 && g.ldy % 8 == 0;
     const int fixed = 1024 + (g.experts + 1) * (int)sizeof(MxExpert) + g.experts * 4 + (p.wide ? kMxEpiWarps * kMxPatch : 0);
     auto bytes = [&] { return fixed + p.stages * p.stage_bytes + kMxScaleSets * p.raw_bytes + 2 * p.scale_bytes; };
 
-    // Tokens a tile: as wide as the tokens (of an expert, twice the mean) fill, at most 224, and what leaves room for four stages.
+    // Tokens a tile: as wide as the tokens (of an expert, twice the mean: with the mean alone more experts of unequal ones take two
+    // tiles; 4096 rows of 32 experts, N 4096, K 2048: 34 us, 36 with the mean) fill, at most 224, and what leaves room
+    // for four stages.
     const int64_t per = g.offsets ? (2 * g.M + g.experts - 1) / g.experts : g.M;
     p.nt = (int32_t)std::min<int64_t>(kMxMaxTok, (std::min(per, g.M) + 15) / 16 * 16);
     if (p.nt > 32) p.nt = (p.nt + 31) / 32 * 32;
     int64_t tiles;
     for (;; p.nt -= 32) {
         const int64_t token_tiles = g.offsets ? std::min<int64_t>(g.M, g.M / p.nt + g.experts) : (g.M + p.nt - 1) / p.nt;  // at most
-        // Pairs where they fill the chip with tiles wide enough to be bound by operands
+        // Pairs start and end some 1.5 us later and then take a sixth less time a block of K, so they are for a K above 1024 and 20 blocks
+        // or more a pair of SMs (one CTA a tile against pairs, in us: 12800 x 384 x 1536, 9 blocks, 11.7 and 12.5; 6400 x 2048 x
+        // 1536, 18 blocks, 16.6 and 16.8; 12800 x 1536 x 1536, 27 blocks, 22.5 and 20.7; 8192 cubed 199 and 171), and for
+        // tiles of 64 tokens or more, whose MMAs take longer than their rows of W
         const int64_t pair_tiles = token_tiles * ((g.N + 2 * kMxRowsW - 1) / (2 * kMxRowsW));
-        p.mode = p.nt >= 64 && g.N > kMxRowsW && 2 * pair_tiles >= sms ? MX_PAIR : MX_ONE;
+        p.mode = p.nt >= 64 && g.N > kMxRowsW && p.nkb > 4 && 2 * pair_tiles * p.nkb >= 20 * sms ? MX_PAIR : MX_ONE;
         const int rows_w = p.mode == MX_PAIR ? 2 * kMxRowsW : kMxRowsW;
         p.wtiles = (g.N + rows_w - 1) / rows_w;
         tiles = token_tiles * p.wtiles;
         const int32_t tokens = p.mode == MX_PAIR ? p.nt / 2 : p.nt;  // whose codes a CTA loads
-        p.abox = g.offsets ? 0 : tokens;
         p.stage_bytes = kMxRowsW * 128 + tokens * 128;
         p.raw_bytes = kMxRowsW * 16 + (p.nt + 31) / 32 * 512;
         p.scale_bytes = 4 * kMxAtom * (1 + (p.nt + 127) / 128);
@@ -76,19 +80,25 @@ cudaError_t launch_mx_gemm(const MxGemmProblem &g, cudaStream_t s) {
     // t / wtiles for t < 2^31 (round-up reciprocal of Granlund and Montgomery, 1994)
     while ((1ll << p.wdiv_s) < p.wtiles) ++p.wdiv_s;
     p.wdiv_m = (uint32_t)((((uint64_t)1 << 32) * ((1ull << p.wdiv_s) - p.wtiles)) / p.wtiles + 1);
-    // few tiles: as many CTAs to a tile as the chip has room for, each with whole scale stages of K
+    // Few tiles and a long K: 8, 4 or 2 CTAs to a tile, each with whole scale stages of K.  The cluster and its join cost what six
+    // stages of 512 do, more with many tokens (one CTA and split, in us: one token, N 4096, K 4096, by 4, 7.3 and 7.2; K 16384,
+    // 17.8 and 11.0; N 1024 by 8, 17.2 and 7.8; 224 tokens, N and K 4096, by 4, 11.0 and 12.1, which is why it is not split),
+    // and the clusters have to fit side by side: 16 of 8 CTAs do not (N 2048, K 4096: 11.6 us, by 4 6.9).
     p.splits = 1;
     if (p.mode == MX_ONE)
-        while (p.splits < 8 && 2 * p.splits * tiles <= sms && 2 * p.splits <= p.nsb) p.splits *= 2;
+        for (int c = 8; c > 1 && p.splits == 1; c /= 2) {
+            const int64_t room = c == 8 ? sms / 2 : c == 4 ? sms * 7 / 8 : sms;
+            if (c * tiles <= room && p.nsb - (p.nsb + c - 1) / c >= 6 + p.nt / 128) p.splits = c;
+        }
     if (p.splits > 1) p.mode = MX_SPLIT;
 
     p.nb = (g.K + 31) / 32;
     p.w_scales = g.w_scales, p.w_lds = g.w_lds, p.w_scales_stride = g.w_scales_stride;
     p.a_scales = g.a_scales, p.a_lds = g.a_lds;
     if (!code_map(&p.wc, g.w_codes, 16 * p.nb, g.N, g.w_ldc, g.experts, g.w_codes_stride, kMxRowsW) ||
-        !code_map(&p.ac[0], g.a_codes, 16 * p.nb, g.M, g.a_ldc, 0, 0, p.abox ? p.abox : 16))
+        !code_map(&p.ac[0], g.a_codes, 16 * p.nb, g.M, g.a_ldc, 0, 0, 16))
         return cudaErrorInvalidValue;
-    for (int i = 1; i < 4 && !p.abox; ++i)
+    for (int i = 1; i < 4; ++i)
         if (!code_map(&p.ac[i], g.a_codes, 16 * p.nb, g.M, g.a_ldc, 0, 0, 16 << i)) return cudaErrorInvalidValue;
     int grid = (int)std::min<int64_t>(tiles, sms);
     if (p.mode == MX_SPLIT) grid = (int)tiles * p.splits;

@@ -68,7 +68,7 @@ struct MxExpert {
 };
 
 struct MxParams {
-    CUtensorMap wc, ac[4];  // codes of W [E, N, .]; of A [M, .] in boxes of abox rows, or of 16, 32, 64 and 128
+    CUtensorMap wc, ac[4];  // codes of W [E, N, .]; of A [M, .] in boxes of 16, 32, 64 and 128 rows
     const uint8_t *w_scales, *a_scales;
     int64_t w_lds, w_scales_stride, a_lds;
     int32_t nb;             // scale bytes of a row
@@ -81,7 +81,6 @@ struct MxParams {
     int32_t wtiles;         // tiles of rows of W (128, or 256 a pair)
     uint32_t wdiv_m, wdiv_s;  // division by wtiles
     int32_t nt;             // most tokens a tile, a multiple of 16 (a pair's: of 32)
-    int32_t abox;           // rows of A a TMA box, one a stage; 0: as many boxes of 128 to 16 rows as its rows take
     int32_t stages;         // stages of codes
     int32_t stage_bytes, raw_bytes, scale_bytes;
     int32_t wide;           // 2-byte rows of Y take 16-byte stores
@@ -306,7 +305,7 @@ __device__ __forceinline__ void store_chunk(const MxParams &p, float (&v)[16], c
     }
     const int out0 = (kGate ? n >> 1 : n) - (kGate ? lane >> 1 : lane);  // first output of the warp
     const int width = kGate ? p.N / 2 : p.N;
-    if constexpr (sizeof(T) == 2) {
+    if constexpr (sizeof(T) == 2 && ACT != ILW_ACT_NONE) {
         if (p.wide) {
             const uint32_t at = patch + (kGate ? (lane & 1) * 2 * kCols + (lane & ~1) : 2 * lane);
             constexpr int kPieces = kCols / 8, kTokens = 32 / kPieces;  // pieces of a token, tokens the patch holds
@@ -502,7 +501,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
             // a pair's CTA loads its half of the tokens
             const int part = PAIR ? mma_tokens(x) / 2 : x.rows, row = x.row0 + (PAIR ? (int)rank * part : 0);
             const int units = (part + 15) >> 4;
-            const uint32_t bytes = warp == 0 ? kMxRowsW * 128 : p.abox ? p.abox * 128 : units * 2048;
+            const uint32_t bytes = warp == 0 ? kMxRowsW * 128 : units * 2048;
             if (one) {
                 for (int32_t kb = 2 * sb_lo; kb < kb_hi; ++kb) {
                     if (!wait_lane(empty + 8 * s, sp, &abort_flag, p, kStatusTimeoutFree)) {
@@ -514,8 +513,6 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
                         bar_expect_tx(db, bytes);
                         if (warp == 0) {
                             tma_3d(d, &p.wc, kb * 128, x.n0, x.e, db);
-                        } else if (p.abox) {
-                            tma_2d(d, &p.ac[0], kb * 128, row, db);
                         } else {
                             int done = 0;  // (units of 16 rows)
 #pragma unroll

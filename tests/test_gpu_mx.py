@@ -258,6 +258,48 @@ def test_grouped_of_many_tiles(ilw, K, act):
     ilw.device_status()
 
 
+@pytest.mark.parametrize("act,dtype", [("none", torch.float32), ("gelu", torch.bfloat16), ("silu_gate", torch.float16)])
+@pytest.mark.parametrize("M,N,K", [(4, 5000, 8200), (9, 1300, 4200), (1, 130, 4128), (224, 900, 9000)])
+def test_linear_of_a_long_sum(ilw, M, N, K, act, dtype):
+    """Few tiles and a long K, which two, four or eight CTAs share: the same bound, and the same bits on every run."""
+    rng = np.random.default_rng(M + N + K)
+    A, W = packed(ilw, values(rng, M, K)), packed(ilw, rng.standard_normal((N, K)) / np.sqrt(K))
+    b = rng.standard_normal(N).astype(np.float32)
+    got = ilw.mx_linear(A, W, torch.from_numpy(b).cuda(), act=act, out_dtype=dtype)
+    check_product(got, ref_values(*host(A), K), ref_values(*host(W), K), b, act, dtype)
+    assert all(torch.equal(got, ilw.mx_linear(A, W, torch.from_numpy(b).cuda(), act=act, out_dtype=dtype)) for _ in range(3))
+    ilw.device_status()
+
+
+@pytest.mark.parametrize("act,dtype", [("none", torch.float32), ("none", torch.bfloat16), ("gelu", torch.float16), ("silu_gate", torch.bfloat16)])
+@pytest.mark.parametrize("M,N,K", [(4001, 1700, 3000), (3000, 2306, 2080)])
+def test_linear_of_many_long_tiles(ilw, M, N, K, act, dtype):
+    """Tiles that two SMs share, several a pair, with a K that ends inside a block; the same bits again."""
+    rng = np.random.default_rng(M + N + K)
+    A, W = packed(ilw, values(rng, M, K)), packed(ilw, rng.standard_normal((N, K)) / np.sqrt(K))
+    b = rng.standard_normal(N).astype(np.float32)
+    got = ilw.mx_linear(A, W, torch.from_numpy(b).cuda(), act=act, out_dtype=dtype)
+    check_product(got, ref_values(*host(A), K), ref_values(*host(W), K), b, act, dtype)
+    assert all(torch.equal(got, ilw.mx_linear(A, W, torch.from_numpy(b).cuda(), act=act, out_dtype=dtype)) for _ in range(3))
+    ilw.device_status()
+
+
+@pytest.mark.parametrize("counts,N,K", [([700, 0, 1, 333, 1024, 225, 95], 2304, 3000), ([1, 0, 9], 300, 4200), ([0, 2, 130, 0], 140, 8192)],
+                         ids=["pairs", "eight a tile", "rows of two tiles"])
+def test_grouped_with_a_long_sum(ilw, counts, N, K):
+    """Ragged groups in the forms for many tiles and for few."""
+    rng = np.random.default_rng(N + K)
+    off = np.r_[0, np.cumsum(counts)]
+    A, W = packed(ilw, values(rng, int(off[-1]), K)), packed(ilw, rng.standard_normal((len(counts), N, K)) / np.sqrt(K))
+    a, w = ref_values(*host(A), K), ref_values(*host(W), K)
+    for dtype, act in ((torch.float32, "none"), (torch.bfloat16, "silu_gate")):
+        got = ilw.mx_grouped_linear(A, W, torch.from_numpy(off.astype(np.int32)).cuda(), act=act, out_dtype=dtype)
+        for e in range(len(counts)):
+            if counts[e]:
+                check_product(got[off[e]: off[e + 1]], a[off[e]: off[e + 1]], w[e], None, act, dtype)
+    ilw.device_status()
+
+
 def test_linear_rows_with_strides(ilw):
     """Operands inside wider byte arrays, a result inside a wider tensor, fp16."""
     rng = np.random.default_rng(11)
@@ -370,6 +412,22 @@ def test_product_gives_up_a_bounded_wait(ilw):
         ilw.device_status()
 
 
+@pytest.mark.parametrize("M,N,K", [(4, 256, 8192), (3001, 1700, 4096)], ids=["cluster", "pair"])
+def test_product_of_clusters_gives_up_a_bounded_wait(ilw, M, N, K):
+    rng = np.random.default_rng(8)
+    A, W = packed(ilw, values(rng, M, K)), packed(ilw, rng.standard_normal((N, K)) / np.sqrt(K))
+    want = ilw.mx_linear(A, W)
+    assert ilw.lib().ilwdetr_debug_gemm_wait(0, 20_000_000) == 0
+    try:
+        ilw.mx_linear(A, W)
+        with pytest.raises(ilw.IlwError, match="wait"):
+            ilw.device_status()
+    finally:
+        assert ilw.lib().ilwdetr_debug_gemm_wait(-1, 0) == 0
+    assert torch.equal(ilw.mx_linear(A, W), want)
+    ilw.device_status()
+
+
 # ---------------------------------------------------------------------------- routing and combination
 def ref_route(x, k, renormalize):
     """float64 x [T, E] -> expert, weight, offsets, source, slot."""
@@ -409,6 +467,20 @@ def test_route_matches_64_bits(ilw, T, E, k, dtype, renormalize):
         assert np.array_equal(got.cpu().numpy(), want)
     # exp's arguments are exact (a quarter grid); a sum of at most 512 terms and a quotient of fp32 exponentials of 2 ulp
     assert (np.abs(r.weight.double().cpu().numpy() - weight) <= (E + 8) * 2.0**-23 * weight).all()
+
+
+@pytest.mark.parametrize("T", [1, 8, 111, 112, 113, 224, 225, 256, 257])
+def test_route_of_few_tokens(ilw, T):
+    """Either side of where one CTA does all."""
+    rng = np.random.default_rng(T)
+    for E in (8, 128, 256):
+        x = np.round(rng.standard_normal((T, E)) * 4) / 4
+        x[rng.random((T, E)) < 0.2] = -np.inf
+        r = ilw.moe_route(torch.from_numpy(x).float().cuda(), 5, True)
+        expert, weight, offsets, source, slot = ref_route(x, 5, True)
+        for got, want in ((r.expert, expert), (r.offsets, offsets), (r.source, source), (r.slot, slot)):
+            assert (got.cpu().numpy() == want).all()
+        assert (np.abs(r.weight.double().cpu().numpy() - weight) <= (E + 8) * 2.0**-23 * weight).all()
 
 
 def test_route_of_many_experts_after_few(ilw):
