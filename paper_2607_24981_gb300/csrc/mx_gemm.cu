@@ -88,7 +88,7 @@ cudaError_t launch_mx_gemm(const MxGemmProblem &g, cudaStream_t s) {
     if (p.mode == MX_ONE)
         for (int c = 8; c > 1 && p.splits == 1; c /= 2) {
             const int64_t room = c == 8 ? sms / 2 : c == 4 ? sms * 7 / 8 : sms;
-            if (c * tiles <= room && p.nsb - (p.nsb + c - 1) / c >= 6 + p.nt / 128) p.splits = c;
+            if (c <= p.nsb && c * tiles <= room && p.nsb - (p.nsb + c - 1) / c >= 6 + p.nt / 128) p.splits = c;
         }
     if (p.splits > 1) p.mode = MX_SPLIT;
 

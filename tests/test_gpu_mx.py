@@ -259,7 +259,7 @@ def test_grouped_of_many_tiles(ilw, K, act):
 
 
 @pytest.mark.parametrize("act,dtype", [("none", torch.float32), ("gelu", torch.bfloat16), ("silu_gate", torch.float16)])
-@pytest.mark.parametrize("M,N,K", [(4, 5000, 8200), (9, 1300, 4200), (1, 130, 4128), (224, 900, 9000)])
+@pytest.mark.parametrize("M,N,K", [(4, 5000, 8200), (9, 1300, 4200), (1, 130, 4128), (224, 900, 9000), (506, 17, 3178), (3, 300, 3500)])
 def test_linear_of_a_long_sum(ilw, M, N, K, act, dtype):
     """Few tiles and a long K, which two, four or eight CTAs share: the same bound, and the same bits on every run."""
     rng = np.random.default_rng(M + N + K)
