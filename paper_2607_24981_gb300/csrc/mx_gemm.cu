@@ -54,18 +54,30 @@ cudaError_t launch_mx_gemm(const MxGemmProblem &g, cudaStream_t s) {
     const int64_t per = g.offsets ? (2 * g.M + g.experts - 1) / g.experts : g.M;
     p.nt = (int32_t)std::min<int64_t>(kMxMaxTok, (std::min(per, g.M) + 15) / 16 * 16);
     if (p.nt > 32) p.nt = (p.nt + 31) / 32 * 32;
-    int64_t tiles;
-    for (;; p.nt -= 32) {
-        const int64_t token_tiles = g.offsets ? std::min<int64_t>(g.M, g.M / p.nt + g.experts) : (g.M + p.nt - 1) / p.nt;  // at most
+    // tiles of n tokens: at most, and (every other expert's last tile half full) about
+    auto most = [&](int64_t n) { return g.offsets ? std::min<int64_t>(g.M, g.M / n + g.experts) : (g.M + n - 1) / n; };
+    auto about = [&](int64_t n) { return g.offsets ? std::min<int64_t>(g.M, g.M / n + g.experts / 2 + 1) : (g.M + n - 1) / n; };
+    int64_t tiles = 0;
+    for (;; p.nt = (p.nt - 1) / 32 * 32) {  // (a pair's: a multiple of 32)
         // Pairs start and end some 1.5 us later and then take a sixth less time a block of K, so they are for a K above 1024 and 20 blocks
         // or more a pair of SMs (one CTA a tile against pairs, in us: 12800 x 384 x 1536, 9 blocks, 11.7 and 12.5; 6400 x 2048 x
         // 1536, 18 blocks, 16.6 and 16.8; 12800 x 1536 x 1536, 27 blocks, 22.5 and 20.7; 8192 cubed 199 and 171), and for
         // tiles of 64 tokens or more, whose MMAs take longer than their rows of W
-        const int64_t pair_tiles = token_tiles * ((g.N + 2 * kMxRowsW - 1) / (2 * kMxRowsW));
+        const int64_t pair_tiles = most(p.nt) * ((g.N + 2 * kMxRowsW - 1) / (2 * kMxRowsW));
         p.mode = p.nt >= 64 && g.N > kMxRowsW && p.nkb > 4 && 2 * pair_tiles * p.nkb >= 20 * sms ? MX_PAIR : MX_ONE;
         const int rows_w = p.mode == MX_PAIR ? 2 * kMxRowsW : kMxRowsW;
         p.wtiles = (g.N + rows_w - 1) / rows_w;
-        tiles = token_tiles * p.wtiles;
+        if (p.mode == MX_ONE) {
+            // The width, from 64 tokens on, at which the CTA with the most tiles reads the fewest rows of W and tokens (at 224 tokens and so, in
+            // us: 12800 x 384 x 1536, 128 tokens, 11.3 and 9.9; 6400 x 1536 x 384, 176, 14.2 and 12.7; 224 x 4096 x 4096, 64, 10.8
+            // and 8.8; narrower still, 32 and 16 tokens, 12.2 and 15.7; 2048 rows of 16 experts, 768 x 1024, 7.4 and 6.5)
+            int64_t least = INT64_MAX;
+            for (int32_t top = p.nt, n = top; n >= std::min(top, 64); n -= 16) {
+                const int64_t rows = (about(n) * p.wtiles + sms - 1) / sms * (n + kMxRowsW);
+                if (rows < least) least = rows, p.nt = n;
+            }
+        }
+        tiles = most(p.nt) * p.wtiles;
         const int32_t tokens = p.mode == MX_PAIR ? p.nt / 2 : p.nt;  // whose codes a CTA loads
         p.stage_bytes = kMxRowsW * 128 + tokens * 128;
         p.raw_bytes = kMxRowsW * 16 + (p.nt + 31) / 32 * 512;
@@ -74,7 +86,7 @@ cudaError_t launch_mx_gemm(const MxGemmProblem &g, cudaStream_t s) {
         for (p.stages = kMxMaxStages; p.stages >= kMxMinStages && bytes() > kMxSmemLimit; --p.stages) {
         }
         if (p.stages >= kMxMinStages) break;
-        if (p.nt <= 32) return cudaErrorInvalidValue;
+        if (p.nt <= 32) return cudaErrorInvalidValue;  // (never)
     }
     if (tiles > INT32_MAX) return cudaErrorInvalidValue;
     // t / wtiles for t < 2^31 (round-up reciprocal of Granlund and Montgomery, 1994)

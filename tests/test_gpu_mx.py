@@ -259,7 +259,7 @@ def test_grouped_of_many_tiles(ilw, K, act):
 
 
 @pytest.mark.parametrize("act,dtype", [("none", torch.float32), ("gelu", torch.bfloat16), ("silu_gate", torch.float16)])
-@pytest.mark.parametrize("M,N,K", [(4, 5000, 8200), (9, 1300, 4200), (1, 130, 4128), (224, 900, 9000), (506, 17, 3178), (3, 300, 3500)])
+@pytest.mark.parametrize("M,N,K", [(4, 5000, 8200), (9, 1300, 4200), (1, 130, 4128), (224, 900, 9000), (506, 18, 3178), (3, 300, 3500)])
 def test_linear_of_a_long_sum(ilw, M, N, K, act, dtype):
     """Few tiles and a long K, which two, four or eight CTAs share: the same bound, and the same bits on every run."""
     rng = np.random.default_rng(M + N + K)
@@ -359,6 +359,20 @@ def test_grouped_matches_64_bits(ilw, counts, N, K, act):
         for e in range(E):
             if counts[e]:
                 check_product(got[off[e]: off[e + 1]], a[off[e]: off[e + 1]], w[e], b[e], act, dtype)
+    ilw.device_status()
+
+
+def test_grouped_of_very_many_experts(ilw):
+    """The table of 1024 experts takes shared memory from the widest tiles."""
+    rng = np.random.default_rng(21)
+    E, N, K = 1024, 64, 100
+    counts = 90 + 40 * (np.arange(E) % 2)
+    off = np.r_[0, np.cumsum(counts)]
+    A, W = packed(ilw, values(rng, int(off[-1]), K)), packed(ilw, rng.standard_normal((E, N, K)) / np.sqrt(K))
+    a, w = ref_values(*host(A), K), ref_values(*host(W), K)
+    got = ilw.mx_grouped_linear(A, W, torch.from_numpy(off.astype(np.int32)).cuda(), act="gelu", out_dtype=torch.bfloat16)
+    for e in range(E):
+        check_product(got[off[e]: off[e + 1]], a[off[e]: off[e + 1]], w[e], None, "gelu", torch.bfloat16)
     ilw.device_status()
 
 
