@@ -412,34 +412,34 @@ __global__ void __launch_bounds__(256) combine_kernel(const MoeCombineParams p) 
     struct alignas(VEC * sizeof(T)) Pack {
         T t[VEC];
     };
-    const int32_t per = (p.N + VEC - 1) / VEC;
-    for (int32_t t = blockIdx.y; t < p.T; t += gridDim.y) {
-        for (int32_t i = blockIdx.x * blockDim.x + threadIdx.x; i < per; i += gridDim.x * blockDim.x) {
-            const int64_t c = (int64_t)i * VEC;
-            float acc[VEC];
+    // the grid covers a row; tokens go round in 32 bits without a sign, which T and a grid's height together do not pass
+    const uint32_t i = blockIdx.x * blockDim.x + threadIdx.x;
+    if (i >= (uint32_t)p.N / VEC) return;
+    const int64_t c = (int64_t)i * VEC;
+    for (uint32_t t = blockIdx.y; t < (uint32_t)p.T; t += gridDim.y) {
+        float acc[VEC];
 #pragma unroll
-            for (int u = 0; u < VEC; ++u) acc[u] = 0.0f;
-            for (int j = 0; j < p.k; ++j) {
-                const int32_t s = p.slot[(int64_t)t * p.k + j];
-                if (s < 0 || s >= p.rows) {
-                    if (s != -1 && p.status && i == 0) atomicExch(p.status, kStatusBadIndex);
-                    continue;
-                }
-                const float w = p.weight[(int64_t)t * p.k + j];
-                const Pack y = *(const Pack *)((const T *)p.Y + s * p.ldy + c);
-#pragma unroll
-                for (int u = 0; u < VEC; ++u) acc[u] = fmaf(w, to_f(y.t[u]), acc[u]);
+        for (int u = 0; u < VEC; ++u) acc[u] = 0.0f;
+        for (int j = 0; j < p.k; ++j) {
+            const int32_t s = p.slot[(int64_t)t * p.k + j];
+            if (s < 0 || s >= p.rows) {
+                if (s != -1 && p.status && i == 0) atomicExch(p.status, kStatusBadIndex);
+                continue;
             }
-            if (p.res) {
-                const Pack r = *(const Pack *)((const T *)p.res + t * p.ldr + c);
+            const float w = p.weight[(int64_t)t * p.k + j];
+            const Pack y = *(const Pack *)((const T *)p.Y + s * p.ldy + c);
 #pragma unroll
-                for (int u = 0; u < VEC; ++u) acc[u] += to_f(r.t[u]);
-            }
-            Pack o;
-#pragma unroll
-            for (int u = 0; u < VEC; ++u) o.t[u] = from_f<T>(acc[u]);
-            *(Pack *)((T *)p.out + t * p.ldo + c) = o;
+            for (int u = 0; u < VEC; ++u) acc[u] = fmaf(w, to_f(y.t[u]), acc[u]);
         }
+        if (p.res) {
+            const Pack r = *(const Pack *)((const T *)p.res + t * p.ldr + c);
+#pragma unroll
+            for (int u = 0; u < VEC; ++u) acc[u] += to_f(r.t[u]);
+        }
+        Pack o;
+#pragma unroll
+        for (int u = 0; u < VEC; ++u) o.t[u] = from_f<T>(acc[u]);
+        *(Pack *)((T *)p.out + t * p.ldo + c) = o;
     }
 }
 
@@ -448,8 +448,8 @@ cudaError_t combine(const MoeCombineParams &p, cudaStream_t s) {
     constexpr int V = 16 / sizeof(T);
     auto fits = [&](const void *q, int64_t ld) { return (uintptr_t)q % 16 == 0 && ld % V == 0; };
     const bool vec = p.N % V == 0 && fits(p.Y, p.ldy) && fits(p.out, p.ldo) && (!p.res || fits(p.res, p.ldr));
-    const int32_t per = vec ? p.N / V : p.N;
-    const int threads = per >= 256 ? 256 : (per + 31) / 32 * 32;
+    const int64_t per = vec ? p.N / V : p.N;
+    const int threads = per >= 256 ? 256 : (int)(per + 31) / 32 * 32;
     const dim3 grid((unsigned)((per + threads - 1) / threads), (unsigned)std::min(p.T, 65535));
     if (vec) return launch_after(combine_kernel<T, V>, grid, threads, 0, s, p);
     return launch_after(combine_kernel<T, 1>, grid, threads, 0, s, p);

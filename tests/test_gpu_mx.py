@@ -548,6 +548,30 @@ def test_combine_reports_a_bad_slot(ilw):
         ilw.device_status()
 
 
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+def test_combine_of_a_row_past_2_30(ilw, dtype):
+    """Rows of more than 2^30 values off 16-byte boundaries: a column counter stepped by a row passes 2^31."""
+    N = 2**30 + 9
+    Y = (torch.arange(N, dtype=torch.int32, device="cuda") % 251).to(dtype)[None]
+    slot = torch.tensor([[0, -1], [0, 0]], dtype=torch.int32, device="cuda")
+    out = torch.full((3, N), -1.0, dtype=dtype, device="cuda")
+    ilw.moe_combine(Y, slot, torch.ones((2, 2), device="cuda"), out=out[1:])  # (whole numbers up to 500: exact)
+    assert (out[0] == -1).all() and torch.equal(out[1], Y[0]) and torch.equal(out[2], 2 * Y[0])
+    ilw.device_status()
+
+
+def test_combine_of_almost_2_31_tokens(ilw):
+    """As many tokens as are accepted: a token counter stepped by the grid's height passes 2^31."""
+    T = 2**31 - 1
+    slot = torch.zeros((T, 1), dtype=torch.int32, device="cuda")
+    slot[-3:, 0] = torch.tensor([1, -1, 1], device="cuda")
+    Y = torch.tensor([[1.0], [2.0]], dtype=torch.bfloat16, device="cuda")
+    out = torch.full((T + 2, 1), 7.0, dtype=torch.bfloat16, device="cuda")
+    ilw.moe_combine(Y, slot, torch.ones((T, 1), device="cuda"), out=out[1:-1])
+    assert out[-5:, 0].tolist() == [1, 2, 0, 2, 7] and out[0, 0] == 7 and bool((out[1:-4] == 1).all())
+    ilw.device_status()
+
+
 # ---------------------------------------------------------------------------- the feed-forward
 @pytest.mark.parametrize("act,dtype", [("silu_gate", torch.bfloat16), ("gelu", torch.float32), ("silu_gate", torch.float16)])
 @pytest.mark.parametrize("T", [0, 1, 37, 600])
