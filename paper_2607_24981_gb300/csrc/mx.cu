@@ -176,7 +176,7 @@ __global__ void __launch_bounds__(kThreads) mx_quantize_any_kernel(const MxQuant
     grid_wait();
     const int lane = threadIdx.x & 31;
     float *mine = stage[threadIdx.x >> 5];
-    const uint32_t u = (blockIdx.x * kThreads + threadIdx.x) >> 5;
+    const uint32_t u = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
     if (u >= total) return;
     const uint32_t row = segs.div(u), k0 = (u - row * segs.d) * 256;
     const int64_t r = (int64_t)r0 + row, src = source_row(p, r);
@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(kThreads) mx_dequantize_any_kernel(const MxDeq
     grid_wait();
     const int lane = threadIdx.x & 31;
     float *mine = stage[threadIdx.x >> 5];
-    const uint32_t u = (blockIdx.x * kThreads + threadIdx.x) >> 5;
+    const uint32_t u = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
     if (u >= total) return;
     const uint32_t row = segs.div(u), k0 = (u - row * segs.d) * 256, k = k0 + 8 * lane;
     const int64_t r = (int64_t)r0 + row;
@@ -267,7 +267,8 @@ __global__ void __launch_bounds__(kThreads) mx_dequantize_any_kernel(const MxDeq
         if (k0 + 32 * i + lane < K) y[32 * i + lane] = from_f<T>(mine[32 * i + lane]);
 }
 
-// Launches `kernel` over `rows` rows of `per` steps each, `step` of them a CTA, as often as 2^31 steps at a time take.
+// Launches `kernel` over `rows` rows of `per` steps each, `step` of them a CTA, as often as 2^30 steps at a time take (a step is a
+// thread's or a warp's, so 32 bits hold a step's number but not always a thread's).
 template <typename P>
 cudaError_t over_rows(void (*kernel)(const P, Divisor, uint32_t, uint32_t), const P &p, int64_t rows, uint32_t per, uint32_t step, cudaStream_t s) {
     const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 30) / per);

@@ -201,6 +201,22 @@ def test_dequantize_every_code_and_scale(ilw, dtype):
         out.fill_(7)
 
 
+def test_quantize_and_back_of_more_than_2_32_threads(ilw):
+    """Short rows off 16-byte boundaries, a warp each: 2^27 of them are 2^32 threads."""
+    R = 2**27 + 300
+    x = (torch.arange(R, dtype=torch.int32, device="cuda") % 6 + 1).to(torch.int8)[:, None]  # 1 to 6, as 4 or 6 times a power of two; 5: as 4 or 6
+    m = ilw.mx_empty(R, 1)
+    m.codes.fill_(255), m.scales.fill_(255)
+    ilw.mx_quantize(x, out=m)
+    few = ilw.mx_quantize(x[:6].clone())
+    for got, want in ((m.codes, few.codes), (m.scales, few.scales)):
+        assert bool((got[: R // 6 * 6].view(-1, 6, 16) == want).all()) and torch.equal(got[R // 6 * 6:], want[: R % 6])
+    out = torch.full((R, 1), -1.0, dtype=torch.float16, device="cuda")
+    ilw.mx_dequantize(m, out=out)
+    want = ilw.mx_dequantize(few, torch.float16)
+    assert bool((out[: R // 6 * 6].view(-1, 6) == want[:, 0]).all()) and torch.equal(out[R // 6 * 6:], want[: R % 6])
+
+
 # ---------------------------------------------------------------------------- products
 @pytest.mark.parametrize("act,bias", [("none", False), ("none", True), ("gelu", True), ("silu_gate", False), ("silu_gate", True)])
 @pytest.mark.parametrize("M,N,K", [(1, 2, 1), (1, 128, 4096), (3, 130, 512), (16, 300, 33), (17, 128, 250), (33, 1000, 2048),
