@@ -91,7 +91,7 @@ const float *weights(const at::Tensor &t, int64_t n, const char *what, const cha
 
 // An MXFP4 tensor: the tuple (codes, scales, k).
 struct Mx {
-    int64_t lead, rows, k;               // (lead: 1 without a leading dimension)
+    int64_t lead, rows, k, scale_cols;   // (lead: 1 without a leading dimension; scale_cols: bytes of a row of scales)
     const uint8_t *codes, *scales;
     int64_t ldc, lds, between_c, between_s;
     const at::Tensor *t;                 // codes
@@ -111,7 +111,7 @@ Mx mx(PyObject *o, int dims, const char *what) {
     if (!c.is_cuda() || !s.is_cuda() || ((c.stride(dims - 1) != 1 || s.stride(dims - 1) != 1) && c.numel()))
         fail("%s: codes or scales are not on the GPU, or their rows are not contiguous", what);
     m.lead = dims == 3 ? c.size(0) : 1;
-    m.rows = c.size(dims - 2);
+    m.rows = c.size(dims - 2), m.scale_cols = s.size(dims - 1);
     m.ldc = c.stride(dims - 2), m.lds = s.stride(dims - 2);
     if (m.rows <= 1 || c.size(dims - 1) == 0) {  // (no or a single row may carry any stride)
         m.ldc = std::max(m.ldc, (c.size(dims - 1) + 15) / 16 * 16);
@@ -159,17 +159,18 @@ PyObject *quantize(PyObject *const *a) {
         at = indices(g, what);
         rows = g.numel();
     }
-    const int64_t nb = (x.cols + 31) / 32;
+    const int64_t nb = (x.cols + 31) / 32, pad = (nb + 15) / 16 * 16;
     if (given(a[2])) {
         const Mx m = mx(a[2], 2, what);
         if (m.k != x.cols || m.rows != rows)
             fail("%s: out holds %lld rows of %lld, not %lld of %lld", what, (long long)m.rows, (long long)m.k, (long long)rows, (long long)x.cols);
+        // (each row of scales is filled up to a multiple of 16 bytes; more than the tensor holds are not its own)
+        if (m.scale_cols < pad) fail("%s: scales of out have rows of %lld bytes: at least %lld, a multiple of 16", what, (long long)m.scale_cols, (long long)pad);
         check(lib.quantize(x.data, x.form, x.ld, x.rows, at, rows, (int32_t)std::min<int64_t>(x.cols, INT32_MAX), (uint8_t *)m.codes, m.ldc,
                            (uint8_t *)m.scales, m.lds, stream_of(X)),
               what);
         return Py_NewRef(a[2]);
     }
-    const int64_t pad = (nb + 15) / 16 * 16;
     const at::Tensor both = room({rows * (16 * nb + pad)}, at::kByte, X), codes = part_of(both, 0, {rows, 16 * nb}, at::kByte),
                      scales = part_of(both, rows * 16 * nb, {rows, pad}, at::kByte);
     check(lib.quantize(x.data, x.form, x.ld, x.rows, at, rows, (int32_t)std::min<int64_t>(x.cols, INT32_MAX), (uint8_t *)codes.data_ptr(), 16 * nb,

@@ -80,7 +80,8 @@ def mx_empty(rows: int, k: int, device="cuda") -> MxTensor:
 
 def mx_quantize(X, gather=None, out: MxTensor | None = None) -> MxTensor:
     """ilwdetr_mx_quantize: X [rows, K] (float32, float16, bfloat16 or int8), or its rows ``gather`` (int32; -1: a row of
-    zeros), to MXFP4."""
+    zeros), to MXFP4.  Rows of ``out``'s scales hold a multiple of 16 bytes, as mx_empty makes them: the call fills them up
+    with zeros."""
     got = (_bound or _bind()).quantize(X, gather, out)
     return MxTensor(*got) if out is None else out
 

@@ -185,6 +185,24 @@ def test_quantize_rows_with_strides_and_offsets(ilw, dtype):
         assert (codes[:, :16] == 77).all() and (codes[:, 16 + n:] == 77).all() and (scales[:, s:] == 77).all()
 
 
+@pytest.mark.parametrize("R,K,width,stride", [(1, 96, 3, 3), (1, 600, 19, 19), (4, 96, 3, 16), (4, 96, 15, 32), (2, 544, 31, 32)])
+def test_quantize_keeps_to_the_scales_it_is_given(ilw, R, K, width, stride):
+    """Scales of out narrower than the 16 bytes that a row is filled up to: refused, and nothing around them is written."""
+    guard = torch.full((16 + (R - 1) * stride + width + 64,), 77, dtype=torch.uint8, device="cuda")
+    codes = torch.full((R, K // 32 * 16 + 16), 77, dtype=torch.uint8, device="cuda")[:, : -(-K // 32) * 16]
+    out = ilw.MxTensor(codes, guard[16:].as_strided((R, width), (stride, 1)), K)
+    x = torch.ones((R, K), device="cuda")
+    with pytest.raises(ilw.IlwError, match="scales"):
+        ilw.mx_quantize(x, out=out)
+    assert (guard == 77).all() and (codes == 77).all()
+    padded = -(-width // 16) * 16
+    out = out._replace(scales=guard[16:].as_strided((R, padded), (max(stride, padded), 1))) if R == 1 else out._replace(scales=torch.zeros((R, padded), dtype=torch.uint8, device="cuda"))
+    ilw.mx_quantize(x, out=out)
+    want = ilw.mx_quantize(x)
+    assert torch.equal(out.codes, want.codes) and torch.equal(out.scales, want.scales)
+    assert (guard[:16] == 77).all() and (guard[16 + padded:] == 77).all()
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
 def test_dequantize_every_code_and_scale(ilw, dtype):
     codes = np.tile(np.arange(256, dtype=np.uint8), (256, 1))

@@ -147,3 +147,28 @@ def test_binding_fails_loudly_without_its_library(monkeypatch):
     monkeypatch.setattr(mx, "BIND_PATH", mx.BIND_PATH + ".absent")
     with pytest.raises(IlwError, match="missing"):
         mx.moe_route(torch.zeros(2, 4), 1)
+
+
+def on_gpu(size, dtype, device="cuda:0", strides=None):
+    """A tensor on a GPU with nothing behind it: the binding's checks of shapes and devices come before any launch or copy."""
+    torch = pytest.importorskip("torch")
+
+    class Nowhere(torch.Tensor):
+        __torch_function__ = torch._C._disabled_torch_function_impl
+
+        @classmethod
+        def __torch_dispatch__(cls, func, types, args=(), kwargs=None):
+            raise AssertionError(f"{func} called")
+
+    return torch.Tensor._make_wrapper_subclass(Nowhere, size, dtype=dtype, device=device, strides=strides)
+
+
+@pytest.mark.parametrize("R,K,width,stride", [(1, 96, 3, 3), (1, 600, 19, 32), (4, 96, 3, 16), (4, 520, 17, 32)])
+def test_quantize_refuses_scales_without_room_for_their_padding(R, K, width, stride):
+    torch = pytest.importorskip("torch")
+    import paper_2607_24981_gb300 as ilw
+
+    codes = on_gpu((R, -(-K // 32) * 16), torch.uint8)
+    out = ilw.MxTensor(codes, on_gpu((R, width), torch.uint8, strides=(stride, 1)), K)
+    with pytest.raises(ilw.IlwError, match="scales"):
+        ilw.mx_quantize(on_gpu((R, K), torch.float32), out=out)
