@@ -123,11 +123,16 @@ def moe_combine(Y, slot, weight, residual=None, out=None):
     return (_bound or _bind()).combine(Y, slot, weight, residual, out)
 
 
-def gate_rows(gate, up):
-    """Weight rows (or biases) of a gated layer in the order of ``act="silu_gate"``: gate_0, up_0, gate_1, up_1, ..."""
+def gate_rows(gate, up, dim=None):
+    """Weight rows or biases of a gated layer in the order of ``act="silu_gate"``: gate_0, up_0, gate_1, up_1, ...  ``dim`` is
+    the axis of the rows; unless given, that of weights [F, K] or [E, F, K] and of a bias [F].  Biases of experts [E, F] need
+    ``dim=1``: nothing tells them from the weights of one layer."""
     import torch
 
-    dim = 0 if gate.dim() < 3 else 1
+    if dim is None:
+        dim = 0 if gate.dim() < 3 else 1
+    elif dim < 0:
+        dim += gate.dim()
     return torch.stack([gate, up], dim + 1).flatten(dim, dim + 1)
 
 
@@ -136,7 +141,7 @@ class MxExperts:
     product with its activation, quantise, second product, weighted join onto the residual.
 
     ``w1`` [E, F1, d] and ``w2`` [E, d, F] are float CUDA tensors, quantised here once; with ``act`` "silu_gate" F1 = 2 F and
-    the rows of w1 alternate (gate_rows), else F1 = F.  Biases are float32 [E, F1] and [E, d]."""
+    the rows of w1 alternate (gate_rows), else F1 = F.  Biases are float32 [E, F1] (gated: gate_rows with dim=1) and [E, d]."""
 
     def __init__(self, w1, w2, top: int, act="silu_gate", b1=None, b2=None, renormalize=True):
         self.top, self.act, self.b1, self.b2, self.renormalize = top, act, b1, b2, renormalize

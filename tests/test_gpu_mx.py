@@ -649,5 +649,27 @@ def test_experts_feed_forward(ilw, T, act, dtype):
     ilw.device_status()
 
 
+@pytest.mark.parametrize("E", [1, 3])
+def test_gated_products_with_gate_and_up_biases_given_apart(ilw, E):
+    """Weights and biases of the gates and of what they gate, joined by gate_rows: each column takes its own bias."""
+    rng = np.random.default_rng(E)
+    counts, F, K = [40, 0, 9][:E], 50, 96
+    off = np.r_[0, np.cumsum(counts)]
+    gate, up = (torch.from_numpy(rng.standard_normal((E, F, K)) / np.sqrt(K)) for _ in range(2))
+    bg, bu = (torch.from_numpy(rng.standard_normal((E, F))).float() for _ in range(2))
+    A, W = packed(ilw, values(rng, int(off[-1]), K)), packed(ilw, ilw.gate_rows(gate, up).numpy())
+    a, w = ref_values(*host(A), K), ref_values(*host(W), K)
+    b = np.zeros((E, 2 * F))
+    b[:, 0::2], b[:, 1::2] = bg.numpy(), bu.numpy()
+    got = ilw.mx_grouped_linear(A, W, torch.from_numpy(off.astype(np.int32)).cuda(), ilw.gate_rows(bg, bu, dim=1).cuda(), act="silu_gate",
+                                out_dtype=torch.bfloat16)
+    for e in range(E):
+        if counts[e]:
+            check_product(got[off[e]: off[e + 1]], a[off[e]: off[e + 1]], w[e], b[e], "silu_gate", torch.bfloat16)
+    one = ilw.MxTensor(W.codes[0], W.scales[0], K)
+    first = ilw.mx_linear(ilw.MxTensor(A.codes[:40], A.scales[:40], K), one, ilw.gate_rows(bg[0], bu[0]).cuda(), act="silu_gate", out_dtype=torch.float32)
+    check_product(first, a[:40], w[0], b[0], "silu_gate", torch.float32)
+
+
 def _bytes(code, byte):
     return code[:, 0::2] | code[:, 1::2] << 4, byte

@@ -172,3 +172,15 @@ def test_quantize_refuses_scales_without_room_for_their_padding(R, K, width, str
     out = ilw.MxTensor(codes, on_gpu((R, width), torch.uint8, strides=(stride, 1)), K)
     with pytest.raises(ilw.IlwError, match="scales"):
         ilw.mx_quantize(on_gpu((R, K), torch.float32), out=out)
+
+
+def test_gate_rows_alternate_along_their_axis():
+    torch = pytest.importorskip("torch")
+    import paper_2607_24981_gb300 as ilw
+
+    for shape, dim, at in (((5,), None, 0), ((5, 7), None, 0), ((3, 5, 7), None, 1), ((3, 5), 1, 1), ((3, 5), -1, 1), ((1, 5), 1, 1), ((3, 5, 7), -2, 1)):
+        gate, up = torch.rand(shape), torch.rand(shape)
+        got = ilw.gate_rows(gate, up) if dim is None else ilw.gate_rows(gate, up, dim=dim)
+        assert got.shape == torch.Size(2 * n if i == at else n for i, n in enumerate(shape))
+        for r in range(5):
+            assert torch.equal(got.select(at, 2 * r), gate.select(at, r)) and torch.equal(got.select(at, 2 * r + 1), up.select(at, r))
