@@ -83,9 +83,10 @@ const int32_t *indices(const at::Tensor &t, const char *what) {
     if (t.scalar_type() != at::kInt || !t.is_cuda() || !t.is_contiguous()) fail("%s: indices, slots and offsets are contiguous int32 CUDA tensors", what);
     return (const int32_t *)t.data_ptr();
 }
-const float *weights(const at::Tensor &t, int64_t n, const char *what, const char *name) {
-    if (t.scalar_type() != at::kFloat || !t.is_cuda() || !t.is_contiguous() || t.numel() != n)
-        fail("%s: %s is a contiguous float32 CUDA tensor of %lld values", what, name, (long long)n);
+// `rows` rows of `cols` float32 values, or the same values in one dimension.
+const float *weights(const at::Tensor &t, int64_t rows, int64_t cols, const char *what, const char *name) {
+    if (t.scalar_type() != at::kFloat || !t.is_cuda() || !t.is_contiguous() || t.numel() != rows * cols || (t.dim() > 1 && t.size(t.dim() - 1) != cols))
+        fail("%s: %s is a contiguous float32 CUDA tensor (%lld, %lld)", what, name, (long long)rows, (long long)cols);
     return (const float *)t.data_ptr();
 }
 
@@ -209,7 +210,7 @@ PyObject *gemm(PyObject *const *a) {
         p.offsets = indices(off, what);
         if (off.numel() != W.lead + 1) fail("%s: %lld experts need %lld offsets, not %lld", what, (long long)W.lead, (long long)W.lead + 1, (long long)off.numel());
     }
-    if (given(a[3])) p.bias = weights(tensor(a[3], what), W.lead * N, what, "bias");
+    if (given(a[3])) p.bias = weights(tensor(a[3], what), W.lead, N, what, "bias");
     const at::Tensor out = given(a[6]) ? tensor(a[6], what) : room({A.rows, wide}, dtype_or(a[5], at::kBFloat16, what), *A.t);
     const Matrix y = matrix(out, what);
     if (y.rows != A.rows || y.cols != wide)
@@ -249,7 +250,7 @@ PyObject *combine(PyObject *const *a) {
     const int32_t *at = indices(slot, what);
     if (slot.dim() != 2) fail("%s: slot has %d dimensions, not 2", what, (int)slot.dim());
     const int64_t T = slot.size(0), k = slot.size(1);
-    const float *w = weights(tensor(a[2], what), T * k, what, "weight");
+    const float *w = weights(tensor(a[2], what), T, k, what, "weight");
     if (T > INT32_MAX || k > INT32_MAX || y.cols > INT32_MAX) fail("%s: more than 2^31 tokens or columns", what);
     auto same = [&](const Matrix &m, const char *name) {
         if (m.form != y.form || m.rows != T || m.cols != y.cols)

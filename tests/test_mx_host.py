@@ -184,3 +184,23 @@ def test_gate_rows_alternate_along_their_axis():
         assert got.shape == torch.Size(2 * n if i == at else n for i, n in enumerate(shape))
         for r in range(5):
             assert torch.equal(got.select(at, 2 * r), gate.select(at, r)) and torch.equal(got.select(at, 2 * r + 1), up.select(at, r))
+
+
+def test_biases_and_weights_of_another_shape_are_refused():
+    """As many values in rows of another length would be taken in the wrong order."""
+    torch = pytest.importorskip("torch")
+    import paper_2607_24981_gb300 as ilw
+
+    E, N, K = 3, 8, 64
+    mx = lambda *rows: ilw.MxTensor(on_gpu((*rows, 32), torch.uint8), on_gpu((*rows, 16), torch.uint8), K)  # noqa: E731
+    a, w, off = mx(5), mx(E, N), on_gpu((E + 1,), torch.int32)
+    for shape in ((N, E), (2 * E, N // 2), (E * N, 1), (E, N + 1), (E + 1, N)):
+        with pytest.raises(ilw.IlwError, match="bias"):
+            ilw.mx_grouped_linear(a, w, off, bias=on_gpu(shape, torch.float32), act="silu_gate")
+    for shape in ((2, N // 2), (N + 1,), (N, 1)):
+        with pytest.raises(ilw.IlwError, match="bias"):
+            ilw.mx_linear(a, mx(N), bias=on_gpu(shape, torch.float32))
+    y, slot = on_gpu((10, 16), torch.float32), on_gpu((5, 2), torch.int32)
+    for shape in ((2, 5), (5, 3), (10, 1)):
+        with pytest.raises(ilw.IlwError, match="weight"):
+            ilw.moe_combine(y, slot, on_gpu(shape, torch.float32))
