@@ -6,6 +6,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -63,30 +64,38 @@ int form_of(at::ScalarType t, bool int8, const char *what) {
     }
 }
 
+// All tensors of a call are on the GPU of its first one.
+void same_gpu(const at::Tensor &t, const at::Tensor &first, const char *what) {
+    if (t.device() != first.device()) fail("%s: tensors on more than one device, %s and %s", what, first.device().str().c_str(), t.device().str().c_str());
+}
+
 // A float matrix on the GPU with contiguous rows.  No or a single row may carry any stride: then at least what holds a row.
 struct Matrix {
     int form;
     int64_t rows, cols, ld;
     void *data;
 };
-Matrix matrix(const at::Tensor &t, const char *what, bool int8 = false) {
+Matrix matrix(const at::Tensor &t, const at::Tensor &first, const char *what, bool int8 = false) {
     Matrix m;
     m.form = form_of(t.scalar_type(), int8, what);
     if (t.dim() != 2) fail("%s: a tensor of %d dimensions, not 2", what, (int)t.dim());
     m.rows = t.size(0), m.cols = t.size(1), m.ld = t.stride(0);
     if (!t.is_cuda() || (t.stride(1) != 1 && m.cols > 1 && m.rows > 0)) fail("%s: a tensor is not on the GPU, or its rows are not contiguous", what);
+    same_gpu(t, first, what);
     if (m.rows <= 1 || m.cols == 0) m.ld = std::max(m.ld, m.cols);
     m.data = t.data_ptr();
     return m;
 }
-const int32_t *indices(const at::Tensor &t, const char *what) {
+const int32_t *indices(const at::Tensor &t, const at::Tensor &first, const char *what) {
     if (t.scalar_type() != at::kInt || !t.is_cuda() || !t.is_contiguous()) fail("%s: indices, slots and offsets are contiguous int32 CUDA tensors", what);
+    same_gpu(t, first, what);
     return (const int32_t *)t.data_ptr();
 }
 // `rows` rows of `cols` float32 values, or the same values in one dimension.
-const float *weights(const at::Tensor &t, int64_t rows, int64_t cols, const char *what, const char *name) {
+const float *weights(const at::Tensor &t, const at::Tensor &first, int64_t rows, int64_t cols, const char *what, const char *name) {
     if (t.scalar_type() != at::kFloat || !t.is_cuda() || !t.is_contiguous() || t.numel() != rows * cols || (t.dim() > 1 && t.size(t.dim() - 1) != cols))
         fail("%s: %s is a contiguous float32 CUDA tensor (%lld, %lld)", what, name, (long long)rows, (long long)cols);
+    same_gpu(t, first, what);
     return (const float *)t.data_ptr();
 }
 
@@ -97,7 +106,7 @@ struct Mx {
     int64_t ldc, lds, between_c, between_s;
     const at::Tensor *t;                 // codes
 };
-Mx mx(PyObject *o, int dims, const char *what) {
+Mx mx(PyObject *o, int dims, const at::Tensor *first, const char *what) {
     if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 3) fail("%s: an MxTensor is wanted, not %s", what, Py_TYPE(o)->tp_name);
     const at::Tensor &c = tensor(PyTuple_GET_ITEM(o, 0), what), &s = tensor(PyTuple_GET_ITEM(o, 1), what);
     Mx m;
@@ -111,6 +120,8 @@ Mx mx(PyObject *o, int dims, const char *what) {
              (long long)(16 * nb), (long long)nb, dims);
     if (!c.is_cuda() || !s.is_cuda() || ((c.stride(dims - 1) != 1 || s.stride(dims - 1) != 1) && c.numel()))
         fail("%s: codes or scales are not on the GPU, or their rows are not contiguous", what);
+    same_gpu(s, c, what);
+    if (first) same_gpu(c, *first, what);
     m.lead = dims == 3 ? c.size(0) : 1;
     m.rows = c.size(dims - 2), m.scale_cols = s.size(dims - 1);
     m.ldc = c.stride(dims - 2), m.lds = s.stride(dims - 2);
@@ -124,7 +135,12 @@ Mx mx(PyObject *o, int dims, const char *what) {
     return m;
 }
 
-ilw_stream_t stream_of(const at::Tensor &t) { return c10::cuda::getCurrentCUDAStream(t.get_device()).stream(); }
+// A call launches on its tensors' GPU, on that GPU's current stream.
+struct Launch {
+    c10::cuda::CUDAGuard device;
+    ilw_stream_t stream;
+    explicit Launch(const at::Tensor &t) : device(t.device()), stream(c10::cuda::getCurrentCUDAStream(t.get_device()).stream()) {}
+};
 at::Tensor room(at::IntArrayRef size, at::ScalarType type, const at::Tensor &like) { return at::empty(size, at::TensorOptions().dtype(type).device(like.device())); }
 // Several results in one allocation (an allocation is a good part of a short call): the tensor of `size` and `type` that begins
 // `bytes` into `whole`, `bytes` a multiple of its element size.
@@ -152,30 +168,32 @@ int64_t whole(PyObject *o) {
 PyObject *quantize(PyObject *const *a) {
     const char *what = "mx_quantize";
     const at::Tensor &X = tensor(a[0], what);
-    const Matrix x = matrix(X, what, true);
+    const Matrix x = matrix(X, X, what, true);
     int64_t rows = x.rows;
     const int32_t *at = nullptr;
     if (given(a[1])) {
         const at::Tensor &g = tensor(a[1], what);
-        at = indices(g, what);
+        at = indices(g, X, what);
         rows = g.numel();
     }
     const int64_t nb = (x.cols + 31) / 32, pad = (nb + 15) / 16 * 16;
     if (given(a[2])) {
-        const Mx m = mx(a[2], 2, what);
+        const Mx m = mx(a[2], 2, &X, what);
         if (m.k != x.cols || m.rows != rows)
             fail("%s: out holds %lld rows of %lld, not %lld of %lld", what, (long long)m.rows, (long long)m.k, (long long)rows, (long long)x.cols);
         // (each row of scales is filled up to a multiple of 16 bytes; more than the tensor holds are not its own)
         if (m.scale_cols < pad) fail("%s: scales of out have rows of %lld bytes: at least %lld, a multiple of 16", what, (long long)m.scale_cols, (long long)pad);
+        const Launch on(X);
         check(lib.quantize(x.data, x.form, x.ld, x.rows, at, rows, (int32_t)std::min<int64_t>(x.cols, INT32_MAX), (uint8_t *)m.codes, m.ldc,
-                           (uint8_t *)m.scales, m.lds, stream_of(X)),
+                           (uint8_t *)m.scales, m.lds, on.stream),
               what);
         return Py_NewRef(a[2]);
     }
     const at::Tensor both = room({rows * (16 * nb + pad)}, at::kByte, X), codes = part_of(both, 0, {rows, 16 * nb}, at::kByte),
                      scales = part_of(both, rows * 16 * nb, {rows, pad}, at::kByte);
+    const Launch on(X);
     check(lib.quantize(x.data, x.form, x.ld, x.rows, at, rows, (int32_t)std::min<int64_t>(x.cols, INT32_MAX), (uint8_t *)codes.data_ptr(), 16 * nb,
-                       (uint8_t *)scales.data_ptr(), pad, stream_of(X)),
+                       (uint8_t *)scales.data_ptr(), pad, on.stream),
           what);
     return Py_BuildValue("(NNL)", wrap(codes), wrap(scales), (long long)x.cols);
 }
@@ -183,12 +201,13 @@ PyObject *quantize(PyObject *const *a) {
 // dequantize(m, dtype, out)
 PyObject *dequantize(PyObject *const *a) {
     const char *what = "mx_dequantize";
-    const Mx m = mx(a[0], 2, what);
+    const Mx m = mx(a[0], 2, nullptr, what);
     const at::Tensor out = given(a[2]) ? tensor(a[2], what) : room({m.rows, m.k}, dtype_or(a[1], at::kFloat, what), *m.t);
-    const Matrix y = matrix(out, what);
+    const Matrix y = matrix(out, *m.t, what);
     if (y.rows != m.rows || y.cols != m.k)
         fail("%s: out is (%lld, %lld), not (%lld, %lld)", what, (long long)y.rows, (long long)y.cols, (long long)m.rows, (long long)m.k);
-    check(lib.dequantize(m.codes, m.ldc, m.scales, m.lds, m.rows, (int32_t)m.k, y.data, y.form, y.ld, stream_of(*m.t)), what);
+    const Launch on(*m.t);
+    check(lib.dequantize(m.codes, m.ldc, m.scales, m.lds, m.rows, (int32_t)m.k, y.data, y.form, y.ld, on.stream), what);
     return wrap(out);
 }
 
@@ -196,7 +215,7 @@ PyObject *dequantize(PyObject *const *a) {
 PyObject *gemm(PyObject *const *a) {
     const bool grouped = given(a[2]);
     const char *what = grouped ? "mx_grouped_linear" : "mx_linear";
-    const Mx A = mx(a[0], 2, what), W = mx(a[1], grouped ? 3 : 2, what);
+    const Mx A = mx(a[0], 2, nullptr, what), W = mx(a[1], grouped ? 3 : 2, A.t, what);
     const int64_t act = whole(a[4]), N = W.rows, wide = act == ILW_ACT_SILU_GATE ? N / 2 : N;
     if (A.k != W.k) fail("%s: A has k=%lld, W k=%lld", what, (long long)A.k, (long long)W.k);
     if (A.k > INT32_MAX || N > INT32_MAX || W.lead > INT32_MAX) fail("%s: k, rows or experts past 2^31", what);
@@ -207,17 +226,18 @@ PyObject *gemm(PyObject *const *a) {
     p.w_scales = W.scales, p.w_lds = W.lds, p.w_scales_stride = W.between_s;
     if (grouped) {
         const at::Tensor &off = tensor(a[2], what);
-        p.offsets = indices(off, what);
+        p.offsets = indices(off, *A.t, what);
         if (off.numel() != W.lead + 1) fail("%s: %lld experts need %lld offsets, not %lld", what, (long long)W.lead, (long long)W.lead + 1, (long long)off.numel());
     }
-    if (given(a[3])) p.bias = weights(tensor(a[3], what), W.lead, N, what, "bias");
+    if (given(a[3])) p.bias = weights(tensor(a[3], what), *A.t, W.lead, N, what, "bias");
     const at::Tensor out = given(a[6]) ? tensor(a[6], what) : room({A.rows, wide}, dtype_or(a[5], at::kBFloat16, what), *A.t);
-    const Matrix y = matrix(out, what);
+    const Matrix y = matrix(out, *A.t, what);
     if (y.rows != A.rows || y.cols != wide)
         fail("%s: out is (%lld, %lld), not (%lld, %lld)", what, (long long)y.rows, (long long)y.cols, (long long)A.rows, (long long)wide);
     p.M = A.rows, p.N = (int32_t)N, p.K = (int32_t)A.k, p.experts = (int32_t)W.lead, p.act = (int32_t)act, p.y_form = y.form;
     p.Y = y.data, p.ldy = y.ld;
-    check(lib.gemm(&p, stream_of(*A.t)), what);
+    const Launch on(*A.t);
+    check(lib.gemm(&p, on.stream), what);
     return wrap(out);
 }
 
@@ -225,7 +245,7 @@ PyObject *gemm(PyObject *const *a) {
 PyObject *route(PyObject *const *a) {
     const char *what = "moe_route";
     const at::Tensor &x = tensor(a[0], what);
-    const Matrix m = matrix(x, what);
+    const Matrix m = matrix(x, x, what);
     const int64_t k = whole(a[1]), kk = std::max<int64_t>(k, 0);  // (the entry point refuses k < 1)
     if (m.rows > INT32_MAX || m.cols > INT32_MAX || k > INT32_MAX || k < INT32_MIN) fail("%s: more than 2^31 tokens or experts", what);
     const int32_t T = (int32_t)m.rows, E = (int32_t)m.cols;
@@ -235,9 +255,10 @@ PyObject *route(PyObject *const *a) {
     const at::Tensor expert = part_of(all, 0, {T, kk}, at::kInt), weight = part_of(all, 4 * n, {T, kk}, at::kFloat),
                      source = part_of(all, 8 * n, {n}, at::kInt), slot = part_of(all, 12 * n, {T, kk}, at::kInt),
                      offsets = part_of(all, 16 * n, {(int64_t)E + 1}, at::kInt);
+    const Launch on(x);
     check(lib.route(m.data, m.form, m.ld, T, E, (int32_t)k, PyObject_IsTrue(a[2]), (int32_t *)expert.data_ptr(), (float *)weight.data_ptr(),
                     (int32_t *)offsets.data_ptr(), (int32_t *)source.data_ptr(), (int32_t *)slot.data_ptr(), bytes ? (char *)all.data_ptr() + 4 * words : nullptr, bytes,
-                    stream_of(x)),
+                    on.stream),
           what);
     return Py_BuildValue("(NNNNN)", wrap(expert), wrap(weight), wrap(offsets), wrap(source), wrap(slot));
 }
@@ -246,22 +267,23 @@ PyObject *route(PyObject *const *a) {
 PyObject *combine(PyObject *const *a) {
     const char *what = "moe_combine";
     const at::Tensor &Y = tensor(a[0], what), &slot = tensor(a[1], what);
-    const Matrix y = matrix(Y, what);
-    const int32_t *at = indices(slot, what);
+    const Matrix y = matrix(Y, Y, what);
+    const int32_t *at = indices(slot, Y, what);
     if (slot.dim() != 2) fail("%s: slot has %d dimensions, not 2", what, (int)slot.dim());
     const int64_t T = slot.size(0), k = slot.size(1);
-    const float *w = weights(tensor(a[2], what), T, k, what, "weight");
+    const float *w = weights(tensor(a[2], what), Y, T, k, what, "weight");
     if (T > INT32_MAX || k > INT32_MAX || y.cols > INT32_MAX) fail("%s: more than 2^31 tokens or columns", what);
     auto same = [&](const Matrix &m, const char *name) {
         if (m.form != y.form || m.rows != T || m.cols != y.cols)
             fail("%s: %s is (%lld, %lld), not (%lld, %lld), or of another type than Y", what, name, (long long)m.rows, (long long)m.cols, (long long)T, (long long)y.cols);
     };
     Matrix res = {};
-    if (given(a[3])) same(res = matrix(tensor(a[3], what), what), "residual");
+    if (given(a[3])) same(res = matrix(tensor(a[3], what), Y, what), "residual");
     const at::Tensor out = given(a[4]) ? tensor(a[4], what) : room({T, y.cols}, Y.scalar_type(), Y);
-    const Matrix o = matrix(out, what);
+    const Matrix o = matrix(out, Y, what);
     same(o, "out");
-    check(lib.combine(y.data, y.form, y.ld, y.rows, at, w, (int32_t)T, (int32_t)k, (int32_t)y.cols, res.data, res.ld, o.data, o.ld, stream_of(Y)), what);
+    const Launch on(Y);
+    check(lib.combine(y.data, y.form, y.ld, y.rows, at, w, (int32_t)T, (int32_t)k, (int32_t)y.cols, res.data, res.ld, o.data, o.ld, on.stream), what);
     return wrap(out);
 }
 

@@ -204,3 +204,27 @@ def test_biases_and_weights_of_another_shape_are_refused():
     for shape in ((2, 5), (5, 3), (10, 1)):
         with pytest.raises(ilw.IlwError, match="weight"):
             ilw.moe_combine(y, slot, on_gpu(shape, torch.float32))
+
+
+def test_tensors_of_more_than_one_gpu_are_refused():
+    torch = pytest.importorskip("torch")
+    import paper_2607_24981_gb300 as ilw
+
+    def mx(rows, at="cuda:0", scales_at=None):
+        return ilw.MxTensor(on_gpu((*rows, 32), torch.uint8, at), on_gpu((*rows, 16), torch.uint8, scales_at or at), 64)
+
+    def t(*size, dtype=torch.float32, at="cuda:0"):
+        return on_gpu(size, dtype, at)
+
+    far = "cuda:1"
+    i32 = torch.int32
+    for call in (lambda: ilw.mx_quantize(t(4, 64), gather=t(4, dtype=i32, at=far)), lambda: ilw.mx_quantize(t(4, 64), out=mx((4,), far)),
+                 lambda: ilw.mx_quantize(t(4, 64), out=mx((4,), "cuda:0", far)), lambda: ilw.mx_dequantize(mx((4,)), out=t(4, 64, at=far)),
+                 lambda: ilw.mx_linear(mx((4,)), mx((8,), far)), lambda: ilw.mx_linear(mx((4,)), mx((8,), "cuda:0", far)),
+                 lambda: ilw.mx_linear(mx((4,)), mx((8,)), bias=t(8, at=far)), lambda: ilw.mx_linear(mx((4,)), mx((8,)), out=t(4, 8, at=far)),
+                 lambda: ilw.mx_grouped_linear(mx((4,)), mx((2, 8)), t(3, dtype=i32, at=far)),
+                 lambda: ilw.moe_combine(t(8, 16), t(4, 2, dtype=i32, at=far), t(4, 2)), lambda: ilw.moe_combine(t(8, 16), t(4, 2, dtype=i32), t(4, 2, at=far)),
+                 lambda: ilw.moe_combine(t(8, 16), t(4, 2, dtype=i32), t(4, 2), residual=t(4, 16, at=far)),
+                 lambda: ilw.moe_combine(t(8, 16), t(4, 2, dtype=i32), t(4, 2), out=t(4, 16, at=far))):
+        with pytest.raises(ilw.IlwError, match="device"):
+            call()
