@@ -522,7 +522,8 @@ int ilwdetr_mx_gemm(const ilw_mx_gemm_t *p, ilw_stream_t stream);
 
 /* ------------------------------------------------------------------ mixture of experts */
 
-/* Routing of T tokens to k of E experts each (1 <= k <= min(E, 16), E <= 512):
+enum { ILW_MOE_MAX_EXPERTS = 512, ILW_MOE_MAX_TOP = 16 };
+/* Routing of T tokens to k of E experts each (1 <= k <= min(E, ILW_MOE_MAX_TOP), E <= ILW_MOE_MAX_EXPERTS):
  *   expert[t, j]  the experts of the k largest logits of row t in decreasing order, equal ones by index; -inf and
  *                 NaN are never taken: a row with fewer others ends in expert -1, weight 0, slot -1
  *   weight[t, j]  their softmax: over the row's chosen logits (renormalize != 0) or over all of its logits

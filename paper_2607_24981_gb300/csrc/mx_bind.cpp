@@ -246,7 +246,7 @@ PyObject *route(PyObject *const *a) {
     const char *what = "moe_route";
     const at::Tensor &x = tensor(a[0], what);
     const Matrix m = matrix(x, x, what);
-    const int64_t k = whole(a[1]), kk = std::max<int64_t>(k, 0);  // (the entry point refuses k < 1)
+    const int64_t k = whole(a[1]), kk = k >= 1 && k <= ILW_MOE_MAX_TOP ? k : 0;  // (any other k is refused below: nothing is made for it)
     if (m.rows > INT32_MAX || m.cols > INT32_MAX || k > INT32_MAX || k < INT32_MIN) fail("%s: more than 2^31 tokens or experts", what);
     const int32_t T = (int32_t)m.rows, E = (int32_t)m.cols;
     const size_t bytes = lib.route_bytes(T, E);

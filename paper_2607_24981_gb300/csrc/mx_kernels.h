@@ -4,6 +4,8 @@
 #include <cstdint>
 #include <cuda_runtime.h>
 
+#include "ilwdetr.h"
+
 namespace ilw {
 
 // Element forms of a float (or int8) tensor: the C-ABI's codes.
@@ -61,7 +63,7 @@ struct MoeRouteParams {
     int32_t *slot;     // [T, k]
     int32_t *counts;   // workspace [chunks, E]
 };
-constexpr int kRouteMaxExperts = 512, kRouteMaxTop = 16;
+constexpr int kRouteMaxExperts = ILW_MOE_MAX_EXPERTS, kRouteMaxTop = ILW_MOE_MAX_TOP;
 size_t moe_route_workspace(int32_t T, int32_t E);
 cudaError_t launch_moe_route(const MoeRouteParams &p, cudaStream_t s);
 

@@ -550,6 +550,16 @@ def test_route_extremes(ilw):
     assert empty.offsets.tolist() == [0] * 7 and empty.expert.shape == (0, 2)
 
 
+def test_route_refuses_a_huge_k_before_it_makes_room(ilw):
+    x = torch.randn(2000, 8, device="cuda")
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    for k in (0, -3, 9, 17, 1 << 26, (1 << 31) - 1):
+        with pytest.raises(ilw.IlwError, match="moe_route"):
+            ilw.moe_route(x, k)
+    assert torch.cuda.max_memory_allocated() - before < 1 << 20
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
 @pytest.mark.parametrize("T,k,N", [(1, 1, 1), (5, 2, 33), (64, 8, 256), (300, 3, 1000), (17, 16, 40)])
 @pytest.mark.parametrize("residual", [False, True])
