@@ -112,6 +112,7 @@ Mx mx(PyObject *o, int dims, const at::Tensor *first, const char *what) {
     Mx m;
     m.k = PyLong_AsLongLong(PyTuple_GET_ITEM(o, 2));
     if (m.k == -1 && PyErr_Occurred()) throw Failed();
+    if (m.k < 1 || m.k > INT32_MAX) fail("%s: an MXFP4 tensor of k=%lld", what, (long long)m.k);
     const int64_t nb = (m.k + 31) / 32;
     bool fits = c.scalar_type() == at::kByte && s.scalar_type() == at::kByte && c.dim() == dims && s.dim() == dims && c.size(dims - 1) >= 16 * nb && s.size(dims - 1) >= nb;
     for (int i = 0; fits && i + 1 < dims; ++i) fits = c.size(i) == s.size(i);
@@ -218,7 +219,7 @@ PyObject *gemm(PyObject *const *a) {
     const Mx A = mx(a[0], 2, nullptr, what), W = mx(a[1], grouped ? 3 : 2, A.t, what);
     const int64_t act = whole(a[4]), N = W.rows, wide = act == ILW_ACT_SILU_GATE ? N / 2 : N;
     if (A.k != W.k) fail("%s: A has k=%lld, W k=%lld", what, (long long)A.k, (long long)W.k);
-    if (A.k > INT32_MAX || N > INT32_MAX || W.lead > INT32_MAX) fail("%s: k, rows or experts past 2^31", what);
+    if (N > INT32_MAX || W.lead > INT32_MAX) fail("%s: rows or experts past 2^31", what);
     ilw_mx_gemm_t p = {};
     p.struct_size = sizeof(p);
     p.a_codes = A.codes, p.a_ldc = A.ldc, p.a_scales = A.scales, p.a_lds = A.lds;

@@ -228,3 +228,15 @@ def test_tensors_of_more_than_one_gpu_are_refused():
                  lambda: ilw.moe_combine(t(8, 16), t(4, 2, dtype=i32), t(4, 2), out=t(4, 16, at=far))):
         with pytest.raises(ilw.IlwError, match="device"):
             call()
+
+
+@pytest.mark.parametrize("k", [0, -1, -(1 << 40), 2**31, 2**32 + 64])
+def test_an_mxfp4_tensor_of_a_k_outside_32_bits_is_refused(k):
+    torch = pytest.importorskip("torch")
+    import paper_2607_24981_gb300 as ilw
+
+    nb = max(k + 31, 0) // 32
+    m = ilw.MxTensor(on_gpu((2, 16 * nb), torch.uint8), on_gpu((2, -(-nb // 16) * 16), torch.uint8), k)
+    for call in (lambda: ilw.mx_dequantize(m), lambda: ilw.mx_dequantize(m, out=on_gpu((2, max(k, 0)), torch.float16)), lambda: ilw.mx_linear(m, m)):
+        with pytest.raises(ilw.IlwError, match="k="):
+            call()
