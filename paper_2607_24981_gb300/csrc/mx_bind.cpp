@@ -248,6 +248,8 @@ PyObject *route(PyObject *const *a) {
     const at::Tensor &x = tensor(a[0], what);
     const Matrix m = matrix(x, x, what);
     const int64_t k = whole(a[1]), kk = k >= 1 && k <= ILW_MOE_MAX_TOP ? k : 0;  // (any other k is refused below: nothing is made for it)
+    const int renormalize = PyObject_IsTrue(a[2]);
+    if (renormalize < 0) throw Failed();
     if (m.rows > INT32_MAX || m.cols > INT32_MAX || k > INT32_MAX || k < INT32_MIN) fail("%s: more than 2^31 tokens or experts", what);
     const int32_t T = (int32_t)m.rows, E = (int32_t)m.cols;
     const size_t bytes = lib.route_bytes(T, E);
@@ -257,7 +259,7 @@ PyObject *route(PyObject *const *a) {
                      source = part_of(all, 8 * n, {n}, at::kInt), slot = part_of(all, 12 * n, {T, kk}, at::kInt),
                      offsets = part_of(all, 16 * n, {(int64_t)E + 1}, at::kInt);
     const Launch on(x);
-    check(lib.route(m.data, m.form, m.ld, T, E, (int32_t)k, PyObject_IsTrue(a[2]), (int32_t *)expert.data_ptr(), (float *)weight.data_ptr(),
+    check(lib.route(m.data, m.form, m.ld, T, E, (int32_t)k, renormalize, (int32_t *)expert.data_ptr(), (float *)weight.data_ptr(),
                     (int32_t *)offsets.data_ptr(), (int32_t *)source.data_ptr(), (int32_t *)slot.data_ptr(), bytes ? (char *)all.data_ptr() + 4 * words : nullptr, bytes,
                     on.stream),
           what);

@@ -240,3 +240,15 @@ def test_an_mxfp4_tensor_of_a_k_outside_32_bits_is_refused(k):
     for call in (lambda: ilw.mx_dequantize(m), lambda: ilw.mx_dequantize(m, out=on_gpu((2, max(k, 0)), torch.float16)), lambda: ilw.mx_linear(m, m)):
         with pytest.raises(ilw.IlwError, match="k="):
             call()
+
+
+def test_route_passes_on_an_argument_without_a_truth_value():
+    torch = pytest.importorskip("torch")
+    import paper_2607_24981_gb300 as ilw
+
+    class Neither:
+        def __bool__(self):
+            raise ArithmeticError("neither")
+
+    with pytest.raises(ArithmeticError, match="neither"):
+        ilw.moe_route(on_gpu((4, 8), torch.float32), 2, renormalize=Neither())
