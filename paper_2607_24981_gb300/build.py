@@ -1,7 +1,8 @@
 """Build libilwdetr.so (the C-ABI of include/ilwdetr.h) for sm_103a with nvcc, in-tree.
 
 Each translation unit is compiled in parallel; the shared library is written next to this file, and beside it
-_mxbind.so, the Python binding of the operators in mx.py (host code against torch's headers).
+_mxbind.so, the Python binding of the operators in mx.py (host code against torch's headers; where there is no torch,
+whose tensors it takes, it is left out).
 """
 from __future__ import annotations
 
@@ -38,6 +39,14 @@ def _stale(out: str, deps: list[str]) -> bool:
         return True
     t = os.path.getmtime(out)
     return any(os.path.getmtime(d) > t for d in deps)
+
+
+def importable(name: str) -> bool:
+    try:
+        __import__(name)
+    except ImportError:
+        return False
+    return True
 
 
 def build_binding(verbose: bool = False) -> str:
@@ -81,7 +90,7 @@ def build(force: bool = False, verbose: bool = False, extra: list[str] | None = 
             raise RuntimeError(f"nvcc failed on {os.path.basename(s)}:\n{r.stdout}\n{r.stderr}")
         return r.stderr
 
-    bind = force or _stale(BIND, [BIND_SRC, os.path.join(ROOT, "include", "ilwdetr.h")])
+    bind = importable("torch") and (force or _stale(BIND, [BIND_SRC, os.path.join(ROOT, "include", "ilwdetr.h")]))
     with cf.ThreadPoolExecutor(max_workers=min(9, 1 + len(todo))) as ex:
         binding = ex.submit(build_binding, verbose) if bind else None
         for msg in ex.map(compile_one, todo):

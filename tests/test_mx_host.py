@@ -252,3 +252,16 @@ def test_route_passes_on_an_argument_without_a_truth_value():
 
     with pytest.raises(ArithmeticError, match="neither"):
         ilw.moe_route(on_gpu((4, 8), torch.float32), 2, renormalize=Neither())
+
+
+def test_the_library_is_built_where_there_is_no_torch(L, monkeypatch):
+    """The C-ABI needs none; only the binding of torch tensors does, and is then left out."""
+    import sys
+
+    from paper_2607_24981_gb300 import build
+
+    monkeypatch.setitem(sys.modules, "torch", None)  # (an import of it raises ImportError)
+    stale = build._stale
+    monkeypatch.setattr(build, "_stale", lambda out, deps: out == build.BIND or stale(out, deps))
+    at = build.os.path.getmtime(build.BIND)
+    assert build.build() == build.LIB and build.os.path.getmtime(build.BIND) == at
