@@ -18,6 +18,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libilwdetr.so")
 BIND_SRC, BIND = os.path.join(CSRC, "mx_bind.cpp"), os.path.join(HERE, "_mxbind.so")
+BIND_KEY = os.path.join(OBJ, "_mxbind.key")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC, "--expt-relaxed-constexpr"]
@@ -49,6 +50,19 @@ def importable(name: str) -> bool:
     return True
 
 
+def binding_key() -> str:
+    """What _mxbind.so fits besides its source: this interpreter and this torch."""
+    import sysconfig
+
+    import torch
+
+    return " ".join([sysconfig.get_config_var("SOABI") or sys.version, torch.__version__, torch.__path__[0]])
+
+
+def _read(path: str) -> str:
+    return open(path).read() if os.path.exists(path) else ""
+
+
 def build_binding(verbose: bool = False) -> str:
     """_mxbind.so: one host translation unit, linked with torch's own libraries."""
     import sysconfig
@@ -69,6 +83,8 @@ def build_binding(verbose: bool = False) -> str:
     if r.returncode != 0:
         raise RuntimeError(f"g++ failed on {os.path.basename(BIND_SRC)}:\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, BIND)
+    with open(BIND_KEY, "w") as f:
+        f.write(binding_key())
     return r.stderr
 
 
@@ -90,7 +106,7 @@ def build(force: bool = False, verbose: bool = False, extra: list[str] | None = 
             raise RuntimeError(f"nvcc failed on {os.path.basename(s)}:\n{r.stdout}\n{r.stderr}")
         return r.stderr
 
-    bind = importable("torch") and (force or _stale(BIND, [BIND_SRC, os.path.join(ROOT, "include", "ilwdetr.h")]))
+    bind = importable("torch") and (force or _read(BIND_KEY) != binding_key() or _stale(BIND, [BIND_SRC, os.path.join(ROOT, "include", "ilwdetr.h")]))
     with cf.ThreadPoolExecutor(max_workers=min(9, 1 + len(todo))) as ex:
         binding = ex.submit(build_binding, verbose) if bind else None
         for msg in ex.map(compile_one, todo):

@@ -60,7 +60,10 @@ def _bind():
         L = lib()
         if not os.path.exists(BIND_PATH):
             raise IlwError(f"{BIND_PATH} is missing: build it with __graft_entry__.build()")
-        from . import _mxbind
+        try:
+            from . import _mxbind
+        except ImportError as e:  # (of another Python or torch)
+            raise IlwError(f"{BIND_PATH} does not load, build it again with __graft_entry__.build(): {e}") from e
 
         names = ("ilwdetr_last_error", "ilwdetr_mx_quantize", "ilwdetr_mx_dequantize", "ilwdetr_mx_gemm", "ilwdetr_moe_route_workspace_bytes",
                  "ilwdetr_moe_route", "ilwdetr_moe_combine")

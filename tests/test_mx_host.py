@@ -265,3 +265,30 @@ def test_the_library_is_built_where_there_is_no_torch(L, monkeypatch):
     monkeypatch.setattr(build, "_stale", lambda out, deps: out == build.BIND or stale(out, deps))
     at = build.os.path.getmtime(build.BIND)
     assert build.build() == build.LIB and build.os.path.getmtime(build.BIND) == at
+
+
+def test_a_binding_of_another_python_or_torch_is_built_again(L, monkeypatch):
+    from paper_2607_24981_gb300 import build
+
+    built = []
+    monkeypatch.setattr(build, "build_binding", lambda verbose=False: built.append(1))
+    build.build()
+    assert not built
+    torch = pytest.importorskip("torch")
+    monkeypatch.setattr(torch, "__version__", "0.0")
+    build.build()
+    assert built
+
+
+def test_a_binding_that_does_not_load_is_refused(L, monkeypatch):
+    import sys
+
+    import paper_2607_24981_gb300 as ilw
+    from paper_2607_24981_gb300 import IlwError, mx
+
+    torch = pytest.importorskip("torch")
+    monkeypatch.setattr(mx, "_bound", None)
+    monkeypatch.setitem(sys.modules, "paper_2607_24981_gb300._mxbind", None)
+    monkeypatch.delattr(ilw, "_mxbind", raising=False)
+    with pytest.raises(IlwError, match="does not load"):
+        mx.moe_route(torch.zeros(2, 4), 1)
