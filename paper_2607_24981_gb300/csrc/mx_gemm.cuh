@@ -258,7 +258,8 @@ __device__ __forceinline__ float rcp_fast(float x) {
 }
 // z (1 + erf(z / sqrt 2)) / 2 of two values, with erf |x| = 1 - (1 + a1 |x| + ... + a6 |x|^6)^-16 by Abramowitz and Stegun, Handbook
 // of Mathematical Functions, 7.1.28 (absolute error at most 3e-7): two operations of the special-function unit for the
-// two values.  (With 7.1.26, an exponential and a reciprocal each, that unit was the epilogue's time.)
+// two values.  (With 7.1.26, an exponential and a reciprocal each, that unit was the epilogue's time.)  Its error, up to
+// 8e-7 and some five times that of erff in norm, disappears in the rounding to two bytes.
 __device__ __forceinline__ void gelu2(float &a, float &b) {
     const uint64_t z = pack2(a, b), x = pack2(fabsf(a), fabsf(b));
     // the coefficients a_i / 2^(i/2): x here is |z|, not |z| / sqrt 2
@@ -276,6 +277,16 @@ __device__ __forceinline__ void gelu2(float &a, float &b) {
     const float2 r = unpack2(fma2(h, pack2(copysignf(1.0f - rcp_fast(d.x), a), copysignf(1.0f - rcp_fast(d.y), b)), h));
     a = r.x;
     b = r.y;
+}
+// The same for results of type T: 4-byte ones keep all of fp32's accuracy.
+template <typename T>
+__device__ __forceinline__ void gelu_to(float &a, float &b) {
+    if constexpr (sizeof(T) == 4) {
+        a = 0.5f * a * (1.0f + erff(a * 0.70710678f));
+        b = 0.5f * b * (1.0f + erff(b * 0.70710678f));
+    } else {
+        gelu2(a, b);
+    }
 }
 __device__ __forceinline__ float silu_gate(float gate, float up) { return __fdividef(gate, 1.0f + __expf(-gate)) * up; }
 
@@ -303,7 +314,7 @@ __device__ __forceinline__ void store_chunk(const MxParams &p, float (&v)[16], c
         }
     } else if constexpr (ACT == ILW_ACT_GELU) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) gelu2(v[2 * i], v[2 * i + 1]);
+        for (int i = 0; i < 8; ++i) gelu_to<T>(v[2 * i], v[2 * i + 1]);
     }
     const int out0 = (kGate ? n >> 1 : n) - (kGate ? lane >> 1 : lane);  // first output of the warp
     const int width = kGate ? p.N / 2 : p.N;
@@ -789,7 +800,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
                 }
                 constexpr bool kGate = ACT == ILW_ACT_SILU_GATE;
                 const int width = kGate ? p.N / 2 : p.N, col = kGate ? nn >> 1 : nn;
-                if constexpr (ACT == ILW_ACT_GELU) gelu2(z[0], z[1]), gelu2(z[2], z[3]);
+                if constexpr (ACT == ILW_ACT_GELU) gelu_to<T>(z[0], z[1]), gelu_to<T>(z[2], z[3]);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     if constexpr (kGate) z[i] = silu_gate(z[i], __shfl_down_sync(0xffffffffu, z[i], 1));  // (even lanes: gate, odd: gated)

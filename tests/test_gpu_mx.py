@@ -370,6 +370,28 @@ def test_linear_scales_and_nan(ilw):
     assert torch.equal(bad.isnan(), nan) and torch.equal(bad[~nan], got[~nan])
 
 
+def through(ilw, z, act, dtype, split):
+    """act(z) as a product gives it: zeros times zeros, with the values as its bias (fp32 z [n], 64 rows; split: their K shared)."""
+    n, K = z.numel(), 8192 if split else 32
+    zero = lambda rows: ilw.MxTensor(torch.zeros((rows, K // 2), dtype=torch.uint8, device="cuda"), torch.zeros((rows, -(-K // 512) * 16), dtype=torch.uint8, device="cuda"), K)  # noqa: E731
+    got = ilw.mx_linear(zero(5), zero(n), bias=z, act=act, out_dtype=dtype)
+    assert all(torch.equal(got[0], got[i]) for i in range(1, 5))
+    return got[0]
+
+
+@pytest.mark.parametrize("split", [False, True])
+def test_gelu_in_fp32_is_that_of_fp32(ilw, split):
+    """erff is off by 2 ulp at most (2^-23), its argument's rounding adds 2^-24 and that of 1 + erf 2^-24: |z| / 2 times that
+    and two roundings of the result.  In norm no more than a quarter above plain fp32 operations."""
+    n = 1024 if split else 1 << 18
+    for z in (torch.linspace(-12, 12, n, device="cuda"), torch.randn(n, device="cuda", generator=torch.Generator("cuda").manual_seed(1))):
+        got = through(ilw, z, "gelu", torch.float32, split).double()
+        want = 0.5 * z.double() * torch.erfc(-z.double() / 2**0.5)
+        plain = (0.5 * z * (1 + torch.erf(z * 0.5**0.5))).double()
+        assert ((got - want).abs() <= 2.0**-23 * (z.double().abs() + want.abs())).all()
+        assert (got - want).norm() <= 1.25 * (plain - want).norm()
+
+
 GROUPS = {
     "one row each": [1] * 7, "empty ones": [0, 5, 0, 0, 33, 0], "one takes all": [0, 0, 300, 0], "odd": [17, 226, 1, 449, 15],
     "none": [0, 0, 0], "many": [(7 * i) % 5 for i in range(200)],
