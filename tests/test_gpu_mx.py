@@ -375,7 +375,7 @@ def through(ilw, z, act, dtype, split):
     n, K = z.numel(), 8192 if split else 32
     zero = lambda rows: ilw.MxTensor(torch.zeros((rows, K // 2), dtype=torch.uint8, device="cuda"), torch.zeros((rows, -(-K // 512) * 16), dtype=torch.uint8, device="cuda"), K)  # noqa: E731
     got = ilw.mx_linear(zero(5), zero(n), bias=z, act=act, out_dtype=dtype)
-    assert all(torch.equal(got[0], got[i]) for i in range(1, 5))
+    assert all(torch.equal(got[0].nan_to_num(3.0), got[i].nan_to_num(3.0)) for i in range(1, 5))
     return got[0]
 
 
@@ -390,6 +390,30 @@ def test_gelu_in_fp32_is_that_of_fp32(ilw, split):
         plain = (0.5 * z * (1 + torch.erf(z * 0.5**0.5))).double()
         assert ((got - want).abs() <= 2.0**-23 * (z.double().abs() + want.abs())).all()
         assert (got - want).norm() <= 1.25 * (plain - want).norm()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("split", [False, True])
+def test_silu_gates_of_every_size(ilw, split, dtype):
+    """fp32: an exponential off by 1 ulp (2^-23), the sum, the quotient and two products by 2^-24 each; bf16 by its rounding and
+    some 100 of those ulp.  No gate is flushed to zero before exp(-gate) overflows (below -88.7)."""
+    n = 512 if split else 1 << 17
+    for lo, hi in ((-8, 8), (-87.3, -8), (8, 100)):
+        gate = torch.linspace(lo, hi, n, device="cuda")
+        up = torch.randn(n, device="cuda", generator=torch.Generator("cuda").manual_seed(2))
+        got = through(ilw, torch.stack([gate, up], 1).flatten(), "silu_gate", dtype, split).double()
+        want = gate.double() * torch.sigmoid(gate.double()) * up.double()
+        tol = 3 * 2.0**-23 if dtype == torch.float32 else 2.0**-8 + 128 * 2.0**-23
+        assert ((got - want).abs() <= tol * want.abs() + 2.0**-133).all()  # (a subnormal's rounding)
+    gate = torch.linspace(-200, -87.3, n, device="cuda")  # below -88.7 exp(-gate) is infinity in fp32
+    got = through(ilw, torch.stack([gate, torch.full_like(gate, 2.0**100)], 1).flatten(), "silu_gate", dtype, split).double()
+    want = gate.double() * torch.sigmoid(gate.double()) * 2.0**100
+    close = (got - want).abs() <= 2.0**-7 * want.abs()
+    assert close[gate >= -88.7].all() and (close | (got == 0)).all()
+    special = torch.tensor([float("inf"), 2.0, float("nan"), 1.0, 1.0, float("nan"), 0.0, float("-inf"), -3.0, float("inf"), -0.0, 1.0, 3e38, 1.0, -3e38, 1.0], device="cuda")
+    got = through(ilw, special, "silu_gate", dtype, False)
+    assert got[0] == float("inf") and got[1:4].isnan().all() and got[4] == float("-inf") and got[5] == 0
+    assert got[6] == torch.tensor(3e38, dtype=dtype) and got[7] == 0
 
 
 GROUPS = {
