@@ -119,7 +119,7 @@ __device__ __forceinline__ void select_token(const MoeRouteParams &p, float *row
         for (int i = 0; i < G; ++i) {
             const float4 *x = (const float4 *)(row + (L * i + q) * S);
 #pragma unroll
-            for (int c = 0; c < S / 4; ++c) sum += __expf(x[c].x - best) + __expf(x[c].y - best) + (__expf(x[c].z - best) + __expf(x[c].w - best));
+            for (int c = 0; c < S / 4; ++c) sum += expf(x[c].x - best) + expf(x[c].y - best) + (expf(x[c].z - best) + expf(x[c].w - best));
         }
     }
 #pragma unroll
@@ -159,10 +159,10 @@ __device__ __forceinline__ void select_token(const MoeRouteParams &p, float *row
             for (int i = 0; i < G; ++i)
                 if (i == g / L) top[i] = rest;
             out_e[j] = g * S + at;
-            out_w[j] = __expf(m - best);
+            out_w[j] = expf(m - best);
         }
         if (!taken && q == 0) out_e[j] = -1, out_w[j] = 0.0f;
-        if (taken && p.renormalize) sum += __expf(m - best);
+        if (taken && p.renormalize) sum += expf(m - best);
         if (L > 1) __syncwarp();
     }
     const float scale = 1.0f / sum;

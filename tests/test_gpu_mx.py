@@ -577,6 +577,19 @@ def test_route_of_few_tokens(ilw, T):
         assert (np.abs(r.weight.double().cpu().numpy() - weight) <= (E + 8) * 2.0**-23 * weight).all()
 
 
+@pytest.mark.parametrize("T", [100, 3000])
+@pytest.mark.parametrize("renormalize", [True, False])
+def test_route_weights_of_logits_far_apart(ilw, T, renormalize):
+    """Logits on a quarter grid, so that the exponentials' arguments are exact: of up to -80, each off by 2 ulp at most; a sum of
+    8 of them and a quotient as above."""
+    rng = np.random.default_rng(T)
+    x = -rng.integers(0, 321, (T, 8)) / 4
+    r = ilw.moe_route(torch.from_numpy(x).float().cuda(), 8, renormalize)
+    expert, weight, *_ = ref_route(x, 8, renormalize)
+    assert np.array_equal(r.expert.cpu().numpy(), expert)
+    assert (np.abs(r.weight.double().cpu().numpy() - weight) <= (8 + 8) * 2.0**-23 * weight).all()
+
+
 def test_route_of_many_experts_after_few(ilw):
     x = torch.randn(600, 256, device="cuda")
     first = ilw.moe_route(x, 3)
