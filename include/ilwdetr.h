@@ -520,6 +520,11 @@ typedef struct {
 } ilw_mx_gemm_t;
 int ilwdetr_mx_gemm(const ilw_mx_gemm_t *p, ilw_stream_t stream);
 
+/* Test hook: the form that ilwdetr_mx_gemm takes for these arguments (checked as there, read no further) on a device of `sms` SMs (0:
+ * the current one).  form[0]: 0 one CTA a tile, 1 several that share a tile's K, 2 two SMs a tile; form[1]: CTAs that
+ * share a tile's K; form[2]: most tokens a tile.  Launches nothing. */
+int ilwdetr_debug_mx_form(const ilw_mx_gemm_t *p, int32_t sms, int32_t *form);
+
 /* ------------------------------------------------------------------ mixture of experts */
 
 enum { ILW_MOE_MAX_EXPERTS = 512, ILW_MOE_MAX_TOP = 16 };

@@ -166,6 +166,7 @@ SIGNATURES = {
     "ilwdetr_mx_quantize": ([_VP, _I32, _I64, _I64, _VP, _I64, _I32, _VP, _I64, _VP, _I64, _VP], C.c_int),
     "ilwdetr_mx_dequantize": ([_VP, _I64, _VP, _I64, _I64, _I32, _VP, _I32, _I64, _VP], C.c_int),
     "ilwdetr_mx_gemm": ([_VP, _VP], C.c_int),
+    "ilwdetr_debug_mx_form": ([_VP, _I32, C.POINTER(_I32)], C.c_int),
     "ilwdetr_moe_route_workspace_bytes": ([_I32, _I32], C.c_size_t),
     "ilwdetr_moe_route": ([_VP, _I32, _I64, _I32, _I32, _I32, _I32, _VP, _VP, _VP, _VP, _VP, _VP, C.c_size_t, _VP], C.c_int),
     "ilwdetr_moe_combine": ([_VP, _I32, _I64, _I64, _VP, _VP, _I32, _I32, _I32, _VP, _I64, _VP, _I64, _VP], C.c_int),

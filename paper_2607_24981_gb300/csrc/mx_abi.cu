@@ -34,10 +34,46 @@ int mx_array(const char *what, const char *name, const void *p, int64_t ld, int6
 int64_t code_bytes(int32_t K) { return ((int64_t)K + 31) / 32 * 16; }
 int64_t scale_bytes(int32_t K) { return ((int64_t)K + 31) / 32; }
 
-}  // namespace
-
 #define ILW_TRY(x) \
     if (const int rc_ = (x)) return rc_
+
+// Checks a product's arguments and puts them into g; those of an empty one (M or N 0) need no tensors.
+int gemm_problem(const ilw_mx_gemm_t *p, ilw::MxGemmProblem &g) {
+    if (!p || p->struct_size != sizeof(ilw_mx_gemm_t)) return fail(ILW_ERR_INVALID_ARG, "mx_gemm: struct_size");
+    if (p->act < ILW_ACT_NONE || p->act > ILW_ACT_SILU_GATE) return fail(ILW_ERR_INVALID_ARG, "mx_gemm: act=%d", p->act);
+    if (!form_size(p->y_form)) return fail(ILW_ERR_INVALID_ARG, "mx_gemm: y_form=%d", p->y_form);
+    if (p->M < 0 || p->N < 0 || p->K < 1 || p->experts < 1 || (!p->offsets && p->experts != 1))
+        return fail(ILW_ERR_INVALID_ARG, "mx_gemm: bad sizes M=%lld N=%d K=%d experts=%d", (long long)p->M, p->N, p->K, p->experts);
+    const bool gate = p->act == ILW_ACT_SILU_GATE;
+    if (gate && p->N % 2) return fail(ILW_ERR_INVALID_ARG, "mx_gemm: a gated product's N=%d must be even", p->N);
+    if (p->M > INT32_MAX - 1024 || p->N > (1 << 24) || p->K > (1 << 24) || p->experts > ilw::kMxMaxExperts)
+        return fail(ILW_ERR_UNSUPPORTED, "mx_gemm: M < 2^31 - 1024, N and K <= 2^24, experts <= %d", ilw::kMxMaxExperts);
+    // (the tiles a call can come to, counted in 32 bits by the kernel)
+    if ((p->M / 16 + p->experts + 1) * ((p->N + 127) / 128) > INT32_MAX) return fail(ILW_ERR_UNSUPPORTED, "mx_gemm: M x N too large for one call");
+    g = {};
+    g.M = p->M, g.N = p->N;
+    if (p->M == 0 || p->N == 0) return ILW_OK;
+    ILW_TRY(mx_array("mx_gemm", "a_codes", p->a_codes, p->a_ldc, code_bytes(p->K)));
+    ILW_TRY(mx_array("mx_gemm", "a_scales", p->a_scales, p->a_lds, scale_bytes(p->K)));
+    ILW_TRY(mx_array("mx_gemm", "w_codes", p->w_codes, p->w_ldc, code_bytes(p->K)));
+    ILW_TRY(mx_array("mx_gemm", "w_scales", p->w_scales, p->w_lds, scale_bytes(p->K)));
+    const bool one = !p->offsets || p->experts == 1;
+    if (!one && (p->w_codes_stride % 16 || p->w_scales_stride % 16 || p->w_codes_stride < 16 || p->w_scales_stride < 16 ||
+                 p->w_codes_stride >= (int64_t)1 << 40 || p->w_scales_stride >= (int64_t)1 << 40))
+        return fail(ILW_ERR_INVALID_ARG, "mx_gemm: strides between experts are positive multiples of 16 bytes");
+    if (!aligned(p->bias, 4) || !aligned(p->offsets, 4)) return fail(ILW_ERR_INVALID_ARG, "mx_gemm: bias or offsets misaligned");
+    if (!p->Y || !aligned(p->Y, form_size(p->y_form)) || p->ldy < (gate ? p->N / 2 : p->N))
+        return fail(ILW_ERR_INVALID_ARG, "mx_gemm: Y NULL, misaligned or of short rows");
+    g.a_codes = p->a_codes, g.a_scales = p->a_scales, g.w_codes = p->w_codes, g.w_scales = p->w_scales;
+    g.a_ldc = p->a_ldc, g.a_lds = p->a_lds, g.w_ldc = p->w_ldc, g.w_lds = p->w_lds;
+    // (one matrix: any stride that a tensor map takes)
+    g.w_codes_stride = one ? p->w_ldc : p->w_codes_stride, g.w_scales_stride = one ? p->w_lds : p->w_scales_stride;
+    g.bias = p->bias, g.K = p->K, g.experts = p->experts, g.offsets = p->offsets;
+    g.act = p->act, g.form = p->y_form, g.Y = p->Y, g.ldy = p->ldy;
+    return ILW_OK;
+}
+
+}  // namespace
 
 extern "C" {
 
@@ -71,38 +107,20 @@ int ilwdetr_mx_dequantize(const uint8_t *codes, int64_t ldc, const uint8_t *scal
 }
 
 int ilwdetr_mx_gemm(const ilw_mx_gemm_t *p, ilw_stream_t stream) {
-    if (!p || p->struct_size != sizeof(ilw_mx_gemm_t)) return fail(ILW_ERR_INVALID_ARG, "mx_gemm: struct_size");
-    if (p->act < ILW_ACT_NONE || p->act > ILW_ACT_SILU_GATE) return fail(ILW_ERR_INVALID_ARG, "mx_gemm: act=%d", p->act);
-    if (!form_size(p->y_form)) return fail(ILW_ERR_INVALID_ARG, "mx_gemm: y_form=%d", p->y_form);
-    if (p->M < 0 || p->N < 0 || p->K < 1 || p->experts < 1 || (!p->offsets && p->experts != 1))
-        return fail(ILW_ERR_INVALID_ARG, "mx_gemm: bad sizes M=%lld N=%d K=%d experts=%d", (long long)p->M, p->N, p->K, p->experts);
-    const bool gate = p->act == ILW_ACT_SILU_GATE;
-    if (gate && p->N % 2) return fail(ILW_ERR_INVALID_ARG, "mx_gemm: a gated product's N=%d must be even", p->N);
-    if (p->M > INT32_MAX - 1024 || p->N > (1 << 24) || p->K > (1 << 24) || p->experts > ilw::kMxMaxExperts)
-        return fail(ILW_ERR_UNSUPPORTED, "mx_gemm: M < 2^31 - 1024, N and K <= 2^24, experts <= %d", ilw::kMxMaxExperts);
-    // (the tiles a call can come to, counted in 32 bits by the kernel)
-    if ((p->M / 16 + p->experts + 1) * ((p->N + 127) / 128) > INT32_MAX) return fail(ILW_ERR_UNSUPPORTED, "mx_gemm: M x N too large for one call");
-    if (p->M == 0 || p->N == 0) return ILW_OK;
-    ILW_TRY(mx_array("mx_gemm", "a_codes", p->a_codes, p->a_ldc, code_bytes(p->K)));
-    ILW_TRY(mx_array("mx_gemm", "a_scales", p->a_scales, p->a_lds, scale_bytes(p->K)));
-    ILW_TRY(mx_array("mx_gemm", "w_codes", p->w_codes, p->w_ldc, code_bytes(p->K)));
-    ILW_TRY(mx_array("mx_gemm", "w_scales", p->w_scales, p->w_lds, scale_bytes(p->K)));
-    const bool one = !p->offsets || p->experts == 1;
-    if (!one && (p->w_codes_stride % 16 || p->w_scales_stride % 16 || p->w_codes_stride < 16 || p->w_scales_stride < 16 ||
-                 p->w_codes_stride >= (int64_t)1 << 40 || p->w_scales_stride >= (int64_t)1 << 40))
-        return fail(ILW_ERR_INVALID_ARG, "mx_gemm: strides between experts are positive multiples of 16 bytes");
-    if (!aligned(p->bias, 4) || !aligned(p->offsets, 4)) return fail(ILW_ERR_INVALID_ARG, "mx_gemm: bias or offsets misaligned");
-    if (!p->Y || !aligned(p->Y, form_size(p->y_form)) || p->ldy < (gate ? p->N / 2 : p->N))
-        return fail(ILW_ERR_INVALID_ARG, "mx_gemm: Y NULL, misaligned or of short rows");
-    if (ilw::validate_only()) return ILW_OK;
     ilw::MxGemmProblem g;
-    g.a_codes = p->a_codes, g.a_scales = p->a_scales, g.w_codes = p->w_codes, g.w_scales = p->w_scales;
-    g.a_ldc = p->a_ldc, g.a_lds = p->a_lds, g.w_ldc = p->w_ldc, g.w_lds = p->w_lds;
-    // (one matrix: any stride that a tensor map takes)
-    g.w_codes_stride = one ? p->w_ldc : p->w_codes_stride, g.w_scales_stride = one ? p->w_lds : p->w_scales_stride;
-    g.bias = p->bias, g.M = p->M, g.N = p->N, g.K = p->K, g.experts = p->experts, g.offsets = p->offsets;
-    g.act = p->act, g.form = p->y_form, g.Y = p->Y, g.ldy = p->ldy;
+    ILW_TRY(gemm_problem(p, g));
+    if (g.M == 0 || g.N == 0 || ilw::validate_only()) return ILW_OK;
     return done(ilw::launch_mx_gemm(g, (cudaStream_t)stream), "mx_gemm");
+}
+
+int ilwdetr_debug_mx_form(const ilw_mx_gemm_t *p, int32_t sms, int32_t *form) {
+    ilw::MxGemmProblem g;
+    ILW_TRY(gemm_problem(p, g));
+    if (!form || sms < 0 || g.M == 0 || g.N == 0) return fail(ILW_ERR_INVALID_ARG, "debug_mx_form: NULL result, negative sms or empty product");
+    int32_t f[3];
+    if (!ilw::mx_gemm_form(g, sms, f)) return fail(ILW_ERR_UNSUPPORTED, "debug_mx_form: no form");
+    for (int i = 0; i < 3; ++i) form[i] = f[i];
+    return ILW_OK;
 }
 
 size_t ilwdetr_moe_route_workspace_bytes(int32_t T, int32_t E) {

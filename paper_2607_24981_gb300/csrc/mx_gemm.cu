@@ -24,24 +24,13 @@ bool code_map(CUtensorMap *m, const void *base, int64_t cols, int64_t rows, int6
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-}  // namespace
-
-cudaError_t launch_mx_gemm(const MxGemmProblem &g, cudaStream_t s) {
-    if (g.M == 0 || g.N == 0) return cudaSuccess;
-    MxParams p;
-    memset(&p, 0, sizeof(p));
-    p.offsets = g.offsets;
-    p.bias = g.bias;
-    p.Y = g.Y;
-    p.ldy = g.ldy;
+// The form that a product takes on `sms` SMs, in p: mode, tiles, stages, with the number of tiles at most and the shared memory of a CTA.
+bool choose_form(const MxGemmProblem &g, int64_t sms, MxParams &p, int64_t &tiles, int &smem) {
     p.M = g.M;
     p.N = g.N;
     p.E = g.experts;
     p.nkb = (g.K + 255) / 256;
     p.nsb = (g.K + 511) / 512;
-    p.status = status_word_ptr();
-    gemm_debug_wait(&p.dbg_skip, &p.wait_cycles);
-    const int64_t sms = sm_count();
 
     const int64_t out = g.act == ILW_ACT_SILU_GATE ? g.N / 2 : g.N;
     p.wide = g.act != ILW_ACT_NONE && g.form != ILW_FP32 && out % 8 == 0 && (uintptr_t)g.Y % 16 == 0 && g.ldy % 8 == 0;
@@ -57,7 +46,6 @@ cudaError_t launch_mx_gemm(const MxGemmProblem &g, cudaStream_t s) {
     // tiles of n tokens: at most, and (every other expert's last tile half full) about
     auto most = [&](int64_t n) { return g.offsets ? std::min<int64_t>(g.M, g.M / n + g.experts) : (g.M + n - 1) / n; };
     auto about = [&](int64_t n) { return g.offsets ? std::min<int64_t>(g.M, g.M / n + g.experts / 2 + 1) : (g.M + n - 1) / n; };
-    int64_t tiles = 0;
     for (;; p.nt = (p.nt - 1) / 32 * 32) {  // (a pair's: a multiple of 32)
         // Pairs start and end some 1.5 us later and then take a sixth less time a block of K, so they are for a K above 1024 and 20 blocks
         // or more a pair of SMs (one CTA a tile against pairs, in us: 12800 x 384 x 1536, 9 blocks, 11.7 and 12.5; 6400 x 2048 x
@@ -86,9 +74,10 @@ cudaError_t launch_mx_gemm(const MxGemmProblem &g, cudaStream_t s) {
         for (p.stages = kMxMaxStages; p.stages >= kMxMinStages && bytes() > kMxSmemLimit; --p.stages) {
         }
         if (p.stages >= kMxMinStages) break;
-        if (p.nt <= 32) return cudaErrorInvalidValue;  // (never)
+        if (p.nt <= 32) return false;  // (never)
     }
-    if (tiles > INT32_MAX) return cudaErrorInvalidValue;
+    smem = bytes();
+    if (tiles > INT32_MAX) return false;
     // t / wtiles for t < 2^31 (round-up reciprocal of Granlund and Montgomery, 1994)
     while ((1ll << p.wdiv_s) < p.wtiles) ++p.wdiv_s;
     p.wdiv_m = (uint32_t)((((uint64_t)1 << 32) * ((1ull << p.wdiv_s) - p.wtiles)) / p.wtiles + 1);
@@ -103,6 +92,35 @@ cudaError_t launch_mx_gemm(const MxGemmProblem &g, cudaStream_t s) {
             if (c <= p.nsb && c * tiles <= room && p.nsb - (p.nsb + c - 1) / c >= 6 + p.nt / 128) p.splits = c;
         }
     if (p.splits > 1) p.mode = MX_SPLIT;
+    return true;
+}
+
+}  // namespace
+
+bool mx_gemm_form(const MxGemmProblem &g, int32_t sms, int32_t (&form)[3]) {
+    MxParams p;
+    memset(&p, 0, sizeof(p));
+    int64_t tiles;
+    int smem;
+    if (!choose_form(g, sms ? sms : sm_count(), p, tiles, smem)) return false;
+    form[0] = p.mode, form[1] = p.splits, form[2] = p.nt;
+    return true;
+}
+
+cudaError_t launch_mx_gemm(const MxGemmProblem &g, cudaStream_t s) {
+    if (g.M == 0 || g.N == 0) return cudaSuccess;
+    MxParams p;
+    memset(&p, 0, sizeof(p));
+    p.offsets = g.offsets;
+    p.bias = g.bias;
+    p.Y = g.Y;
+    p.ldy = g.ldy;
+    p.status = status_word_ptr();
+    gemm_debug_wait(&p.dbg_skip, &p.wait_cycles);
+    const int64_t sms = sm_count();
+    int64_t tiles;
+    int smem;
+    if (!choose_form(g, sms, p, tiles, smem)) return cudaErrorInvalidValue;
 
     p.nb = (g.K + 31) / 32;
     p.w_scales = g.w_scales, p.w_lds = g.w_lds, p.w_scales_stride = g.w_scales_stride;
@@ -115,9 +133,9 @@ cudaError_t launch_mx_gemm(const MxGemmProblem &g, cudaStream_t s) {
     int grid = (int)std::min<int64_t>(tiles, sms);
     if (p.mode == MX_SPLIT) grid = (int)tiles * p.splits;
     if (p.mode == MX_PAIR) grid = 2 * (int)std::min<int64_t>(tiles, sms / 2);
-    if (g.form == ILW_FP32) return launch_mx<float>(p, g.act, grid, bytes(), s);
-    if (g.form == ILW_FP16) return launch_mx<__half>(p, g.act, grid, bytes(), s);
-    return launch_mx<__nv_bfloat16>(p, g.act, grid, bytes(), s);
+    if (g.form == ILW_FP32) return launch_mx<float>(p, g.act, grid, smem, s);
+    if (g.form == ILW_FP16) return launch_mx<__half>(p, g.act, grid, smem, s);
+    return launch_mx<__nv_bfloat16>(p, g.act, grid, smem, s);
 }
 
 }  // namespace ilw

@@ -49,6 +49,9 @@ struct MxGemmProblem {
     int64_t ldy;
 };
 constexpr int kMxMaxExperts = 1024;
+// What launch_mx_gemm would take on `sms` SMs (0: as many as the current device has): form 0 (a CTA a tile), 1 (several) or 2 (a
+// pair), CTAs that share a tile's K, most tokens a tile.
+bool mx_gemm_form(const MxGemmProblem &g, int32_t sms, int32_t (&form)[3]);
 cudaError_t launch_mx_gemm(const MxGemmProblem &p, cudaStream_t s);
 
 struct MoeRouteParams {

@@ -334,6 +334,116 @@ def test_grouped_with_a_long_sum(ilw, counts, N, K):
     ilw.device_status()
 
 
+def form_of(ilw, M, N, K, experts, act, dtype):
+    """What the library takes for a product with contiguous operands on this GPU: "one" CTA a tile, "pair" of SMs, or how many CTAs
+    share a tile's K; and the tokens of a tile."""
+    import ctypes
+
+    from paper_2607_24981_gb300 import mx
+
+    nb, got = -(-K // 32), (ctypes.c_int32 * 3)()
+    lds, wide = -(-nb // 16) * 16, N // 2 if act == "silu_gate" else N
+    y_form = {torch.float32: 232, torch.float16: 216, torch.bfloat16: 217}[dtype]
+    rc = ilw.lib().ilwdetr_debug_mx_form(mx.gemm_struct(1 << 20, 16 * nb, 1 << 20, lds, 1 << 20, 16 * nb, N * 16 * nb, 1 << 20, lds, N * lds, 0, 1 << 20 if experts else 0,
+                                                        M, N, K, experts or 1, mx.ACTS[act], y_form, 1 << 20, wide), 0, got)
+    assert rc == 0, ilw.lib().ilwdetr_last_error()
+    return ["one", got[1], "pair"][got[0]], got[2]
+
+
+def made(ilw, seed, R, K, weights=False):
+    """Weights, or activations in rows of different sizes, as MXFP4 (by mx_quantize, which has its own tests)."""
+    gen = torch.Generator("cuda").manual_seed(seed)
+    x = torch.randn((R, K), generator=gen, device="cuda")
+    return ilw.mx_quantize(x / K**0.5 if weights else x * torch.exp2(torch.randint(-6, 4, (R, 1), generator=gen, device="cuda").float()))
+
+
+def check_product_on_gpu(ilw, got, A, W, bias, act):
+    """check_product with its 64-bit product on the GPU: got [M, n], MXFP4 A and W, fp32 bias or None."""
+    a, w = ilw.mx_dequantize(A).double(), ilw.mx_dequantize(W).double()
+    z, mass = a @ w.T, a.abs() @ w.abs().T
+    if bias is not None:
+        z, mass = z + bias.double(), mass + bias.double().abs()
+    tol = (A.k + 8) * 2.0**-23 * mass
+    if act == "silu_gate":
+        g, u = z[:, 0::2], z[:, 1::2]
+        s = torch.sigmoid(g)
+        want = g * s * u
+        tol = 1.1 * tol[:, 0::2] * (u.abs() + tol[:, 1::2]) + (g * s).abs() * tol[:, 1::2] + 8 * 2.0**-24 * want.abs()
+    elif act == "gelu":
+        want = 0.5 * z * torch.erfc(-z / 2**0.5)
+        tol = 1.13 * tol + 8 * 2.0**-24 * z.abs()
+    else:
+        want = z
+    tol = tol + EPS[got.dtype] * (want.abs() + tol) + (2.0**-25 if got.dtype == torch.float16 else 0.0)
+    err = (got.double() - want).abs()
+    assert got.shape == want.shape and (err <= tol).all(), f"{int((err > tol).sum())} of {err.numel()} outside, worst {float((err / tol).max()):.3g} times the bound"
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("form,M,N,K,act,bias", [
+    ("pair", 1500, 1712, 8200, "none", True), ("pair", 1500, 1712, 8200, "gelu", True), ("pair", 1500, 1712, 8200, "silu_gate", True),
+    ("pair", 1500, 1712, 8200, "gelu", False), ("pair", 1570, 1701, 8200, "none", True), ("pair", 1570, 1701, 8200, "gelu", True),
+    ("pair", 1570, 1702, 8200, "silu_gate", False),
+    (8, 5, 1000, 4096, "gelu", True), (8, 40, 1000, 4200, "silu_gate", True), (8, 1, 257, 8000, "none", True),
+    (4, 5, 2600, 4128, "silu_gate", True), (4, 200, 1000, 6200, "gelu", True), (4, 100, 1001, 4200, "none", False),
+    (2, 5, 6000, 6200, "gelu", True), (2, 224, 2000, 9000, "silu_gate", True), (2, 224, 1999, 9000, "none", True),
+    ("one", 1500, 1712, 1000, "gelu", True), ("one", 1500, 1712, 1000, "silu_gate", True), ("one", 333, 1701, 1000, "none", True)])
+def test_every_form_with_every_activation(ilw, form, M, N, K, act, bias, dtype):
+    assert form_of(ilw, M, N, K, None, act, dtype)[0] == form
+    A, W = made(ilw, 1, M, K), made(ilw, 2, N, K, weights=True)
+    b = torch.randn(N, device="cuda", generator=torch.Generator("cuda").manual_seed(3)) if bias else None
+    got = ilw.mx_linear(A, W, b, act=act, out_dtype=dtype)
+    check_product_on_gpu(ilw, got, A, W, b, act)
+    assert all(torch.equal(got, ilw.mx_linear(A, W, b, act=act, out_dtype=dtype)) for _ in range(3))
+    ilw.device_status()
+
+
+@pytest.mark.parametrize("M,tokens", [(65, 96), (100, 128), (130, 160), (165, 192), (200, 224), (250, 224)])
+def test_pairs_on_tiles_of_every_width(ilw, M, tokens):
+    N, K = 19008, 8200
+    assert form_of(ilw, M, N, K, None, "gelu", torch.bfloat16) == ("pair", tokens)
+    A, W = made(ilw, 1, M, K), made(ilw, 2, N, K, weights=True)
+    b = torch.randn(N, device="cuda", generator=torch.Generator("cuda").manual_seed(3))
+    check_product_on_gpu(ilw, ilw.mx_linear(A, W, b, act="gelu"), A, W, b, "gelu")
+    ilw.device_status()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("form,counts,N,K,act", [
+    ("pair", [700, 0, 1, 333, 1024, 225, 95], 2304, 2600, "none"), ("pair", [700, 0, 1, 333, 1024, 225, 95], 2304, 2600, "gelu"),
+    ("pair", [700, 0, 1, 333, 1024, 225, 95], 2304, 2600, "silu_gate"), (8, [1, 0, 9], 300, 4200, "gelu"), (4, [0, 2, 130, 0], 140, 8192, "silu_gate"),
+    ("one", [700, 0, 1, 333, 1024, 225, 95], 1704, 600, "gelu")])
+def test_every_form_by_expert(ilw, form, counts, N, K, act, dtype):
+    off, E = np.r_[0, np.cumsum(counts)], len(counts)
+    assert form_of(ilw, int(off[-1]), N, K, E, act, dtype)[0] == form
+    A, W = made(ilw, 1, int(off[-1]), K), made(ilw, 2, E * N, K, weights=True)
+    W = ilw.MxTensor(W.codes.view(E, N, -1), W.scales.view(E, N, -1), K)
+    b = torch.randn((E, N), device="cuda", generator=torch.Generator("cuda").manual_seed(3))
+    got = ilw.mx_grouped_linear(A, W, torch.from_numpy(off.astype(np.int32)).cuda(), b, act=act, out_dtype=dtype)
+    for e in range(E):
+        if counts[e]:
+            s = slice(int(off[e]), int(off[e + 1]))
+            check_product_on_gpu(ilw, got[s], ilw.MxTensor(A.codes[s], A.scales[s], K), ilw.MxTensor(W.codes[e], W.scales[e], K), b[e], act)
+    ilw.device_status()
+
+
+@pytest.mark.parametrize("form,M,N,K", [("one", 300, 256, 2048), (8, 4, 256, 8192), (4, 5, 2600, 4128), (2, 5, 6000, 6200), ("pair", 3001, 1700, 4096)])
+def test_every_form_gives_up_a_bounded_wait(ilw, form, M, N, K):
+    """As test_product_gives_up_a_bounded_wait, with the form that each product takes."""
+    assert form_of(ilw, M, N, K, None, "none", torch.bfloat16)[0] == form
+    A, W = made(ilw, 1, M, K), made(ilw, 2, N, K, weights=True)
+    want = ilw.mx_linear(A, W)
+    assert ilw.lib().ilwdetr_debug_gemm_wait(0, 20_000_000) == 0
+    try:
+        ilw.mx_linear(A, W)
+        with pytest.raises(ilw.IlwError, match="wait"):
+            ilw.device_status()
+    finally:
+        assert ilw.lib().ilwdetr_debug_gemm_wait(-1, 0) == 0
+    assert torch.equal(ilw.mx_linear(A, W), want)
+    ilw.device_status()
+
+
 def test_linear_rows_with_strides(ilw):
     """Operands inside wider byte arrays, a result inside a wider tensor, fp16."""
     rng = np.random.default_rng(11)

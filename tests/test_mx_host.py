@@ -292,3 +292,46 @@ def test_a_binding_that_does_not_load_is_refused(L, monkeypatch):
     monkeypatch.delattr(ilw, "_mxbind", raising=False)
     with pytest.raises(IlwError, match="does not load"):
         mx.moe_route(torch.zeros(2, 4), 1)
+
+
+def form_of(L, M, N, K, counts=None, act="none", y_form=217, sms=152):
+    """(form, CTAs that share a tile's K, tokens a tile) of a product with contiguous operands; `counts`: experts."""
+    from paper_2607_24981_gb300 import mx
+
+    nb = -(-K // 32)
+    lds, wide = -(-nb // 16) * 16, N // 2 if act == "silu_gate" else N
+    got = (ctypes.c_int32 * 3)()
+    rc = L.ilwdetr_debug_mx_form(mx.gemm_struct(1 << 20, 16 * nb, 1 << 20, lds, 1 << 20, 16 * nb, N * 16 * nb, 1 << 20, lds, N * lds, 0, 1 << 20 if counts else 0,
+                                                M, N, K, counts or 1, mx.ACTS[act], y_form, 1 << 20, wide), sms, got)
+    assert rc == 0, L.ilwdetr_last_error()
+    return tuple(got)
+
+
+def test_forms_of_products(L):
+    assert form_of(L, 1, 4096, 4096) == (1, 4, 16)
+    assert form_of(L, 8192, 8192, 8192) == (2, 1, 224)
+    assert form_of(L, 32, 4096, 2048, counts=64, act="silu_gate")[0] == 0
+    refused(L, L.ilwdetr_debug_mx_form(None, 152, (ctypes.c_int32 * 3)()), -1, b"struct_size")
+    assert L.ilwdetr_debug_mx_form(None, 152, None) == -1
+
+
+@pytest.mark.parametrize("sms", [132, 148, 152, 160])
+def test_forms_keep_to_what_the_kernel_takes(L, sms):
+    """Over sizes of all kinds: tiles in steps that the MMA takes, clusters no larger than K has stages and all of them resident at once."""
+    import random
+
+    rng = random.Random(sms)
+    seen = set()
+    for _ in range(4000):
+        size = lambda top: int(round(2 ** rng.uniform(0, top)))  # noqa: E731
+        M, N, K, E = size(15), 2 * size(13), size(14), rng.choice([None, None, size(10)])
+        act = rng.choice(["none", "gelu", "silu_gate"])
+        form, splits, tokens = form_of(L, M, N, K, E, act, rng.choice([217, 232]), sms)
+        seen.add((form, splits))
+        assert 16 <= tokens <= 224 and tokens % (32 if form == 2 else 16) == 0
+        tiles = min(M, M // tokens + E) if E else -(-M // tokens)
+        if form == 1:
+            assert splits in (2, 4, 8) and splits <= -(-K // 512) and splits * tiles * -(-N // 128) <= sms
+        else:
+            assert splits == 1 and (form == 0 or (N > 128 and K > 1024))
+    assert seen == {(0, 1), (1, 2), (1, 4), (1, 8), (2, 1)}
