@@ -112,13 +112,13 @@ def build(force: bool = False, verbose: bool = False, extra: list[str] | None = 
         for msg in ex.map(compile_one, todo):
             if verbose and msg:
                 print(msg, file=sys.stderr)
-        if binding:
-            binding.result()
     if force or todo or _stale(LIB, objs):
         tmp = LIB + ".tmp%d" % os.getpid()
         cmd = [nvcc()] + ARCH + ["-shared", "-Xcompiler", "-fPIC", "-o", tmp] + objs
         subprocess.run(cmd, check=True)
         os.replace(tmp, LIB)
+    if binding:
+        binding.result()  # (an error of the binding's build leaves the library built)
     return LIB
 
 

@@ -267,6 +267,20 @@ def test_the_library_is_built_where_there_is_no_torch(L, monkeypatch):
     assert build.build() == build.LIB and build.os.path.getmtime(build.BIND) == at
 
 
+def test_a_binding_that_does_not_build_leaves_the_library_built(L, monkeypatch, tmp_path):
+    from paper_2607_24981_gb300 import build
+
+    def no_headers(verbose=False):
+        raise RuntimeError("no Python.h")
+
+    monkeypatch.setattr(build, "build_binding", no_headers)
+    monkeypatch.setattr(build, "BIND", str(tmp_path / "absent.so"))
+    monkeypatch.setattr(build, "LIB", str(tmp_path / "lib.so"))
+    with pytest.raises(RuntimeError, match="Python.h"):
+        build.build()
+    assert build.os.path.exists(build.LIB)
+
+
 def test_a_binding_of_another_python_or_torch_is_built_again(L, monkeypatch):
     from paper_2607_24981_gb300 import build
 
