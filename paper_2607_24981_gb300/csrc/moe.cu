@@ -95,6 +95,17 @@ __device__ __forceinline__ void clear_row(float *row, bool is_token) {
     __syncwarp();
 }
 
+// exp(x - best) of 4 N values, added up in four parts and pairwise.
+template <int N>
+__device__ __forceinline__ float4 sum_exp(const float4 *x, float best) {
+    if constexpr (N == 1) {
+        return make_float4(expf(x->x - best), expf(x->y - best), expf(x->z - best), expf(x->w - best));
+    } else {
+        const float4 a = sum_exp<N / 2>(x, best), b = sum_exp<N / 2>(x + N / 2, best);
+        return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
+    }
+}
+
 // The k largest of a token's row by L lanes (lane q of them here; all 32 lanes of the warp call it): its experts and weights to
 // out_e and out_w, in order.  `row` loses what is taken.
 template <int L, int S>
@@ -114,13 +125,15 @@ __device__ __forceinline__ void select_token(const MoeRouteParams &p, float *row
 #pragma unroll
     for (int d = 1; d < L; d <<= 1) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, d));
     float sum = 0.0f;
-    if (!p.renormalize && best > none) {  // over every expert of the row
+    if (!p.renormalize && best > none) {  // over every expert of the row, by group and in four parts: short chains of roundings
+        float4 part = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 4
         for (int i = 0; i < G; ++i) {
             const float4 *x = (const float4 *)(row + (L * i + q) * S);
-#pragma unroll
-            for (int c = 0; c < S / 4; ++c) sum += expf(x[c].x - best) + expf(x[c].y - best) + (expf(x[c].z - best) + expf(x[c].w - best));
+            const float4 of = sum_exp<S / 4>(x, best);
+            part.x += of.x, part.y += of.y, part.z += of.z, part.w += of.w;
         }
+        sum = (part.x + part.y) + (part.z + part.w);
     }
 #pragma unroll
     for (int d = 1; d < L; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
@@ -162,12 +175,13 @@ __device__ __forceinline__ void select_token(const MoeRouteParams &p, float *row
             out_w[j] = expf(m - best);
         }
         if (!taken && q == 0) out_e[j] = -1, out_w[j] = 0.0f;
-        if (taken && p.renormalize) sum += expf(m - best);
         if (L > 1) __syncwarp();
     }
-    const float scale = 1.0f / sum;
+    if (p.renormalize)
+        for (int j = p.k - 1; j >= 0; --j) sum += out_w[j];  // (the small ones first)
+    if (L > 1) __syncwarp();
     for (int j = q; j < p.k; j += L)
-        if (out_e[j] >= 0) out_w[j] *= scale;
+        if (out_e[j] >= 0) out_w[j] /= sum;
 }
 
 // Places of a chunk's entries: base[e] + the earlier tokens of e in the chunk.  Entry i of the chunk (token i / k) is ex[i / threads] of

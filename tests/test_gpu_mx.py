@@ -700,6 +700,23 @@ def test_route_weights_of_logits_far_apart(ilw, T, renormalize):
     assert (np.abs(r.weight.double().cpu().numpy() - weight) <= (8 + 8) * 2.0**-23 * weight).all()
 
 
+@pytest.mark.parametrize("T,E,k", [(4000, 256, 8), (4000, 64, 8), (20000, 128, 4), (200, 64, 16)])
+@pytest.mark.parametrize("renormalize", [True, False])
+def test_route_weights_as_exact_as_plain_operations(ilw, T, E, k, renormalize):
+    """In norm, over many weights, no further from 64 bits than plain fp32 operations are (a tenth more for chance)."""
+    x = 2 * torch.randn((T, E), device="cuda", generator=torch.Generator("cuda").manual_seed(T + E))
+    r = ilw.moe_route(x, k, renormalize)
+
+    def weights(x):
+        top = torch.gather(x, 1, r.expert.long())
+        p = torch.exp(x - top[:, :1])
+        q = torch.exp(top - top[:, :1])
+        return q / (q if renormalize else p).sum(1, keepdim=True)
+
+    want = weights(x.double())
+    assert (r.weight.double() - want).norm() <= 1.1 * (weights(x).double() - want).norm()
+
+
 def test_route_of_many_experts_after_few(ilw):
     x = torch.randn(600, 256, device="cuda")
     first = ilw.moe_route(x, 3)
