@@ -487,7 +487,8 @@ int ilwdetr_gather_rows_batched(const void *src, int64_t src_ld, int64_t src_row
  * ilwdetr_device_status.  K >= 1. */
 int ilwdetr_mx_quantize(const void *X, int32_t x_form, int64_t ldx, int64_t x_rows, const int32_t *gather, int64_t rows,
                         int32_t K, uint8_t *codes, int64_t ldc, uint8_t *scales, int64_t lds, ilw_stream_t stream);
-/* MXFP4 back to values, rounded to y_form (exact in fp32, and in bf16; fp16 overflows to infinity past 65504). */
+/* MXFP4 back to values, rounded to y_form: exact in fp32 and bf16, infinite past their largest numbers (which scale bytes from
+ * 253 on can come to, but none of ilwdetr_mx_quantize) and past fp16's. */
 int ilwdetr_mx_dequantize(const uint8_t *codes, int64_t ldc, const uint8_t *scales, int64_t lds, int64_t rows, int32_t K,
                           void *Y, int32_t y_form, int64_t ldy, ilw_stream_t stream);
 
@@ -537,7 +538,7 @@ enum { ILW_MOE_MAX_EXPERTS = 512, ILW_MOE_MAX_TOP = 16 };
  *   source[s]     the token at place s; -1 past the last
  * logits [T, ld] in `form` (ILW_FP32, ILW_FP16, ILW_BF16).  weight fp32, the rest int32: [T, k], offsets [E + 1], source
  * [T k].  workspace: ilwdetr_moe_route_workspace_bytes (0 for a few hundred tokens: then it may be NULL), 4-byte
- * aligned. */
+ * aligned.  T k < 2^31; past a million tokens the order's time grows with T^2.  T = 0 writes offsets. */
 size_t ilwdetr_moe_route_workspace_bytes(int32_t T, int32_t E);
 int ilwdetr_moe_route(const void *logits, int32_t form, int64_t ld, int32_t T, int32_t E, int32_t k, int32_t renormalize,
                       int32_t *expert, float *weight, int32_t *offsets, int32_t *source, int32_t *slot, void *workspace,

@@ -5,12 +5,15 @@
 //
 // Selection: two lanes a token (four in calls of few tokens), its row in shared memory, its experts in 16 groups of
 // consecutive ones, of which they know the largest logit.  The k times the largest group is found and scanned again
-// without what was taken: some 150 instructions a token, where a warp a token, with its warp-wide maxima, took 525.
-// 65536 rows of 128 fp32 logits, 8 taken: 29.7 us with the order, bound by those instructions (the bytes take 6 us).
+// without what was taken: some 155 instructions a token, where a warp a token, with its warp-wide maxima, took 525.
+// 65536 rows of 128 fp32 logits, 8 taken: 30 us with the order (the bytes take 6 us).  Bound by latency: the rows in shared
+// memory leave room for five CTAs, 20 warps, an SM, whose schedulers issue in 42 of 100 cycles, and 1024 CTAs are one round
+// of 760 and a third of one.
 //
 // Order: a counting sort over chunks of 512 tokens (256 where rows are long), one to a cluster of 8 CTAs.  The first kernel selects, and
 // adds up in distributed shared memory how many tokens of the chunk each expert gets; the second finds its chunk's places from
-// the counts of all chunks.  A token names an expert at most once, so within a chunk an entry's place is the number
+// the counts of all chunks (each placing CTA reads them: T^2 E / 2^18 words in all, from the L2; 8 MB of 65536 tokens and 128
+// experts, but 2 GB of a million tokens).  A token names an expert at most once, so within a chunk an entry's place is the number
 // of earlier tokens in its expert's bitmap: the same whatever order the bits were set in.  Calls of few tokens do
 // both in one CTA.
 #include <algorithm>
@@ -418,7 +421,8 @@ cudaError_t route_form(const MoeRouteParams &p, cudaStream_t s) {
 }
 
 // out[t, c] = (res[t, c] +) sum_j weight[t, j] Y[slot[t, j], c], j ascending, in fp32.  Bound by HBM: 16384 tokens of 8 rows of 4096
-// bf16 take 204 us (5.9 TB/s) in pieces of 16 bytes, 1060 us value by value, as rows off 16-byte boundaries are.
+// bf16 take 204 us (5.9 TB/s) in pieces of 16 bytes; rows off 16-byte boundaries go value by value: 1033 us of 4097, bound by the latency
+// of one load of 2 bytes in flight a thread.
 // Four rows in flight a thread instead of what the CTAs of an SM have among them: 283 us.
 template <typename T, int VEC>
 __global__ void __launch_bounds__(256) combine_kernel(const MoeCombineParams p) {

@@ -11,7 +11,8 @@
 // compared two at a time), eight a thread back, several steps in flight.  Other rows: a warp takes 256 values of a row, one
 // after the other in memory, and hands them over through shared memory, so that its accesses stay whole lines
 // (eight values a lane in a row of its own would touch every line eight times).  Measured, first form and second: 65536 x 1536 bf16
-// to codes 40.0 us (6.4 TB/s) and 82, back 38.3 us (6.7 TB/s) and 71; 16384 x 4096 fp32 to codes 44.2 us (6.9 TB/s) and 51.
+// to codes 40.1 us (6.4 TB/s) and 78, back 38.3 us (6.7 TB/s) and 77; 16384 x 4096 fp32 to codes 44.2 us (6.9 TB/s) and 52, back 62 and
+// 57; int8 65536 x 1536 to codes 66 us (2.3 TB/s) and 74.
 #include <algorithm>
 #include <cstdint>
 

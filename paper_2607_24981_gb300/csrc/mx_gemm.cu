@@ -38,8 +38,8 @@ bool choose_form(const MxGemmProblem &g, int64_t sms, MxParams &p, int64_t &tile
     auto bytes = [&] { return fixed + p.stages * p.stage_bytes + kMxScaleSets * p.raw_bytes + 2 * p.scale_bytes; };
 
     // Tokens a tile: as wide as the tokens (of an expert, twice the mean: with the mean alone more experts of unequal ones take two
-    // tiles; 4096 rows of 32 experts, N 4096, K 2048: 34 us, 36 with the mean) fill, at most 224, and what leaves room
-    // for four stages.
+    // tiles; 1000 rows of 32 experts, N 4096, K 1024: 18.8 to 20.1 us as they are dealt out, 21.3 to 22.1 with the mean; 4096
+    // rows, K 2048, 34.7 to 36.8 and 34.3 to 38.6) fill, at most 224, and what leaves room for four stages.
     const int64_t per = g.offsets ? (2 * g.M + g.experts - 1) / g.experts : g.M;
     p.nt = (int32_t)std::min<int64_t>(kMxMaxTok, (std::min(per, g.M) + 15) / 16 * 16);
     if (p.nt > 32) p.nt = (p.nt + 31) / 32 * 32;
@@ -48,8 +48,8 @@ bool choose_form(const MxGemmProblem &g, int64_t sms, MxParams &p, int64_t &tile
     auto about = [&](int64_t n) { return g.offsets ? std::min<int64_t>(g.M, g.M / n + g.experts / 2 + 1) : (g.M + n - 1) / n; };
     for (;; p.nt = (p.nt - 1) / 32 * 32) {  // (a pair's: a multiple of 32)
         // Pairs start and end some 1.5 us later and then take a sixth less time a block of K, so they are for a K above 1024 and 20 blocks
-        // or more a pair of SMs (one CTA a tile against pairs, in us: 12800 x 384 x 1536, 9 blocks, 11.7 and 12.5; 6400 x 2048 x
-        // 1536, 18 blocks, 16.6 and 16.8; 12800 x 1536 x 1536, 27 blocks, 22.5 and 20.7; 8192 cubed 199 and 171), and for
+        // or more a pair of SMs (one CTA a tile against pairs, in us: 12800 x 384 x 1536, 9 blocks, 9.7 and 12.2; 6400 x 2048 x
+        // 1536, 18 blocks, 16.6 and 16.8; 12800 x 1536 x 1536, 27 blocks, 21.8 and 20.8; 8192 cubed 194 and 169), and for
         // tiles of 64 tokens or more, whose MMAs take longer than their rows of W
         const int64_t pair_tiles = most(p.nt) * ((g.N + 2 * kMxRowsW - 1) / (2 * kMxRowsW));
         p.mode = p.nt >= 64 && g.N > kMxRowsW && p.nkb > 4 && 2 * pair_tiles * p.nkb >= 20 * sms ? MX_PAIR : MX_ONE;
@@ -57,8 +57,8 @@ bool choose_form(const MxGemmProblem &g, int64_t sms, MxParams &p, int64_t &tile
         p.wtiles = (g.N + rows_w - 1) / rows_w;
         if (p.mode == MX_ONE) {
             // The width, from 64 tokens on, at which the CTA with the most tiles reads the fewest rows of W and tokens (at 224 tokens and so, in
-            // us: 12800 x 384 x 1536, 128 tokens, 11.3 and 9.9; 6400 x 1536 x 384, 176, 14.2 and 12.7; 224 x 4096 x 4096, 64, 10.8
-            // and 8.8; narrower still, 32 and 16 tokens, 12.2 and 15.7; 2048 rows of 16 experts, 768 x 1024, 7.4 and 6.5)
+            // us: 12800 x 384 x 1536, 128 tokens, 11.5 and 9.7; 6400 x 1536 x 384, 176, 11.5 and 10.4; 224 x 4096 x 4096, 64, 10.8
+            // and 8.9; narrower still, 32 and 16 tokens, 12.3 and 15.6; 2048 rows of 16 experts, 768 x 1024, 7.2 and 6.6)
             int64_t least = INT64_MAX;
             for (int32_t top = p.nt, n = top; n >= std::min(top, 64); n -= 16) {
                 const int64_t rows = (about(n) * p.wtiles + sms - 1) / sms * (n + kMxRowsW);
@@ -82,9 +82,9 @@ bool choose_form(const MxGemmProblem &g, int64_t sms, MxParams &p, int64_t &tile
     while ((1ll << p.wdiv_s) < p.wtiles) ++p.wdiv_s;
     p.wdiv_m = (uint32_t)((((uint64_t)1 << 32) * ((1ull << p.wdiv_s) - p.wtiles)) / p.wtiles + 1);
     // Few tiles and a long K: 8, 4 or 2 CTAs to a tile, each with whole scale stages of K.  The cluster and its join cost what six
-    // stages of 512 do, more with many tokens (one CTA and split, in us: one token, N 4096, K 4096, by 4, 7.3 and 7.2; K 16384,
-    // 17.8 and 11.0; N 1024 by 8, 17.2 and 7.8; 224 tokens, N and K 4096, by 4, 11.0 and 12.1, which is why it is not split),
-    // and the clusters have to fit side by side: 16 of 8 CTAs do not (N 2048, K 4096: 11.6 us, by 4 6.9).
+    // stages of 512 do, more with many tokens (one CTA and split, in us: one token, N 4096, K 4096, by 4, 7.1 and 7.0; K 16384,
+    // 17.7 and 10.8; N 1024 by 8, 16.9 and 7.6; 224 tokens, N and K 4096, by 4, 10.8 and 12.0, which is why it is not split),
+    // and the clusters have to fit side by side: 16 of 8 CTAs do not (N 2048, K 4096: 11.4 us, by 4 6.7).
     p.splits = 1;
     if (p.mode == MX_ONE)
         for (int c = 8; c > 1 && p.splits == 1; c /= 2) {

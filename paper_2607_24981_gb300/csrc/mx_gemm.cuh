@@ -18,7 +18,8 @@
 // many: two SMs share a tile of 256 outputs (cta_group::2), each with its own 128 rows of W and half of
 // the tokens.  One CTA's shared memory takes 45 KB of operands for each 256 of K of its tile and gives them to the
 // tensor core once, at 128 bytes a clock 700 clocks for MMAs of 450; in a pair it is 30 KB.  8192 cubed: 168 us in pairs (6.5
-// PFLOP/s; 48 bytes a clock reach each SM, of 64 at most), 199 us without.
+// PFLOP/s; some 50 bytes a clock reach each SM, of nominally 64; back to back for seconds, at the power limit, 182 to 187 us), 194 us
+// without.  Tensor pipe active 63 % of the time (4096 x 4096 x 8192).
 //
 // Scales are stored row-major, 16 bytes of a row for 512 values of K.  Four pairs of warps take turns (a turn is a chain of
 // latencies of some 2000 clocks, the MMAs of 512 values are done in 900) to bring them in by asynchronous copies
@@ -301,7 +302,8 @@ __device__ __forceinline__ float silu_gate(float gate, float up) {
 // One warp's 32 rows of W (this lane: row n) x 16 tokens (c0 .. c0 + 15 of the tile).  A lane holds one output of 16
 // tokens, so its own stores are 2 bytes wide; where there is an activation and rows of Y allow it (`wide`), 2-byte results
 // pass through the warp's patch of shared memory [token][output] and leave in 16-byte pieces (12800 x 1536 x 384 with GELU:
-// 22.3 us, 23.2 without; 32 rows of 64 experts, gated, 24.7 and 25.2; without activation 8192 cubed took 175 us so and takes 170).
+// 20.2 us, 20.9 without; 32 rows of 64 experts, gated, 21.3 and 21.7; 16384 rows of 32, gated, either way 125; without
+// activation 8192 cubed takes 181 us so and 169 as it is, 12800 x 1536 x 384 15.8 and 14.9).
 template <int ACT, typename T>
 __device__ __forceinline__ void store_chunk(const MxParams &p, float (&v)[16], const Tile &t, int c0, int n, float bias, uint32_t patch,
                                             int lane) {
