@@ -526,6 +526,47 @@ int ilwdetr_mx_gemm(const ilw_mx_gemm_t *p, ilw_stream_t stream);
  * share a tile's K; form[2]: most tokens a tile.  Launches nothing. */
 int ilwdetr_debug_mx_form(const ilw_mx_gemm_t *p, int32_t sms, int32_t *form);
 
+/* ------------------------------------------------------------------ int8 with float scales */
+
+/* Linear layers of 8-bit integers between float activations: every token (row of A) and every output channel (row of W) has
+ * a scale of its own.  Floating point like the MXFP4 entry points, whose element forms and activations they share.
+ *
+ * An int8 matrix [rows, K] is its codes, rows of K bytes that begin on 16-byte boundaries (bytes past K are neither read nor
+ * written), and fp32 scales [rows]: its values are code x scale. */
+
+/* Rows to int8.  Row i of the result is row gather[i] of X (gather NULL: row i).
+ *   scale = max|x| / 127 rounded to fp32, at least 2^-126; 0 for a row of zeros, NaN if a value is not finite (codes 0)
+ *   code  = x / scale rounded to the nearest whole number (of the exact quotient; ties to the even one)
+ * X [x_rows, ldx] in x_form (ILW_FP32, ILW_FP16, ILW_BF16), aligned to its elements, ldx >= K; gather as in ilwdetr_mx_quantize;
+ * codes 16-byte aligned, ldc a multiple of 16; K >= 1. */
+int ilwdetr_i8_quantize(const void *X, int32_t x_form, int64_t ldx, int64_t x_rows, const int32_t *gather, int64_t rows,
+                        int32_t K, int8_t *codes, int64_t ldc, float *scales, ilw_stream_t stream);
+/* int8 back to values, rounded to y_form (infinite past its largest number). */
+int ilwdetr_i8_dequantize(const int8_t *codes, int64_t ldc, const float *scales, int64_t rows, int32_t K, void *Y,
+                          int32_t y_form, int64_t ldy, ilw_stream_t stream);
+
+/* Y = act(sa sw (A W^T) + bias) of int8 matrices A [M, K] and W [N, K], or of the W [experts, N, K] of each group of rows:
+ * row r uses expert e where offsets[e] <= r < offsets[e + 1]; rows of no expert are written as zeros.
+ *   a_scales fp32 [M], w_scales fp32 [experts, N], bias fp32 [experts, N] or NULL; all device
+ *   w_codes_stride  bytes between experts (a multiple of 16; ignored for one expert without offsets)
+ *   offsets, y_form, Y, ldy, act   as in ilw_mx_gemm_t
+ * Products are exact; sums are exact while they stay below 2^24 (so whenever K <= 1024) and of fp32's accuracy past
+ * that, or 32-bit whole numbers throughout where there are few tokens.  Scaling, bias and activation in fp32, the result is
+ * rounded once.  1 <= experts <= 1024, K < 2^17, M < 2^31 - 1024. */
+typedef struct {
+    uint32_t struct_size;
+    const int8_t *a_codes; int64_t a_ldc;
+    const float *a_scales;
+    const int8_t *w_codes; int64_t w_ldc, w_codes_stride;
+    const float *w_scales;
+    const float *bias;
+    const int32_t *offsets;
+    int64_t M;
+    int32_t N, K, experts, act, y_form;
+    void *Y; int64_t ldy;
+} ilw_i8_gemm_t;
+int ilwdetr_i8_gemm(const ilw_i8_gemm_t *p, ilw_stream_t stream);
+
 /* ------------------------------------------------------------------ mixture of experts */
 
 enum { ILW_MOE_MAX_EXPERTS = 512, ILW_MOE_MAX_TOP = 16 };
@@ -543,6 +584,26 @@ size_t ilwdetr_moe_route_workspace_bytes(int32_t T, int32_t E);
 int ilwdetr_moe_route(const void *logits, int32_t form, int64_t ld, int32_t T, int32_t E, int32_t k, int32_t renormalize,
                       int32_t *expert, float *weight, int32_t *offsets, int32_t *source, int32_t *slot, void *workspace,
                       size_t workspace_bytes, ilw_stream_t stream);
+/* The same routing by other scores, with a bias for balance and by groups of experts:
+ *   s[e] = sigmoid(x[e]) or the softmax of the row's logits;  c[e] = s[e] + bias[e]
+ *   the E / groups consecutive experts of a group give it the rank of their largest c, or the sum of their two
+ *   largest (group_best 1 or 2); experts of the top_groups best groups can be taken, equal groups by index
+ *   the k largest c of these are taken, in decreasing order, equal ones by index; without a bias c has the logits' order
+ *   weight = s, over the sum of the taken s if renormalize, times scale
+ * Experts whose logit or c is -inf or NaN are never taken and add nothing to a group or a softmax; a logit of +inf is the
+ * limit of large ones.  What is taken is what these comparisons give in 64-bit floating point, the sigmoid as 1 / (1 + exp(-x)).
+ * bias fp32 [E] device or NULL; groups divides E, 1 <= top_groups <= groups <= ILW_MOE_MAX_GROUPS, k <= E / groups * top_groups; scale
+ * finite.  All else as in ilwdetr_moe_route, the workspace too. */
+enum { ILW_SCORE_SOFTMAX = 0, ILW_SCORE_SIGMOID = 1, ILW_MOE_MAX_GROUPS = 32 };
+typedef struct {
+    uint32_t struct_size;
+    int32_t score, groups, top_groups, group_best;
+    float scale;
+    const float *bias;
+} ilw_moe_scores_t;
+int ilwdetr_moe_route_scored(const void *logits, int32_t form, int64_t ld, int32_t T, int32_t E, int32_t k, int32_t renormalize,
+                             const ilw_moe_scores_t *scores, int32_t *expert, float *weight, int32_t *offsets, int32_t *source,
+                             int32_t *slot, void *workspace, size_t workspace_bytes, ilw_stream_t stream);
 /* out[t] = (res[t] +) sum_j weight[t, j] Y[slot[t, j]], added in fp32 in the order of j, rounded once.  A slot of -1 adds
  * nothing; any other outside [0, rows) neither, and is reported by the next ilwdetr_device_status.  Y [rows, ldy], res
  * [T, ldr] (or NULL) and out [T, ldo] in `form`; out may be res; 1 <= k. */

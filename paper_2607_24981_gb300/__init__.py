@@ -1,4 +1,5 @@
-"""GB300 (sm_103a) integer-only I-LW-DETR forward path, and microscaled 4-bit linear layers and experts beside it (mx.py).
+"""GB300 (sm_103a) integer-only I-LW-DETR forward path, and microscaled 4-bit (mx.py) and int8 (int8.py) linear layers and experts
+beside it.
 
 Python names mirror the C-ABI of ``include/ilwdetr.h`` (``libilwdetr.so`` in this directory).
 This module only marshals arguments: torch tensors provide device memory and the current CUDA
@@ -20,6 +21,7 @@ __all__ = [
     "QueryPos", "BoxRefine", "ivit_shiftgelu",
     "MxTensor", "Routing", "mx_empty", "mx_quantize", "mx_dequantize", "mx_linear", "mx_grouped_linear", "moe_route", "moe_combine",
     "gate_rows", "MxExperts",
+    "I8Tensor", "i8_empty", "i8_quantize", "i8_dequantize", "i8_linear", "i8_grouped_linear", "I8Experts",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -169,6 +171,10 @@ SIGNATURES = {
     "ilwdetr_debug_mx_form": ([_VP, _I32, C.POINTER(_I32)], C.c_int),
     "ilwdetr_moe_route_workspace_bytes": ([_I32, _I32], C.c_size_t),
     "ilwdetr_moe_route": ([_VP, _I32, _I64, _I32, _I32, _I32, _I32, _VP, _VP, _VP, _VP, _VP, _VP, C.c_size_t, _VP], C.c_int),
+    "ilwdetr_moe_route_scored": ([_VP, _I32, _I64, _I32, _I32, _I32, _I32, _VP, _VP, _VP, _VP, _VP, _VP, _VP, C.c_size_t, _VP], C.c_int),
+    "ilwdetr_i8_quantize": ([_VP, _I32, _I64, _I64, _VP, _I64, _I32, _VP, _I64, _VP, _VP], C.c_int),
+    "ilwdetr_i8_dequantize": ([_VP, _I64, _VP, _I64, _I32, _VP, _I32, _I64, _VP], C.c_int),
+    "ilwdetr_i8_gemm": ([_VP, _VP], C.c_int),
     "ilwdetr_moe_combine": ([_VP, _I32, _I64, _I64, _VP, _VP, _I32, _I32, _I32, _VP, _I64, _VP, _I64, _VP], C.c_int),
 }
 
@@ -952,7 +958,8 @@ def ivit_shiftgelu(X, gelu: dict, out=None):
     return out
 
 
-# the microscaled 4-bit and mixture-of-experts operators (they use the helpers above)
+# the microscaled 4-bit, int8 and mixture-of-experts operators (they use the helpers above)
 from .mx import (  # noqa: E402
     MxExperts, MxTensor, Routing, gate_rows, moe_combine, moe_route, mx_dequantize, mx_empty, mx_grouped_linear, mx_linear, mx_quantize,
 )
+from .int8 import I8Experts, I8Tensor, i8_dequantize, i8_empty, i8_grouped_linear, i8_linear, i8_quantize  # noqa: E402

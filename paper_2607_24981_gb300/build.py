@@ -1,7 +1,7 @@
 """Build libilwdetr.so (the C-ABI of include/ilwdetr.h) for sm_103a with nvcc, in-tree.
 
 Each translation unit is compiled in parallel; the shared library is written next to this file, and beside it
-_mxbind.so, the Python binding of the operators in mx.py (host code against torch's headers; where there is no torch,
+_mxbind.so, the Python binding of the operators in mx.py and int8.py (host code against torch's headers; where there is no torch,
 whose tensors it takes, it is left out).
 """
 from __future__ import annotations

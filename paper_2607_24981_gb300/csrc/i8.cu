@@ -1,0 +1,220 @@
+// i8.cu -- rows to int8 codes with a float scale each, and back.
+//
+// Of a row x with largest magnitude m: scale s = m / 127 rounded to fp32, at least 2^-126 (0 for a row of zeros, NaN where a value is
+// not finite), codes x / s rounded to the nearest whole number, ties to the even one.
+//
+// The codes are those of the exact quotient.  n = rint(x (1 / s)) is it, or its neighbour where x / s lies within 127 roundings of fp32
+// of a half; x - n s is exact in fp32 (a multiple of the smaller of the units of x and s that is at most about s / 2), so comparing it with
+// s / 2 tells.  That is five operations a value, and a rare branch a unit of values, where a division would take some ten.
+//
+// Bytes are what it moves.  A row is held in registers between its maximum and its codes, by a warp (to 64 16-bit values a lane), 128
+// or 512 threads; past that it is read twice.  Rows on 16-byte boundaries are loaded 16 bytes at a time, others value by value, four
+// consecutive ones a thread.
+#include <algorithm>
+#include <cstdint>
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "divisor.cuh"
+#include "float_act.cuh"
+#include "i8_kernels.h"
+#include "ilw_kernels.h"
+#include "ilwdetr.h"
+
+namespace ilw {
+namespace {
+
+__device__ __forceinline__ float to_f(float v) { return v; }
+__device__ __forceinline__ float to_f(__half v) { return __half2float(v); }
+__device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
+
+// V consecutive values of T: 16 bytes of them, or four.
+template <typename T, int V> struct alignas(V * sizeof(T) == 16 ? 16 : sizeof(T)) Unit {
+    T t[V];
+};
+
+// The largest magnitude of a unit as the bits of a T without a sign (infinities and NaN are above all others).
+template <int V> __device__ __forceinline__ uint32_t magnitude(const Unit<float, V> &x) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) m = max(m, __float_as_uint(x.t[i]) & 0x7fffffffu);
+    return m;
+}
+template <typename T, int V> __device__ __forceinline__ uint32_t magnitude(const Unit<T, V> &x) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < V; i += 2) m = __vmaxu2(m, ((uint32_t)*(const uint16_t *)&x.t[i] | (uint32_t)*(const uint16_t *)&x.t[i + 1] << 16) & 0x7fff7fffu);
+    return max(m & 0xffffu, m >> 16);
+}
+__device__ __forceinline__ float magnitude_value(uint32_t m, float) { return __uint_as_float(m); }
+__device__ __forceinline__ float magnitude_value(uint32_t m, __half) { return __half2float(__ushort_as_half((unsigned short)m)); }
+__device__ __forceinline__ float magnitude_value(uint32_t m, __nv_bfloat16) { return __uint_as_float(m << 16); }
+
+constexpr float kMagic = 12582912.0f;  // 1.5 2^23: x + kMagic holds rint(x) in its low bits
+
+// Codes of a unit, four to a word.
+template <typename T, int V> __device__ __forceinline__ void encode(const Unit<T, V> &x, float s, float inv, uint32_t (&w)[V / 4]) {
+    float t[V], worst = 0.0f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const float v = to_f(x.t[i]);
+        t[i] = fmaf(v, inv, kMagic);
+        worst = fmaxf(worst, fabsf(fmaf(kMagic - t[i], s, v)));
+    }
+    if (worst > 0.4999f * s) {  // near a half
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float v = to_f(x.t[i]), r = fmaf(kMagic - t[i], s, v), half = 0.5f * s;
+            if (fabsf(r) > half || (fabsf(r) == half && (__float_as_uint(t[i]) & 1))) t[i] += copysignf(1.0f, r);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < V / 4; ++i)
+        w[i] = __byte_perm(__byte_perm(__float_as_uint(t[4 * i]), __float_as_uint(t[4 * i + 1]), 0x0040),
+                           __byte_perm(__float_as_uint(t[4 * i + 2]), __float_as_uint(t[4 * i + 3]), 0x0040), 0x5410);
+}
+
+// G threads a row (a warp, or the whole CTA); each holds up to kHeld units of it.
+constexpr int kHeld = 8;
+template <typename T, bool WIDE, int G>
+__global__ void __launch_bounds__(G == 32 ? 256 : G) i8_quantize_kernel(const I8QuantParams p) {
+    constexpr int V = WIDE ? 16 / (int)sizeof(T) : 4;
+    __shared__ uint32_t warp_max[G / 32];
+    grid_wait();
+    const int q = G == 32 ? threadIdx.x & 31 : threadIdx.x;
+    const int64_t r = G == 32 ? blockIdx.x * (int64_t)8 + (threadIdx.x >> 5) : blockIdx.x;
+    if (r >= p.rows) return;  // (whole warps, or no one)
+    int64_t src = r;
+    if (p.gather) {
+        src = p.gather[r];
+        if (src < 0 || src >= p.x_rows) {
+            if (src != -1 && q == 0 && p.status) atomicExch(p.status, kStatusBadIndex);
+            src = -1;
+        }
+    }
+    const T *x = (const T *)p.X + (src < 0 ? 0 : src) * p.ldx;
+    const int32_t K = p.K, units = (K + V - 1) / V;
+    auto load = [&](int32_t u) {
+        Unit<T, V> y;
+        if constexpr (WIDE) {
+            if (u < units && src >= 0) return *(const Unit<T, V> *)(x + (int64_t)u * V);
+#pragma unroll
+            for (int i = 0; i < V; ++i) y.t[i] = T(0.0f);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) y.t[i] = src >= 0 && (int64_t)u * V + i < K ? x[(int64_t)u * V + i] : T(0.0f);
+        }
+        return y;
+    };
+    Unit<T, V> held[kHeld];
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) held[j] = load(q + j * G);
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) m = max(m, magnitude(held[j]));
+    for (int32_t u = q + kHeld * G; u < units; u += G) m = max(m, magnitude(load(u)));
+    m = __reduce_max_sync(0xffffffffu, m);
+    if constexpr (G > 32) {
+        if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = m;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < G / 32; ++i) m = max(m, warp_max[i]);
+    }
+    const float largest = magnitude_value(m, T());
+    const bool fine = largest < __int_as_float(0x7f800000);
+    const float s = largest > 0.0f ? fmaxf(__fdiv_rn(largest, 127.0f), 1.17549435e-38f) : 0.0f, inv = s > 0.0f && fine ? __frcp_rn(s) : 0.0f;
+    if (q == 0) p.scales[r] = fine ? s : __int_as_float(0x7fc00000);
+    int8_t *c = p.codes + r * p.ldc;
+    auto store = [&](int32_t u, const Unit<T, V> &y) {
+        if (u >= units) return;
+        uint32_t w[V / 4];
+        if (fine) {
+            encode(y, s, inv, w);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V / 4; ++i) w[i] = 0;
+        }
+        int8_t *at = c + (int64_t)u * V;
+        if constexpr (V == 8) {
+            *(uint2 *)at = make_uint2(w[0], w[1]);
+        } else {
+            if (WIDE || (int64_t)u * 4 + 4 <= K) *(uint32_t *)at = w[0];
+            else
+                for (int i = 0; u * 4 + i < K; ++i) at[i] = (int8_t)(w[0] >> (8 * i));
+        }
+    };
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) store(q + j * G, held[j]);
+    for (int32_t u = q + kHeld * G; u < units; u += G) store(u, load(u));
+}
+
+// Values: 16 codes a thread where rows of Y are on 16-byte boundaries and K is a multiple of 16, else one.
+template <typename T, int V>
+__global__ void __launch_bounds__(256) i8_dequantize_kernel(const I8DequantParams p, Divisor per, uint32_t r0, uint32_t total) {
+    grid_wait();
+    const uint32_t i = blockIdx.x * 256 + threadIdx.x;
+    if (i >= total) return;
+    const uint32_t row = per.div(i), k = (i - row * per.d) * V;
+    const int64_t r = (int64_t)r0 + row;
+    const float s = p.scales[r];
+    T *y = (T *)p.Y + r * p.ldy + k;
+    if constexpr (V == 1) {
+        *y = to_out<T>((float)p.codes[r * p.ldc + k] * s);
+    } else {
+        const int4 c = *(const int4 *)(p.codes + r * p.ldc + k);
+        const int32_t w[4] = {c.x, c.y, c.z, c.w};
+        struct alignas(16) Pack {
+            T t[V];
+        } o;
+#pragma unroll
+        for (int j = 0; j < V; ++j) o.t[j] = to_out<T>((float)(int8_t)(w[j / 4] >> (8 * (j % 4))) * s);
+        *(Pack *)y = o;
+    }
+}
+
+template <typename T, bool WIDE> cudaError_t quantize_rows(const I8QuantParams &p, cudaStream_t s) {
+    const int64_t units = WIDE ? p.K / (16 / (int)sizeof(T)) : ((int64_t)p.K + 3) / 4;
+    if (units <= 32 * kHeld) return launch_after(i8_quantize_kernel<T, WIDE, 32>, (unsigned)((p.rows + 7) / 8), 256, 0, s, p);
+    if (units <= 128 * kHeld) return launch_after(i8_quantize_kernel<T, WIDE, 128>, (unsigned)p.rows, 128, 0, s, p);
+    return launch_after(i8_quantize_kernel<T, WIDE, 512>, (unsigned)p.rows, 512, 0, s, p);
+}
+template <typename T> cudaError_t quantize(const I8QuantParams &p, cudaStream_t s) {
+    constexpr int V = 16 / sizeof(T);
+    if ((uintptr_t)p.X % 16 == 0 && p.ldx % V == 0 && p.K % V == 0) return quantize_rows<T, true>(p, s);
+    return quantize_rows<T, false>(p, s);
+}
+template <typename T, int V> cudaError_t dequantize_rows(const I8DequantParams &p, cudaStream_t s) {
+    const uint32_t per = p.K / V;
+    const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 30) / per);
+    for (int64_t r0 = 0; r0 < p.rows; r0 += most) {
+        const uint32_t total = (uint32_t)(std::min(most, p.rows - r0) * per);
+        const cudaError_t e = launch_after(i8_dequantize_kernel<T, V>, (total + 255) / 256, 256, 0, s, p, divisor(per), (uint32_t)r0, total);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+template <typename T> cudaError_t dequantize(const I8DequantParams &p, cudaStream_t s) {
+    if ((uintptr_t)p.Y % 16 == 0 && p.ldy * (int64_t)sizeof(T) % 16 == 0 && p.K % 16 == 0) return dequantize_rows<T, 16>(p, s);
+    return dequantize_rows<T, 1>(p, s);
+}
+
+}  // namespace
+
+cudaError_t launch_i8_quantize(const I8QuantParams &q, cudaStream_t s) {
+    if (q.rows == 0) return cudaSuccess;
+    I8QuantParams p = q;
+    p.status = status_word_ptr();
+    if (p.form == ILW_FP32) return quantize<float>(p, s);
+    if (p.form == ILW_FP16) return quantize<__half>(p, s);
+    return quantize<__nv_bfloat16>(p, s);
+}
+
+cudaError_t launch_i8_dequantize(const I8DequantParams &p, cudaStream_t s) {
+    if (p.rows == 0) return cudaSuccess;
+    if (p.form == ILW_FP32) return dequantize<float>(p, s);
+    if (p.form == ILW_FP16) return dequantize<__half>(p, s);
+    return dequantize<__nv_bfloat16>(p, s);
+}
+
+}  // namespace ilw

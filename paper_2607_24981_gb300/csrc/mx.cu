@@ -19,6 +19,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include "divisor.cuh"
 #include "ilw_kernels.h"
 #include "ilwdetr.h"
 #include "mx_kernels.h"
@@ -28,17 +29,6 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kSteps = 4;  // groups of eight values of a thread in flight, on the way back
-
-// n / d for n < 2^31 (round-up reciprocal of Granlund and Montgomery, 1994)
-struct Divisor {
-    uint32_t d, m, s;
-    __device__ __forceinline__ uint32_t div(uint32_t n) const { return (__umulhi(n, m) + n) >> s; }
-};
-Divisor divisor(uint32_t d) {
-    uint32_t s = 0;
-    while (((uint64_t)1 << s) < d) ++s;
-    return {d, (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << s) - d)) / d + 1), s};
-}
 
 __device__ __forceinline__ float to_f(float v) { return v; }
 __device__ __forceinline__ float to_f(__half v) { return __half2float(v); }

@@ -1,6 +1,8 @@
 // mx_abi.cu -- the C-ABI entry points of the microscaled 4-bit and mixture-of-experts operators: argument
 // checks and dispatch.
+#include <algorithm>
 #include <climits>
+#include <cmath>
 #include <cstdarg>
 #include <cstdint>
 #include <cstdio>
@@ -73,6 +75,25 @@ int gemm_problem(const ilw_mx_gemm_t *p, ilw::MxGemmProblem &g) {
     return ILW_OK;
 }
 
+// Checks a routing's arguments and puts them into p.
+int route_problem(const void *logits, int32_t form, int64_t ld, int32_t T, int32_t E, int32_t k, int32_t renormalize, int32_t *expert, float *weight,
+                  int32_t *offsets, int32_t *source, int32_t *slot, void *workspace, size_t workspace_bytes, ilw::MoeRouteParams &p) {
+    if (!form_size(form)) return fail(ILW_ERR_INVALID_ARG, "moe_route: form=%d", form);
+    if (T < 0 || E < 1 || k < 1 || k > E || ld < E) return fail(ILW_ERR_INVALID_ARG, "moe_route: bad sizes T=%d E=%d k=%d", T, E, k);
+    if (E > ilw::kRouteMaxExperts || k > ilw::kRouteMaxTop || (int64_t)T * k > INT32_MAX)
+        return fail(ILW_ERR_UNSUPPORTED, "moe_route: E <= %d, k <= %d, T k < 2^31", ilw::kRouteMaxExperts, ilw::kRouteMaxTop);
+    if (T > 0 && (!logits || !expert || !weight || !source || !slot))
+        return fail(ILW_ERR_INVALID_ARG, "moe_route: NULL tensor");
+    if (!offsets || !aligned(logits, form_size(form)) || !aligned(expert, 4) || !aligned(weight, 4) || !aligned(offsets, 4) ||
+        !aligned(source, 4) || !aligned(slot, 4))
+        return fail(ILW_ERR_INVALID_ARG, "moe_route: offsets NULL or a tensor misaligned");
+    const size_t need = ilw::moe_route_workspace(T, E);
+    if (need && (!workspace || !aligned(workspace, 4) || workspace_bytes < need))
+        return fail(ILW_ERR_INVALID_ARG, "moe_route: workspace NULL, misaligned or smaller than %zu bytes", need);
+    p = {logits, form, ld, T, E, k, renormalize, expert, weight, offsets, source, slot, (int32_t *)workspace, {}};
+    return ILW_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -131,21 +152,33 @@ size_t ilwdetr_moe_route_workspace_bytes(int32_t T, int32_t E) {
 int ilwdetr_moe_route(const void *logits, int32_t form, int64_t ld, int32_t T, int32_t E, int32_t k, int32_t renormalize,
                       int32_t *expert, float *weight, int32_t *offsets, int32_t *source, int32_t *slot, void *workspace,
                       size_t workspace_bytes, ilw_stream_t stream) {
-    if (!form_size(form)) return fail(ILW_ERR_INVALID_ARG, "moe_route: form=%d", form);
-    if (T < 0 || E < 1 || k < 1 || k > E || ld < E) return fail(ILW_ERR_INVALID_ARG, "moe_route: bad sizes T=%d E=%d k=%d", T, E, k);
-    if (E > ilw::kRouteMaxExperts || k > ilw::kRouteMaxTop || (int64_t)T * k > INT32_MAX)
-        return fail(ILW_ERR_UNSUPPORTED, "moe_route: E <= %d, k <= %d, T k < 2^31", ilw::kRouteMaxExperts, ilw::kRouteMaxTop);
-    if (T > 0 && (!logits || !expert || !weight || !source || !slot))
-        return fail(ILW_ERR_INVALID_ARG, "moe_route: NULL tensor");
-    if (!offsets || !aligned(logits, form_size(form)) || !aligned(expert, 4) || !aligned(weight, 4) || !aligned(offsets, 4) ||
-        !aligned(source, 4) || !aligned(slot, 4))
-        return fail(ILW_ERR_INVALID_ARG, "moe_route: offsets NULL or a tensor misaligned");
-    const size_t need = ilw::moe_route_workspace(T, E);
-    if (need && (!workspace || !aligned(workspace, 4) || workspace_bytes < need))
-        return fail(ILW_ERR_INVALID_ARG, "moe_route: workspace NULL, misaligned or smaller than %zu bytes", need);
+    ilw::MoeRouteParams p;
+    ILW_TRY(route_problem(logits, form, ld, T, E, k, renormalize, expert, weight, offsets, source, slot, workspace, workspace_bytes, p));
     if (ilw::validate_only()) return ILW_OK;
-    const ilw::MoeRouteParams p{logits, form, ld, T, E, k, renormalize, expert, weight, offsets, source, slot, (int32_t *)workspace};
     return done(ilw::launch_moe_route(p, (cudaStream_t)stream), "moe_route");
+}
+
+int ilwdetr_moe_route_scored(const void *logits, int32_t form, int64_t ld, int32_t T, int32_t E, int32_t k, int32_t renormalize,
+                             const ilw_moe_scores_t *scores, int32_t *expert, float *weight, int32_t *offsets, int32_t *source,
+                             int32_t *slot, void *workspace, size_t workspace_bytes, ilw_stream_t stream) {
+    ilw::MoeRouteParams p;
+    ILW_TRY(route_problem(logits, form, ld, T, E, k, renormalize, expert, weight, offsets, source, slot, workspace, workspace_bytes, p));
+    if (!scores || scores->struct_size != sizeof(ilw_moe_scores_t)) return fail(ILW_ERR_INVALID_ARG, "moe_route: scores NULL or struct_size");
+    const ilw_moe_scores_t &q = *scores;
+    if (q.score != ILW_SCORE_SOFTMAX && q.score != ILW_SCORE_SIGMOID) return fail(ILW_ERR_INVALID_ARG, "moe_route: score=%d", q.score);
+    if (q.groups < 1 || E % q.groups || q.top_groups < 1 || q.top_groups > q.groups || (q.group_best != 1 && q.group_best != 2))
+        return fail(ILW_ERR_INVALID_ARG, "moe_route: groups=%d of E=%d, top_groups=%d, group_best=%d", q.groups, E, q.top_groups, q.group_best);
+    if (q.groups > ILW_MOE_MAX_GROUPS) return fail(ILW_ERR_UNSUPPORTED, "moe_route: groups <= %d", ILW_MOE_MAX_GROUPS);
+    if (k > E / q.groups * q.top_groups)
+        return fail(ILW_ERR_INVALID_ARG, "moe_route: k=%d of %d experts in %d groups", k, E / q.groups * q.top_groups, q.top_groups);
+    if (!(q.scale > -INFINITY && q.scale < INFINITY)) return fail(ILW_ERR_INVALID_ARG, "moe_route: scale is not finite");
+    if (!aligned(q.bias, 4)) return fail(ILW_ERR_INVALID_ARG, "moe_route: bias misaligned");
+    if (ilw::validate_only()) return ILW_OK;
+    p.scores.score = q.score, p.scores.bias = q.bias, p.scores.groups = q.groups;
+    // (where every group stays they are none)
+    if (q.top_groups == q.groups) p.scores.groups = 1;
+    p.scores.top_groups = std::min(q.top_groups, p.scores.groups), p.scores.group_best = q.group_best, p.scores.scale = q.scale;
+    return done(ilw::launch_moe_route_scored(p, (cudaStream_t)stream), "moe_route");
 }
 
 int ilwdetr_moe_combine(const void *Y, int32_t form, int64_t ldy, int64_t rows, const int32_t *slot, const float *weight,

@@ -1,4 +1,4 @@
-// mx_bind.cpp -- the Python side of the microscaled 4-bit and mixture-of-experts entry points (mx.py) as a CPython extension.
+// mx_bind.cpp -- the Python side of the microscaled 4-bit, int8 and mixture-of-experts entry points (mx.py, int8.py) as a CPython extension.
 //
 // It does what the rest of the binding does in Python: reads tensors' addresses, sizes and strides, makes room for
 // results, and calls the C-ABI on the current stream; nothing is computed here.  These calls are a few microseconds on
@@ -28,6 +28,10 @@ struct Library {
     decltype(&ilwdetr_moe_route_workspace_bytes) route_bytes;
     decltype(&ilwdetr_moe_route) route;
     decltype(&ilwdetr_moe_combine) combine;
+    decltype(&ilwdetr_moe_route_scored) route_scored;
+    decltype(&ilwdetr_i8_quantize) i8_quantize;
+    decltype(&ilwdetr_i8_dequantize) i8_dequantize;
+    decltype(&ilwdetr_i8_gemm) i8_gemm;
 } lib = {};
 PyObject *g_error = nullptr;
 
@@ -136,6 +140,35 @@ Mx mx(PyObject *o, int dims, const at::Tensor *first, const char *what) {
     return m;
 }
 
+// An int8 tensor: the tuple (codes, scales).
+struct I8 {
+    int64_t lead, rows, k, ldc, between;  // (lead: 1 without a leading dimension)
+    const int8_t *codes;
+    const float *scales;
+    const at::Tensor *t;                  // codes
+};
+I8 i8(PyObject *o, int dims, const at::Tensor *first, const char *what) {
+    if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 2) fail("%s: an I8Tensor is wanted, not %s", what, Py_TYPE(o)->tp_name);
+    const at::Tensor &c = tensor(PyTuple_GET_ITEM(o, 0), what), &s = tensor(PyTuple_GET_ITEM(o, 1), what);
+    bool fits = c.scalar_type() == at::kChar && s.scalar_type() == at::kFloat && c.dim() == dims && s.dim() == dims - 1;
+    for (int i = 0; fits && i + 1 < dims; ++i) fits = c.size(i) == s.size(i);
+    if (!fits) fail("%s: an int8 tensor has int8 codes [..., rows, k] of %d dimensions and float32 scales [..., rows]", what, dims);
+    I8 m;
+    m.k = c.size(dims - 1);
+    if (m.k < 1 || m.k > INT32_MAX) fail("%s: an int8 tensor of k=%lld", what, (long long)m.k);
+    if (!c.is_cuda() || !s.is_cuda() || (c.stride(dims - 1) != 1 && m.k > 1 && c.numel()) || !s.is_contiguous())
+        fail("%s: codes or scales are not on the GPU, or their rows are not contiguous", what);
+    same_gpu(s, c, what);
+    if (first) same_gpu(c, *first, what);
+    m.lead = dims == 3 ? c.size(0) : 1;
+    m.rows = c.size(dims - 2);
+    m.ldc = m.rows <= 1 ? (m.k + 15) / 16 * 16 : c.stride(dims - 2);  // (no or a single row may carry any stride)
+    m.between = dims == 3 ? c.stride(0) : 0;
+    m.codes = (const int8_t *)c.data_ptr(), m.scales = (const float *)s.data_ptr();
+    m.t = &c;
+    return m;
+}
+
 // A call launches on its tensors' GPU, on that GPU's current stream.
 struct Launch {
     c10::cuda::CUDAGuard device;
@@ -150,6 +183,13 @@ at::Tensor part_of(const at::Tensor &whole, int64_t bytes, at::IntArrayRef size,
     at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::TensorImpl::VIEW, c10::Storage(whole.storage()), whole.key_set(), meta);
     t.unsafeGetTensorImpl()->set_storage_offset(bytes / (int64_t)meta.itemsize());
     t.unsafeGetTensorImpl()->set_sizes_contiguous(size);
+    return t;
+}
+// The same with rows `ld` elements apart.
+at::Tensor rows_of(const at::Tensor &whole, int64_t bytes, int64_t rows, int64_t cols, int64_t ld, at::ScalarType type) {
+    const at::Tensor t = part_of(whole, bytes, {rows, cols}, type);
+    const int64_t size[] = {rows, cols}, stride[] = {ld, 1};
+    t.unsafeGetTensorImpl()->set_sizes_and_strides(at::IntArrayRef(size, 2), at::IntArrayRef(stride, 2));
     return t;
 }
 PyObject *wrap(const at::Tensor &t) { return THPVariable_Wrap(t); }
@@ -242,8 +282,8 @@ PyObject *gemm(PyObject *const *a) {
     return wrap(out);
 }
 
-// route(logits, k, renormalize) -> (expert, weight, offsets, source, slot)
-PyObject *route(PyObject *const *a) {
+// route(logits, k, renormalize[, score, bias, groups, top_groups, group_best, scale]) -> (expert, weight, offsets, source, slot)
+PyObject *route_by(PyObject *const *a, bool scored) {
     const char *what = "moe_route";
     const at::Tensor &x = tensor(a[0], what);
     const Matrix m = matrix(x, x, what);
@@ -252,6 +292,20 @@ PyObject *route(PyObject *const *a) {
     if (renormalize < 0) throw Failed();
     if (m.rows > INT32_MAX || m.cols > INT32_MAX || k > INT32_MAX || k < INT32_MIN) fail("%s: more than 2^31 tokens or experts", what);
     const int32_t T = (int32_t)m.rows, E = (int32_t)m.cols;
+    ilw_moe_scores_t q = {};
+    if (scored) {
+        int32_t *const to[] = {&q.score, &q.groups, &q.top_groups, &q.group_best};
+        const int from[] = {3, 5, 6, 7};
+        for (int i = 0; i < 4; ++i) {
+            const int64_t v = whole(a[from[i]]);
+            *to[i] = v < 0 || v > INT32_MAX ? -1 : (int32_t)v;  // (any of them: refused below)
+        }
+        q.struct_size = sizeof(q);
+        const double scale = PyFloat_AsDouble(a[8]);
+        if (scale == -1.0 && PyErr_Occurred()) throw Failed();
+        q.scale = (float)scale;
+        if (given(a[4])) q.bias = weights(tensor(a[4], what), x, 1, E, what, "bias");
+    }
     const size_t bytes = lib.route_bytes(T, E);
     const int64_t n = T * kk, words = 4 * n + E + 1;  // expert, weight, source, slot, offsets, then the workspace
     const at::Tensor all = room({4 * words + (int64_t)bytes}, at::kByte, x);
@@ -259,11 +313,88 @@ PyObject *route(PyObject *const *a) {
                      source = part_of(all, 8 * n, {n}, at::kInt), slot = part_of(all, 12 * n, {T, kk}, at::kInt),
                      offsets = part_of(all, 16 * n, {(int64_t)E + 1}, at::kInt);
     const Launch on(x);
-    check(lib.route(m.data, m.form, m.ld, T, E, (int32_t)k, renormalize, (int32_t *)expert.data_ptr(), (float *)weight.data_ptr(),
-                    (int32_t *)offsets.data_ptr(), (int32_t *)source.data_ptr(), (int32_t *)slot.data_ptr(), bytes ? (char *)all.data_ptr() + 4 * words : nullptr, bytes,
-                    on.stream),
+    void *const ws = bytes ? (char *)all.data_ptr() + 4 * words : nullptr;
+    int32_t *const ep = (int32_t *)expert.data_ptr(), *const op = (int32_t *)offsets.data_ptr(), *const sp = (int32_t *)source.data_ptr(),
+            *const lp = (int32_t *)slot.data_ptr();
+    float *const wp = (float *)weight.data_ptr();
+    check(scored ? lib.route_scored(m.data, m.form, m.ld, T, E, (int32_t)k, renormalize, &q, ep, wp, op, sp, lp, ws, bytes, on.stream)
+                 : lib.route(m.data, m.form, m.ld, T, E, (int32_t)k, renormalize, ep, wp, op, sp, lp, ws, bytes, on.stream),
           what);
     return Py_BuildValue("(NNNNN)", wrap(expert), wrap(weight), wrap(offsets), wrap(source), wrap(slot));
+}
+
+PyObject *route(PyObject *const *a) { return route_by(a, false); }
+PyObject *route_scored(PyObject *const *a) { return route_by(a, true); }
+
+// i8_quantize(X, gather, out) -> (codes, scales)
+PyObject *i8_quantize(PyObject *const *a) {
+    const char *what = "i8_quantize";
+    const at::Tensor &X = tensor(a[0], what);
+    const Matrix x = matrix(X, X, what);
+    int64_t rows = x.rows;
+    const int32_t *at = nullptr;
+    if (given(a[1])) {
+        const at::Tensor &g = tensor(a[1], what);
+        at = indices(g, X, what);
+        rows = g.numel();
+    }
+    const int32_t K = (int32_t)std::min<int64_t>(x.cols, INT32_MAX);
+    if (given(a[2])) {
+        const I8 m = i8(a[2], 2, &X, what);
+        if (m.k != x.cols || m.rows != rows)
+            fail("%s: out holds %lld rows of %lld, not %lld of %lld", what, (long long)m.rows, (long long)m.k, (long long)rows, (long long)x.cols);
+        const Launch on(X);
+        check(lib.i8_quantize(x.data, x.form, x.ld, x.rows, at, rows, K, (int8_t *)m.codes, m.ldc, (float *)m.scales, on.stream), what);
+        return Py_NewRef(a[2]);
+    }
+    const int64_t ld = (x.cols + 15) / 16 * 16;
+    const at::Tensor both = room({rows * (ld + 4)}, at::kByte, X), codes = rows_of(both, 0, rows, x.cols, ld, at::kChar),
+                     scales = part_of(both, rows * ld, {rows}, at::kFloat);
+    const Launch on(X);
+    check(lib.i8_quantize(x.data, x.form, x.ld, x.rows, at, rows, K, (int8_t *)codes.data_ptr(), ld, (float *)scales.data_ptr(), on.stream), what);
+    return Py_BuildValue("(NN)", wrap(codes), wrap(scales));
+}
+
+// i8_dequantize(m, dtype, out)
+PyObject *i8_dequantize(PyObject *const *a) {
+    const char *what = "i8_dequantize";
+    const I8 m = i8(a[0], 2, nullptr, what);
+    const at::Tensor out = given(a[2]) ? tensor(a[2], what) : room({m.rows, m.k}, dtype_or(a[1], at::kFloat, what), *m.t);
+    const Matrix y = matrix(out, *m.t, what);
+    if (y.rows != m.rows || y.cols != m.k)
+        fail("%s: out is (%lld, %lld), not (%lld, %lld)", what, (long long)y.rows, (long long)y.cols, (long long)m.rows, (long long)m.k);
+    const Launch on(*m.t);
+    check(lib.i8_dequantize(m.codes, m.ldc, m.scales, m.rows, (int32_t)m.k, y.data, y.form, y.ld, on.stream), what);
+    return wrap(out);
+}
+
+// i8_gemm(A, W, offsets, bias, act, dtype, out)
+PyObject *i8_gemm(PyObject *const *a) {
+    const bool grouped = given(a[2]);
+    const char *what = grouped ? "i8_grouped_linear" : "i8_linear";
+    const I8 A = i8(a[0], 2, nullptr, what), W = i8(a[1], grouped ? 3 : 2, A.t, what);
+    const int64_t act = whole(a[4]), N = W.rows, wide = act == ILW_ACT_SILU_GATE ? N / 2 : N;
+    if (A.k != W.k) fail("%s: A has k=%lld, W k=%lld", what, (long long)A.k, (long long)W.k);
+    if (N > INT32_MAX || W.lead > INT32_MAX) fail("%s: rows or experts past 2^31", what);
+    ilw_i8_gemm_t p = {};
+    p.struct_size = sizeof(p);
+    p.a_codes = A.codes, p.a_ldc = A.ldc, p.a_scales = A.scales;
+    p.w_codes = W.codes, p.w_ldc = W.ldc, p.w_codes_stride = W.between, p.w_scales = W.scales;
+    if (grouped) {
+        const at::Tensor &off = tensor(a[2], what);
+        p.offsets = indices(off, *A.t, what);
+        if (off.numel() != W.lead + 1) fail("%s: %lld experts need %lld offsets, not %lld", what, (long long)W.lead, (long long)W.lead + 1, (long long)off.numel());
+    }
+    if (given(a[3])) p.bias = weights(tensor(a[3], what), *A.t, W.lead, N, what, "bias");
+    const at::Tensor out = given(a[6]) ? tensor(a[6], what) : room({A.rows, wide}, dtype_or(a[5], at::kBFloat16, what), *A.t);
+    const Matrix y = matrix(out, *A.t, what);
+    if (y.rows != A.rows || y.cols != wide)
+        fail("%s: out is (%lld, %lld), not (%lld, %lld)", what, (long long)y.rows, (long long)y.cols, (long long)A.rows, (long long)wide);
+    p.M = A.rows, p.N = (int32_t)N, p.K = (int32_t)A.k, p.experts = (int32_t)W.lead, p.act = (int32_t)act, p.y_form = y.form;
+    p.Y = y.data, p.ldy = y.ld;
+    const Launch on(*A.t);
+    check(lib.i8_gemm(&p, on.stream), what);
+    return wrap(out);
 }
 
 // combine(Y, slot, weight, residual, out)
@@ -313,8 +444,9 @@ PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t n) {
     return nullptr;
 }
 #define ILW_METHOD(f, n) {#f, (PyCFunction)(void (*)(void))call<f, n>, METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {ILW_METHOD(bind, 8), ILW_METHOD(quantize, 3), ILW_METHOD(dequantize, 3), ILW_METHOD(gemm, 7), ILW_METHOD(route, 3),
-                         ILW_METHOD(combine, 5), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {ILW_METHOD(bind, 12), ILW_METHOD(quantize, 3), ILW_METHOD(dequantize, 3), ILW_METHOD(gemm, 7), ILW_METHOD(route, 3),
+                         ILW_METHOD(combine, 5), ILW_METHOD(route_scored, 9), ILW_METHOD(i8_quantize, 3), ILW_METHOD(i8_dequantize, 3),
+                         ILW_METHOD(i8_gemm, 7), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_mxbind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

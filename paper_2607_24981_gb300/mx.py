@@ -17,6 +17,7 @@ __all__ = ["MxTensor", "Routing", "mx_empty", "mx_quantize", "mx_dequantize", "m
            "gate_rows", "MxExperts"]
 
 ACTS = {"none": 0, "gelu": 1, "silu_gate": 2}
+SCORES = {"softmax": 0, "sigmoid": 1}
 BIND_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_mxbind.so")
 
 # ilw_mx_gemm_t, in its natural alignment
@@ -66,7 +67,7 @@ def _bind():
             raise IlwError(f"{BIND_PATH} does not load, build it again with __graft_entry__.build(): {e}") from e
 
         names = ("ilwdetr_last_error", "ilwdetr_mx_quantize", "ilwdetr_mx_dequantize", "ilwdetr_mx_gemm", "ilwdetr_moe_route_workspace_bytes",
-                 "ilwdetr_moe_route", "ilwdetr_moe_combine")
+                 "ilwdetr_moe_route", "ilwdetr_moe_combine", "ilwdetr_moe_route_scored", "ilwdetr_i8_quantize", "ilwdetr_i8_dequantize", "ilwdetr_i8_gemm")
         _mxbind.bind(IlwError, *(ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in names))
         _bound = _mxbind
     return _bound
@@ -116,9 +117,20 @@ def mx_grouped_linear(A: MxTensor, W: MxTensor, offsets, bias=None, act="none", 
     return (_bound or _bind()).gemm(A, W, offsets, bias, _act(act), out_dtype, out)
 
 
-def moe_route(logits, k: int, renormalize=True) -> Routing:
-    """ilwdetr_moe_route: the k experts of each row of logits [T, E], their weights, and the rows' order by expert."""
-    return Routing(*(_bound or _bind()).route(logits, k, renormalize))
+def moe_route(logits, k: int, renormalize=True, score="softmax", bias=None, groups=1, top_groups=None, group_best=2, scale=1.0) -> Routing:
+    """ilwdetr_moe_route: the k experts of each row of logits [T, E], their weights, and the rows' order by expert.
+
+    ilwdetr_moe_route_scored, where anything after ``renormalize`` is given: experts are taken by their ``score`` ("softmax" or
+    "sigmoid") plus ``bias`` (float32 [E], for balance: it chooses but does not weigh), among the ``top_groups`` (all) of ``groups``
+    groups of consecutive experts that rank best by the sum of their ``group_best`` (1 or 2) largest; the weights are the scores, over
+    their sum with ``renormalize``, times ``scale``."""
+    bound = _bound or _bind()
+    if score == "softmax" and bias is None and groups == 1 and scale == 1.0 and top_groups in (None, 1) and group_best in (1, 2):
+        return Routing(*bound.route(logits, k, renormalize))
+    code = SCORES.get(score)
+    if code is None:
+        raise IlwError(f"score {score!r} is none of {', '.join(SCORES)}")
+    return Routing(*bound.route_scored(logits, k, renormalize, code, bias, groups, groups if top_groups is None else top_groups, group_best, scale))
 
 
 def moe_combine(Y, slot, weight, residual=None, out=None):
@@ -144,24 +156,28 @@ class MxExperts:
     product with its activation, quantise, second product, weighted join onto the residual.
 
     ``w1`` [E, F1, d] and ``w2`` [E, d, F] are float CUDA tensors, quantised here once; with ``act`` "silu_gate" F1 = 2 F and
-    the rows of w1 alternate (gate_rows), else F1 = F.  Biases are float32 [E, F1] (gated: gate_rows with dim=1) and [E, d]."""
+    the rows of w1 alternate (gate_rows), else F1 = F.  Biases are float32 [E, F1] (gated: gate_rows with dim=1) and [E, d].
+    ``routing`` goes to moe_route: score, bias, groups and so on."""
 
-    def __init__(self, w1, w2, top: int, act="silu_gate", b1=None, b2=None, renormalize=True):
-        self.top, self.act, self.b1, self.b2, self.renormalize = top, act, b1, b2, renormalize
-
-        def pack(w):
-            E, N, K = w.shape
-            q = mx_quantize(w.reshape(E * N, K))
-            return MxTensor(q.codes.view(E, N, -1), q.scales.view(E, N, -1), K)
-
-        self.w1, self.w2 = pack(w1), pack(w2)
+    def __init__(self, w1, w2, top: int, act="silu_gate", b1=None, b2=None, renormalize=True, **routing):
+        self.top, self.act, self.b1, self.b2, self.renormalize, self.routing = top, act, b1, b2, renormalize, routing
+        self.w1, self.w2 = self.pack(w1), self.pack(w2)
         if w1.shape[0] != w2.shape[0] or w2.shape[2] * (2 if act == "silu_gate" else 1) != w1.shape[1] or w1.shape[2] != w2.shape[1]:
-            raise IlwError(f"MxExperts: w1 {tuple(w1.shape)} and w2 {tuple(w2.shape)} do not follow one another")
+            raise IlwError(f"{type(self).__name__}: w1 {tuple(w1.shape)} and w2 {tuple(w2.shape)} do not follow one another")
+
+    quantize = staticmethod(mx_quantize)
+    grouped_linear = staticmethod(mx_grouped_linear)
+
+    @staticmethod
+    def pack(w):
+        E, N, K = w.shape
+        q = mx_quantize(w.reshape(E * N, K))
+        return MxTensor(q.codes.view(E, N, -1), q.scales.view(E, N, -1), K)
 
     def forward(self, x, logits, residual=None):
         """x [T, d] and its router logits [T, E] -> [T, d] in x's type (plus ``residual``)."""
-        r = moe_route(logits, self.top, self.renormalize)
-        a = mx_quantize(x, gather=r.source)
-        h = mx_grouped_linear(a, self.w1, r.offsets, bias=self.b1, act=self.act, out_dtype=x.dtype)
-        y = mx_grouped_linear(mx_quantize(h), self.w2, r.offsets, bias=self.b2, out_dtype=x.dtype)
+        r = moe_route(logits, self.top, self.renormalize, **self.routing)
+        a = self.quantize(x, gather=r.source)
+        h = self.grouped_linear(a, self.w1, r.offsets, bias=self.b1, act=self.act, out_dtype=x.dtype)
+        y = self.grouped_linear(self.quantize(h), self.w2, r.offsets, bias=self.b2, out_dtype=x.dtype)
         return moe_combine(y, r.slot, r.weight, residual=residual)

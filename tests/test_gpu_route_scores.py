@@ -1,0 +1,199 @@
+"""Routing by scores, a bias and groups on the GPU against a plain restatement in 64 bits.
+
+Experts, places and offsets are exact, ties included.  Weights: exponentials of at most 2 ulp whose arguments (differences of
+logits) are off by half an ulp of at most 2^6 here, so 2^6 2^-24 relative; sums of at most E terms; and a few roundings."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module")
+def ilw():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    import paper_2607_24981_gb300 as m
+    from paper_2607_24981_gb300 import build
+
+    build.build()
+    m.lib()
+    return m
+
+
+def ref_route(x, k, renormalize, score="softmax", bias=None, groups=1, top_groups=None, group_best=2, scale=1.0):
+    """float64 x [T, E] (numpy) -> expert, weight, offsets, source, slot."""
+    T, E = x.shape
+    # The scores of x and -x add up to 1 for every x: which of two such groups ranks better is a matter of the last bit of 64, so
+    # that bit is taken where the operator says it takes it, from 1 / (1 + exp(-x)) on the device.
+    sigmoids = (1 / (1 + torch.exp(-torch.from_numpy(x).cuda()))).cpu().numpy()
+    x = np.where(np.isnan(x), -np.inf, x)
+    expert, weight, size = np.full((T, k), -1), np.zeros((T, k)), E // groups
+    for t in range(T):
+        v = x[t]
+        on = v > -np.inf
+        if not on.any():
+            continue
+        with np.errstate(over="ignore", invalid="ignore"):
+            p = np.where(on, np.where(v == v.max(), 1.0, np.exp(v - v.max())), 0)
+            s = np.where(on, sigmoids[t], 0) if score == "sigmoid" else p / p.sum()
+        c = s if bias is None else s + bias
+        c = np.where(on & ~np.isnan(c), c, -np.inf)
+        order = v if bias is None else c
+        if groups > 1 and (top_groups or groups) < groups:
+            rank = np.full(groups, -np.inf)
+            for g in range(groups):
+                of = (order if group_best == 1 else c)[g * size: (g + 1) * size]
+                best = np.sort(of[of > -np.inf])[::-1][:group_best]
+                if len(best):
+                    rank[g] = best.sum()
+            take = [g for g in np.argsort(-rank, kind="stable")[:top_groups] if rank[g] > -np.inf]
+            order = np.where(np.isin(np.arange(E) // size, take), order, -np.inf)
+        best = np.argsort(-order, kind="stable")[:k]
+        best = best[order[best] > -np.inf]
+        expert[t, : len(best)] = best
+        if not len(best):
+            continue
+        if renormalize and score == "sigmoid":  # scores too small for 64 bits keep their ratios
+            z = -np.logaddexp(0, -v[best])
+            w = np.exp(z - z.max())
+        else:
+            w = s[best]
+        weight[t, : len(best)] = scale * w / (w.sum() if renormalize else 1)
+    entries = sorted((expert[t, j], t, j) for t in range(T) for j in range(k) if expert[t, j] >= 0)
+    offsets = np.searchsorted([e for e, _, _ in entries], np.arange(E + 1))
+    source, slot = np.full(T * k, -1), np.full((T, k), -1)
+    for s, (_, t, j) in enumerate(entries):
+        source[s], slot[t, j] = t, s
+    return expert, weight, offsets, source, slot
+
+
+def check(ilw, x, k, renormalize, bias=None, **how):
+    """moe_route of x (a GPU tensor) against ref_route."""
+    r = ilw.moe_route(x, k, renormalize, bias=bias, **how)
+    expert, weight, offsets, source, slot = ref_route(x.double().cpu().numpy(), k, renormalize, bias=None if bias is None else bias.double().cpu().numpy(), **how)
+    got = r.expert.cpu().numpy()
+    assert np.array_equal(got, expert), f"{(got != expert).any(1).sum()} of {len(got)} tokens went elsewhere"
+    for a, b in ((r.offsets, offsets), (r.source, source), (r.slot, slot)):
+        assert np.array_equal(a.cpu().numpy(), b)
+    err = np.abs(r.weight.double().cpu().numpy() - weight)
+    assert (err <= (x.shape[1] + 64 + 16) * 2.0**-23 * np.abs(weight) + 1e-44).all(), (err / (np.abs(weight) + 1e-300)).max()
+    return r
+
+
+SHAPES = [(1, 1, 1, 1, 1), (1, 8, 2, 2, 1), (7, 33, 4, 3, 2), (33, 64, 8, 8, 4), (300, 130, 6, 10, 3), (17, 256, 8, 8, 4), (700, 512, 16, 32, 5), (3000, 16, 1, 4, 1), (9000, 6, 2, 3, 2),
+          (260, 160, 6, 8, 3), (1500, 63, 6, 9, 3), (400, 128, 8, 1, 1), (257, 96, 4, 32, 16)]
+
+
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("T,E,k,groups,top_groups", SHAPES)
+def test_route_by_scores_matches_64_bits(ilw, T, E, k, groups, top_groups, dtype, score):
+    """Many equal logits (a coarse grid), masked experts, whole groups and rows masked, NaN; with and without a bias."""
+    rng = np.random.default_rng(T + E + k)
+    x = np.round(rng.standard_normal((T, E)) * 4) / 4
+    x[rng.random((T, E)) < 0.1] = -np.inf
+    x[rng.random((T, E)) < 0.02] = np.nan
+    x[rng.random(T) < 0.1] = -np.inf
+    if groups > 1:
+        x.reshape(T, groups, -1)[rng.random((T, groups)) < 0.2] = -np.inf
+    wide = torch.from_numpy(np.pad(x, ((0, 0), (1, 2)))).to(dtype).cuda()
+    x = wide[:, 1: 1 + E]
+    bias = torch.from_numpy(0.1 * rng.standard_normal(E)).float().cuda()
+    for b in (None, bias, torch.zeros_like(bias), torch.round(bias * 20) / 20):
+        for best in (1, 2):
+            check(ilw, x if best == 1 else x.contiguous(), k, b is None, bias=b, score=score, groups=groups, top_groups=top_groups, group_best=best, scale=2.5 if best == 1 else 1.0)
+    ilw.device_status()
+
+
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("groups,top_groups,group_best", [(1, 1, 2), (8, 4, 2), (8, 3, 1)])
+@pytest.mark.parametrize("T", [200, 4000])
+def test_scores_that_32_bits_do_not_separate(ilw, T, groups, top_groups, group_best, score):
+    """Biases that undo the scores' differences but for a few units of 2^-26 or none, so that fp32 scores tie or exchange their order."""
+    rng = np.random.default_rng(T + groups)
+    E = 64
+    x = torch.from_numpy(rng.standard_normal(E)).float()
+    s = torch.sigmoid(x.double()) if score == "sigmoid" else torch.softmax(x.double(), 0)
+    bias = (0.75 - s).float().cuda()  # c = 0.75 but for the rounding of the bias, which differs from expert to expert
+    rows = x.expand(T, E).clone()
+    away = torch.from_numpy(rng.random((T, E)) < 0.3)
+    rows = torch.where(away, float("-inf") if score == "sigmoid" else rows, rows).cuda()
+    check(ilw, rows, 8, False, bias=bias, score=score, groups=groups, top_groups=top_groups, group_best=group_best)
+
+
+def test_biases_that_pin_or_ban_experts(ilw):
+    inf, nan = float("inf"), float("nan")
+    bias = torch.tensor([0.0, 1e6, -1e6, -inf, nan, inf, 3e38, 0.0], device="cuda")
+    x = torch.randn((50, 8), generator=torch.Generator("cuda").manual_seed(1), device="cuda")
+    for score in ("sigmoid", "softmax"):
+        r = check(ilw, x, 6, True, bias=bias, score=score)
+        assert r.expert[:, :3].tolist() == [[5, 6, 1]] * 50 and r.expert[:, 5].tolist() == [2] * 50
+        check(ilw, x, 3, True, bias=bias, score=score, groups=4, top_groups=2, group_best=2)
+        check(ilw, x, 3, True, bias=bias, score=score, groups=4, top_groups=2, group_best=1)
+
+
+def test_logits_of_every_size(ilw):
+    """Infinities, the largest numbers, scores that are 1 or 0 in 64 bits, and weights of scores below fp32's range."""
+    big, inf = float(np.float32(3.4028234e38)), float("inf")
+    x = torch.tensor([[big, -big, 0.0, -0.0], [-big, -big, -big, -inf], [0.0, -0.0, -0.0, 0.0], [float("nan")] * 4, [inf, 1.0, 2.0, 3.0], [inf, inf, 0.0, -inf],
+                      [-200.0, -201.0, -202.0, -300.0], [50.0, 60.0, 70.0, 55.0], [-90.0, -95.0, 0.0, -1.0], [-101.0, -100.0, -99.0, -98.0]]).cuda()
+    zero = torch.zeros(4, device="cuda")
+    for score in ("sigmoid", "softmax"):
+        for bias in (None, zero, zero + 0.1):
+            for renormalize in (True, False):
+                check(ilw, x, 3, renormalize, score=score, bias=bias, scale=2.0)
+                for best in (1, 2):
+                    check(ilw, x, 2, renormalize, score=score, bias=bias, groups=2, top_groups=1, group_best=best)
+    w = ilw.moe_route(x, 3, score="sigmoid").weight
+    assert torch.allclose(w[6].cpu(), torch.softmax(torch.tensor([-200.0, -201.0, -202.0]), 0), rtol=1e-5)
+    empty = ilw.moe_route(torch.empty((0, 6), device="cuda"), 2, score="sigmoid", groups=3, top_groups=2)
+    assert empty.offsets.tolist() == [0] * 7 and empty.expert.shape == (0, 2)
+
+
+@pytest.mark.parametrize("T,E,k,how", [(4000, 256, 8, dict(score="sigmoid")), (20000, 128, 4, dict(score="sigmoid", groups=8, top_groups=4)), (200, 64, 16, dict(score="softmax", scale=2.5)),
+                                       (5000, 64, 6, dict(score="softmax", scale=2.5))])
+@pytest.mark.parametrize("renormalize", [True, False])
+def test_weights_as_exact_as_plain_operations(ilw, T, E, k, how, renormalize):
+    """In norm, over many weights, no further from 64 bits than plain fp32 operations are (a tenth more for chance)."""
+    x = 2 * torch.randn((T, E), device="cuda", generator=torch.Generator("cuda").manual_seed(T + E))
+    r = ilw.moe_route(x, k, renormalize, **how)
+
+    def weights(x):
+        s = 1 / (1 + torch.exp(-x)) if how["score"] == "sigmoid" else torch.exp(x - x.amax(1, keepdim=True))
+        s = s if how["score"] == "sigmoid" else s / s.sum(1, keepdim=True)
+        top = torch.gather(s, 1, r.expert.long())
+        return how.get("scale", 1.0) * (top / top.sum(1, keepdim=True) if renormalize else top)
+
+    want = weights(x.double())
+    assert (r.weight.double() - want).norm() <= 1.1 * (weights(x).double() - want).norm()
+
+
+def test_defaults_are_those_of_plain_routing(ilw):
+    """Without a bias, groups or a scale the scores' path gives what the plain one does."""
+    x = torch.randn((3000, 64), generator=torch.Generator("cuda").manual_seed(1), device="cuda")
+    plain = ilw.moe_route(x, 4)
+    same = ilw.moe_route(x, 4, groups=4, top_groups=4)
+    for a, b in zip((plain.expert, plain.offsets, plain.source, plain.slot), (same.expert, same.offsets, same.source, same.slot)):
+        assert torch.equal(a, b)
+    assert torch.allclose(plain.weight, same.weight, rtol=2e-6, atol=0)
+
+
+@pytest.mark.parametrize("T", [16, 2000])
+def test_routing_follows_its_stream_and_graphs(ilw, T):
+    x = [torch.randn((T, 64), generator=torch.Generator("cuda").manual_seed(i), device="cuda") for i in range(3)]
+    how = dict(score="sigmoid", bias=torch.linspace(-0.1, 0.1, 64, device="cuda"), groups=8, top_groups=3)
+    want = [ilw.moe_route(v, 4, **how) for v in x]
+    graphs = []
+    for i in range(2):
+        b, g = x[0].clone(), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            r = ilw.moe_route(b, 4, **how)
+        graphs.append((b, g, r))
+    for i, j in ((1, 2), (2, 0), (0, 1)):
+        for (b, g, r), n in zip(graphs, (i, j)):
+            b.copy_(x[n])
+            g.replay()
+        torch.cuda.synchronize()
+        for (b, g, r), n in zip(graphs, (i, j)):
+            assert all(torch.equal(u, v) for u, v in zip(r, want[n]))
