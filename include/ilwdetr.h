@@ -567,6 +567,9 @@ typedef struct {
 } ilw_i8_gemm_t;
 int ilwdetr_i8_gemm(const ilw_i8_gemm_t *p, ilw_stream_t stream);
 
+/* Test hook, as ilwdetr_debug_mx_form: form[0] 0, 1 or 2 as there, 3 the kernel for few tokens. */
+int ilwdetr_debug_i8_form(const ilw_i8_gemm_t *p, int32_t sms, int32_t *form);
+
 /* ------------------------------------------------------------------ mixture of experts */
 
 enum { ILW_MOE_MAX_EXPERTS = 512, ILW_MOE_MAX_TOP = 16 };

@@ -175,6 +175,7 @@ SIGNATURES = {
     "ilwdetr_i8_quantize": ([_VP, _I32, _I64, _I64, _VP, _I64, _I32, _VP, _I64, _VP, _VP], C.c_int),
     "ilwdetr_i8_dequantize": ([_VP, _I64, _VP, _I64, _I32, _VP, _I32, _I64, _VP], C.c_int),
     "ilwdetr_i8_gemm": ([_VP, _VP], C.c_int),
+    "ilwdetr_debug_i8_form": ([_VP, _I32, C.POINTER(_I32)], C.c_int),
     "ilwdetr_moe_combine": ([_VP, _I32, _I64, _I64, _VP, _VP, _I32, _I32, _I32, _VP, _I64, _VP, _I64, _VP], C.c_int),
 }
 

@@ -103,7 +103,17 @@ int ilwdetr_i8_gemm(const ilw_i8_gemm_t *p, ilw_stream_t stream) {
     ilw::I8GemmProblem g;
     ILW_TRY(gemm_problem(p, g));
     if (g.M == 0 || g.N == 0 || ilw::validate_only()) return ILW_OK;
-    return done(ilw::launch_i8_few(g, (cudaStream_t)stream), "i8_gemm");
+    return done(ilw::launch_i8_gemm(g, (cudaStream_t)stream), "i8_gemm");
+}
+
+int ilwdetr_debug_i8_form(const ilw_i8_gemm_t *p, int32_t sms, int32_t *form) {
+    ilw::I8GemmProblem g;
+    ILW_TRY(gemm_problem(p, g));
+    if (!form || sms < 0 || g.M == 0 || g.N == 0) return fail(ILW_ERR_INVALID_ARG, "debug_i8_form: NULL result, negative sms or empty product");
+    int32_t f[3];
+    ilw::i8_gemm_form(g, sms, f);
+    for (int i = 0; i < 3; ++i) form[i] = f[i];
+    return ILW_OK;
 }
 
 }  // extern "C"

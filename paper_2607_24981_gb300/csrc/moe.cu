@@ -24,7 +24,7 @@
 
 #include "ilw_kernels.h"
 #include "ilwdetr.h"
-#include "moe_scores.cuh"
+#include "moe_order.cuh"
 #include "mx_kernels.h"
 
 namespace ilw {
@@ -35,25 +35,6 @@ template <> __device__ __forceinline__ float from_f<float>(float v) { return v; 
 template <> __device__ __forceinline__ __half from_f<__half>(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
-// Two lanes a token (65536 rows of 128, 8 experts: 30 us with the order; 31 with four, 38 with one), 64 tokens a CTA; 32 where
-// 64 rows are all of an SM's shared memory (8192 rows of 512: 24 us instead of 41).
-constexpr int kSelectLanes = 2, kSelectCtas = 8;
-__host__ __device__ constexpr int select_tokens(int S) { return S >= 32 ? 32 : 64; }
-__host__ __device__ constexpr int chunk_tokens(int S) { return select_tokens(S) * kSelectCtas; }
-constexpr int kPlaceThreads = 1024;
-// What one CTA takes alone (one kernel and two, in us: 16 tokens of 64 experts 3.6 and 7.6, 256 of 64 7.1 and 8.1, 128 of 256 11.1 and
-// 12.1, 224 of 128 10.6 and 10.4, 256 of 128 11.6 and 10.7)
-constexpr int kOneTokens = 256, kOneLogits = 32 * 1024 - 4096, kOneSmem = 200 * 1024;
-constexpr int kGroups = 16;
-
-// Experts a group (4, 8, 16 or 32), and words between the rows of the tokens' logits in shared memory: 16 groups, filled up with
-// -inf, and one more piece of 16 bytes, so that pieces of eight rows in a row meet in no bank.
-__host__ __device__ inline int group_size(int E) { return E <= 64 ? 4 : E <= 128 ? 8 : E <= 256 ? 16 : 32; }
-__host__ __device__ inline int row_words(int E) { return kGroups * group_size(E) + 4; }
-
-// i / k for i < 2^13 and k <= 16: i * ceil(2^17 / k) / 2^17 (the rounding adds less than i / 2^17 < 1 / k)
-__device__ __forceinline__ uint32_t reciprocal(int k) { return ((1u << 17) + k - 1) / k; }
-__device__ __forceinline__ int over(int i, uint32_t r) { return (int)(((uint64_t)(uint32_t)i * r) >> 17); }
 // n rows of the logits from token t0 on to shared memory, by one warp; 16 bytes of them at a time where rows allow it
 // (65536 rows of 128: 30 us, else 82; 257 rows 11 and 21).
 template <typename T, int S>
@@ -182,82 +163,6 @@ __device__ __forceinline__ void select_token(const MoeRouteParams &p, float *row
         if (out_e[j] >= 0) out_w[j] /= sum;
 }
 
-// Places of a chunk's entries: base[e] + the earlier tokens of e in the chunk.  Entry i of the chunk (token i / k) is ex[i / threads] of
-// thread i % threads.  bits [E][W + 1]: bitmaps of W words, and their words' running counts in pre.
-template <int W, int N>
-__device__ __forceinline__ void place_chunk(const MoeRouteParams &p, int32_t t0, int n, const int32_t (&ex)[N], uint32_t *bits,
-                                            int32_t *pre, const int32_t *base) {
-    constexpr int row = W + 1;  // (an odd number of words a row apart: no bank met by all)
-    const uint32_t over_k = reciprocal(p.k);
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-        const int i = j * blockDim.x + threadIdx.x, t = over(i, over_k);
-        if (i < n && ex[j] >= 0) atomicOr(&bits[ex[j] * row + (t >> 5)], 1u << (t & 31));
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < (p.E * W + 31) / 32 * 32; i += blockDim.x) {  // W lanes a bitmap
-        const int e = i / W, w = i % W;
-        const int32_t c = e < p.E ? __popc(bits[e * row + w]) : 0;
-        int32_t x = c;
-#pragma unroll
-        for (int d = 1; d < W; d <<= 1) {
-            const int32_t y = __shfl_up_sync(0xffffffffu, x, d, W);
-            if (w >= d) x += y;
-        }
-        if (e < p.E) pre[e * row + w] = base[e] + x - c;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-        const int i = j * blockDim.x + threadIdx.x, t = over(i, over_k);
-        if (i >= n) break;
-        int32_t s = -1;
-        if (ex[j] >= 0) {
-            const int at = ex[j] * row + (t >> 5);
-            s = pre[at] + __popc(bits[at] & ((1u << (t & 31)) - 1));
-            p.source[s] = t0 + t;
-        }
-        p.slot[(int64_t)t0 * p.k + i] = s;
-    }
-}
-
-// Exclusive sums over the experts of total[e] (shared, E <= 512) into base[e] by one warp; returns the sum of all.
-__device__ __forceinline__ int32_t scan_experts(int E, const int32_t *total, int32_t *base, int lane) {
-    int32_t carry = 0;
-    for (int e0 = 0; e0 < E; e0 += 32) {
-        const int e = e0 + lane;
-        const int32_t n = e < E ? total[e] : 0;
-        int32_t x = n;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int32_t y = __shfl_up_sync(0xffffffffu, x, d);
-            if (lane >= d) x += y;
-        }
-        if (e < E) base[e] = carry + x - n;
-        carry += __shfl_sync(0xffffffffu, x, 31);
-    }
-    return carry;
-}
-
-// The counts of a cluster's CTAs, added up, to their chunk's.
-__device__ __forceinline__ void add_counts(const MoeRouteParams &p, const int32_t *count) {
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-    const uint32_t rank = blockIdx.x % kSelectCtas, at = (uint32_t)__cvta_generic_to_shared(count);
-    for (int e = rank * blockDim.x + threadIdx.x; e < p.E; e += kSelectCtas * blockDim.x) {
-        int32_t sum = 0;
-#pragma unroll
-        for (int r = 0; r < kSelectCtas; ++r) {
-            uint32_t a;
-            int32_t c;
-            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(at + 4 * e), "r"(r));
-            asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(c) : "r"(a) : "memory");
-            sum += c;
-        }
-        p.counts[(int64_t)(blockIdx.x / kSelectCtas) * p.E + e] = sum;
-    }
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-
 // Selection of a chunk's tokens by a cluster, and the chunk's counts.  Each warp loads its own tokens' rows.
 template <typename T, int S>
 __global__ void __cluster_dims__(kSelectCtas, 1, 1) __launch_bounds__(select_tokens(S) * kSelectLanes) route_select_kernel(const MoeRouteParams p, int wide) {
@@ -289,7 +194,7 @@ __global__ void __cluster_dims__(kSelectCtas, 1, 1) __launch_bounds__(select_tok
         p.weight[(int64_t)t0 * p.k + i] = out_w[at];
         if (e >= 0) atomicAdd(&count[e], 1);  // (whole numbers: any order gives the same)
     }
-    add_counts(p, count);
+    add_counts<kSelectThreads>(p, count);
 }
 
 template <int W>  // words of a chunk's bitmap
@@ -381,84 +286,6 @@ __global__ void __launch_bounds__(4 * kOneTokens) route_one_kernel(const MoeRout
     for (int i = all + threadIdx.x; i < p.T * p.k; i += blockDim.x) p.source[i] = -1;
 }
 
-// max|bias| of what fp32 scores are added to, by a warp
-__device__ __forceinline__ float largest_bias(const MoeRouteParams &p, int lane) {
-    float m = 0.0f;
-    if (p.scores.bias)
-        for (int e = lane; e < p.E; e += 32) m = fmaxf(m, fabsf(__ldg(p.scores.bias + e)));
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-    return m;
-}
-
-// Selection by scores of a chunk's tokens by a cluster, a warp a token, and the chunk's counts.
-constexpr int kScoredThreads = 512;
-template <typename T, int S>
-__global__ void __cluster_dims__(kSelectCtas, 1, 1) __launch_bounds__(kScoredThreads) route_scored_kernel(const __grid_constant__ MoeRouteParams p, int wide) {
-    __shared__ int32_t count[kRouteMaxExperts];
-    constexpr int kTokens = select_tokens(S);
-    const int lane = threadIdx.x & 31;
-    for (int e = threadIdx.x; e < p.E; e += kScoredThreads) count[e] = 0;
-    __syncthreads();
-    grid_wait();
-    const float bias_max = largest_bias(p, lane);
-    for (int i = threadIdx.x >> 5; i < kTokens; i += kScoredThreads / 32) {
-        const int64_t t = (int64_t)blockIdx.x * kTokens + i;
-        if (t >= p.T) break;
-        int32_t e;
-        float w;
-        select_scored<T, S / 2>(p, t, wide, bias_max, lane, e, w);
-        if (lane < p.k) {
-            p.expert[t * p.k + lane] = e;
-            p.weight[t * p.k + lane] = w;
-            if (e >= 0) atomicAdd(&count[e], 1);  // (whole numbers: any order gives the same)
-        }
-    }
-    __syncthreads();
-    add_counts(p, count);
-}
-
-// Few tokens by scores: all of it by one CTA, a warp a token.
-template <typename T, int S>
-__global__ void __launch_bounds__(4 * kOneTokens) route_one_scored_kernel(const __grid_constant__ MoeRouteParams p, int wide) {
-    extern __shared__ __align__(16) uint32_t dyn[];
-    __shared__ int32_t base[kRouteMaxExperts], count[kRouteMaxExperts], all;
-    constexpr int words = kOneTokens / 32, row = words + 1, kEntries = kRouteMaxTop / 4;
-    int32_t *out_e = (int32_t *)dyn;  // [T][k], then bits [E][row] and the running counts
-    uint32_t *bits = dyn + p.T * p.k;
-    const int lane = threadIdx.x & 31;
-    for (int i = threadIdx.x; i < p.E * row; i += blockDim.x) bits[i] = 0;
-    for (int e = threadIdx.x; e < p.E; e += blockDim.x) count[e] = 0;
-    __syncthreads();
-    grid_wait();
-    const float bias_max = largest_bias(p, lane);
-    for (int t = threadIdx.x >> 5; t < p.T; t += blockDim.x / 32) {
-        int32_t e;
-        float w;
-        select_scored<T, S / 2>(p, t, wide, bias_max, lane, e, w);
-        if (lane < p.k) {
-            out_e[t * p.k + lane] = p.expert[t * p.k + lane] = e;
-            p.weight[t * p.k + lane] = w;
-            if (e >= 0) atomicAdd(&count[e], 1);
-        }
-    }
-    __syncthreads();
-    int32_t ex[kEntries];
-#pragma unroll
-    for (int j = 0; j < kEntries; ++j) {
-        const int i = j * blockDim.x + threadIdx.x;
-        ex[j] = i < p.T * p.k ? out_e[i] : -1;
-    }
-    if (threadIdx.x < 32) {
-        const int32_t x = scan_experts(p.E, count, base, threadIdx.x);
-        if (threadIdx.x == 0) all = x;
-    }
-    __syncthreads();
-    for (int e = threadIdx.x; e <= p.E; e += blockDim.x) p.offsets[e] = e < p.E ? base[e] : all;
-    place_chunk<words>(p, 0, p.T * p.k, ex, bits, (int32_t *)bits + p.E * row, base);
-    for (int i = all + threadIdx.x; i < p.T * p.k; i += blockDim.x) p.source[i] = -1;
-}
-
 size_t select_smem(int32_t E, int32_t k) {
     return ((size_t)select_tokens(group_size(E)) * (row_words(E) + 2 * (k | 1)) + E) * 4;
 }
@@ -495,33 +322,6 @@ cudaError_t route_form(const MoeRouteParams &p, cudaStream_t s) {
         case 8: return route<T, 8>(p, s);
         case 16: return route<T, 16>(p, s);
         default: return route<T, 32>(p, s);
-    }
-}
-
-size_t one_scored_smem(int32_t T, int32_t E, int32_t k) { return ((size_t)2 * E * (kOneTokens / 32 + 1) + (size_t)T * k) * 4; }
-template <typename T, int S>
-cudaError_t route_scored(const MoeRouteParams &p, cudaStream_t s) {
-    constexpr int kLane = std::min(16, S / 2 * (int)sizeof(T));  // bytes of a lane's loads
-    const int wide = (uintptr_t)p.logits % kLane == 0 && p.ld * (int64_t)sizeof(T) % kLane == 0 && p.E * sizeof(T) % kLane == 0;
-    if (route_in_one(p.T, p.E)) {
-        static SmemLimit limit;
-        const cudaError_t e = raise_smem_limit(limit, (const void *)route_one_scored_kernel<T, S>, (int)one_scored_smem(kOneTokens, kRouteMaxExperts, kRouteMaxTop));
-        if (e != cudaSuccess) return e;
-        return launch_after(route_one_scored_kernel<T, S>, 1, 4 * kOneTokens, one_scored_smem(p.T, p.E, p.k), s, p, wide);
-    }
-    constexpr int kChunk = chunk_tokens(S), W = kChunk / 32;
-    const int32_t chunks = (int32_t)((p.T + (int64_t)kChunk - 1) / kChunk);
-    const cudaError_t e = launch_after(route_scored_kernel<T, S>, chunks * kSelectCtas, kScoredThreads, 0, s, p, wide);
-    if (e != cudaSuccess) return e;
-    return launch_after(route_place_kernel<W>, chunks, kPlaceThreads, (size_t)2 * p.E * (W + 1) * 4, s, p, chunks);
-}
-template <typename T>
-cudaError_t route_scored_form(const MoeRouteParams &p, cudaStream_t s) {
-    switch (group_size(p.E)) {
-        case 4: return route_scored<T, 4>(p, s);
-        case 8: return route_scored<T, 8>(p, s);
-        case 16: return route_scored<T, 16>(p, s);
-        default: return route_scored<T, 32>(p, s);
     }
 }
 
@@ -580,6 +380,14 @@ cudaError_t combine(const MoeCombineParams &p, cudaStream_t s) {
 
 }  // namespace
 
+bool moe_route_in_one(int32_t T, int32_t E) { return route_in_one(T, E); }
+
+cudaError_t launch_moe_place(const MoeRouteParams &p, int32_t chunk, cudaStream_t s) {
+    const int32_t chunks = (int32_t)((p.T + (int64_t)chunk - 1) / chunk);
+    if (chunk == 256) return launch_after(route_place_kernel<8>, chunks, kPlaceThreads, (size_t)2 * p.E * 9 * 4, s, p, chunks);
+    return launch_after(route_place_kernel<16>, chunks, kPlaceThreads, (size_t)2 * p.E * 17 * 4, s, p, chunks);
+}
+
 size_t moe_route_workspace(int32_t T, int32_t E) {
     const int64_t chunk = chunk_tokens(group_size(E));
     return route_in_one(T, E) ? 0 : (size_t)((T + chunk - 1) / chunk) * E * sizeof(int32_t);
@@ -589,18 +397,6 @@ cudaError_t launch_moe_route(const MoeRouteParams &p, cudaStream_t s) {
     if (p.form == ILW_FP32) return route_form<float>(p, s);
     if (p.form == ILW_FP16) return route_form<__half>(p, s);
     return route_form<__nv_bfloat16>(p, s);
-}
-
-cudaError_t launch_moe_route_scored(const MoeRouteParams &r, cudaStream_t s) {
-    MoeRouteParams p = r;
-    RouteScores &q = p.scores;
-    q.group_size = p.E / q.groups;
-    q.per_group = divisor(q.group_size);
-    const int per = group_size(p.E) / 2, lanes = q.group_size / per;  // experts a lane
-    q.lanes_per_group = q.group_size % per == 0 && (lanes & (lanes - 1)) == 0 ? lanes : 0;
-    if (p.form == ILW_FP32) return route_scored_form<float>(p, s);
-    if (p.form == ILW_FP16) return route_scored_form<__half>(p, s);
-    return route_scored_form<__nv_bfloat16>(p, s);
 }
 
 cudaError_t launch_moe_combine(const MoeCombineParams &q, cudaStream_t s) {

@@ -1,4 +1,4 @@
-// moe_scores.cuh -- selection of a token's experts by scores, with a bias and by groups (a part of moe.cu).
+// moe_scores.cuh -- selection of a token's experts by scores, with a bias and by groups (a part of moe_scored.cu).
 //
 //   s[e] = 1 / (1 + exp(-x[e])), or the softmax of the row;  c[e] = s[e] + bias[e]
 //   a group's rank is its largest c, or the sum of its two largest; the best `top_groups` groups stay
@@ -16,20 +16,12 @@
 #pragma once
 #include <cstdint>
 
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-
 #include "divisor.cuh"
+#include "moe_order.cuh"
 #include "mx_kernels.h"
 
 namespace ilw {
 namespace {
-
-__device__ __forceinline__ float to_f(float v) { return v; }
-__device__ __forceinline__ float to_f(__half v) { return __half2float(v); }
-__device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
-// A logit as it is compared: -inf for what is never taken.
-__device__ __forceinline__ float logit(float x) { return x > __int_as_float(0xff800000) ? x : __int_as_float(0xff800000); }
 
 __device__ __forceinline__ float none_of(float) { return __int_as_float(0xff800000); }
 __device__ __forceinline__ double none_of(double) { return __longlong_as_double(0xfff0000000000000ll); }
@@ -83,7 +75,7 @@ template <typename V> __device__ __forceinline__ void merge2(V &a1, V &a2, V b1,
 // The experts of a token, the j-th in lane j's `mine` (-1: none); false if fp32 cannot tell (V double: never).  x: this lane's logits, -inf where
 // no expert is to be taken; `best` their row's largest; `sum` their softmax's denominator.
 template <typename V, int PER>
-__device__ __forceinline__ bool choose(const MoeRouteParams &p, const float (&x)[PER], float best, V sum, float bias_max, int lane, int32_t &mine) {
+__device__ __forceinline__ bool choose(const MoeScoredParams &p, const float (&x)[PER], float best, V sum, float bias_max, int lane, int32_t &mine) {
     constexpr bool kCheck = sizeof(V) == 4;
     const RouteScores &q = p.scores;
     const V none = none_of(V());
@@ -203,7 +195,7 @@ __device__ __forceinline__ bool choose(const MoeRouteParams &p, const float (&x)
 
 // The same in 64 bits, from the logits on.
 template <int PER>
-__device__ __noinline__ int32_t choose_exactly(const MoeRouteParams &p, const float *xs, float best, int lane) {
+__device__ __noinline__ int32_t choose_exactly(const MoeScoredParams &p, const float *xs, float best, int lane) {
     float x[PER];
     double sum = 0.0;
 #pragma unroll
@@ -219,7 +211,7 @@ __device__ __noinline__ int32_t choose_exactly(const MoeRouteParams &p, const fl
 }
 
 // Lane j: the weight of expert `e`, the j-th taken (-1: 0), whose logit is x.
-__device__ __forceinline__ float weight_of(const MoeRouteParams &p, int32_t e, float x, float best, float sum) {
+__device__ __forceinline__ float weight_of(const MoeScoredParams &p, int32_t e, float x, float best, float sum) {
     const bool on = e >= 0;
     float s = 0.0f;
     if (p.scores.score == ILW_SCORE_SOFTMAX) {
@@ -248,7 +240,7 @@ __device__ __forceinline__ float weight_of(const MoeRouteParams &p, int32_t e, f
 
 // Token t by one warp: lane j < k gets its j-th expert and weight.
 template <typename T, int PER>
-__device__ __forceinline__ void select_scored(const MoeRouteParams &p, int64_t t, bool wide, float bias_max, int lane, int32_t &expert, float &weight) {
+__device__ __forceinline__ void select_scored(const MoeScoredParams &p, int64_t t, bool wide, float bias_max, int lane, int32_t &expert, float &weight) {
     const T *row = (const T *)p.logits + t * p.ld;
     const float none = none_of(0.0f);
     const int e0 = lane * PER;

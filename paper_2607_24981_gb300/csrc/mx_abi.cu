@@ -90,7 +90,7 @@ int route_problem(const void *logits, int32_t form, int64_t ld, int32_t T, int32
     const size_t need = ilw::moe_route_workspace(T, E);
     if (need && (!workspace || !aligned(workspace, 4) || workspace_bytes < need))
         return fail(ILW_ERR_INVALID_ARG, "moe_route: workspace NULL, misaligned or smaller than %zu bytes", need);
-    p = {logits, form, ld, T, E, k, renormalize, expert, weight, offsets, source, slot, (int32_t *)workspace, {}};
+    p = {logits, form, ld, T, E, k, renormalize, expert, weight, offsets, source, slot, (int32_t *)workspace};
     return ILW_OK;
 }
 
@@ -161,7 +161,7 @@ int ilwdetr_moe_route(const void *logits, int32_t form, int64_t ld, int32_t T, i
 int ilwdetr_moe_route_scored(const void *logits, int32_t form, int64_t ld, int32_t T, int32_t E, int32_t k, int32_t renormalize,
                              const ilw_moe_scores_t *scores, int32_t *expert, float *weight, int32_t *offsets, int32_t *source,
                              int32_t *slot, void *workspace, size_t workspace_bytes, ilw_stream_t stream) {
-    ilw::MoeRouteParams p;
+    ilw::MoeScoredParams p;
     ILW_TRY(route_problem(logits, form, ld, T, E, k, renormalize, expert, weight, offsets, source, slot, workspace, workspace_bytes, p));
     if (!scores || scores->struct_size != sizeof(ilw_moe_scores_t)) return fail(ILW_ERR_INVALID_ARG, "moe_route: scores NULL or struct_size");
     const ilw_moe_scores_t &q = *scores;

@@ -34,7 +34,7 @@ bool choose_form(const MxGemmProblem &g, int64_t sms, MxParams &p, int64_t &tile
 
     const int64_t out = g.act == ILW_ACT_SILU_GATE ? g.N / 2 : g.N;
     p.wide = g.act != ILW_ACT_NONE && g.form != ILW_FP32 && out % 8 == 0 && (uintptr_t)g.Y % 16 == 0 && g.ldy % 8 == 0;
-    const int fixed = 1024 + (g.experts + 1) * (int)sizeof(MxExpert) + g.experts * 4 + (p.wide ? kMxEpiWarps * kMxPatch : 0);
+    const int fixed = 1024 + (g.experts + 1) * (int)sizeof(TileExpert) + g.experts * 4 + (p.wide ? kMxEpiWarps * kMxPatch : 0);
     auto bytes = [&] { return fixed + p.stages * p.stage_bytes + kMxScaleSets * p.raw_bytes + 2 * p.scale_bytes; };
 
     // Tokens a tile: as wide as the tokens (of an expert, twice the mean: with the mean alone more experts of unequal ones take two
@@ -51,24 +51,24 @@ bool choose_form(const MxGemmProblem &g, int64_t sms, MxParams &p, int64_t &tile
         // or more a pair of SMs (one CTA a tile against pairs, in us: 12800 x 384 x 1536, 9 blocks, 9.7 and 12.2; 6400 x 2048 x
         // 1536, 18 blocks, 16.6 and 16.8; 12800 x 1536 x 1536, 27 blocks, 21.8 and 20.8; 8192 cubed 194 and 169), and for
         // tiles of 64 tokens or more, whose MMAs take longer than their rows of W
-        const int64_t pair_tiles = most(p.nt) * ((g.N + 2 * kMxRowsW - 1) / (2 * kMxRowsW));
-        p.mode = p.nt >= 64 && g.N > kMxRowsW && p.nkb > 4 && 2 * pair_tiles * p.nkb >= 20 * sms ? MX_PAIR : MX_ONE;
-        const int rows_w = p.mode == MX_PAIR ? 2 * kMxRowsW : kMxRowsW;
+        const int64_t pair_tiles = most(p.nt) * ((g.N + 2 * kTileRowsW - 1) / (2 * kTileRowsW));
+        p.mode = p.nt >= 64 && g.N > kTileRowsW && p.nkb > 4 && 2 * pair_tiles * p.nkb >= 20 * sms ? TILE_PAIR : TILE_ONE;
+        const int rows_w = p.mode == TILE_PAIR ? 2 * kTileRowsW : kTileRowsW;
         p.wtiles = (g.N + rows_w - 1) / rows_w;
-        if (p.mode == MX_ONE) {
+        if (p.mode == TILE_ONE) {
             // The width, from 64 tokens on, at which the CTA with the most tiles reads the fewest rows of W and tokens (at 224 tokens and so, in
             // us: 12800 x 384 x 1536, 128 tokens, 11.5 and 9.7; 6400 x 1536 x 384, 176, 11.5 and 10.4; 224 x 4096 x 4096, 64, 10.8
             // and 8.9; narrower still, 32 and 16 tokens, 12.3 and 15.6; 2048 rows of 16 experts, 768 x 1024, 7.2 and 6.6)
             int64_t least = INT64_MAX;
             for (int32_t top = p.nt, n = top; n >= std::min(top, 64); n -= 16) {
-                const int64_t rows = (about(n) * p.wtiles + sms - 1) / sms * (n + kMxRowsW);
+                const int64_t rows = (about(n) * p.wtiles + sms - 1) / sms * (n + kTileRowsW);
                 if (rows < least) least = rows, p.nt = n;
             }
         }
         tiles = most(p.nt) * p.wtiles;
-        const int32_t tokens = p.mode == MX_PAIR ? p.nt / 2 : p.nt;  // whose codes a CTA loads
-        p.stage_bytes = kMxRowsW * 128 + tokens * 128;
-        p.raw_bytes = kMxRowsW * 16 + (p.nt + 31) / 32 * 512;
+        const int32_t tokens = p.mode == TILE_PAIR ? p.nt / 2 : p.nt;  // whose codes a CTA loads
+        p.stage_bytes = kTileRowsW * 128 + tokens * 128;
+        p.raw_bytes = kTileRowsW * 16 + (p.nt + 31) / 32 * 512;
         p.scale_bytes = 4 * kMxAtom * (1 + (p.nt + 127) / 128);
         // as many stages as fit
         for (p.stages = kMxMaxStages; p.stages >= kMxMinStages && bytes() > kMxSmemLimit; --p.stages) {
@@ -86,12 +86,12 @@ bool choose_form(const MxGemmProblem &g, int64_t sms, MxParams &p, int64_t &tile
     // 17.7 and 10.8; N 1024 by 8, 16.9 and 7.6; 224 tokens, N and K 4096, by 4, 10.8 and 12.0, which is why it is not split),
     // and the clusters have to fit side by side: 16 of 8 CTAs do not (N 2048, K 4096: 11.4 us, by 4 6.7).
     p.splits = 1;
-    if (p.mode == MX_ONE)
+    if (p.mode == TILE_ONE)
         for (int c = 8; c > 1 && p.splits == 1; c /= 2) {
             const int64_t room = c == 8 ? sms / 2 : c == 4 ? sms * 7 / 8 : sms;
             if (c <= p.nsb && c * tiles <= room && p.nsb - (p.nsb + c - 1) / c >= 6 + p.nt / 128) p.splits = c;
         }
-    if (p.splits > 1) p.mode = MX_SPLIT;
+    if (p.splits > 1) p.mode = TILE_SPLIT;
     return true;
 }
 
@@ -125,14 +125,14 @@ cudaError_t launch_mx_gemm(const MxGemmProblem &g, cudaStream_t s) {
     p.nb = (g.K + 31) / 32;
     p.w_scales = g.w_scales, p.w_lds = g.w_lds, p.w_scales_stride = g.w_scales_stride;
     p.a_scales = g.a_scales, p.a_lds = g.a_lds;
-    if (!code_map(&p.wc, g.w_codes, 16 * p.nb, g.N, g.w_ldc, g.experts, g.w_codes_stride, kMxRowsW) ||
+    if (!code_map(&p.wc, g.w_codes, 16 * p.nb, g.N, g.w_ldc, g.experts, g.w_codes_stride, kTileRowsW) ||
         !code_map(&p.ac[0], g.a_codes, 16 * p.nb, g.M, g.a_ldc, 0, 0, 16))
         return cudaErrorInvalidValue;
     for (int i = 1; i < 4; ++i)
         if (!code_map(&p.ac[i], g.a_codes, 16 * p.nb, g.M, g.a_ldc, 0, 0, 16 << i)) return cudaErrorInvalidValue;
     int grid = (int)std::min<int64_t>(tiles, sms);
-    if (p.mode == MX_SPLIT) grid = (int)tiles * p.splits;
-    if (p.mode == MX_PAIR) grid = 2 * (int)std::min<int64_t>(tiles, sms / 2);
+    if (p.mode == TILE_SPLIT) grid = (int)tiles * p.splits;
+    if (p.mode == TILE_PAIR) grid = 2 * (int)std::min<int64_t>(tiles, sms / 2);
     if (g.form == ILW_FP32) return launch_mx<float>(p, g.act, grid, smem, s);
     if (g.form == ILW_FP16) return launch_mx<__half>(p, g.act, grid, smem, s);
     return launch_mx<__nv_bfloat16>(p, g.act, grid, smem, s);

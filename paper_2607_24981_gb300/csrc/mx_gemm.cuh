@@ -45,30 +45,21 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
-#include "attn_ptx.cuh"
-#include "float_act.cuh"
 #include "ilwdetr.h"
-#include "ilw_kernels.h"
 #include "mx_kernels.h"
+#include "tile_gemm.cuh"
 
 namespace ilw {
 
-constexpr int kMxRowsW = 128;   // rows of W a CTA
 constexpr int kMxMaxTok = 224;  // tokens a tile; a multiple of 32, as tiles of pairs are
 constexpr int kMxMaxStages = 16, kMxMinStages = 4;
 constexpr int kMxScaleWarp0 = 3, kMxScaleSets = 4;  // pairs of scale warps
 constexpr int kMxEpiWarp0 = kMxScaleWarp0 + 2 * kMxScaleSets, kMxEpiWarps = 16, kMxTileWarp = kMxEpiWarp0 + kMxEpiWarps;
 constexpr int kMxThreads = 32 * (kMxTileWarp + 1);
+constexpr int kMxPatch = 512;   // bytes of shared memory in which an epilogue warp turns 2-byte results
 constexpr int kMxTiles = 16;    // tiles found ahead
 constexpr int kMxAtom = 512;    // bytes of the scales of 128 rows and 128 values of K
-constexpr int kMxPatch = 512;   // bytes of shared memory in which an epilogue warp turns 2-byte results
 constexpr int kMxSmemLimit = 226 * 1024;  // dynamic; the barriers are static
-
-enum MxMode { MX_ONE = 0, MX_SPLIT = 1, MX_PAIR = 2 };
-
-struct MxExpert {
-    int32_t start, row, end, width;  // first token tile, its rows [row, end), rows a tile
-};
 
 struct MxParams {
     CUtensorMap wc, ac[4];  // codes of W [E, N, .]; of A [M, .] in boxes of 16, 32, 64 and 128 rows
@@ -99,62 +90,6 @@ cudaError_t launch_mx(const MxParams &p, int32_t act, int grid, size_t smem, cud
 
 namespace {
 
-struct Tile {
-    int32_t e, row0, rows, n0;
-};
-
-// Bounded wait: false (after latching `code` and raising the abort flag) when it ran out, or when another role aborted.
-__device__ __forceinline__ bool wait_bar(uint32_t b, uint32_t parity, volatile int *abort, const MxParams &p, int code) {
-    if (bar_try(b, parity)) return true;
-    const long long t0 = clock64();
-    for (uint32_t i = 0;; ++i) {
-        if (bar_try(b, parity)) return true;
-        if ((i & 63) == 63) {
-            if (*abort) return false;
-            if (clock64() - t0 > p.wait_cycles) {
-                if (p.status) atomicExch(p.status, code);
-                *abort = 1;
-                return false;
-            }
-        }
-    }
-}
-// The same for a whole warp, one answer for all lanes (the tcgen05 instructions after it are warp-wide).
-__device__ __forceinline__ bool wait_warp(uint32_t b, uint32_t parity, volatile int *abort, const MxParams &p, int code) {
-    return __all_sync(0xffffffffu, wait_bar(b, parity, abort, p, code));
-}
-// The same for a lane that issues loads or MMAs on its own, with the long way out of line: its loop then keeps the operands in
-// uniform registers and a wait with nothing to wait for costs next to nothing (a block of K: 225 clocks for 6 copies and 4
-// MMAs of 16 tokens, what they take; with a vote of the warp 395).
-__device__ __noinline__ bool wait_long(uint32_t b, uint32_t parity, volatile int *abort, const MxParams *p, int code) {
-    return wait_bar(b, parity, abort, *p, code);
-}
-__device__ __forceinline__ bool wait_lane(uint32_t b, uint32_t parity, volatile int *abort, const MxParams &p, int code) {
-    return bar_try(b, parity) || wait_long(b, parity, abort, &p, code);
-}
-
-// This barrier's address in CTA `rank` of the cluster, and an arrival there.  What the arrivals of a pair order is read by the
-// tensor core alone, through the async proxy, to which its writers hand it themselves (TMA, or fence.proxy.async
-// after the stores); a release at cluster scope on top of that held each arrival up by some 1000 clocks.
-__device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank) {
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-    return r;
-}
-__device__ __forceinline__ void arrive_cluster(uint32_t addr) {
-    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
-}
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void prefetch_map(const CUtensorMap *m) {
-    asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)m) : "memory");
-}
-
-// A value that is the same in every lane, in a uniform register: the operands of TMA loads and MMAs are uniform
-// registers, and each one that has to be moved there at its instruction costs some 50 clocks (with values that the
-// compiler could not know to be uniform a TMA load took 300 clocks, which was the rate of every product).
-__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __reduce_max_sync(0xffffffffu, v); }
 // Of a pair (PAIR) only the first CTA issues, for both.  All by one lane.
 template <bool PAIR>
 __device__ __forceinline__ void mma_mx(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t acc) {
@@ -171,20 +106,6 @@ __device__ __forceinline__ void mma_mx(uint32_t d, uint64_t a, uint64_t b, uint3
             "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(acc)
             : "memory");
 }
-// An arrival at `bar` (of a pair: in both CTAs, unless `local`) when the MMAs and copies issued so far have ended.
-template <bool PAIR>
-__device__ __forceinline__ void commit_mma(uint32_t bar, bool local = false) {
-    if constexpr (PAIR) {
-        if (!local)
-            asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
-                         "h"((uint16_t)3)
-                         : "memory");
-        else
-            asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-    } else {
-        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-    }
-}
 // Descriptor of scales in order: rows of 16 bytes, eight of them (128 bytes) a core matrix, no swizzle
 __device__ __forceinline__ uint64_t scale_desc(uint32_t saddr) {
     return (uint64_t)((saddr >> 4) & 0x3FFFu) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
@@ -196,35 +117,10 @@ __device__ __forceinline__ void copy_scales(uint32_t t, uint64_t d) {
     if constexpr (PAIR) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(t), "l"(d) : "memory");
     else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(t), "l"(d) : "memory");
 }
-__device__ __forceinline__ void lds128(uint32_t a, uint32_t (&v)[4]) {
-    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
-                 : "r"(a)
-                 : "memory");
-}
-
 // Instruction descriptor of kind::mxf4: E2M1 operands (format 1), UE8M0 scales, M = m, N = n, both
 // operands K-major; `id` (0 or 2) is the byte of a scale word at which this MMA's two scales begin.
 __device__ __forceinline__ uint32_t idesc_mx(uint32_t m, uint32_t n, uint32_t id) {
     return (id << 4) | (1u << 7) | (1u << 10) | ((n >> 3) << 17) | (1u << 23) | ((m >> 4) << 24) | (id << 29);
-}
-
-// (By a whole warp.) Tile t: the tile of W's rows runs fastest, so CTAs that run together share a token tile's rows.  tab: the
-// experts that have rows, n of them (n <= 1024: two probes of 32), and an end.
-template <int MODE>
-__device__ __forceinline__ Tile find_tile(const MxParams &p, const MxExpert *tab, const int32_t *id, int n, int32_t t, uint32_t rank) {
-    const int lane = threadIdx.x & 31;
-    const int32_t tt = (int32_t)((__umulhi((uint32_t)t, p.wdiv_m) + (uint32_t)t) >> p.wdiv_s);  // t / wtiles
-    int a = 0;  // the expert with start <= tt < the next one's
-    if (n > 32) a = 32 * (__popc(__ballot_sync(0xffffffffu, 32 * lane < n && tab[min(32 * lane, n)].start <= tt)) - 1);
-    a += __popc(__ballot_sync(0xffffffffu, a + lane < n && tab[min(a + lane, n)].start <= tt)) - 1;
-    const int4 x = *(const int4 *)(tab + a);
-    Tile r;
-    r.e = id[a];
-    r.row0 = x.y + (tt - x.x) * x.w;
-    r.rows = min(x.w, x.z - r.row0);
-    r.n0 = (t - tt * p.wtiles) * (MODE == MX_PAIR ? 2 * kMxRowsW : kMxRowsW) + (MODE == MX_PAIR ? rank * kMxRowsW : 0);
-    return r;
 }
 
 // One warp's 32 rows of W (this lane: row n) x 16 tokens (c0 .. c0 + 15 of the tile).  A lane holds one output of 16
@@ -289,7 +185,7 @@ __device__ __forceinline__ void store_chunk(const MxParams &p, float (&v)[16], c
 
 template <int ACT, typename T, int MODE>
 __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_constant__ MxParams p) {
-    constexpr bool SPLIT = MODE == MX_SPLIT, PAIR = MODE == MX_PAIR;
+    constexpr bool SPLIT = MODE == TILE_SPLIT, PAIR = MODE == TILE_PAIR;
     // tensor-memory columns: two accumulators, then two buffers of the scales of 256 values of K (2 x 4 columns of
     // W's rows, 2 x 8 of A's)
     constexpr int kScaleCol = 2 * kMxMaxTok, kScaleCols = 24;
@@ -303,7 +199,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
     const uint32_t data0 = (su32(smem_raw) + 1023) & ~1023u;
     const uint32_t raw0 = data0 + p.stages * p.stage_bytes, scale0 = raw0 + kMxScaleSets * p.raw_bytes;
     const uint32_t patch0 = scale0 + 2 * p.scale_bytes;
-    MxExpert *tab = (MxExpert *)(smem_raw + (patch0 - su32(smem_raw)) + (p.wide ? kMxEpiWarps * kMxPatch : 0));
+    TileExpert *tab = (TileExpert *)(smem_raw + (patch0 - su32(smem_raw)) + (p.wide ? kMxEpiWarps * kMxPatch : 0));
     int32_t *tab_id = (int32_t *)(tab + p.E + 1);
 
     uint32_t next_bar = su32(bars);
@@ -354,52 +250,14 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
         }
     }
     grid_wait();
-    // the list of tiles: the experts that have rows, in order.  Their ranges are held in order, apart and inside [0, M],
-    // whatever the offsets say.
     if (warp == 2) {
-        const int32_t M = (int32_t)p.M;
-        int32_t sum = 0, count = 0, before = 0, head = M;  // of the experts before this round: tiles, those with rows, end of the last range
-        for (int e0 = 0; e0 < p.E; e0 += 32) {
-            const int e = e0 + lane;
-            int32_t l = 0, h = e < p.E ? M : 0;
-            if (p.offsets && e < p.E) {
-                l = max(0, min(p.offsets[e], M));
-                h = max(0, min(p.offsets[e + 1], M));
-            }
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int32_t y = __shfl_up_sync(0xffffffffu, h, d);
-                if (lane >= d) h = max(h, y);
-            }
-            h = max(h, before);
-            const int32_t prev = __shfl_up_sync(0xffffffffu, h, 1);
-            l = min(max(l, lane ? prev : before), h);
-            if (e0 == 0) head = __shfl_sync(0xffffffffu, l, 0);
-            before = __shfl_sync(0xffffffffu, h, 31);
-            const int32_t rows = e < p.E ? h - l : 0, tiles = (rows + p.nt - 1) / p.nt;
-            int32_t x = tiles;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int32_t y = __shfl_up_sync(0xffffffffu, x, d);
-                if (lane >= d) x += y;
-            }
-            const uint32_t with = __ballot_sync(0xffffffffu, rows > 0);
-            if (rows > 0) {  // equal tiles of at most nt, multiples of 16 (a pair's: of 32)
-                constexpr int kStep = PAIR ? 32 : 16;
-                const int i = count + __popc(with & ((1u << lane) - 1));
-                *(int4 *)(tab + i) = make_int4(sum + x - tiles, l, h, ((rows + tiles - 1) / tiles + kStep - 1) & ~(kStep - 1));
-                tab_id[i] = e;
-            }
-            sum += __shfl_sync(0xffffffffu, x, 31);
-            count += __popc(with);
-        }
+        int32_t sum, count, head, tail;
+        list_tiles<PAIR ? 32 : 16>(p, tab, tab_id, lane, sum, count, head, tail);
         if (lane == 0) {
-            tab[count].start = sum;
             s_experts = count;
             s_head = head;
-            s_tail = before;
+            s_tail = tail;
         }
-        __syncwarp();
         if (first < sum * p.wtiles) {  // the first tile at once; the others follow from the last warp
             const Tile y = find_tile<MODE>(p, tab, tab_id, count, first, rank);
             if (lane == 0) tile_ring[0] = make_int4(y.e, y.row0, y.rows, y.n0);
@@ -452,14 +310,14 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
             // a pair's CTA loads its half of the tokens
             const int part = PAIR ? mma_tokens(x) / 2 : x.rows, row = x.row0 + (PAIR ? (int)rank * part : 0);
             const int units = (part + 15) >> 4;
-            const uint32_t bytes = warp == 0 ? kMxRowsW * 128 : units * 2048;
+            const uint32_t bytes = warp == 0 ? kTileRowsW * 128 : units * 2048;
             if (one) {
                 for (int32_t kb = 2 * sb_lo; kb < kb_hi; ++kb) {
                     if (!wait_lane(empty + 8 * s, sp, &abort_flag, p, kStatusTimeoutFree)) {
                         ok = false;
                         break;
                     }
-                    const uint32_t d = data0 + s * p.stage_bytes + (warp == 0 ? 0 : kMxRowsW * 128), db = arrives + 8 * s;
+                    const uint32_t d = data0 + s * p.stage_bytes + (warp == 0 ? 0 : kTileRowsW * 128), db = arrives + 8 * s;
                     if ((int32_t)it != p.dbg_skip) {
                         bar_expect_tx(db, bytes);
                         if (warp == 0) {
@@ -515,7 +373,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
                     if (atoms > 2) copy_scales<PAIR>(sc + 12 + 8 * w, src + 2 * kMxAtom / 16);
                     src += kMxAtom * atoms / 16;
                 }
-                const uint64_t wd = desc0 + at, ad = wd + kMxRowsW * 128 / 16;
+                const uint64_t wd = desc0 + at, ad = wd + kTileRowsW * 128 / 16;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const uint32_t w = j >> 1, sf = (j & 1) * 2;
@@ -570,7 +428,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
         const uint32_t turn = (warp - kMxScaleWarp0) >> 1;
         const int part = (warp - kMxScaleWarp0) & 1, parts = part == 0 ? 1 : atoms - 1;
         const int64_t pitch = part == 0 ? p.w_lds : p.a_lds;
-        const uint32_t raw = raw0 + turn * p.raw_bytes + part * kMxRowsW * 16 + lane * 16;
+        const uint32_t raw = raw0 + turn * p.raw_bytes + part * kTileRowsW * 16 + lane * 16;
         int32_t lt = first, lsb = sb_lo;  // the stage to load next
         const uint8_t *base = nullptr;    // its rows: from `base` on, `pitch` apart, `rows` of them
         int rows = 0;
@@ -618,7 +476,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         w[i][c][0] = w[i][c][1] = w[i][c][2] = w[i][c][3] = 0;
-                        if (i < parts && (part == 0 || 128 * i + 32 * c < p.nt)) lds128(raw + i * kMxRowsW * 16 + c * 512, w[i][c]);
+                        if (i < parts && (part == 0 || 128 * i + 32 * c < p.nt)) lds128(raw + i * kTileRowsW * 16 + c * 512, w[i][c]);
                     }
             }
             if (mine && st >= 2) {
@@ -684,7 +542,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
                 if constexpr (SPLIT) {  // this CTA's part of the sums: [token][row of W] over the stages, which are all read
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(data0 + ((c0 + i) * kMxRowsW + row) * 4), "f"(v[i]) : "memory");
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(data0 + ((c0 + i) * kTileRowsW + row) * 4), "f"(v[i]) : "memory");
                 } else {
                     store_chunk<ACT, T>(p, v, x, c0, nn, bias, patch, lane);
                 }
@@ -723,10 +581,10 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
 #pragma unroll
                 for (int r = 0; r < 8; ++r)
                     if (r < p.splits) {
-                        const uint32_t at = in_cta(data0 + (c0 * kMxRowsW + row) * 4, r);
+                        const uint32_t at = in_cta(data0 + (c0 * kTileRowsW + row) * 4, r);
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[r][i]) : "r"(at + i * kMxRowsW * 4) : "memory");
+                            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[r][i]) : "r"(at + i * kTileRowsW * 4) : "memory");
                     }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -758,7 +616,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx_gemm_kernel(const __grid_con
     }
     fence_before();
     __syncwarp();
-    if constexpr (MODE != MX_ONE) cluster_sync();  // nothing of this CTA is read or signalled any more
+    if constexpr (MODE != TILE_ONE) cluster_sync();  // nothing of this CTA is read or signalled any more
     else __syncthreads();
     if (warp == 3) {
         fence_after();
@@ -781,18 +639,18 @@ cudaError_t launch_mode(const MxParams &p, int grid, size_t smem, cudaStream_t s
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = MODE == MX_SPLIT ? p.splits : 2;
+    at[1].val.clusterDim.x = MODE == TILE_SPLIT ? p.splits : 2;
     at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
-    cfg.numAttrs = MODE == MX_ONE ? 1 : 2;
+    cfg.numAttrs = MODE == TILE_ONE ? 1 : 2;
     e = cudaLaunchKernelEx(&cfg, mx_gemm_kernel<ACT, T, MODE>, p);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 template <int ACT, typename T>
 cudaError_t launch_act(const MxParams &p, int grid, size_t smem, cudaStream_t s) {
-    if (p.mode == MX_SPLIT) return launch_mode<ACT, T, MX_SPLIT>(p, grid, smem, s);
-    if (p.mode == MX_PAIR) return launch_mode<ACT, T, MX_PAIR>(p, grid, smem, s);
-    return launch_mode<ACT, T, MX_ONE>(p, grid, smem, s);
+    if (p.mode == TILE_SPLIT) return launch_mode<ACT, T, TILE_SPLIT>(p, grid, smem, s);
+    if (p.mode == TILE_PAIR) return launch_mode<ACT, T, TILE_PAIR>(p, grid, smem, s);
+    return launch_mode<ACT, T, TILE_ONE>(p, grid, smem, s);
 }
 
 }  // namespace

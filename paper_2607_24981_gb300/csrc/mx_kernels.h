@@ -55,15 +55,6 @@ constexpr int kMxMaxExperts = 1024;
 bool mx_gemm_form(const MxGemmProblem &g, int32_t sms, int32_t (&form)[3]);
 cudaError_t launch_mx_gemm(const MxGemmProblem &p, cudaStream_t s);
 
-// How experts are taken and weighted beside plain softmax (ilw_moe_scores_t).
-struct RouteScores {
-    int32_t score;             // ILW_SCORE_*
-    const float *bias;         // [E] or NULL
-    int32_t groups, top_groups, group_best, group_size;
-    int32_t lanes_per_group;   // of a warp whose lanes hold consecutive experts of one group each; 0: they do not
-    Divisor per_group;         // by group_size
-    float scale;
-};
 struct MoeRouteParams {
     const void *logits;
     int32_t form;
@@ -75,12 +66,26 @@ struct MoeRouteParams {
     int32_t *source;   // [T k]
     int32_t *slot;     // [T, k]
     int32_t *counts;   // workspace [chunks, E]
+};
+// How experts are taken and weighted beside plain softmax (ilw_moe_scores_t).
+struct RouteScores {
+    int32_t score;             // ILW_SCORE_*
+    const float *bias;         // [E] or NULL
+    int32_t groups, top_groups, group_best, group_size;
+    int32_t lanes_per_group;   // of a warp whose lanes hold consecutive experts of one group each; 0: they do not
+    Divisor per_group;         // by group_size
+    float scale;
+};
+struct MoeScoredParams : MoeRouteParams {
     RouteScores scores;
 };
 constexpr int kRouteMaxExperts = ILW_MOE_MAX_EXPERTS, kRouteMaxTop = ILW_MOE_MAX_TOP;
 size_t moe_route_workspace(int32_t T, int32_t E);
-cudaError_t launch_moe_route(const MoeRouteParams &p, cudaStream_t s);         // (scores is not read)
-cudaError_t launch_moe_route_scored(const MoeRouteParams &p, cudaStream_t s);  // (fills in what follows from groups and E)
+cudaError_t launch_moe_route(const MoeRouteParams &p, cudaStream_t s);
+cudaError_t launch_moe_route_scored(const MoeScoredParams &p, cudaStream_t s);  // (fills in what follows from groups and E)
+// For the latter: whether one CTA takes all, and the order from chunks' counts (chunks of 256 or 512 tokens).
+bool moe_route_in_one(int32_t T, int32_t E);
+cudaError_t launch_moe_place(const MoeRouteParams &p, int32_t chunk, cudaStream_t s);
 constexpr int kRouteMaxGroups = ILW_MOE_MAX_GROUPS;
 
 struct MoeCombineParams {

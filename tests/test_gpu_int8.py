@@ -385,3 +385,101 @@ def test_experts_feed_forward(ilw, T, act, dtype):
             check_product(y[s], ilw.I8Tensor(q.codes[s], q.scales[s]), ilw.I8Tensor(ffn.w2.codes[e], ffn.w2.scales[e]), None, "none")
     assert torch.equal(got, ilw.moe_combine(y, r.slot, r.weight, residual=x))
     ilw.device_status()
+
+
+# ---------------------------------------------------------------------------- every form of the products
+def form_of(ilw, M, N, K, experts, act, dtype):
+    """What the library takes for a product with contiguous operands on this GPU: "one" CTA a tile, "pair" of SMs, "few" tokens, or how many
+    CTAs share a tile's K; and the tokens of a tile."""
+    import ctypes
+
+    from paper_2607_24981_gb300 import int8, mx
+
+    got, ld, wide = (ctypes.c_int32 * 3)(), -(-K // 16) * 16, N // 2 if act == "silu_gate" else N
+    y_form = {torch.float32: 232, torch.float16: 216, torch.bfloat16: 217}[dtype]
+    rc = ilw.lib().ilwdetr_debug_i8_form(int8.gemm_struct(1 << 20, ld, 1 << 20, 1 << 20, ld, N * ld, 1 << 20, 0, 1 << 20 if experts else 0, M, N, K, experts or 1,
+                                                          mx.ACTS[act], y_form, 1 << 20, wide), 0, got)
+    assert rc == 0, ilw.lib().ilwdetr_last_error()
+    return ["one", got[1], "pair", "few"][got[0]], got[2]
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("form,M,N,K,bias", [
+    ("pair", 5000, 2600, 500, True), ("pair", 3001, 1712, 1030, False), ("pair", 3001, 514, 1030, True), ("pair", 700, 1000, 1030, False), ("pair", 200, 1712, 2100, True),
+    ("pair", 1500, 1000, 4200, True), (2, 16, 5000, 8200, True), (2, 40, 5000, 4200, False), (2, 100, 5000, 4200, True), (4, 130, 1000, 2100, True), (4, 333, 514, 2100, False),
+    (4, 700, 514, 4200, True), (8, 40, 1000, 8200, True), (8, 60, 1000, 4200, False), (8, 333, 130, 8200, True), ("one", 130, 1712, 500, True), ("one", 700, 1712, 200, False),
+    ("one", 5000, 514, 200, True), ("few", 5, 1000, 500, True), ("few", 40, 260, 300, False), ("few", 8, 5000, 4200, True), ("few", 3, 34, 9000, True)])
+def test_every_form_with_every_activation(ilw, form, M, N, K, bias, dtype):
+    A, W = made(ilw, 1, M, K), made(ilw, 3, N, K, weights=True)
+    b = torch.randn(N, device="cuda", generator=generator(5)) if bias else None
+    for act in ("none", "gelu", "silu_gate"):
+        assert form_of(ilw, M, N, K, None, act, dtype)[0] == form
+        got = ilw.i8_linear(A, W, b, act=act, out_dtype=dtype)
+        check_product(got, A, W, b, act)
+        assert all(torch.equal(got, ilw.i8_linear(A, W, b, act=act, out_dtype=dtype)) for _ in range(2))
+    ilw.device_status()
+
+
+@pytest.mark.parametrize("M,N", [(1200, 2600), (1201, 2601), (333, 9000), (5001, 1026), (97, 20010)])
+@pytest.mark.parametrize("K", [2200, 65])
+def test_tiles_that_end_anywhere(ilw, M, N, K):
+    """Columns and rows past the last tile, blocks of K that end in each half; results in rows that take wide stores and such that do not."""
+    A, W = made(ilw, 1, M, K), made(ilw, 3, N, K, weights=True)
+    for pad, dtype in ((0, torch.bfloat16), (3, torch.float16), (-N % 8, torch.float16)):
+        wide = torch.full((M, N + pad + 8), 9.0, device="cuda", dtype=dtype)
+        got = ilw.i8_linear(A, W, out=wide[:, :N])
+        check_product(got, A, W, None, "none")
+        got.fill_(9.0)
+        assert bool((wide == 9).all())
+    ilw.device_status()
+
+
+@pytest.mark.parametrize("act,dtype", [("none", torch.float32), ("gelu", torch.bfloat16), ("silu_gate", torch.float16)])
+@pytest.mark.parametrize("form,counts,N,K", [
+    ("pair", [700, 0, 1, 333, 1024, 225, 95], 2304, 2600), ("pair", [700, 0, 1, 333, 1024, 225, 95], 1704, 600), ("few", [1, 0, 9], 300, 4200), ("few", [0, 2, 130, 0], 140, 8192),
+    ("one", [5, 0, 1, 2] * 4, 1000, 700), ("one", [100] * 9, 514, 700), ("one", [40, 3, 0, 60], 2000, 1000), (4, [60, 0, 70], 520, 4200)])
+def test_every_form_by_expert(ilw, form, counts, N, K, act, dtype):
+    off, E = np.r_[0, np.cumsum(counts)], len(counts)
+    M = int(off[-1])
+    assert form_of(ilw, M, N, K, E, act, dtype)[0] == form
+    A, W = made(ilw, 1, M, K), made(ilw, 3, E * N, K, weights=True)
+    W = ilw.I8Tensor(W.codes.unflatten(0, (E, N)), W.scales.view(E, N))
+    b = torch.randn((E, N), device="cuda", generator=generator(5))
+    got = ilw.i8_grouped_linear(A, W, torch.from_numpy(off.astype(np.int32)).cuda(), b, act=act, out_dtype=dtype)
+    for e in range(E):
+        if counts[e]:
+            s = slice(int(off[e]), int(off[e + 1]))
+            check_product(got[s], ilw.I8Tensor(A.codes[s], A.scales[s]), ilw.I8Tensor(W.codes[e], W.scales[e]), b[e], act)
+    ilw.device_status()
+
+
+@pytest.mark.parametrize("form,M,N,K", [("one", 130, 1712, 500), (8, 40, 1000, 8200), (4, 130, 1000, 2100), (2, 16, 5000, 8200), ("pair", 5000, 2600, 500), ("pair", 3001, 514, 1030)])
+def test_every_form_gives_up_a_bounded_wait(ilw, form, M, N, K):
+    """A load that never comes (a debug hook skips one and shortens the waits): the kernel reports it and ends, and the next call is right."""
+    assert form_of(ilw, M, N, K, None, "none", torch.bfloat16)[0] == form
+    A, W = made(ilw, 1, M, K), made(ilw, 3, N, K, weights=True)
+    want = ilw.i8_linear(A, W)
+    assert ilw.lib().ilwdetr_debug_gemm_wait(0, 20_000_000) == 0
+    try:
+        ilw.i8_linear(A, W)
+        with pytest.raises(ilw.IlwError, match="wait"):
+            ilw.device_status()
+    finally:
+        assert ilw.lib().ilwdetr_debug_gemm_wait(-1, 0) == 0
+    assert torch.equal(ilw.i8_linear(A, W), want)
+    ilw.device_status()
+
+
+def test_two_products_at_once(ilw):
+    """Calls on two streams, each larger than half of the GPU, and a chain on each that reads what the call before it wrote."""
+    A, W = made(ilw, 1, 3001, 1030), made(ilw, 3, 1712, 1030, weights=True)
+    V = made(ilw, 7, 514, 1712, weights=True)
+    want = ilw.i8_linear(ilw.i8_quantize(ilw.i8_linear(A, W, act="gelu")), V)
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], []
+    for s in streams:
+        with torch.cuda.stream(s):
+            got += [ilw.i8_linear(ilw.i8_quantize(ilw.i8_linear(A, W, act="gelu")), V) for _ in range(4)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, want) for g in got)
+    ilw.device_status()

@@ -79,6 +79,28 @@ def test_product_checks(L):  # noqa: F811
     refused(L, g(Y=0x500001), -1, b"Y")
 
 
+def test_form_checks(L):  # noqa: F811
+    from paper_2607_24981_gb300 import int8
+
+    def f(M, N, K, experts=0, sms=152, out=True):
+        got, ld = (ctypes.c_int32 * 3)(), -(-K // 16) * 16
+        p = int8.gemm_struct(0x100000, ld, 0x200000, 0x300000, ld, N * ld, 0x400000, 0, 0x600000 if experts else 0, M, N, K, experts or 1, 0, 217, 0x500000, N)
+        rc = L.ilwdetr_debug_i8_form(p, sms, got if out else None)
+        return rc if rc else tuple(got)
+
+    assert f(1, 4096, 4096) == (3, 1, 8) and f(8192, 8192, 8192) == (2, 1, 192)
+    assert f(64, 4096, 4096)[:2] == (1, 4) and f(32, 4096, 2048, 64)[0] == 3
+    for M in (1, 7, 100, 3000, 1 << 20):
+        for N in (1, 130, 5000):
+            for K in (1, 129, 9000, (1 << 17) - 1):
+                for experts in (0, 1, 13, 1024):
+                    got = f(M, N, K, experts)
+                    assert got[0] in (0, 1, 2, 3) and got[1] in (1, 2, 4, 8) and 8 <= got[2] <= 192
+    refused(L, f(0, 10, 10), -1, b"empty")
+    refused(L, f(10, 10, 10, out=False), -1, b"NULL")
+    refused(L, f(10, 10, 10, sms=-1), -1, b"sms")
+
+
 def scores(size=None, score=1, groups=8, top_groups=4, group_best=2, scale=1.0, bias=0x100000):
     """An ilw_moe_scores_t."""
     s = struct.Struct("@IiiiifP")
