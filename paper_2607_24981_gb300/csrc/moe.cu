@@ -35,45 +35,6 @@ template <> __device__ __forceinline__ float from_f<float>(float v) { return v; 
 template <> __device__ __forceinline__ __half from_f<__half>(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
-// n rows of the logits from token t0 on to shared memory, by one warp; 16 bytes of them at a time where rows allow it
-// (65536 rows of 128: 30 us, else 82; 257 rows 11 and 21).
-template <typename T, int S>
-__device__ __forceinline__ void load_rows(const MoeRouteParams &p, int32_t t0, int n, float *rows, bool wide, int lane) {
-    constexpr int V = 16 / sizeof(T), kWords = kGroups * S, kStride = kWords + 4;
-    const float none = __int_as_float(0xff800000);
-    const T *x = (const T *)p.logits + (int64_t)t0 * p.ld;
-    if (wide) {
-        struct alignas(16) Pack {
-            T v[V];
-        };
-        for (int c = lane * V; c < kWords; c += 32 * V) {
-#pragma unroll 8
-            for (int t = 0; t < n; ++t) {
-                Pack y;
-                if (c < p.E) y = *(const Pack *)(x + t * p.ld + c);
-#pragma unroll
-                for (int j = 0; j < V; j += 4)
-                    *(float4 *)(rows + t * kStride + c + j) =
-                        c < p.E ? make_float4(logit(to_f(y.v[j])), logit(to_f(y.v[j + 1])), logit(to_f(y.v[j + 2])), logit(to_f(y.v[j + 3])))
-                                : make_float4(none, none, none, none);
-            }
-        }
-    } else {
-        for (int c = lane; c < kWords; c += 32) {
-#pragma unroll 8
-            for (int t = 0; t < n; ++t) rows[t * kStride + c] = c < p.E ? logit(to_f(x[t * p.ld + c])) : none;
-        }
-    }
-}
-
-// A row past the last token (the rest of its warp has one): nothing to select from.
-template <int L, int S>
-__device__ __forceinline__ void clear_row(float *row, bool is_token) {
-    if (!is_token)
-        for (int c = threadIdx.x % L; c < kGroups * S; c += L) row[c] = __int_as_float(0xff800000);
-    __syncwarp();
-}
-
 // exp(x - best) of 4 N values, added up in four parts and pairwise.
 template <int N>
 __device__ __forceinline__ float4 sum_exp(const float4 *x, float best) {

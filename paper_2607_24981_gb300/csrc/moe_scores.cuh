@@ -7,12 +7,12 @@
 // Without a bias the order of c is that of the logits, and no score is computed to find it.
 //
 // Who is taken is decided as in 64 bits: one rounding of 32 bits could exchange two experts, and a token would go elsewhere.  c is first computed
-// in fp32, and its error is known: s has a relative error below 2^-22 (and in the softmax, where x - max is rounded, one of
-// |x - max| 2^-24, which times exp(x - max) stays below 2^-25), so c is off by less than 2^-21 min(1, |c| + max|bias|) + 2^-23 |c| (+ 2^-24).
-// Where two of those that are taken, or one and another that is not, lie closer than that, and are not equal logits with equal biases, the row
-// is done again in 64 bits; of random logits and biases that is one row in some thousand.
-//
-// A warp takes a token, each lane PER consecutive experts.
+// in fp32 with the fast exponential and reciprocal, and its error is bounded: of s by a relative 2^-21.5 (2^-22.5 and 2^-23 of the two
+// functions, roundings) and, for the rounding of an exponent y = x or x - max, |y| 2^-24 relative to exp(-|y|), which stays below
+// 2^-25; of the sum with the bias by 2^-24 |c|.  So c is off by less than doubt() = 2^-20 min(1, |c| + max|bias|) + 2^-23 |c| + 2^-24.
+// Where two of those that are taken, or one and another that is not, lie closer than their doubts, and are not equal logits with equal biases,
+// they are ordered again in 64 bits by the whole warp (one row in some hundred of random logits and biases), and where the groups are in doubt the
+// whole row is done again.
 #pragma once
 #include <cstdint>
 
@@ -23,154 +23,111 @@
 namespace ilw {
 namespace {
 
-__device__ __forceinline__ float none_of(float) { return __int_as_float(0xff800000); }
-__device__ __forceinline__ double none_of(double) { return __longlong_as_double(0xfff0000000000000ll); }
-__device__ __forceinline__ float exp_of(float x) { return expf(x); }
-__device__ __forceinline__ double exp_of(double x) { return exp(x); }
+constexpr float kNone = -__builtin_huge_valf();
+
+// ---- the exact way: a warp a token, each lane PER consecutive experts, in 64 bits
+
+__device__ __forceinline__ double none64() { return __longlong_as_double(0xfff0000000000000ll); }
 // exp(x - best), where both may be infinite
-template <typename V> __device__ __forceinline__ V exp_below(float x, float best) { return x == best ? V(1) : exp_of(V(x) - V(best)); }
+__device__ __forceinline__ float exp_below(float x, float best) { return x == best ? 1.0f : expf(x - best); }
+__device__ __forceinline__ double exp_below64(float x, float best) { return x == best ? 1.0 : exp((double)x - (double)best); }
 // 1 / (1 + exp(-x)).  fp32: by the exponential that cannot overflow, for scores below its normal range.  64 bits, which only compare: as it is
 // written, so that sums that are equal but for roundings (of the scores of x and -x) fall as plain operations let them.
-template <typename V> __device__ __forceinline__ V sigmoid(float x);
-template <> __device__ __forceinline__ float sigmoid<float>(float x) {
+__device__ __forceinline__ float sigmoid(float x) {
     const float e = expf(-fabsf(x));
     return (x >= 0.0f ? 1.0f : e) / (1.0f + e);
 }
-template <> __device__ __forceinline__ double sigmoid<double>(float x) { return 1.0 / (1.0 + exp(-(double)x)); }
+__device__ __forceinline__ double sigmoid64(float x) { return 1.0 / (1.0 + exp(-(double)x)); }
 
-// Values as unsigned numbers of the same order, 0 for -inf and NaN: their largest in a warp, by whole-word reductions.
-__device__ __forceinline__ uint32_t order_key(float v) {
-    const uint32_t b = __float_as_uint(v + 0.0f);  // (-0 is 0)
-    return v > none_of(v) ? (b & 0x80000000u ? ~b : b | 0x80000000u) : 0u;
-}
+// A value as an unsigned number of the same order, 0 for -inf and NaN; the largest in a warp.
 __device__ __forceinline__ uint64_t order_key(double v) {
-    const uint64_t b = (uint64_t)__double_as_longlong(v + 0.0);
-    return v > none_of(v) ? (b >> 63 ? ~b : b | 1ull << 63) : 0ull;
+    const uint64_t b = (uint64_t)__double_as_longlong(v + 0.0);  // (-0 is 0)
+    return v > none64() ? (b >> 63 ? ~b : b | 1ull << 63) : 0ull;
 }
-__device__ __forceinline__ uint32_t warp_max(uint32_t k) { return __reduce_max_sync(0xffffffffu, k); }
 __device__ __forceinline__ uint64_t warp_max(uint64_t k) {
     const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(k >> 32));
     const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(k >> 32) == hi ? (uint32_t)k : 0u);
     return (uint64_t)hi << 32 | lo;
 }
-__device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
-__device__ __forceinline__ float key_value(uint64_t) { return 0.0f; }  // (not asked for)
-template <typename V> struct Key { typedef uint32_t type; };
-template <> struct Key<double> { typedef uint64_t type; };
+__device__ __forceinline__ double key_value(uint64_t k) { return __longlong_as_double((long long)(k >> 63 ? k & ~(1ull << 63) : ~k)); }
 
-// How far c may be off (see above).
-__device__ __forceinline__ float doubt(const RouteScores &q, float c, float bias_max) {
-    const float a = fabsf(c);
-    return fminf(1.0f, a + bias_max) * 4.76837158e-07f + a * 1.1920929e-07f + (q.score == ILW_SCORE_SOFTMAX ? 5.96046448e-08f : 0.0f);
+// Scores of a row in 64 bits: of its logit x, given the row's largest and, for the softmax, its denominator.
+struct Exact {
+    int32_t score;
+    float best;
+    double sum;
+    __device__ __forceinline__ double operator()(float x) const { return score == ILW_SCORE_SIGMOID ? sigmoid64(x) : exp_below64(x, best) / sum; }
+};
+template <typename T> __device__ __forceinline__ Exact exact_scores(const MoeScoredParams &p, const T *row, int lane) {
+    Exact s = {p.scores.score, kNone, 0.0};
+    if (s.score == ILW_SCORE_SIGMOID) return s;
+    for (int e = lane; e < p.E; e += 32) s.best = fmaxf(s.best, logit(to_f(row[e])));
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) s.best = fmaxf(s.best, __shfl_xor_sync(0xffffffffu, s.best, d));
+    for (int e = lane; e < p.E; e += 32) {
+        const float x = logit(to_f(row[e]));
+        if (x > kNone) s.sum += exp_below64(x, s.best);
+    }
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) s.sum += __shfl_xor_sync(0xffffffffu, s.sum, d);
+    return s;
 }
 
-// The two largest of (a1, a2) and (b1, b2), each pair in order.
-template <typename V> __device__ __forceinline__ void merge2(V &a1, V &a2, V b1, V b2) {
-    const V low = a1 < b1 ? a1 : b1;
-    a2 = a2 > b2 ? a2 : b2;
-    a2 = a2 > low ? a2 : low;
-    a1 = a1 > b1 ? a1 : b1;
-}
-
-// The experts of a token, the j-th in lane j's `mine` (-1: none); false if fp32 cannot tell (V double: never).  x: this lane's logits, -inf where
-// no expert is to be taken; `best` their row's largest; `sum` their softmax's denominator.
-template <typename V, int PER>
-__device__ __forceinline__ bool choose(const MoeScoredParams &p, const float (&x)[PER], float best, V sum, float bias_max, int lane, int32_t &mine) {
-    constexpr bool kCheck = sizeof(V) == 4;
+// The experts of a token, the j-th in lane j (-1: none): all of it in 64 bits, each lane PER consecutive experts.  (Comparisons are of keys: those of
+// 64-bit numbers would be the slower part.)
+template <typename T, int PER>
+__device__ __noinline__ int32_t choose_exactly(const MoeScoredParams &p, const T *row, int lane) {
     const RouteScores &q = p.scores;
-    const V none = none_of(V());
     const int e0 = lane * PER;
-    V c[PER];
+    const Exact score = exact_scores(p, row, lane);
+    uint64_t key[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        c[i] = V(x[i]);
-        if (q.bias) {
-            const V s = q.score == ILW_SCORE_SIGMOID ? sigmoid<V>(x[i]) : exp_below<V>(x[i], best) / sum;
-            const V v = s + V(e0 + i < p.E ? __ldg(q.bias + e0 + i) : 0.0f);
-            c[i] = x[i] > none_of(0.0f) && v > none ? v : none;
-        }
+        const float x = e0 + i < p.E ? logit(to_f(row[e0 + i])) : kNone;
+        key[i] = x > kNone ? order_key(q.bias ? score(x) + (double)__ldg(q.bias + e0 + i) : (double)x) : 0;
     }
-    uint32_t groups = 0xffffffffu;  // those that stay
-    bool sure = true;
     if (q.groups > 1) {
-        V t1 = none, t2 = none;  // the two largest of group `lane`
-        if (q.lanes_per_group) {  // a lane's experts are of one group, whose lanes are a power of two
+        uint64_t mine1 = 0, mine2 = 0;  // the two largest of group `lane`
+        for (int g = 0; g < q.groups; ++g) {
+            uint64_t m1 = 0, m2 = 0;  // this lane's two largest of the group
+            const int lo = g * q.group_size - e0;
 #pragma unroll
-            for (int i = 0; i < PER; ++i) merge2(t1, t2, c[i], none);
-            for (int d = 1; d < q.lanes_per_group; d <<= 1) merge2(t1, t2, __shfl_xor_sync(0xffffffffu, t1, d), __shfl_xor_sync(0xffffffffu, t2, d));
-            t1 = __shfl_sync(0xffffffffu, t1, lane * q.lanes_per_group);
-            t2 = __shfl_sync(0xffffffffu, t2, lane * q.lanes_per_group);
-        } else {
-            for (int g = 0; g < q.groups; ++g) {
-                V a1 = none, a2 = none;
-                const int lo = g * q.group_size - e0;
-#pragma unroll
-                for (int i = 0; i < PER; ++i) merge2(a1, a2, i >= lo && i < lo + q.group_size ? c[i] : none, none);
-#pragma unroll
-                for (int d = 1; d < 32; d <<= 1) merge2(a1, a2, __shfl_xor_sync(0xffffffffu, a1, d), __shfl_xor_sync(0xffffffffu, a2, d));
-                if (lane == g) t1 = a1, t2 = a2;
-            }
+            for (int i = 0; i < PER; ++i)
+                if (i >= lo && i < lo + q.group_size) {
+                    m2 = max(m2, min(m1, key[i]));
+                    m1 = max(m1, key[i]);
+                }
+            const uint64_t t1 = warp_max(m1);
+            const int holder = __ffs(__ballot_sync(0xffffffffu, m1 == t1)) - 1;
+            const uint64_t t2 = warp_max(lane == holder ? m2 : m1);
+            if (lane == g) mine1 = t1, mine2 = t2;
         }
-        V rank = t1;
-        if (q.group_best == 2) {  // (of logits: their scores' sum, the softmax's without its denominator)
-            if (!q.bias) {
-                const bool sig = q.score == ILW_SCORE_SIGMOID;
-                rank = t1 > none ? (sig ? sigmoid<V>((float)t1) : exp_below<V>((float)t1, best)) + (t2 > none ? (sig ? sigmoid<V>((float)t2) : exp_below<V>((float)t2, best)) : V(0))
-                                 : none;
-            } else if (t2 > none) {
-                rank = t1 + t2;
-            }
+        uint64_t rank = mine1;
+        if (q.group_best == 2 && mine1) {  // (of logits: their scores' sum)
+            if (!q.bias) rank = order_key(score((float)key_value(mine1)) + (mine2 ? score((float)key_value(mine2)) : 0.0));
+            else if (mine2) rank = order_key(key_value(mine1) + key_value(mine2));
         }
-        if (lane >= q.groups) rank = none;
         int place = 0;  // of this lane's group among all
         for (int g = 0; g < q.groups; ++g) {
-            const V other = __shfl_sync(0xffffffffu, rank, g);
+            const uint64_t other = __shfl_sync(0xffffffffu, rank, g);
             place += other > rank || (other == rank && g < lane);
         }
-        groups = __ballot_sync(0xffffffffu, lane < q.groups && place < q.top_groups && rank > none);
-        if (kCheck && (q.bias || q.group_best == 2)) {
-            // the last group that stays and the first that does not; who lies close to the other side's, and is not its equal, is in doubt
-            const uint32_t last = __ballot_sync(0xffffffffu, lane < q.groups && place == q.top_groups - 1 && rank > none);
-            const uint32_t next = __ballot_sync(0xffffffffu, lane < q.groups && place == q.top_groups && rank > none);
-            if (last && next) {
-                const bool stays = groups >> lane & 1;
-                const int of = __ffs(stays ? next : last) - 1;
-                // (a rank without a bias: one or two scores of a relative error, the softmax's without their denominator)
-                const float off = q.bias ? doubt(q, (float)t1, bias_max) + (q.group_best == 2 && t2 > none ? doubt(q, (float)t2, bias_max) : 0.0f) + fabsf((float)rank) * 1.1920929e-07f
-                                         : (float)rank * 4.76837158e-07f + (q.score == ILW_SCORE_SOFTMAX ? 1.1920929e-07f : 0.0f);
-                const V other = __shfl_sync(0xffffffffu, rank, of), o1 = __shfl_sync(0xffffffffu, t1, of), o2 = __shfl_sync(0xffffffffu, t2, of);
-                const float other_off = __shfl_sync(0xffffffffu, off, of);
-                const bool close = rank > none && fabsf((float)(rank - other)) <= 2.0f * (off + other_off);
-                if (__any_sync(0xffffffffu, close && !(!q.bias && t1 == o1 && (t2 == o2 || q.group_best == 1)))) sure = false;
-            }
-        }
-    }
-    typename Key<V>::type key[PER];
+        const uint32_t stay = __ballot_sync(0xffffffffu, lane < q.groups && place < q.top_groups && rank);
 #pragma unroll
-    for (int i = 0; i < PER; ++i) key[i] = (q.groups == 1 || (groups >> min(q.per_group.div(e0 + i), 31u) & 1)) && e0 + i < p.E ? order_key(c[i]) : 0;
-    mine = -1;
-    float last = 0.0f, last_x = 0.0f, last_b = 0.0f;  // c, logit and bias of the one taken before
+        for (int i = 0; i < PER; ++i)
+            if (e0 + i < p.E && !(stay >> q.per_group.div(e0 + i) & 1)) key[i] = 0;
+    }
+    int32_t mine = -1;
     for (int j = 0; j < p.k; ++j) {
-        typename Key<V>::type m = key[0];
+        uint64_t m = key[0];
         int at = 0;
 #pragma unroll
         for (int i = 1; i < PER; ++i)
             if (key[i] > m) m = key[i], at = i;
-        const typename Key<V>::type top = warp_max(m);
-        if (top == 0) return sure;
+        const uint64_t top = warp_max(m);
+        if (top == 0) break;
         const int src = __ffs(__ballot_sync(0xffffffffu, m == top)) - 1;
         const int32_t e = __shfl_sync(0xffffffffu, e0 + at, src);
-        if constexpr (kCheck) {
-            if (q.bias) {
-                float xe = 0.0f;
-#pragma unroll
-                for (int i = 0; i < PER; ++i) xe = i == at ? x[i] : xe;
-                xe = __shfl_sync(0xffffffffu, xe, src);
-                const float v = key_value(top), be = __ldg(q.bias + e);
-                if (j > 0 && last - v <= doubt(q, last, bias_max) + doubt(q, v, bias_max) && !(xe == last_x && be == last_b)) sure = false;
-                last = v, last_x = xe, last_b = be;
-            }
-        }
         if (lane == j) mine = e;
         if (lane == src) {
 #pragma unroll
@@ -178,104 +135,350 @@ __device__ __forceinline__ bool choose(const MoeScoredParams &p, const float (&x
                 if (i == at) key[i] = 0;
         }
     }
-    if constexpr (kCheck) {
-        if (q.bias) {  // is the last one taken clear of all that are left
-            bool close = false;
-#pragma unroll
-            for (int i = 0; i < PER; ++i)
-                if (key[i] != 0) {
-                    const float v = key_value(key[i]);
-                    close |= last - v <= doubt(q, last, bias_max) + doubt(q, v, bias_max) && !(x[i] == last_x && __ldg(q.bias + e0 + i) == last_b);
-                }
-            if (__any_sync(0xffffffffu, close)) sure = false;
-        }
-    }
-    return sure;
-}
-
-// The same in 64 bits, from the logits on.
-template <int PER>
-__device__ __noinline__ int32_t choose_exactly(const MoeScoredParams &p, const float *xs, float best, int lane) {
-    float x[PER];
-    double sum = 0.0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        x[i] = xs[i];
-        if (p.scores.score == ILW_SCORE_SOFTMAX && x[i] > none_of(0.0f)) sum += exp_below<double>(x[i], best);
-    }
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    int32_t mine;
-    choose<double, PER>(p, x, best, sum, 0.0f, lane, mine);
     return mine;
 }
 
-// Lane j: the weight of expert `e`, the j-th taken (-1: 0), whose logit is x.
-__device__ __forceinline__ float weight_of(const MoeScoredParams &p, int32_t e, float x, float best, float sum) {
-    const bool on = e >= 0;
-    float s = 0.0f;
-    if (p.scores.score == ILW_SCORE_SOFTMAX) {
-        if (on) s = exp_below<float>(x, best);
-        if (p.renormalize) {
-            sum = s;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-        }
-    } else if (p.renormalize) {
-        // exp(min(x, 0)) / (1 + exp(-|x|)), all times exp(-m) for the largest m of min(x, 0): scores too small for fp32 keep their ratios
-        const float low = on ? fminf(x, 0.0f) : none_of(0.0f);
-        float m = low;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-        if (on) s = exp_below<float>(low, m) / (1.0f + expf(-fabsf(x)));
-        sum = s;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    } else {
-        if (on) s = sigmoid<float>(x);
-        sum = 1.0f;
+// The same where only the order of those taken, and of some that were left, is in doubt: lane l has candidate `e` (-1: none), and the first
+// p.k places of them all go to out_e.
+template <typename T>
+__device__ __noinline__ void order_exactly(const MoeScoredParams &p, const T *row, int32_t e, int candidates, int32_t *out_e, int lane) {
+    const Exact score = exact_scores(p, row, lane);
+    const uint64_t key = e >= 0 ? order_key(score(to_f(row[e])) + (double)__ldg(p.scores.bias + e)) : 0;
+    int place = 0;
+    for (int l = 0; l < candidates; ++l) {
+        const uint64_t other = __shfl_sync(0xffffffffu, key, l);
+        const int32_t o = __shfl_sync(0xffffffffu, e, l);
+        place += other > key || (other == key && o < e);
     }
-    return on ? s / sum * p.scores.scale : 0.0f;
+    if (e >= 0 && place < p.k) out_e[place] = e;
 }
 
-// Token t by one warp: lane j < k gets its j-th expert and weight.
-template <typename T, int PER>
-__device__ __forceinline__ void select_scored(const MoeScoredParams &p, int64_t t, bool wide, float bias_max, int lane, int32_t &expert, float &weight) {
-    const T *row = (const T *)p.logits + t * p.ld;
-    const float none = none_of(0.0f);
-    const int e0 = lane * PER;
-    float x[PER];
-    constexpr int V = PER * sizeof(T) <= 16 ? PER : 16 / (int)sizeof(T);
-    struct alignas(V * sizeof(T)) Pack {
-        T v[V];
+// ---- the fast way: L lanes a token, its row in shared memory, its experts in 16 search groups as in moe.cu
+
+__device__ __forceinline__ float fast_exp2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float fast_rcp(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+// How far c may be off (see above).
+__device__ __forceinline__ float doubt(float c, float bias_max) { return fmaf(fminf(1.0f, fabsf(c) + bias_max), 9.53674316e-07f, fmaf(fabsf(c), 1.1920929e-07f, 5.96046448e-08f)); }
+
+// The two largest of n values from `at` on (16-byte aligned if n is a multiple of four).
+__device__ __forceinline__ void top2(const float *at, int n, float &t1, float &t2) {
+    t1 = t2 = kNone;
+    auto take = [&](float v) {
+        t2 = fmaxf(t2, fminf(t1, v));
+        t1 = fmaxf(t1, v);
     };
-    if (wide) {
-#pragma unroll
-        for (int i = 0; i < PER; i += V) {
-            Pack y;
-            if (e0 + i < p.E) y = *(const Pack *)(row + e0 + i);
-#pragma unroll
-            for (int j = 0; j < V; ++j) x[i + j] = e0 + i < p.E ? logit(to_f(y.v[j])) : none;
+    if (n % 4 == 0) {
+        for (int i = 0; i < n; i += 4) {
+            const float4 v = *(const float4 *)(at + i);
+            take(v.x), take(v.y), take(v.z), take(v.w);
         }
     } else {
-#pragma unroll
-        for (int i = 0; i < PER; ++i) x[i] = e0 + i < p.E ? logit(to_f(row[e0 + i])) : none;
+        for (int i = 0; i < n; ++i) take(at[i]);
     }
-    float best = x[0], sum = 1.0f;
+}
+template <int L> __device__ __forceinline__ float max_of_lanes(float v) {
 #pragma unroll
-    for (int i = 1; i < PER; ++i) best = fmaxf(best, x[i]);
+    for (int d = 1; d < L; d <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
+    return v;
+}
+template <int L> __device__ __forceinline__ float sum_of_lanes(float v) {
 #pragma unroll
-    for (int d = 1; d < 32; d <<= 1) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, d));
-    if (p.scores.score == ILW_SCORE_SOFTMAX && (p.scores.bias || !p.renormalize)) {
-        sum = 0.0f;
+    for (int d = 1; d < L; d <<= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    return v;
+}
+template <int L> __device__ __forceinline__ uint32_t any_of_lanes(uint32_t v) {
 #pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (x[i] > none) sum += exp_below<float>(x[i], best);
+    for (int d = 1; d < L; d <<= 1) v |= __shfl_xor_sync(0xffffffffu, v, d);
+    return v;
+}
+
+// The experts of a token by L lanes (lane q of them here; all 32 lanes of the warp call it) to out_e, in order; 1 if fp32 cannot tell that
+// order, 2 if it cannot tell the groups.  `row` holds its logits and is lost, but for the c of those left; `logits` are its row in memory; `bias` [E] and its largest magnitude; ranks [2 groups]: room.
+// best and sum: largest logit, and the softmax's denominator if that is needed.  least: the smallest c taken.
+template <typename T, int L, int S>
+__device__ __forceinline__ uint32_t select_scored(const MoeScoredParams &p, const T *logits, const float *bias, float bias_max, float *row, float *ranks, int q,
+                                              int32_t *out_e, float *out_w, float &best, float &sum, float &least) {
+    constexpr int G = kGroups / L;  // this lane's search groups: q, L + q, ...
+    const RouteScores &r = p.scores;
+    const bool softmax = r.score == ILW_SCORE_SOFTMAX;
+    best = kNone, sum = 1.0f;
+    if (softmax) {
 #pragma unroll
-        for (int d = 1; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        for (int i = 0; i < G; ++i) {
+            const float4 *x = (const float4 *)(row + (L * i + q) * S);
+#pragma unroll
+            for (int c = 0; c < S / 4; ++c) best = fmaxf(fmaxf(fmaxf(best, x[c].x), fmaxf(x[c].y, x[c].z)), x[c].w);
+        }
+        best = max_of_lanes<L>(best);
+        if (bias || !p.renormalize) {  // by group and in four parts: short chains of roundings
+            float4 part = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 1
+            for (int i = 0; i < G; ++i) {
+                const float4 *x = (const float4 *)(row + (L * i + q) * S);
+                float4 of = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                for (int c = 0; c < S / 4; ++c) {
+                    const float4 v = x[c];
+                    of.x += v.x > kNone ? exp_below(v.x, best) : 0.0f, of.y += v.y > kNone ? exp_below(v.y, best) : 0.0f;
+                    of.z += v.z > kNone ? exp_below(v.z, best) : 0.0f, of.w += v.w > kNone ? exp_below(v.w, best) : 0.0f;
+                }
+                part.x += of.x, part.y += of.y, part.z += of.z, part.w += of.w;
+            }
+            sum = sum_of_lanes<L>((part.x + part.y) + (part.z + part.w));
+        }
     }
-    if (!choose<float, PER>(p, x, best, sum, bias_max, lane, expert)) expert = choose_exactly<PER>(p, x, best, lane);
-    weight = weight_of(p, expert, expert >= 0 ? to_f(row[expert]) : 0.0f, best, sum);
+    const float over_sum = fast_rcp(sum), log2e = 1.44269504f;
+    auto score = [&](float x) {
+        if (softmax) return x == best ? over_sum : fast_exp2((x - best) * log2e) * over_sum;
+        return fast_rcp(1.0f + fast_exp2(x * -log2e));
+    };
+    if (bias) {
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            float4 *x = (float4 *)(row + (L * i + q) * S);
+            const float4 *b = (const float4 *)(bias + (L * i + q) * S);
+#pragma unroll
+            for (int c = 0; c < S / 4; ++c) {
+                float4 v = x[c];
+                const float4 w = b[c];
+                auto add = [&](float y, float z) {
+                    const float u = score(y) + z;
+                    return y > kNone && u > kNone ? u : kNone;
+                };
+                x[c] = make_float4(add(v.x, w.x), add(v.y, w.y), add(v.z, w.z), add(v.w, w.w));
+            }
+        }
+        __syncwarp();
+    }
+    uint32_t unsure = 0;
+    if (r.groups > 1) {
+        float *offs = ranks + r.groups;  // how far each rank may be off
+        for (int g = q; g < r.groups; g += L) {
+            float t1, t2, off = 0.0f;
+            top2(row + g * r.group_size, r.group_size, t1, t2);
+            float rank = t1;
+            if (r.group_best == 2 && t1 > kNone) {
+                if (!bias) {  // (of logits: the sum of their scores, the softmax's without its denominator)
+                    rank = score(t1) + (t2 > kNone ? score(t2) : 0.0f);
+                    off = fmaf(rank, 6.7434957e-07f, 1.1920929e-07f);
+                } else if (t2 > kNone) {
+                    rank = t1 + t2;
+                }
+            }
+            if (bias) off = doubt(t1, bias_max) + (r.group_best == 2 && t2 > kNone ? doubt(t2, bias_max) : 0.0f) + fabsf(rank) * 1.1920929e-07f;
+            ranks[g] = rank, offs[g] = off;
+        }
+        __syncwarp();
+        uint32_t stay = 0;
+        int last = -1, next = -1;  // the last group that stays, the first that does not
+        for (int g = q; g < r.groups; g += L) {
+            const float mine = ranks[g];
+            int place = 0;
+            for (int o = 0; o < r.groups; ++o) {
+                const float other = ranks[o];
+                place += other > mine || (other == mine && o < g);
+            }
+            if (mine > kNone) {
+                if (place < r.top_groups) stay |= 1u << g;
+                if (place == r.top_groups - 1) last = g;
+                if (place == r.top_groups) next = g;
+            }
+        }
+        stay = any_of_lanes<L>(stay);
+#pragma unroll
+        for (int d = 1; d < L; d <<= 1) {
+            last = max(last, __shfl_xor_sync(0xffffffffu, last, d));
+            next = max(next, __shfl_xor_sync(0xffffffffu, next, d));
+        }
+        if ((bias || r.group_best == 2) && last >= 0 && next >= 0) {  // who lies close to the other side's, and is not its equal, is in doubt
+            for (int g = q; g < r.groups; g += L) {
+                const int of = stay >> g & 1 ? next : last;
+                if (ranks[g] > kNone && fabsf(ranks[g] - ranks[of]) <= 2.0f * (offs[g] + offs[of])) {
+                    float a1, a2, b1, b2;
+                    top2(row + g * r.group_size, r.group_size, a1, a2);
+                    top2(row + of * r.group_size, r.group_size, b1, b2);
+                    if (bias || a1 != b1 || (a2 != b2 && r.group_best == 2)) unsure |= 2;
+                }
+            }
+        }
+        __syncwarp();
+        for (int g = q; g < r.groups; g += L)
+            if (!(stay >> g & 1)) {
+                float *at = row + g * r.group_size;
+                if (r.group_size % 4 == 0)
+                    for (int i = 0; i < r.group_size; i += 4) *(float4 *)(at + i) = make_float4(kNone, kNone, kNone, kNone);
+                else
+                    for (int i = 0; i < r.group_size; ++i) at[i] = kNone;
+            }
+        __syncwarp();
+    }
+    float top[G];
+#pragma unroll
+    for (int i = 0; i < G; ++i) {
+        const float4 *x = (const float4 *)(row + (L * i + q) * S);
+        float m = kNone;
+#pragma unroll
+        for (int c = 0; c < S / 4; ++c) m = fmaxf(fmaxf(fmaxf(m, x[c].x), fmaxf(x[c].y, x[c].z)), x[c].w);
+        top[i] = m;
+    }
+    // the same logit and the same bias
+    auto equal = [&](int a, int b) { return to_f(logits[a]) == to_f(logits[b]) && bias[a] == bias[b]; };
+    float before = __int_as_float(0x7f800000);
+    int taken = 0;
+    bool close = false;  // the last two taken
+    for (int j = 0; j < p.k; ++j) {
+        // the largest search group, the first of equal ones
+        float m = top[0];
+        int g = 0;
+#pragma unroll
+        for (int i = 1; i < G; ++i)
+            if (top[i] > m) m = top[i], g = i;
+        g = L * g + q;
+#pragma unroll
+        for (int d = 1; d < L; d <<= 1) {
+            const float m2 = __shfl_xor_sync(0xffffffffu, m, d);
+            const int g2 = __shfl_xor_sync(0xffffffffu, g, d);
+            if (m2 > m || (m2 == m && g2 < g)) m = m2, g = g2;
+        }
+        if (close && !equal(out_e[j - 2], out_e[j - 1])) unsure |= 1;
+        const bool on = m > kNone;
+        if (on && g % L == q) {  // its lane takes the first expert with that value
+            const float4 *x = (const float4 *)(row + g * S);
+            int at = S;
+            float rest = kNone;
+#pragma unroll
+            for (int c = 0; c < S / 4; ++c) {
+                const float4 v = x[c];
+                const float u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const bool hit = u[w] == m && at == S;
+                    at = hit ? 4 * c + w : at;
+                    rest = fmaxf(rest, hit ? kNone : u[w]);
+                }
+            }
+            row[g * S + min(at, S - 1)] = kNone;
+#pragma unroll
+            for (int i = 0; i < G; ++i)
+                if (i == g / L) top[i] = rest;
+            out_e[j] = g * S + at;
+            out_w[j] = m;  // (without a bias the logit)
+        }
+        if (!on && q == 0) out_e[j] = -1;
+        close = bias && on && j > 0 && before - m <= doubt(before, bias_max) + doubt(m, bias_max);
+        if (on) before = m, taken = j + 1;
+        __syncwarp();
+    }
+    if (bias) {
+        if (close && !equal(out_e[p.k - 2], out_e[p.k - 1])) unsure |= 1;
+        // is the last one taken clear of all that are left
+        float m = top[0];
+#pragma unroll
+        for (int i = 1; i < G; ++i) m = fmaxf(m, top[i]);
+        const float off = doubt(before, bias_max);
+        if (taken == p.k && m > kNone && before - m <= off + doubt(m, bias_max)) {
+            const int e = out_e[p.k - 1];
+            for (int i = 0; i < G; ++i)
+                for (int c = 0; c < S; ++c) {
+                    const float v = row[(L * i + q) * S + c];
+                    if (v > kNone && before - v <= off + doubt(v, bias_max) && !equal((L * i + q) * S + c, e)) unsure |= 1;
+                }
+        }
+    }
+    least = taken == p.k ? before : __int_as_float(0x7f800000);
+    return any_of_lanes<L>(unsure);
+}
+
+// The weights of a token's experts to out_w, by its L lanes, an expert each in turn.
+template <typename T, int L>
+__device__ __forceinline__ void weigh_scored(const MoeScoredParams &p, const T *logits, int q, const int32_t *out_e, float *out_w, float best, float sum, bool biased) {
+    const bool softmax = p.scores.score == ILW_SCORE_SOFTMAX;
+    // renormalised sigmoids: exp(min(x, 0)) / (1 + exp(-|x|)), all times exp(-m) for the largest m of min(x, 0), so that scores too small for
+    // fp32 keep their ratios
+    const bool ratios = !softmax && p.renormalize;
+    float m = kNone;
+    for (int j = q; j < p.k; j += L)
+        if (out_e[j] >= 0) {
+            const float x = biased ? to_f(logits[out_e[j]]) : out_w[j];
+            out_w[j] = x;
+            m = fmaxf(m, fminf(x, 0.0f));
+        }
+    if (ratios) m = max_of_lanes<L>(m);
+    float of = 0.0f;
+    for (int j = q < p.k ? q + (p.k - 1 - q) / L * L : -1; j >= q; j -= L) {  // (the small ones first)
+        const float x = out_w[j];
+        float s = 0.0f;
+        if (out_e[j] >= 0) s = softmax ? exp_below(x, best) : ratios ? exp_below(fminf(x, 0.0f), m) / (1.0f + expf(-fabsf(x))) : sigmoid(x);
+        out_w[j] = s;
+        of += s;
+    }
+    if (p.renormalize) sum = sum_of_lanes<L>(of);
+    for (int j = q; j < p.k; j += L) out_w[j] = out_e[j] >= 0 ? out_w[j] / sum * p.scores.scale : 0.0f;
+}
+
+// A warp's tokens, L lanes each, the first of them token t0 of the call: this lane's token's experts and weights to out_e and out_w.
+template <typename T, int L, int S>
+__device__ __forceinline__ void route_tokens(const MoeScoredParams &p, int64_t t0, bool is_token, const float *bias, float bias_max, float *row, float *ranks,
+                                             int32_t *out_e, int entries, float *out_w) {
+    const int lane = threadIdx.x & 31, q = lane % L;
+    const T *logits = (const T *)p.logits + (t0 + (is_token ? lane / L : 0)) * p.ld;
+    float best, sum, least;
+    const uint32_t unsure = select_scored<T, L, S>(p, logits, bias, bias_max, row, ranks, q, out_e, out_w, best, sum, least);
+    uint32_t again = __ballot_sync(0xffffffffu, unsure && is_token && q == 0);
+    while (again) {
+        const int l = __ffs(again) - 1, t = l / L;  // a token of this warp's
+        again &= again - 1;
+        int32_t *to = out_e + (t - lane / L) * entries;
+        float *its = row + (t - lane / L) * (kGroups * S + 4);
+        const T *x = (const T *)p.logits + (t0 + t) * p.ld;
+        const float low = __shfl_sync(0xffffffffu, least, l);
+        bool whole = __shfl_sync(0xffffffffu, unsure, l) & 2;
+        if (!whole) {
+            // candidates: those taken, and those left whose c comes close to the least of them
+            int32_t hits = 0, n = 0;
+            uint32_t which = 0;
+            for (int i = 0; i < S / 2; ++i) {
+                const float v = its[32 * i + lane];
+                const bool hit = v > kNone && low - v <= doubt(low, bias_max) + doubt(v, bias_max);
+                which |= (uint32_t)hit << i;
+                hits += hit;
+            }
+            int32_t before = hits;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int32_t y = __shfl_up_sync(0xffffffffu, before, d);
+                if (lane >= d) before += y;
+            }
+            n = p.k + __shfl_sync(0xffffffffu, before, 31);
+            whole = n > 32;
+            if (!whole) {
+                __syncwarp();
+                int32_t *list = (int32_t *)its + before - hits;  // (what the row held has been read)
+                for (; which; which &= which - 1) *list++ = 32 * (__ffs(which) - 1) + lane;
+                __syncwarp();
+                const int32_t e = lane < p.k ? to[lane] : lane < n ? ((int32_t *)its)[lane - p.k] : -1;
+                __syncwarp();
+                order_exactly<T>(p, x, e, n, to, lane);
+            }
+        }
+        if (whole) {
+            const int32_t e = choose_exactly<T, S / 2>(p, x, lane);
+            if (lane < p.k) {
+                to[lane] = e;
+                if (!bias && e >= 0) out_w[(t - lane / L) * entries + lane] = to_f(x[e]);
+            }
+        }
+    }
+    __syncwarp();
+    weigh_scored<T, L>(p, logits, q, out_e, out_w, best, sum, bias != nullptr);
 }
 
 }  // namespace

@@ -72,7 +72,6 @@ struct RouteScores {
     int32_t score;             // ILW_SCORE_*
     const float *bias;         // [E] or NULL
     int32_t groups, top_groups, group_best, group_size;
-    int32_t lanes_per_group;   // of a warp whose lanes hold consecutive experts of one group each; 0: they do not
     Divisor per_group;         // by group_size
     float scale;
 };

@@ -122,6 +122,37 @@ def test_scores_that_32_bits_do_not_separate(ilw, T, groups, top_groups, group_b
     check(ilw, rows, 8, False, bias=bias, score=score, groups=groups, top_groups=top_groups, group_best=group_best)
 
 
+@pytest.mark.parametrize("T", [1, 2, 31, 32, 33, 60, 111, 113, 224, 225, 256, 257, 511, 513])
+def test_route_of_few_tokens(ilw, T):
+    """Either side of where a CTA does all and of the lanes it gives a token; with 32 groups, ranks that leave no room for that."""
+    rng = np.random.default_rng(T)
+    for E, k, groups in ((8, 3, 2), (96, 5, 32), (112, 16, 14), (256, 5, 32)):
+        x = np.round(rng.standard_normal((T, E)) * 4) / 4
+        x[rng.random((T, E)) < 0.2] = -np.inf
+        x = torch.from_numpy(x).float().cuda()
+        bias = torch.from_numpy(0.1 * rng.standard_normal(E)).float().cuda()
+        check(ilw, x, k, True, bias=bias, score="sigmoid", groups=groups, top_groups=max(groups // 2, 2))
+        check(ilw, x, k, False, score="softmax", groups=groups, top_groups=max(groups // 2, 2), group_best=1)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("E,k,groups,top_groups", [(128, 8, 8, 4), (256, 8, 1, 1), (63, 6, 9, 3)])
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+def test_many_random_tokens(ilw, score, E, k, groups, top_groups, dtype):
+    """Enough tokens that some have neighbours that fp32 cannot tell apart; experts against plain operations in 64 bits on the GPU."""
+    gen = torch.Generator("cuda").manual_seed(E + groups)
+    x = (1.5 * torch.randn((60000, E), generator=gen, device="cuda")).to(dtype)
+    bias = 0.1 * torch.randn(E, generator=gen, device="cuda")
+    r = ilw.moe_route(x, k, score=score, bias=bias, groups=groups, top_groups=top_groups)
+    c = (1 / (1 + torch.exp(-x.double())) if score == "sigmoid" else torch.softmax(x.double(), 1)) + bias.double()
+    if groups > 1:
+        of = c.view(-1, groups, E // groups)
+        rank = torch.sort(of, dim=2, descending=True).values[..., :2].sum(2)
+        stay = torch.zeros_like(rank, dtype=torch.bool).scatter_(1, torch.sort(rank, dim=1, descending=True, stable=True).indices[:, :top_groups], True)
+        c = torch.where(stay[..., None], of, -torch.inf).view(-1, E)
+    assert torch.equal(r.expert.long(), torch.sort(c, dim=1, descending=True, stable=True).indices[:, :k])
+
+
 def test_biases_that_pin_or_ban_experts(ilw):
     inf, nan = float("inf"), float("nan")
     bias = torch.tensor([0.0, 1e6, -1e6, -inf, nan, inf, 3e38, 0.0], device="cuda")
