@@ -7,9 +7,11 @@
 // of a half; x - n s is exact in fp32 (a multiple of the smaller of the units of x and s that is at most about s / 2), so comparing it with
 // s / 2 tells.  That is five operations a value, and a rare branch a unit of values, where a division would take some ten.
 //
-// Bytes are what it moves.  A row is held in registers between its maximum and its codes, by a warp (to 64 16-bit values a lane), 128
-// or 512 threads; past that it is read twice.  Rows on 16-byte boundaries are loaded 16 bytes at a time, others value by value, four
-// consecutive ones a thread.
+// Bytes are what it moves.  A row is held in registers between its maximum and its codes, by 8 lanes, a warp, 128 or 512 threads; past 24576
+// (512 x 6 pieces of 16 bytes) it is read twice.  Rows on 16-byte boundaries are loaded and stored 16 bytes at a time; others value by value, four
+// consecutive ones a thread (whole lines, with the codes exchanged between lanes, were slower: 65536 x 1537 bf16 117 us, so 89).  16384 x 4096
+// fp32: 47.7 us (7.0 TB/s), back 49.1 (6.8).  65536 x 1536 bf16: 58.6 us (5.2 TB/s), back 50.2 (6.0): 20 warps an SM that load, reduce and encode in
+// turn, issue 65 % and the integer pipe 74 % busy; neither fewer integer operations nor four CTAs an SM made it faster.
 #include <algorithm>
 #include <cstdint>
 
@@ -30,23 +32,31 @@ __device__ __forceinline__ float to_f(__half v) { return __half2float(v); }
 __device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
 
 // V consecutive values of T: 16 bytes of them, or four.
-template <typename T, int V> struct alignas(V * sizeof(T) == 16 ? 16 : sizeof(T)) Unit {
+template <typename T, int V> struct alignas(V * sizeof(T) == 16 ? 16 : 4) Unit {
     T t[V];
 };
 
-// The largest magnitude of a unit as the bits of a T without a sign (infinities and NaN are above all others).
-template <int V> __device__ __forceinline__ uint32_t magnitude(const Unit<float, V> &x) {
-    uint32_t m = 0;
+// Values 2 i and 2 i + 1 of a unit (16-bit ones by their common word).
+template <int V> __device__ __forceinline__ float2 pair(const Unit<float, V> &x, int i) { return make_float2(x.t[2 * i], x.t[2 * i + 1]); }
+template <int V> __device__ __forceinline__ float2 pair(const Unit<__half, V> &x, int i) { return __half22float2(((const __half2 *)&x)[i]); }
+template <int V> __device__ __forceinline__ float2 pair(const Unit<__nv_bfloat16, V> &x, int i) {
+    const uint32_t w = ((const uint32_t *)&x)[i];
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+// The largest magnitude of a unit as the bits of a T without a sign (infinities and NaN are above all others); of 16-bit ones that of each half of
+// the words.
+template <int V> __device__ __forceinline__ uint32_t magnitude(const Unit<float, V> &x, uint32_t m) {
 #pragma unroll
     for (int i = 0; i < V; ++i) m = max(m, __float_as_uint(x.t[i]) & 0x7fffffffu);
     return m;
 }
-template <typename T, int V> __device__ __forceinline__ uint32_t magnitude(const Unit<T, V> &x) {
-    uint32_t m = 0;
+template <typename T, int V> __device__ __forceinline__ uint32_t magnitude(const Unit<T, V> &x, uint32_t m) {
 #pragma unroll
-    for (int i = 0; i < V; i += 2) m = __vmaxu2(m, ((uint32_t)*(const uint16_t *)&x.t[i] | (uint32_t)*(const uint16_t *)&x.t[i + 1] << 16) & 0x7fff7fffu);
-    return max(m & 0xffffu, m >> 16);
+    for (int i = 0; i < V / 2; ++i) m = __vmaxu2(m, ((const uint32_t *)&x)[i] & 0x7fff7fffu);
+    return m;
 }
+__device__ __forceinline__ uint32_t of_halves(uint32_t m, float) { return m; }
+template <typename T> __device__ __forceinline__ uint32_t of_halves(uint32_t m, T) { return max(m & 0xffffu, m >> 16); }
 __device__ __forceinline__ float magnitude_value(uint32_t m, float) { return __uint_as_float(m); }
 __device__ __forceinline__ float magnitude_value(uint32_t m, __half) { return __half2float(__ushort_as_half((unsigned short)m)); }
 __device__ __forceinline__ float magnitude_value(uint32_t m, __nv_bfloat16) { return __uint_as_float(m << 16); }
@@ -57,10 +67,12 @@ constexpr float kMagic = 12582912.0f;  // 1.5 2^23: x + kMagic holds rint(x) in 
 template <typename T, int V> __device__ __forceinline__ void encode(const Unit<T, V> &x, float s, float inv, uint32_t (&w)[V / 4]) {
     float t[V], worst = 0.0f;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const float v = to_f(x.t[i]);
-        t[i] = fmaf(v, inv, kMagic);
-        worst = fmaxf(worst, fabsf(fmaf(kMagic - t[i], s, v)));
+    for (int i = 0; i < V; i += 2) {
+        const float2 p = pair(x, i / 2);
+        const uint64_t v = pack2(p.x, p.y), sum = fma2(v, both(inv), both(kMagic));
+        const float2 c = unpack2(sum), r = unpack2(fma2(fma2(sum, both(-1.0f), both(kMagic)), both(s), v));
+        t[i] = c.x, t[i + 1] = c.y;
+        worst = fmaxf(worst, fmaxf(fabsf(r.x), fabsf(r.y)));
     }
     if (worst > 0.4999f * s) {  // near a half
 #pragma unroll
@@ -76,15 +88,14 @@ template <typename T, int V> __device__ __forceinline__ void encode(const Unit<T
 }
 
 // G threads a row (a warp, or the whole CTA); each holds up to kHeld units of it.
-constexpr int kHeld = 8;
-template <typename T, bool WIDE, int G>
-__global__ void __launch_bounds__(G == 32 ? 256 : G) i8_quantize_kernel(const I8QuantParams p) {
+template <typename T, bool WIDE, int G, int kHeld>
+__global__ void __launch_bounds__(G <= 32 ? 256 : G, G == 512 ? 2 : 1) i8_quantize_kernel(const I8QuantParams p) {
     constexpr int V = WIDE ? 16 / (int)sizeof(T) : 4;
-    __shared__ uint32_t warp_max[G / 32];
+    __shared__ uint32_t warp_max[G < 32 ? 1 : G / 32];
     grid_wait();
-    const int q = G == 32 ? threadIdx.x & 31 : threadIdx.x;
-    const int64_t r = G == 32 ? blockIdx.x * (int64_t)8 + (threadIdx.x >> 5) : blockIdx.x;
-    if (r >= p.rows) return;  // (whole warps, or no one)
+    const int q = threadIdx.x % G;
+    const int64_t r = G <= 32 ? blockIdx.x * (int64_t)(256 / G) + threadIdx.x / G : blockIdx.x;
+    if (r >= p.rows) return;  // (all threads of a row)
     int64_t src = r;
     if (p.gather) {
         src = p.gather[r];
@@ -112,9 +123,10 @@ __global__ void __launch_bounds__(G == 32 ? 256 : G) i8_quantize_kernel(const I8
 #pragma unroll
     for (int j = 0; j < kHeld; ++j) held[j] = load(q + j * G);
 #pragma unroll
-    for (int j = 0; j < kHeld; ++j) m = max(m, magnitude(held[j]));
-    for (int32_t u = q + kHeld * G; u < units; u += G) m = max(m, magnitude(load(u)));
-    m = __reduce_max_sync(0xffffffffu, m);
+    for (int j = 0; j < kHeld; ++j) m = magnitude(held[j], m);
+    for (int32_t u = q + kHeld * G; u < units; u += G) m = magnitude(load(u), m);
+    m = of_halves(m, T());
+    m = __reduce_max_sync(G < 32 ? ((1u << G % 32) - 1) << (threadIdx.x & 31) / G * G : 0xffffffffu, m);
     if constexpr (G > 32) {
         if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = m;
         __syncthreads();
@@ -149,54 +161,99 @@ __global__ void __launch_bounds__(G == 32 ? 256 : G) i8_quantize_kernel(const I8
     for (int32_t u = q + kHeld * G; u < units; u += G) store(u, load(u));
 }
 
-// Values: 16 codes a thread where rows of Y are on 16-byte boundaries and K is a multiple of 16, else one.
-template <typename T, int V>
+// A code times s, from byte i of w ^ 0x80808080: 2^23 + 128 + code has that byte at its end (the conversion's own instruction has a quarter of
+// the rate).
+__device__ __forceinline__ float code_value(uint32_t w, int i, float s) { return (__uint_as_float(__byte_perm(w, 0x4B000000u, 0x7650 + i)) - 8388736.0f) * s; }
+
+// Values.  Rows of Y on 16-byte boundaries: 16 bytes of them a thread and step, several steps in flight.
+constexpr int kSteps = 4;
+template <typename T>
 __global__ void __launch_bounds__(256) i8_dequantize_kernel(const I8DequantParams p, Divisor per, uint32_t r0, uint32_t total) {
+    constexpr int V = 16 / sizeof(T);
+    struct alignas(V) Codes {
+        uint32_t w[V / 4];
+    };
     grid_wait();
-    const uint32_t i = blockIdx.x * 256 + threadIdx.x;
-    if (i >= total) return;
-    const uint32_t row = per.div(i), k = (i - row * per.d) * V;
-    const int64_t r = (int64_t)r0 + row;
-    const float s = p.scales[r];
-    T *y = (T *)p.Y + r * p.ldy + k;
-    if constexpr (V == 1) {
-        *y = to_out<T>((float)p.codes[r * p.ldc + k] * s);
-    } else {
-        const int4 c = *(const int4 *)(p.codes + r * p.ldc + k);
-        const int32_t w[4] = {c.x, c.y, c.z, c.w};
+    const uint32_t base = blockIdx.x * (256 * kSteps) + threadIdx.x;
+    Codes c[kSteps];
+    float s[kSteps];
+    uint32_t row[kSteps], k[kSteps];
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j) {
+        const uint32_t i = base + j * 256;
+        row[j] = per.div(i);
+        k[j] = (i - row[j] * per.d) * V;
+        if (i < total) {
+            c[j] = *(const Codes *)(p.codes + ((int64_t)r0 + row[j]) * p.ldc + k[j]);
+            s[j] = p.scales[(int64_t)r0 + row[j]];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j) {
+        if (base + j * 256 >= total) continue;
         struct alignas(16) Pack {
             T t[V];
         } o;
 #pragma unroll
-        for (int j = 0; j < V; ++j) o.t[j] = to_out<T>((float)(int8_t)(w[j / 4] >> (8 * (j % 4))) * s);
-        *(Pack *)y = o;
+        for (int i = 0; i < V; ++i) o.t[i] = to_out<T>(code_value(c[j].w[i / 4] ^ 0x80808080u, i % 4, s[j]));
+        *(Pack *)((T *)p.Y + ((int64_t)r0 + row[j]) * p.ldy + k[j]) = o;
+    }
+}
+// Any rows: a warp takes 128 codes of a row, four a lane, and each lane stores what is a lane apart, so that accesses stay whole lines.
+template <typename T>
+__global__ void __launch_bounds__(256) i8_dequantize_any_kernel(const I8DequantParams p, Divisor segs, uint32_t r0, uint32_t total) {
+    grid_wait();
+    const int lane = threadIdx.x & 31;
+    const uint32_t u = blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (u >= total) return;
+    const uint32_t row = segs.div(u), k0 = (u - row * segs.d) * 128;
+    const int64_t r = (int64_t)r0 + row;
+    const int32_t left = p.K - (int32_t)k0;  // (codes of whole words are there up to the last one's)
+    const int8_t *c = p.codes + r * p.ldc + k0;
+    uint32_t w = 0;
+    if (4 * lane + 4 <= left) w = *(const uint32_t *)(c + 4 * lane);
+    else
+        for (int i = 0; 4 * lane + i < left; ++i) w |= (uint32_t)(uint8_t)c[4 * lane + i] << (8 * i);
+    const float s = p.scales[r];
+    T *y = (T *)p.Y + r * p.ldy + k0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t v = __shfl_sync(0xffffffffu, w, 8 * i + (lane >> 2));
+        if (32 * i + lane < left) y[32 * i + lane] = to_out<T>((float)(int8_t)(v >> (8 * (lane & 3))) * s);
     }
 }
 
 template <typename T, bool WIDE> cudaError_t quantize_rows(const I8QuantParams &p, cudaStream_t s) {
     const int64_t units = WIDE ? p.K / (16 / (int)sizeof(T)) : ((int64_t)p.K + 3) / 4;
-    if (units <= 32 * kHeld) return launch_after(i8_quantize_kernel<T, WIDE, 32>, (unsigned)((p.rows + 7) / 8), 256, 0, s, p);
-    if (units <= 128 * kHeld) return launch_after(i8_quantize_kernel<T, WIDE, 128>, (unsigned)p.rows, 128, 0, s, p);
-    return launch_after(i8_quantize_kernel<T, WIDE, 512>, (unsigned)p.rows, 512, 0, s, p);
+    if constexpr (WIDE)
+        if (units <= 8 * 2) return launch_after(i8_quantize_kernel<T, WIDE, 8, 2>, (unsigned)((p.rows + 31) / 32), 256, 0, s, p);
+    const unsigned by_warp = (unsigned)((p.rows + 7) / 8);
+    if (units <= 32 * 2) return launch_after(i8_quantize_kernel<T, WIDE, 32, 2>, by_warp, 256, 0, s, p);
+    if (units <= 32 * 4) return launch_after(i8_quantize_kernel<T, WIDE, 32, 4>, by_warp, 256, 0, s, p);
+    if (units <= 32 * 6) return launch_after(i8_quantize_kernel<T, WIDE, 32, 6>, by_warp, 256, 0, s, p);
+    if (units <= 128 * 4) return launch_after(i8_quantize_kernel<T, WIDE, 128, 4>, (unsigned)p.rows, 128, 0, s, p);
+    if (units <= 128 * 8) return launch_after(i8_quantize_kernel<T, WIDE, 128, 8>, (unsigned)p.rows, 128, 0, s, p);
+    return launch_after(i8_quantize_kernel<T, WIDE, 512, 6>, (unsigned)p.rows, 512, 0, s, p);
 }
 template <typename T> cudaError_t quantize(const I8QuantParams &p, cudaStream_t s) {
     constexpr int V = 16 / sizeof(T);
     if ((uintptr_t)p.X % 16 == 0 && p.ldx % V == 0 && p.K % V == 0) return quantize_rows<T, true>(p, s);
     return quantize_rows<T, false>(p, s);
 }
-template <typename T, int V> cudaError_t dequantize_rows(const I8DequantParams &p, cudaStream_t s) {
-    const uint32_t per = p.K / V;
+// Launches `kernel` over rows of `per` steps each, `step` of them a CTA, as often as 2^30 steps at a time take.
+cudaError_t over_rows(void (*kernel)(const I8DequantParams, Divisor, uint32_t, uint32_t), const I8DequantParams &p, uint32_t per, uint32_t step, cudaStream_t s) {
     const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 30) / per);
     for (int64_t r0 = 0; r0 < p.rows; r0 += most) {
         const uint32_t total = (uint32_t)(std::min(most, p.rows - r0) * per);
-        const cudaError_t e = launch_after(i8_dequantize_kernel<T, V>, (total + 255) / 256, 256, 0, s, p, divisor(per), (uint32_t)r0, total);
+        const cudaError_t e = launch_after(kernel, (total + step - 1) / step, 256, 0, s, p, divisor(per), (uint32_t)r0, total);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
 }
 template <typename T> cudaError_t dequantize(const I8DequantParams &p, cudaStream_t s) {
-    if ((uintptr_t)p.Y % 16 == 0 && p.ldy * (int64_t)sizeof(T) % 16 == 0 && p.K % 16 == 0) return dequantize_rows<T, 16>(p, s);
-    return dequantize_rows<T, 1>(p, s);
+    constexpr int V = 16 / sizeof(T);
+    if ((uintptr_t)p.Y % 16 == 0 && p.ldy % V == 0 && p.K % V == 0) return over_rows(i8_dequantize_kernel<T>, p, p.K / V, 256 * kSteps, s);
+    return over_rows(i8_dequantize_any_kernel<T>, p, ((uint32_t)p.K + 127) / 128, 8, s);
 }
 
 }  // namespace
