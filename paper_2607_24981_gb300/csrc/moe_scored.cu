@@ -40,8 +40,8 @@ __global__ void __cluster_dims__(kSelectCtas, 1, 1) __launch_bounds__(select_tok
     int32_t *count = (int32_t *)out_w + kSelectTokens * ks;
     for (int e = threadIdx.x; e < p.E; e += kSelectThreads) count[e] = 0;
     grid_wait();
-    const int32_t t0 = blockIdx.x * kSelectTokens;
-    const int n = max(0, min(kSelectTokens, p.T - t0));
+    const int64_t t0 = (int64_t)blockIdx.x * kSelectTokens;
+    const int n = (int)max((int64_t)0, min((int64_t)kSelectTokens, p.T - t0));
     if (p.scores.bias && threadIdx.x < 32) {
         const float m = load_bias(p, bias, kGroups * S, lane);
         if (lane == 0) s_bias_max = m;
@@ -58,8 +58,8 @@ __global__ void __cluster_dims__(kSelectCtas, 1, 1) __launch_bounds__(select_tok
     for (int i = threadIdx.x; i < n * p.k; i += kSelectThreads) {
         const int t = over(i, over_k), at = t * ks + i - t * p.k;
         const int32_t e = out_e[at];
-        p.expert[(int64_t)t0 * p.k + i] = e;
-        p.weight[(int64_t)t0 * p.k + i] = out_w[at];
+        p.expert[t0 * p.k + i] = e;
+        p.weight[t0 * p.k + i] = out_w[at];
         if (e >= 0) atomicAdd(&count[e], 1);  // (whole numbers: any order gives the same)
     }
     add_counts<kSelectThreads>(p, count);

@@ -8,8 +8,9 @@
 //
 // Who is taken is decided as in 64 bits: one rounding of 32 bits could exchange two experts, and a token would go elsewhere.  c is first computed
 // in fp32 with the fast exponential and reciprocal, and its error is bounded: of s by a relative 2^-21.5 (2^-22.5 and 2^-23 of the two
-// functions, roundings) and, for the rounding of an exponent y = x or x - max, |y| 2^-24 relative to exp(-|y|), which stays below
-// 2^-25; of the sum with the bias by 2^-24 |c|.  So c is off by less than doubt() = 2^-20 min(1, |c| + max|bias|) + 2^-23 |c| + 2^-24.
+// functions, roundings), a softmax's denominator by 23 roundings more (chains of 17 sums, exponentials), so 2^-19 in all; for the two roundings of
+// an exponent y = x or x - max, |y| 2^-23 relative to exp(-|y|), which stays below 2^-24; of the sum with the bias by 2^-24 |c|.  So c is off by
+// less than doubt() = u min(1, |c| + max|bias|) + 2^-23 |c| + 2^-24, with u 2^-21 for the sigmoid and 2^-19 for the softmax.
 // Where two of those that are taken, or one and another that is not, lie closer than their doubts, and are not equal logits with equal biases,
 // they are ordered again in 64 bits by the whole warp (one row in some hundred of random logits and biases), and where the groups are in doubt the
 // whole row is done again.
@@ -166,7 +167,11 @@ __device__ __forceinline__ float fast_rcp(float x) {
     return r;
 }
 // How far c may be off (see above).
-__device__ __forceinline__ float doubt(float c, float bias_max) { return fmaf(fminf(1.0f, fabsf(c) + bias_max), 9.53674316e-07f, fmaf(fabsf(c), 1.1920929e-07f, 5.96046448e-08f)); }
+struct Doubt {
+    float unit, bias_max;
+    __device__ __forceinline__ Doubt(int32_t score, float bias_max) : unit(score == ILW_SCORE_SIGMOID ? 4.76837158e-07f : 1.90734863e-06f), bias_max(bias_max) {}
+    __device__ __forceinline__ float operator()(float c) const { return fmaf(fminf(1.0f, fabsf(c) + bias_max), unit, fmaf(fabsf(c), 1.1920929e-07f, 5.96046448e-08f)); }
+};
 
 // The two largest of n values from `at` on (16-byte aligned if n is a multiple of four).
 __device__ __forceinline__ void top2(const float *at, int n, float &t1, float &t2) {
@@ -208,6 +213,7 @@ __device__ __forceinline__ uint32_t select_scored(const MoeScoredParams &p, cons
                                               int32_t *out_e, float *out_w, float &best, float &sum, float &least) {
     constexpr int G = kGroups / L;  // this lane's search groups: q, L + q, ...
     const RouteScores &r = p.scores;
+    const Doubt doubt(r.score, bias_max);
     const bool softmax = r.score == ILW_SCORE_SOFTMAX;
     best = kNone, sum = 1.0f;
     if (softmax) {
@@ -273,7 +279,7 @@ __device__ __forceinline__ uint32_t select_scored(const MoeScoredParams &p, cons
                     rank = t1 + t2;
                 }
             }
-            if (bias) off = doubt(t1, bias_max) + (r.group_best == 2 && t2 > kNone ? doubt(t2, bias_max) : 0.0f) + fabsf(rank) * 1.1920929e-07f;
+            if (bias) off = doubt(t1) + (r.group_best == 2 && t2 > kNone ? doubt(t2) : 0.0f) + fabsf(rank) * 1.1920929e-07f;
             ranks[g] = rank, offs[g] = off;
         }
         __syncwarp();
@@ -373,7 +379,7 @@ __device__ __forceinline__ uint32_t select_scored(const MoeScoredParams &p, cons
             out_w[j] = m;  // (without a bias the logit)
         }
         if (!on && q == 0) out_e[j] = -1;
-        close = bias && on && j > 0 && before - m <= doubt(before, bias_max) + doubt(m, bias_max);
+        close = bias && on && j > 0 && before - m <= doubt(before) + doubt(m);
         if (on) before = m, taken = j + 1;
         __syncwarp();
     }
@@ -383,13 +389,13 @@ __device__ __forceinline__ uint32_t select_scored(const MoeScoredParams &p, cons
         float m = top[0];
 #pragma unroll
         for (int i = 1; i < G; ++i) m = fmaxf(m, top[i]);
-        const float off = doubt(before, bias_max);
-        if (taken == p.k && m > kNone && before - m <= off + doubt(m, bias_max)) {
+        const float off = doubt(before);
+        if (taken == p.k && m > kNone && before - m <= off + doubt(m)) {
             const int e = out_e[p.k - 1];
             for (int i = 0; i < G; ++i)
                 for (int c = 0; c < S; ++c) {
                     const float v = row[(L * i + q) * S + c];
-                    if (v > kNone && before - v <= off + doubt(v, bias_max) && !equal((L * i + q) * S + c, e)) unsure |= 1;
+                    if (v > kNone && before - v <= off + doubt(v) && !equal((L * i + q) * S + c, e)) unsure |= 1;
                 }
         }
     }
@@ -432,6 +438,7 @@ __device__ __forceinline__ void route_tokens(const MoeScoredParams &p, int64_t t
     const T *logits = (const T *)p.logits + (t0 + (is_token ? lane / L : 0)) * p.ld;
     float best, sum, least;
     const uint32_t unsure = select_scored<T, L, S>(p, logits, bias, bias_max, row, ranks, q, out_e, out_w, best, sum, least);
+    const Doubt doubt(p.scores.score, bias_max);
     uint32_t again = __ballot_sync(0xffffffffu, unsure && is_token && q == 0);
     while (again) {
         const int l = __ffs(again) - 1, t = l / L;  // a token of this warp's
@@ -447,7 +454,7 @@ __device__ __forceinline__ void route_tokens(const MoeScoredParams &p, int64_t t
             uint32_t which = 0;
             for (int i = 0; i < S / 2; ++i) {
                 const float v = its[32 * i + lane];
-                const bool hit = v > kNone && low - v <= doubt(low, bias_max) + doubt(v, bias_max);
+                const bool hit = v > kNone && low - v <= doubt(low) + doubt(v);
                 which |= (uint32_t)hit << i;
                 hits += hit;
             }

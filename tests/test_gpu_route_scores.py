@@ -228,3 +228,14 @@ def test_routing_follows_its_stream_and_graphs(ilw, T):
         torch.cuda.synchronize()
         for (b, g, r), n in zip(graphs, (i, j)):
             assert all(torch.equal(u, v) for u, v in zip(r, want[n]))
+
+
+def test_logits_past_32_bits(ilw):
+    """The last tokens of more than 2^31 logits go where they go alone."""
+    T, E = 8500000, 256
+    x = torch.empty((T, E), dtype=torch.bfloat16, device="cuda").normal_(generator=torch.Generator("cuda").manual_seed(1))
+    how = dict(score="sigmoid", bias=torch.linspace(-0.1, 0.1, E, device="cuda"), groups=8, top_groups=4)
+    r, alone = ilw.moe_route(x, 2, **how), ilw.moe_route(x[-500:], 2, **how)
+    assert torch.equal(r.expert[-500:], alone.expert) and torch.equal(r.weight[-500:], alone.weight)
+    assert torch.equal(torch.bincount(r.expert.flatten(), minlength=E).cumsum(0).int(), r.offsets[1:])
+    assert torch.equal(r.source[r.slot[-500:].long()], torch.arange(T - 500, T, dtype=torch.int32, device="cuda")[:, None].expand(500, 2))
