@@ -552,7 +552,7 @@ int ilwdetr_i8_dequantize(const int8_t *codes, int64_t ldc, const float *scales,
  *   offsets, y_form, Y, ldy, act   as in ilw_mx_gemm_t
  * Products are exact; sums are exact while they stay below 2^24 (so whenever K <= 1024) and of fp32's accuracy past
  * that, or 32-bit whole numbers throughout where there are few tokens.  Scaling, bias and activation in fp32, the result is
- * rounded once.  1 <= experts <= 1024, K < 2^17, M < 2^31 - 1024. */
+ * rounded once.  1 <= experts <= 1024, K < 2^17, N <= 2^24, M < 2^31 - 1024, (M / 32 + experts) N / 128 < 2^31 - 4096. */
 typedef struct {
     uint32_t struct_size;
     const int8_t *a_codes; int64_t a_ldc;

@@ -46,8 +46,8 @@ int gemm_problem(const ilw_i8_gemm_t *p, ilw::I8GemmProblem &g) {
     if (gate && p->N % 2) return fail(ILW_ERR_INVALID_ARG, "i8_gemm: a gated product's N=%d must be even", p->N);
     if (p->M > INT32_MAX - 1024 || p->N > (1 << 24) || p->K > ilw::kI8MaxK || p->experts > ilw::kI8MaxExperts)
         return fail(ILW_ERR_UNSUPPORTED, "i8_gemm: M < 2^31 - 1024, N <= 2^24, K < 2^17, experts <= %d", ilw::kI8MaxExperts);
-    // (the pieces of work that a call can come to, counted in 32 bits by the kernels)
-    if ((p->M / 8 + p->experts + 1) * (((int64_t)p->N + 3) / 4) > INT32_MAX) return fail(ILW_ERR_UNSUPPORTED, "i8_gemm: M x N too large for one call");
+    // (tiles are counted in 32 bits; products of this size take those of 32 tokens or more)
+    if ((p->M / 32 + p->experts + 1) * (((int64_t)p->N + 127) / 128) > INT32_MAX - 4096) return fail(ILW_ERR_UNSUPPORTED, "i8_gemm: M x N too large for one call");
     g = {};
     g.M = p->M, g.N = p->N;
     if (p->M == 0 || p->N == 0) return ILW_OK;

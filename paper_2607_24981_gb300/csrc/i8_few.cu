@@ -45,12 +45,6 @@ __device__ __forceinline__ int32_t sums(const FewParams &g, const int8_t *w, int
 #pragma unroll
     for (int r = 0; r < kRows; ++r) wr[r] = w + (int64_t)min(n0 + r, g.N - 1) * g.w_ldc;
     auto token = [&](int t) { return a0 + min(t, rows - 1) * g.a_ldc; };
-#ifndef ST1
-#define ST1 4
-#define ST2 4
-#define ST4 3
-#define ST8 2
-#endif
     // steps of 512 of K, two at a time: their loads of W first; the tokens, which every warp reads, come from the L1
     const int32_t whole = g.K / 512, stride = g.ksplit * 512;
     int32_t n = (whole - part + g.ksplit - 1) / g.ksplit, k = part * 512 + lane * 16;

@@ -49,7 +49,8 @@ Choice choose(const I8GemmProblem &g, int64_t sms) {
     const double met = g.offsets ? std::max(1.0, g.experts * (1.0 - std::exp(-M / g.experts))) : 1.0, mean = M / met;
     const double units = g.offsets ? std::max(met, M / 8 + met / 2) : std::ceil(M / 8);
     const double turns = std::ceil(units * ((g.N + 3) / 4) / (16.0 * sms));
-    Choice best = {-1, 8, 1, 2200 + std::max(units * weights / (mean > 2 ? 4400 : 5800), (1000 + 2 * std::min(g.K, 1024)) * turns)};
+    const bool countable = (M / 8 + g.experts + 1) * ((g.N + 3) / 4) < INT32_MAX;  // (pieces of work of the few)
+    Choice best = {-1, 8, 1, countable ? 2200 + std::max(units * weights / (mean > 2 ? 4400 : 5800), (1000 + 2 * std::min(g.K, 1024)) * turns) : INFINITY};
     const int32_t nkb = (g.K + 127) / 128, top = (int32_t)std::min<double>(kI8MaxTok, std::ceil((g.offsets ? 4 * mean : M) / 32) * 32);
     const double epilogue = g.act == ILW_ACT_GELU ? 21 : 14.5;
     for (const bool pair : {true, false})
@@ -97,15 +98,14 @@ bool lay_out(const I8GemmProblem &g, const Choice &c, I8Params &p, int64_t &tile
         if (p.wides == kI8Sets || p.stages >= 4) break;
     }
     smem = bytes();
-    return p.stages >= kI8MinStages && tiles <= INT32_MAX;
+    return p.stages >= kI8MinStages && tiles <= INT32_MAX - 4096;
 }
 
 }  // namespace
 
-bool i8_gemm_form(const I8GemmProblem &g, int32_t sms, int32_t (&form)[3]) {
+void i8_gemm_form(const I8GemmProblem &g, int32_t sms, int32_t (&form)[3]) {
     const Choice c = choose(g, sms ? sms : sm_count());
     form[0] = c.mode < 0 ? 3 : c.mode, form[1] = c.splits, form[2] = c.nt;
-    return true;
 }
 
 cudaError_t launch_i8_gemm(const I8GemmProblem &g, cudaStream_t s) {

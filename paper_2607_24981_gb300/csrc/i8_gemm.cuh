@@ -117,7 +117,6 @@ __device__ __forceinline__ void tst16(uint32_t taddr, const uint32_t (&v)[16]) {
 
 // Two values to 2 bytes each, the first in the low half.
 template <typename T> __device__ __forceinline__ uint32_t pair_out(float a, float b);
-template <> __device__ __forceinline__ uint32_t pair_out<float>(float, float) { return 0; }  // (not asked for)
 template <> __device__ __forceinline__ uint32_t pair_out<__half>(float a, float b) {
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t *>(&h);
@@ -473,7 +472,7 @@ __global__ void __launch_bounds__(kI8Threads, 1) i8_gemm_kernel(const __grid_con
                 if constexpr (!PAIR) {
                     const uint32_t tsrc = data0 + s * p.stage_bytes + kTileRowsW * 128 + (8 * q + trow) * 128 + (((4 * h + tc) ^ trow) << 4);
 #pragma unroll
-                    for (int i = kHeld; i < kI8MaxTok / 32; ++i)
+                    for (int i = kHeld; i < kI8MaxTokOne / 32; ++i)
                         if ((int)q + 4 * i < groups) {
                             lds128(tsrc + i * 4096, a[0]);
                             put(i, a[0]);

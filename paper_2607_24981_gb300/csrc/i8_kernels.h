@@ -50,7 +50,7 @@ constexpr int kI8MaxExperts = 1024;
 constexpr int kI8MaxK = (1 << 17) - 1;  // |sum| <= 2^14 K < 2^31
 // What launch_i8_gemm would take on `sms` SMs (0: as many as the current device has): form 0 (a CTA a tile), 1 (several), 2 (a pair) or 3
 // (launch_i8_few), CTAs that share a tile's K, most tokens a tile.
-bool i8_gemm_form(const I8GemmProblem &g, int32_t sms, int32_t (&form)[3]);
+void i8_gemm_form(const I8GemmProblem &g, int32_t sms, int32_t (&form)[3]);
 cudaError_t launch_i8_few(const I8GemmProblem &g, cudaStream_t s);
 cudaError_t launch_i8_gemm(const I8GemmProblem &g, cudaStream_t s);
 

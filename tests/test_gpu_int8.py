@@ -483,3 +483,43 @@ def test_two_products_at_once(ilw):
     torch.cuda.synchronize()
     assert all(torch.equal(g, want) for g in got)
     ilw.device_status()
+
+
+# ---------------------------------------------------------------------------- past 2^31 elements
+def test_rows_past_32_bits(ilw):
+    """The last rows of a matrix of more than 2^31 values are those that they are alone, there and back."""
+    R, K = 270000, 8192
+    x = torch.empty((R, K), dtype=torch.bfloat16, device="cuda").normal_(generator=generator(1))
+    q = ilw.i8_quantize(x)
+    last = ilw.i8_quantize(x[-300:])
+    assert torch.equal(q.codes[-300:], last.codes) and torch.equal(q.scales[-300:], last.scales)
+    at = torch.tensor([R - 1, 0, R - 2], dtype=torch.int32, device="cuda")
+    some, want = ilw.i8_quantize(x, gather=at), ilw.i8_quantize(x[at.long()])
+    assert torch.equal(some.codes, want.codes) and torch.equal(some.scales, want.scales)
+    y = ilw.i8_dequantize(q, dtype=torch.bfloat16, out=x)
+    assert torch.equal(y[-300:], ilw.i8_dequantize(last, dtype=torch.bfloat16))
+
+
+@pytest.mark.parametrize("act", ["none", "silu_gate"])
+def test_results_past_32_bits(ilw, act):
+    """The last rows of a result of more than 2^31 values (sums below 2^24, so that the order of additions does not matter)."""
+    M, N, K = 140000, 16400 * (2 if act == "silu_gate" else 1), 70
+    A, W = ilw.i8_quantize(torch.randn((M, K), generator=generator(1), device="cuda")), made(ilw, 3, N, K, weights=True)
+    y = ilw.i8_linear(A, W, act=act)
+    for lo, hi in ((0, 130), (M - 130, M)):
+        check_product(y[lo:hi], ilw.I8Tensor(A.codes[lo:hi], A.scales[lo:hi]), W, None, act)
+
+
+@pytest.mark.parametrize("count", [1, 60])
+def test_weights_past_32_bits(ilw, count):
+    """The last of experts with more than 2^31 codes, by the kernel for few tokens and by tiles."""
+    E, N, K = 36, 8200, 8192
+    x = torch.empty((E * N, K), dtype=torch.bfloat16, device="cuda").normal_(generator=generator(1))
+    q = ilw.i8_quantize(x)
+    W = ilw.I8Tensor(q.codes.unflatten(0, (E, N)), q.scales.view(E, N))
+    A = made(ilw, 3, E * count, K)
+    offsets = torch.arange(0, E * count + 1, count, dtype=torch.int32, device="cuda")
+    y = ilw.i8_grouped_linear(A, W, offsets, out_dtype=torch.float32)
+    for e in (0, E - 2, E - 1):
+        rows = slice(e * count, (e + 1) * count)
+        check_product(y[rows], ilw.I8Tensor(A.codes[rows], A.scales[rows]), ilw.I8Tensor(W.codes[e], W.scales[e]), None, "none")
