@@ -4,14 +4,16 @@
 // not finite), codes x / s rounded to the nearest whole number, ties to the even one.
 //
 // The codes are those of the exact quotient.  n = rint(x (1 / s)) is it, or its neighbour where x / s lies within 127 roundings of fp32
-// of a half; x - n s is exact in fp32 (a multiple of the smaller of the units of x and s that is at most about s / 2), so comparing it with
-// s / 2 tells.  That is five operations a value, and a rare branch a unit of values, where a division would take some ten.
+// of a half; d = x - n s is exact in fp32 (a multiple of the smaller of the units of x and s that is at most about s / 2), and rint(n + d (1 / s)),
+// one fma, is the code unless x lies on a half: 2 x is a multiple of the unit u = 2^-23 2^e of s = m 2^e (1 <= m < 2) where it comes close to an odd
+// multiple of s, so from the half it is u / 2 s = 2^-24 / m away at least, and 1 / s rounded moves d / s by at most 2^-26 m, which is less.  On
+// a half it is right too if 1 / s is exact.  fp32 values may lie on halves of any other scale, 16-bit ones of scales with no more bits than theirs:
+// there d is compared with s / 2 (65536 x 1536 bf16 that way 63 us, so 44.8).
 //
 // Bytes are what it moves.  A row is held in registers between its maximum and its codes, by 8 lanes, a warp, 128 or 512 threads; past 24576
 // (512 x 6 pieces of 16 bytes) it is read twice.  Rows on 16-byte boundaries are loaded and stored 16 bytes at a time; others value by value, four
-// consecutive ones a thread (whole lines, with the codes exchanged between lanes, were slower: 65536 x 1537 bf16 117 us, so 89).  16384 x 4096
-// fp32: 47.7 us (7.0 TB/s), back 49.1 (6.8).  65536 x 1536 bf16: 58.6 us (5.2 TB/s), back 50.2 (6.0): 20 warps an SM that load, reduce and encode in
-// turn, issue 65 % and the integer pipe 74 % busy; neither fewer integer operations nor four CTAs an SM made it faster.
+// consecutive ones a thread (whole lines, with the codes exchanged between lanes, were slower: 65536 x 1537 bf16 117 us, so 80).  16384 x 4096
+// fp32: 47.8 us (7.0 TB/s), back 49.1 (6.8).  65536 x 1536 bf16: 44.8 us (6.75 TB/s), back 50.2 (6.0).
 #include <algorithm>
 #include <cstdint>
 
@@ -63,8 +65,35 @@ __device__ __forceinline__ float magnitude_value(uint32_t m, __nv_bfloat16) { re
 
 constexpr float kMagic = 12582912.0f;  // 1.5 2^23: x + kMagic holds rint(x) in its low bits
 
+// Whether a value of T can lie on a half of s without 1 / s being exact: x = (n + 1/2) s takes a scale of no more bits than T has.
+__device__ __forceinline__ bool halves(float, float) { return true; }
+__device__ __forceinline__ bool halves_of(float s, uint32_t past) {
+    const uint32_t b = __float_as_uint(s);
+    return (b & past) == 0 && (b & 0x7fffff) != 0;
+}
+__device__ __forceinline__ bool halves(float s, __half) { return halves_of(s, 0x1fff); }
+__device__ __forceinline__ bool halves(float s, __nv_bfloat16) { return halves_of(s, 0xffff); }
+
+template <int V> __device__ __forceinline__ void code_words(const float (&t)[V], uint32_t (&w)[V / 4]) {
+#pragma unroll
+    for (int i = 0; i < V / 4; ++i)
+        w[i] = __byte_perm(__byte_perm(__float_as_uint(t[4 * i]), __float_as_uint(t[4 * i + 1]), 0x0040),
+                           __byte_perm(__float_as_uint(t[4 * i + 2]), __float_as_uint(t[4 * i + 3]), 0x0040), 0x5410);
+}
 // Codes of a unit, four to a word.
 template <typename T, int V> __device__ __forceinline__ void encode(const Unit<T, V> &x, float s, float inv, uint32_t (&w)[V / 4]) {
+    float t[V];
+#pragma unroll
+    for (int i = 0; i < V; i += 2) {
+        const float2 p = pair(x, i / 2);
+        const uint64_t v = pack2(p.x, p.y), sum = fma2(v, both(inv), both(kMagic));
+        const float2 c = unpack2(fma2(fma2(fma2(sum, both(-1.0f), both(kMagic)), both(s), v), both(inv), sum));
+        t[i] = c.x, t[i + 1] = c.y;
+    }
+    code_words(t, w);
+}
+// The same where values may lie on a half.
+template <typename T, int V> __device__ __forceinline__ void encode_halves(const Unit<T, V> &x, float s, float inv, uint32_t (&w)[V / 4]) {
     float t[V], worst = 0.0f;
 #pragma unroll
     for (int i = 0; i < V; i += 2) {
@@ -81,15 +110,15 @@ template <typename T, int V> __device__ __forceinline__ void encode(const Unit<T
             if (fabsf(r) > half || (fabsf(r) == half && (__float_as_uint(t[i]) & 1))) t[i] += copysignf(1.0f, r);
         }
     }
-#pragma unroll
-    for (int i = 0; i < V / 4; ++i)
-        w[i] = __byte_perm(__byte_perm(__float_as_uint(t[4 * i]), __float_as_uint(t[4 * i + 1]), 0x0040),
-                           __byte_perm(__float_as_uint(t[4 * i + 2]), __float_as_uint(t[4 * i + 3]), 0x0040), 0x5410);
+    code_words(t, w);
 }
 
+// CTAs an SM, so that loads of some rows overlap the arithmetic of others (65536 x 1536 bf16: with three 47.7 us, so 44.8, with five 45.3 and
+// spills; 4096 x 8192 fp32: with six 52.3, so 27.5, with ten 32.5; 2000 x 20000 fp32: with one 69.5, so 44.5).
+constexpr int quantize_ctas(int G, int held) { return G == 512 ? 3 : G == 128 ? (held > 4 ? 8 : 10) : held > 4 ? 4 : 5; }
 // G threads a row (a warp, or the whole CTA); each holds up to kHeld units of it.
 template <typename T, bool WIDE, int G, int kHeld>
-__global__ void __launch_bounds__(G <= 32 ? 256 : G, G == 512 ? 2 : 1) i8_quantize_kernel(const I8QuantParams p) {
+__global__ void __launch_bounds__(G <= 32 ? 256 : G, quantize_ctas(G, kHeld)) i8_quantize_kernel(const I8QuantParams p) {
     constexpr int V = WIDE ? 16 / (int)sizeof(T) : 4;
     __shared__ uint32_t warp_max[G < 32 ? 1 : G / 32];
     grid_wait();
@@ -138,15 +167,7 @@ __global__ void __launch_bounds__(G <= 32 ? 256 : G, G == 512 ? 2 : 1) i8_quanti
     const float s = largest > 0.0f ? fmaxf(__fdiv_rn(largest, 127.0f), 1.17549435e-38f) : 0.0f, inv = s > 0.0f && fine ? __frcp_rn(s) : 0.0f;
     if (q == 0) p.scales[r] = fine ? s : __int_as_float(0x7fc00000);
     int8_t *c = p.codes + r * p.ldc;
-    auto store = [&](int32_t u, const Unit<T, V> &y) {
-        if (u >= units) return;
-        uint32_t w[V / 4];
-        if (fine) {
-            encode(y, s, inv, w);
-        } else {
-#pragma unroll
-            for (int i = 0; i < V / 4; ++i) w[i] = 0;
-        }
+    auto put = [&](int32_t u, const uint32_t (&w)[V / 4]) {
         int8_t *at = c + (int64_t)u * V;
         if constexpr (V == 8) {
             *(uint2 *)at = make_uint2(w[0], w[1]);
@@ -156,9 +177,26 @@ __global__ void __launch_bounds__(G <= 32 ? 256 : G, G == 512 ? 2 : 1) i8_quanti
                 for (int i = 0; u * 4 + i < K; ++i) at[i] = (int8_t)(w[0] >> (8 * i));
         }
     };
+    uint32_t w[V / 4] = {};
+    if (!fine) {
+        for (int32_t u = q; u < units; u += G) put(u, w);
+    } else if (sizeof(T) == 2 && halves(s, T())) {  // (rare: from memory again)
+#pragma unroll 1
+        for (int32_t u = q; u < units; u += G) {
+            encode_halves(load(u), s, inv, w);
+            put(u, w);
+        }
+    } else {
+        auto code = [&](int32_t u, const Unit<T, V> &y) {
+            if (u >= units) return;
+            if constexpr (sizeof(T) == 2) encode(y, s, inv, w);
+            else encode_halves(y, s, inv, w);
+            put(u, w);
+        };
 #pragma unroll
-    for (int j = 0; j < kHeld; ++j) store(q + j * G, held[j]);
-    for (int32_t u = q + kHeld * G; u < units; u += G) store(u, load(u));
+        for (int j = 0; j < kHeld; ++j) code(q + j * G, held[j]);
+        for (int32_t u = q + kHeld * G; u < units; u += G) code(u, load(u));
+    }
 }
 
 // A code times s, from byte i of w ^ 0x80808080: 2^23 + 128 + code has that byte at its end (the conversion's own instruction has a quarter of

@@ -116,6 +116,21 @@ def test_quantize_halves_and_their_neighbours(ilw, dtype, K):
         assert int(odd.sum()) > 100 and bool((got.codes[odd] % 2 == 0).all())
 
 
+@pytest.mark.parametrize("dtype,digits", [(torch.float16, 10), (torch.bfloat16, 7)])
+@pytest.mark.parametrize("exponent", [0, 5, -9])
+def test_quantize_every_pair_of_significands(ilw, dtype, digits, exponent):
+    """Every largest value of a binade (a row each) with every smaller value down to 1/256 of the binade, of both signs."""
+    n = 1 << digits
+    largest = (1 + torch.arange(n, device="cuda", dtype=torch.float64) / n) * 2.0**exponent
+    values = torch.cat([largest * 2.0**-b for b in range(9)])
+    x = torch.minimum(values[None, :], largest[:, None]) * torch.where(torch.arange(len(values), device="cuda") % 3 == 1, -1.0, 1.0)
+    x[:, 0] = largest
+    q = ilw.i8_quantize(x.to(dtype))
+    for rows in torch.arange(n, device="cuda").split(128):
+        code, scale = ref_quantize(x[rows].to(dtype).double())
+        assert torch.equal(q.scales[rows], scale) and torch.equal(q.codes[rows], code)
+
+
 def test_quantize_special_values(ilw):
     """Rows of zeros, subnormals, the largest numbers, infinities and NaN."""
     big, inf, nan = 3.4028234e38, float("inf"), float("nan")
