@@ -1,4 +1,4 @@
-// moe_order.cuh -- what routing kernels share (moe.cu, moe_scored.cu): the sizes of chunks, tokens' rows in shared memory and the places of entries.
+// moe_order.cuh -- what routing kernels share (moe.cu, moe_scored.cuh): the sizes of chunks, tokens' rows in shared memory and the places of entries.
 #pragma once
 #include <algorithm>
 #include <cstdint>

@@ -1,4 +1,4 @@
-// moe_scores.cuh -- selection of a token's experts by scores, with a bias and by groups (a part of moe_scored.cu).
+// moe_scores.cuh -- selection of a token's experts by scores, with a bias and by groups (a part of moe_scored.cuh).
 //
 //   s[e] = 1 / (1 + exp(-x[e])), or the softmax of the row;  c[e] = s[e] + bias[e]
 //   a group's rank is its largest c, or the sum of its two largest; the best `top_groups` groups stay

@@ -85,7 +85,6 @@ cudaError_t launch_moe_route_scored(const MoeScoredParams &p, cudaStream_t s);  
 // For the latter: whether one CTA takes all, and the order from chunks' counts (chunks of 256 or 512 tokens).
 bool moe_route_in_one(int32_t T, int32_t E);
 cudaError_t launch_moe_place(const MoeRouteParams &p, int32_t chunk, cudaStream_t s);
-constexpr int kRouteMaxGroups = ILW_MOE_MAX_GROUPS;
 
 struct MoeCombineParams {
     const void *Y;

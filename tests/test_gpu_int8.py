@@ -218,7 +218,7 @@ def test_linear_matches_64_bits(ilw, M, N, K, act, bias):
 
 @pytest.mark.parametrize("M", [1, 8, 40, 400])
 @pytest.mark.parametrize("code", [127, -128])
-@pytest.mark.parametrize("K", [1024, 1030, 8192])
+@pytest.mark.parametrize("K", [1024, 1030, 8192, (1 << 17) - 1])
 def test_linear_of_the_largest_codes(ilw, M, code, K):
     """Sums past 2^24, and up to K = 1024 (2^24 itself) exact ones."""
     A, W = ilw.i8_empty(M, K), ilw.i8_empty(130, K)
@@ -399,6 +399,35 @@ def test_experts_feed_forward(ilw, T, act, dtype):
             check_product(h[s], ilw.I8Tensor(a.codes[s], a.scales[s]), ilw.I8Tensor(ffn.w1.codes[e], ffn.w1.scales[e]), b1[e], act)
             check_product(y[s], ilw.I8Tensor(q.codes[s], q.scales[s]), ilw.I8Tensor(ffn.w2.codes[e], ffn.w2.scales[e]), None, "none")
     assert torch.equal(got, ilw.moe_combine(y, r.slot, r.weight, residual=x))
+    ilw.device_status()
+
+
+def test_experts_in_two_graphs(ilw):
+    """Captured twice, replayed in turn on new inputs, some of whose tokens have no expert."""
+    E, d, F, T = 16, 96, 160, 700
+    gen = generator(5)
+    ffn = ilw.I8Experts(torch.randn((E, 2 * F, d), generator=gen, device="cuda") / d**0.5, torch.randn((E, d, F), generator=gen, device="cuda") / F**0.5, 3,
+                        score="sigmoid", bias=0.1 * torch.randn(E, generator=gen, device="cuda"), groups=4, top_groups=2)
+    x = [torch.randn((T, d), generator=gen, device="cuda").half() for _ in range(3)]
+    logits = [torch.randn((T, E), generator=gen, device="cuda") for _ in range(3)]
+    for i, v in enumerate(logits):
+        v[100 * i:200 * i] = float("-inf")
+    want = [ffn.forward(a, b) for a, b in zip(x, logits)]
+    graphs = []
+    for _ in range(2):
+        a, b, g = x[0].clone(), logits[0].clone(), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            y = ffn.forward(a, b)
+        graphs.append((a, b, g, y))
+    for pair in ((1, 2), (2, 0), (0, 1)):
+        for (a, b, g, y), i in zip(graphs, pair):
+            a.copy_(x[i])
+            b.copy_(logits[i])
+            g.replay()
+        torch.cuda.synchronize()
+        for (a, b, g, y), i in zip(graphs, pair):
+            assert torch.equal(y, want[i])
+    assert bool((want[2][200:400] == 0).all())
     ilw.device_status()
 
 
