@@ -23,9 +23,6 @@ __device__ __forceinline__ float load_bias(const MoeScoredParams &p, float *to, 
     return max_of_lanes<32>(m);
 }
 
-// Words of a token's ranks (an odd number, so that tokens meet in no bank), and of the biases.
-__host__ __device__ inline int rank_words(const RouteScores &q) { return q.groups > 1 ? 2 * q.groups | 1 : 0; }
-
 // Selection of a chunk's tokens by a cluster, L lanes each, and the chunk's counts, as route_select_kernel.
 template <typename T, int S, int L>
 __global__ void __cluster_dims__(kSelectCtas, 1, 1) __launch_bounds__(select_tokens(S) * L) route_scored_kernel(const __grid_constant__ MoeScoredParams p, int wide) {

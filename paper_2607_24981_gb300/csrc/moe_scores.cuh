@@ -12,8 +12,9 @@
 // an exponent y = x or x - max, |y| 2^-23 relative to exp(-|y|), which stays below 2^-24; of the sum with the bias by 2^-24 |c|.  So c is off by
 // less than doubt() = u min(1, |c| + max|bias|) + 2^-23 |c| + 2^-24, with u 2^-21 for the sigmoid and 2^-19 for the softmax.
 // Where two of those that are taken, or one and another that is not, lie closer than their doubts, and are not equal logits with equal biases,
-// they are ordered again in 64 bits by the whole warp (one row in some hundred of random logits and biases), and where the groups are in doubt the
-// whole row is done again.
+// they are ordered again in 64 bits by the whole warp (one row in some hundred of random logits and biases), and so are groups that lie that close.
+// 64-bit operations have some 1/60 of the rate of fp32 here, and one row that is done again holds up its warp, so it is those few values and not the row
+// (2084 tokens of 112 experts, softmax, 7 of 16 groups: 30 us with whole rows, so TAIL).
 #pragma once
 #include <cstdint>
 
@@ -23,6 +24,9 @@
 
 namespace ilw {
 namespace {
+
+// Words of a token's ranks (an odd number, so that tokens meet in no bank).
+__host__ __device__ inline int rank_words(const RouteScores &q) { return q.groups > 1 ? 2 * q.groups | 1 : 0; }
 
 constexpr float kNone = -__builtin_huge_valf();
 
@@ -74,7 +78,7 @@ template <typename T> __device__ __forceinline__ Exact exact_scores(const MoeSco
     return s;
 }
 
-// The experts of a token, the j-th in lane j (-1: none): all of it in 64 bits, each lane PER consecutive experts.  (Comparisons are of keys: those of
+// The experts of a token with biases, the j-th in lane j (-1: none): all of it in 64 bits, each lane PER consecutive experts.  (Comparisons are of keys: those of
 // 64-bit numbers would be the slower part.)
 template <typename T, int PER>
 __device__ __noinline__ int32_t choose_exactly(const MoeScoredParams &p, const T *row, int lane) {
@@ -85,7 +89,7 @@ __device__ __noinline__ int32_t choose_exactly(const MoeScoredParams &p, const T
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const float x = e0 + i < p.E ? logit(to_f(row[e0 + i])) : kNone;
-        key[i] = x > kNone ? order_key(q.bias ? score(x) + (double)__ldg(q.bias + e0 + i) : (double)x) : 0;
+        key[i] = x > kNone ? order_key(score(x) + (double)__ldg(q.bias + e0 + i)) : 0;
     }
     if (q.groups > 1) {
         uint64_t mine1 = 0, mine2 = 0;  // the two largest of group `lane`
@@ -104,10 +108,7 @@ __device__ __noinline__ int32_t choose_exactly(const MoeScoredParams &p, const T
             if (lane == g) mine1 = t1, mine2 = t2;
         }
         uint64_t rank = mine1;
-        if (q.group_best == 2 && mine1) {  // (of logits: their scores' sum)
-            if (!q.bias) rank = order_key(score((float)key_value(mine1)) + (mine2 ? score((float)key_value(mine2)) : 0.0));
-            else if (mine2) rank = order_key(key_value(mine1) + key_value(mine2));
-        }
+        if (q.group_best == 2 && mine2) rank = order_key(key_value(mine1) + key_value(mine2));
         int place = 0;  // of this lane's group among all
         for (int g = 0; g < q.groups; ++g) {
             const uint64_t other = __shfl_sync(0xffffffffu, rank, g);
@@ -152,6 +153,41 @@ __device__ __noinline__ void order_exactly(const MoeScoredParams &p, const T *ro
         place += other > key || (other == key && o < e);
     }
     if (e >= 0 && place < p.k) out_e[place] = e;
+}
+
+// The groups of a token that stay, where fp32 cannot tell: `stay` by their ranks in fp32, `last` of those that stay and `next` of the others (ranks,
+// and behind them how far each may be off).  Those that lie clear of the other side keep it; the others' ranks are computed in 64 bits.
+template <typename T>
+__device__ __noinline__ uint32_t groups_exactly(const MoeScoredParams &p, const T *row, const float *ranks, uint32_t stay, int last, int next, int lane) {
+    const RouteScores &q = p.scores;
+    const Exact score = exact_scores(p, row, lane);
+    const int mine = min(lane, q.groups - 1), of = stay >> mine & 1 ? next : last;
+    const uint32_t doubtful =
+        __ballot_sync(0xffffffffu, lane < q.groups && ranks[mine] > kNone && fabsf(ranks[mine] - ranks[of]) <= 2.0f * (ranks[q.groups + mine] + ranks[q.groups + of]));
+    uint64_t rank = 0;  // of group `lane`
+    for (uint32_t left = doubtful; left; left &= left - 1) {
+        const int g = __ffs(left) - 1;
+        uint64_t m1 = 0, m2 = 0;  // this lane's two largest of the group
+        for (int i = lane; i < q.group_size; i += 32) {
+            const int e = g * q.group_size + i;
+            const float x = logit(to_f(row[e]));
+            const uint64_t key = x > kNone ? order_key(score(x) + (q.bias ? (double)__ldg(q.bias + e) : 0.0)) : 0;
+            m2 = max(m2, min(m1, key));
+            m1 = max(m1, key);
+        }
+        const uint64_t t1 = warp_max(m1);
+        const int holder = __ffs(__ballot_sync(0xffffffffu, m1 == t1)) - 1;
+        const uint64_t t2 = warp_max(lane == holder ? m2 : m1);
+        if (lane == g) rank = q.group_best == 2 && t2 ? order_key(key_value(t1) + key_value(t2)) : t1;
+    }
+    int place = 0;  // of this lane's group among the doubtful
+    for (uint32_t left = doubtful; left; left &= left - 1) {
+        const int g = __ffs(left) - 1;
+        const uint64_t other = __shfl_sync(0xffffffffu, rank, g);
+        place += other > rank || (other == rank && g < lane);
+    }
+    const uint32_t in = __ballot_sync(0xffffffffu, rank && place < __popc(stay & doubtful));
+    return (stay & ~doubtful) | (in & doubtful);
 }
 
 // ---- the fast way: L lanes a token, its row in shared memory, its experts in 16 search groups as in moe.cu
@@ -205,8 +241,8 @@ template <int L> __device__ __forceinline__ uint32_t any_of_lanes(uint32_t v) {
     return v;
 }
 
-// The experts of a token by L lanes (lane q of them here; all 32 lanes of the warp call it) to out_e, in order; 1 if fp32 cannot tell that
-// order, 2 if it cannot tell the groups.  `row` holds its logits and is lost, but for the c of those left; `logits` are its row in memory; `bias` [E] and its largest magnitude; ranks [2 groups]: room.
+// The experts of a token by L lanes (lane q of them here; all 32 lanes of the warp call it) to out_e, in order; not 0 if fp32 cannot tell that
+// order.  `row` holds its logits and is lost, but for the c of those left; `logits` are its row in memory; `bias` [E] and its largest magnitude; ranks [2 groups]: room.
 // best and sum: largest logit, and the softmax's denominator if that is needed.  least: the smallest c taken.
 template <typename T, int L, int S>
 __device__ __forceinline__ uint32_t select_scored(const MoeScoredParams &p, const T *logits, const float *bias, float bias_max, float *row, float *ranks, int q,
@@ -264,7 +300,6 @@ __device__ __forceinline__ uint32_t select_scored(const MoeScoredParams &p, cons
         }
         __syncwarp();
     }
-    uint32_t unsure = 0;
     if (r.groups > 1) {
         float *offs = ranks + r.groups;  // how far each rank may be off
         for (int g = q; g < r.groups; g += L) {
@@ -304,6 +339,7 @@ __device__ __forceinline__ uint32_t select_scored(const MoeScoredParams &p, cons
             last = max(last, __shfl_xor_sync(0xffffffffu, last, d));
             next = max(next, __shfl_xor_sync(0xffffffffu, next, d));
         }
+        bool close = false;
         if ((bias || r.group_best == 2) && last >= 0 && next >= 0) {  // who lies close to the other side's, and is not its equal, is in doubt
             for (int g = q; g < r.groups; g += L) {
                 const int of = stay >> g & 1 ? next : last;
@@ -311,9 +347,16 @@ __device__ __forceinline__ uint32_t select_scored(const MoeScoredParams &p, cons
                     float a1, a2, b1, b2;
                     top2(row + g * r.group_size, r.group_size, a1, a2);
                     top2(row + of * r.group_size, r.group_size, b1, b2);
-                    if (bias || a1 != b1 || (a2 != b2 && r.group_best == 2)) unsure |= 2;
+                    if (bias || a1 != b1 || (a2 != b2 && r.group_best == 2)) close = true;
                 }
             }
+        }
+        for (uint32_t again = __ballot_sync(0xffffffffu, any_of_lanes<L>(close) && q == 0); again; again &= again - 1) {
+            const int l = __ffs(again) - 1, lane = threadIdx.x & 31, t = l / L - lane / L;  // a token of this warp's, from this lane's
+            const T *x = (const T *)__shfl_sync(0xffffffffu, (unsigned long long)logits, l);
+            const uint32_t exact = groups_exactly<T>(p, x, ranks + t * rank_words(r), __shfl_sync(0xffffffffu, stay, l),
+                                                     __shfl_sync(0xffffffffu, last, l), __shfl_sync(0xffffffffu, next, l), lane);
+            if (t == 0) stay = exact;
         }
         __syncwarp();
         for (int g = q; g < r.groups; g += L)
@@ -339,6 +382,7 @@ __device__ __forceinline__ uint32_t select_scored(const MoeScoredParams &p, cons
     auto equal = [&](int a, int b) { return to_f(logits[a]) == to_f(logits[b]) && bias[a] == bias[b]; };
     float before = __int_as_float(0x7f800000);
     int taken = 0;
+    uint32_t unsure = 0;
     bool close = false;  // the last two taken
     for (int j = 0; j < p.k; ++j) {
         // the largest search group, the first of equal ones
@@ -354,7 +398,7 @@ __device__ __forceinline__ uint32_t select_scored(const MoeScoredParams &p, cons
             const int g2 = __shfl_xor_sync(0xffffffffu, g, d);
             if (m2 > m || (m2 == m && g2 < g)) m = m2, g = g2;
         }
-        if (close && !equal(out_e[j - 2], out_e[j - 1])) unsure |= 1;
+        if (close && !equal(out_e[j - 2], out_e[j - 1])) unsure = 1;
         const bool on = m > kNone;
         if (on && g % L == q) {  // its lane takes the first expert with that value
             const float4 *x = (const float4 *)(row + g * S);
@@ -384,7 +428,7 @@ __device__ __forceinline__ uint32_t select_scored(const MoeScoredParams &p, cons
         __syncwarp();
     }
     if (bias) {
-        if (close && !equal(out_e[p.k - 2], out_e[p.k - 1])) unsure |= 1;
+        if (close && !equal(out_e[p.k - 2], out_e[p.k - 1])) unsure = 1;
         // is the last one taken clear of all that are left
         float m = top[0];
 #pragma unroll
@@ -395,7 +439,7 @@ __device__ __forceinline__ uint32_t select_scored(const MoeScoredParams &p, cons
             for (int i = 0; i < G; ++i)
                 for (int c = 0; c < S; ++c) {
                     const float v = row[(L * i + q) * S + c];
-                    if (v > kNone && before - v <= off + doubt(v) && !equal((L * i + q) * S + c, e)) unsure |= 1;
+                    if (v > kNone && before - v <= off + doubt(v) && !equal((L * i + q) * S + c, e)) unsure = 1;
                 }
         }
     }
@@ -447,41 +491,33 @@ __device__ __forceinline__ void route_tokens(const MoeScoredParams &p, int64_t t
         float *its = row + (t - lane / L) * (kGroups * S + 4);
         const T *x = (const T *)p.logits + (t0 + t) * p.ld;
         const float low = __shfl_sync(0xffffffffu, least, l);
-        bool whole = __shfl_sync(0xffffffffu, unsure, l) & 2;
-        if (!whole) {
-            // candidates: those taken, and those left whose c comes close to the least of them
-            int32_t hits = 0, n = 0;
-            uint32_t which = 0;
-            for (int i = 0; i < S / 2; ++i) {
-                const float v = its[32 * i + lane];
-                const bool hit = v > kNone && low - v <= doubt(low) + doubt(v);
-                which |= (uint32_t)hit << i;
-                hits += hit;
-            }
-            int32_t before = hits;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int32_t y = __shfl_up_sync(0xffffffffu, before, d);
-                if (lane >= d) before += y;
-            }
-            n = p.k + __shfl_sync(0xffffffffu, before, 31);
-            whole = n > 32;
-            if (!whole) {
-                __syncwarp();
-                int32_t *list = (int32_t *)its + before - hits;  // (what the row held has been read)
-                for (; which; which &= which - 1) *list++ = 32 * (__ffs(which) - 1) + lane;
-                __syncwarp();
-                const int32_t e = lane < p.k ? to[lane] : lane < n ? ((int32_t *)its)[lane - p.k] : -1;
-                __syncwarp();
-                order_exactly<T>(p, x, e, n, to, lane);
-            }
+        // candidates: those taken, and those left whose c comes close to the least of them
+        int32_t hits = 0;
+        uint32_t which = 0;
+        for (int i = 0; i < S / 2; ++i) {
+            const float v = its[32 * i + lane];
+            const bool hit = v > kNone && low - v <= doubt(low) + doubt(v);
+            which |= (uint32_t)hit << i;
+            hits += hit;
         }
-        if (whole) {
+        int32_t before = hits;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int32_t y = __shfl_up_sync(0xffffffffu, before, d);
+            if (lane >= d) before += y;
+        }
+        const int32_t n = p.k + __shfl_sync(0xffffffffu, before, 31);
+        if (n <= 32) {
+            __syncwarp();
+            int32_t *list = (int32_t *)its + before - hits;  // (what the row held has been read)
+            for (; which; which &= which - 1) *list++ = 32 * (__ffs(which) - 1) + lane;
+            __syncwarp();
+            const int32_t e = lane < p.k ? to[lane] : lane < n ? ((int32_t *)its)[lane - p.k] : -1;
+            __syncwarp();
+            order_exactly<T>(p, x, e, n, to, lane);
+        } else {
             const int32_t e = choose_exactly<T, S / 2>(p, x, lane);
-            if (lane < p.k) {
-                to[lane] = e;
-                if (!bias && e >= 0) out_w[(t - lane / L) * entries + lane] = to_f(x[e]);
-            }
+            if (lane < p.k) to[lane] = e;
         }
     }
     __syncwarp();
