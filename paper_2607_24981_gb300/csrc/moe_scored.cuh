@@ -63,9 +63,12 @@ __global__ void __cluster_dims__(kSelectCtas, 1, 1) __launch_bounds__(select_tok
     add_counts<kSelectThreads>(p, count);
 }
 
+// Lanes a token where one CTA takes all (16 tokens of 256 experts in groups and with a bias: 11.6 us with eight, 13.0 with 16, 12.8 with four).
+constexpr int kManyLanes = 8, kManyTokens = 64, kFewLanes = 4;
+
 // Few tokens (a multiple of 32 / L, the last ones filled up): all of it by one CTA, L threads a token, as route_one_kernel.
 template <typename T, int S, int L>
-__global__ void __launch_bounds__(4 * kOneTokens) route_one_scored_kernel(const __grid_constant__ MoeScoredParams p, int wide, int tokens) {
+__global__ void __launch_bounds__(L == kManyLanes ? kManyLanes * kManyTokens : kFewLanes * kOneTokens) route_one_scored_kernel(const __grid_constant__ MoeScoredParams p, int wide, int tokens) {
     extern __shared__ __align__(16) uint32_t dyn[];
     __shared__ int32_t base[kRouteMaxExperts], count[kRouteMaxExperts], all;
     __shared__ float s_bias_max;
@@ -116,9 +119,7 @@ __global__ void __launch_bounds__(4 * kOneTokens) route_one_scored_kernel(const 
 size_t scored_smem(int tokens, int32_t E, int32_t k, const RouteScores &q) {
     return ((size_t)tokens * (row_words(E) + rank_words(q) + 2 * k) + (q.bias ? kGroups * group_size(E) : 0)) * 4;
 }
-// Lanes a token where one CTA takes all (16 tokens of 256 experts in groups and with a bias: 12.1 us with eight, 13.0 with 16, 12.8 with four).
-constexpr int kManyLanes = 8, kFewLanes = 4;
-int one_lanes(int32_t T) { return T <= 64 ? kManyLanes : kFewLanes; }
+int one_lanes(int32_t T) { return T <= kManyTokens ? kManyLanes : kFewLanes; }
 size_t one_scored_smem(int32_t T, int32_t E, int32_t k, const RouteScores &q) {
     const int per = 32 / one_lanes(T), tokens = (std::max(T, 1) + per - 1) / per * per;
     return scored_smem(tokens, E, k, q) + (size_t)2 * E * (kOneTokens / 32 + 1) * 4;

@@ -14,7 +14,7 @@
 // Where two of those that are taken, or one and another that is not, lie closer than their doubts, and are not equal logits with equal biases,
 // they are ordered again in 64 bits by the whole warp (one row in some hundred of random logits and biases), and so are groups that lie that close.
 // 64-bit operations have some 1/60 of the rate of fp32 here, and one row that is done again holds up its warp, so it is those few values and not the row
-// (2084 tokens of 112 experts, softmax, 7 of 16 groups: 30 us with whole rows, so TAIL).
+// (2084 tokens of 112 experts, softmax, 7 of 16 groups: 30 us with whole rows, so 23).
 #pragma once
 #include <cstdint>
 
@@ -35,14 +35,15 @@ constexpr float kNone = -__builtin_huge_valf();
 __device__ __forceinline__ double none64() { return __longlong_as_double(0xfff0000000000000ll); }
 // exp(x - best), where both may be infinite
 __device__ __forceinline__ float exp_below(float x, float best) { return x == best ? 1.0f : expf(x - best); }
-__device__ __forceinline__ double exp_below64(float x, float best) { return x == best ? 1.0 : exp((double)x - (double)best); }
+// (Out of line, like all that 64 bits take: where few tokens take this way, fetching its instructions is most of it.)
+__device__ __noinline__ double exp64(double x) { return exp(x); }
+__device__ __forceinline__ double exp_below64(float x, float best) { return x == best ? 1.0 : exp64((double)x - (double)best); }
 // 1 / (1 + exp(-x)).  fp32: by the exponential that cannot overflow, for scores below its normal range.  64 bits, which only compare: as it is
 // written, so that sums that are equal but for roundings (of the scores of x and -x) fall as plain operations let them.
 __device__ __forceinline__ float sigmoid(float x) {
     const float e = expf(-fabsf(x));
     return (x >= 0.0f ? 1.0f : e) / (1.0f + e);
 }
-__device__ __forceinline__ double sigmoid64(float x) { return 1.0 / (1.0 + exp(-(double)x)); }
 
 // A value as an unsigned number of the same order, 0 for -inf and NaN; the largest in a warp.
 __device__ __forceinline__ uint64_t order_key(double v) {
@@ -61,14 +62,20 @@ struct Exact {
     int32_t score;
     float best;
     double sum;
-    __device__ __forceinline__ double operator()(float x) const { return score == ILW_SCORE_SIGMOID ? sigmoid64(x) : exp_below64(x, best) / sum; }
+    __device__ __forceinline__ double operator()(float x) const {
+        const bool sigmoid = score == ILW_SCORE_SIGMOID;
+        const double e = !sigmoid && x == best ? 1.0 : exp64(sigmoid ? -(double)x : (double)x - (double)best);
+        return (sigmoid ? 1.0 : e) / (sigmoid ? 1.0 + e : sum);
+    }
 };
 template <typename T> __device__ __forceinline__ Exact exact_scores(const MoeScoredParams &p, const T *row, int lane) {
     Exact s = {p.scores.score, kNone, 0.0};
     if (s.score == ILW_SCORE_SIGMOID) return s;
+#pragma unroll 1
     for (int e = lane; e < p.E; e += 32) s.best = fmaxf(s.best, logit(to_f(row[e])));
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) s.best = fmaxf(s.best, __shfl_xor_sync(0xffffffffu, s.best, d));
+#pragma unroll 1
     for (int e = lane; e < p.E; e += 32) {
         const float x = logit(to_f(row[e]));
         if (x > kNone) s.sum += exp_below64(x, s.best);
@@ -168,6 +175,7 @@ __device__ __noinline__ uint32_t groups_exactly(const MoeScoredParams &p, const 
     for (uint32_t left = doubtful; left; left &= left - 1) {
         const int g = __ffs(left) - 1;
         uint64_t m1 = 0, m2 = 0;  // this lane's two largest of the group
+#pragma unroll 1
         for (int i = lane; i < q.group_size; i += 32) {
             const int e = g * q.group_size + i;
             const float x = logit(to_f(row[e]));

@@ -122,7 +122,7 @@ def test_scores_that_32_bits_do_not_separate(ilw, T, groups, top_groups, group_b
     check(ilw, rows, 8, False, bias=bias, score=score, groups=groups, top_groups=top_groups, group_best=group_best)
 
 
-@pytest.mark.parametrize("T", [1, 2, 31, 32, 33, 60, 111, 113, 224, 225, 256, 257, 511, 513])
+@pytest.mark.parametrize("T", [1, 2, 31, 32, 33, 60, 64, 65, 111, 113, 224, 225, 256, 257, 511, 513])
 def test_route_of_few_tokens(ilw, T):
     """Either side of where a CTA does all and of the lanes it gives a token; with 32 groups, ranks that leave no room for that."""
     rng = np.random.default_rng(T)
