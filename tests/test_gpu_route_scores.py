@@ -122,6 +122,20 @@ def test_scores_that_32_bits_do_not_separate(ilw, T, groups, top_groups, group_b
     check(ilw, rows, 8, False, bias=bias, score=score, groups=groups, top_groups=top_groups, group_best=group_best)
 
 
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("biased", [False, True])
+@pytest.mark.parametrize("T,E,groups,top_groups,group_best", [(100, 256, 2, 1, 2), (60, 96, 32, 9, 2), (700, 256, 32, 9, 2), (300, 512, 4, 2, 1), (300, 112, 16, 7, 2), (1000, 24, 12, 5, 2)])
+def test_groups_that_32_bits_do_not_separate(ilw, T, E, groups, top_groups, group_best, biased, score):
+    """The groups of a token hold the same logits in another order, some of them one unit of fp32 larger."""
+    rng, size = np.random.default_rng(T + E), E // groups
+    same = rng.standard_normal((T, 1, size)).astype(np.float32)
+    nudged = np.where(rng.random((T, groups, size)) < 0.3, np.nextafter(same, np.float32(np.inf)), same)
+    x = rng.permuted(nudged, axis=2).reshape(T, E)
+    x[rng.random((T, E)) < 0.02] = -np.inf
+    bias = torch.full((E,), 0.125, device="cuda") if biased else None
+    check(ilw, torch.from_numpy(x).cuda(), 3, True, bias=bias, score=score, groups=groups, top_groups=top_groups, group_best=group_best)
+
+
 @pytest.mark.parametrize("T", [1, 2, 31, 32, 33, 60, 64, 65, 111, 113, 224, 225, 256, 257, 511, 513])
 def test_route_of_few_tokens(ilw, T):
     """Either side of where a CTA does all and of the lanes it gives a token; with 32 groups, ranks that leave no room for that."""
