@@ -139,7 +139,7 @@ __device__ __forceinline__ void lds128(uint32_t a, uint32_t (&v)[4]) {
 template <int kStep, typename P>
 __device__ __forceinline__ void list_tiles(const P &p, TileExpert *tab, int32_t *tab_id, int lane, int32_t &sum, int32_t &count, int32_t &head, int32_t &tail) {
     const int32_t M = (int32_t)p.M;
-    int32_t before = 0;  // (sum, count, before: of the experts before this round: tiles, those with rows, end of the last range)
+    int32_t before = 0;  // (sum, count, before: of the experts before these 32: tiles, those with rows, end of the last range)
     sum = count = 0, head = M;
     for (int e0 = 0; e0 < p.E; e0 += 32) {
         const int e = e0 + lane;
