@@ -459,22 +459,22 @@ __device__ __forceinline__ uint32_t select_scored(const MoeScoredParams &p, cons
 template <typename T, int L>
 __device__ __forceinline__ void weigh_scored(const MoeScoredParams &p, const T *logits, int q, const int32_t *out_e, float *out_w, float best, float sum, bool biased) {
     const bool softmax = p.scores.score == ILW_SCORE_SOFTMAX;
-    // renormalised sigmoids: exp(min(x, 0)) / (1 + exp(-|x|)), all times exp(-m) for the largest m of min(x, 0), so that scores too small for
-    // fp32 keep their ratios
-    const bool ratios = !softmax && p.renormalize;
+    // renormalised: exp(x), of sigmoids exp(min(x, 0)) / (1 + exp(-|x|)), all times exp(-m) for the largest m of those x or min(x, 0) that are taken,
+    // so that scores too small for fp32 keep their ratios (a bias may leave a softmax's largest logits untaken)
+    const bool ratios = p.renormalize;
     float m = kNone;
     for (int j = q; j < p.k; j += L)
         if (out_e[j] >= 0) {
             const float x = biased ? to_f(logits[out_e[j]]) : out_w[j];
             out_w[j] = x;
-            m = fmaxf(m, fminf(x, 0.0f));
+            m = fmaxf(m, softmax ? x : fminf(x, 0.0f));
         }
-    if (ratios) m = max_of_lanes<L>(m);
+    m = ratios ? max_of_lanes<L>(m) : best;
     float of = 0.0f;
     for (int j = q < p.k ? q + (p.k - 1 - q) / L * L : -1; j >= q; j -= L) {  // (the small ones first)
         const float x = out_w[j];
         float s = 0.0f;
-        if (out_e[j] >= 0) s = softmax ? exp_below(x, best) : ratios ? exp_below(fminf(x, 0.0f), m) / (1.0f + expf(-fabsf(x))) : sigmoid(x);
+        if (out_e[j] >= 0) s = softmax ? exp_below(x, m) : ratios ? exp_below(fminf(x, 0.0f), m) / (1.0f + expf(-fabsf(x))) : sigmoid(x);
         out_w[j] = s;
         of += s;
     }

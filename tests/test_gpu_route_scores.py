@@ -253,3 +253,41 @@ def test_logits_past_32_bits(ilw):
     assert torch.equal(r.expert[-500:], alone.expert) and torch.equal(r.weight[-500:], alone.weight)
     assert torch.equal(torch.bincount(r.expert.flatten(), minlength=E).cumsum(0).int(), r.offsets[1:])
     assert torch.equal(r.source[r.slot[-500:].long()], torch.arange(T - 500, T, dtype=torch.int32, device="cuda")[:, None].expand(500, 2))
+
+
+# Of a softmax that is renormalised only the taken logits count: their differences d from the largest of them are below 2^6 here and exact to
+# 2^-24 d, the exponentials off by 2 ulp, and there are a sum of k terms, a quotient and a factor.
+FAR = 2.0**6 * 2.0**-24 + (4 + 16 + 4) * 2.0**-23
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("T", [5, 300, 3000])
+@pytest.mark.parametrize("groups,top_groups", [(1, 1), (8, 3)])
+@pytest.mark.parametrize("away", [88.0, 104.0, 130.0, 3000.0, float("inf")])
+def test_softmax_of_experts_far_below_the_largest(ilw, away, groups, top_groups, T, dtype):
+    """Biases ban the experts with the largest logits (every other row: none of them has such); the weights of those taken are their softmax."""
+    rng = np.random.default_rng(T + groups)
+    E, k = 64, 6
+    x = torch.from_numpy(4 * rng.standard_normal((T, E))).to(dtype)
+    ban = torch.arange(E) % 5 == 3
+    x[::2, ban] += away
+    bias = torch.where(ban, torch.tensor([-1e6, -float("inf")])[torch.arange(E) % 2], torch.from_numpy(0.3 * rng.permutation(E)).float())
+    x, bias = x.cuda(), bias.cuda()
+    r = ilw.moe_route(x, k, True, score="softmax", bias=bias, groups=groups, top_groups=top_groups, scale=1.5)
+    assert not bool(ban.cuda()[r.expert.long()].any())
+    want = 1.5 * torch.softmax(torch.gather(x.double(), 1, r.expert.long()), 1)
+    assert bool(((r.weight.double() - want).abs() <= FAR * want + 1e-44).all())
+    if away < float("inf"):  # (the restatement takes a softmax of the row)
+        expert = ref_route(x.double().cpu().numpy(), k, False, "softmax", bias.double().cpu().numpy(), groups, top_groups)[0]
+        assert np.array_equal(r.expert.cpu().numpy(), expert)
+
+
+def test_a_taken_infinity_takes_all_the_weight(ilw):
+    """Among taken logits +inf is the limit of large ones; several share."""
+    inf = float("inf")
+    x = torch.tensor([[inf, 0.0, 1.0, 2.0], [inf, inf, 0.0, 1.0], [0.0, -150.0, -151.0, inf], [-200.0, 0.0, -200.0, -201.0]]).cuda()
+    bias = torch.tensor([0.0, 0.0, 0.0, -1e6]).cuda()
+    w = ilw.moe_route(x, 3, True, score="softmax", bias=bias).weight
+    assert w[0].tolist() == [1.0, 0.0, 0.0] and w[1].tolist() == [0.5, 0.5, 0.0] and w[2].tolist() == [1.0, 0.0, 0.0]
+    one = ilw.moe_route(torch.tensor([[0.0, -120.0]]).cuda(), 1, True, score="softmax", bias=torch.tensor([0.0, 10.0]).cuda())
+    assert one.expert.tolist() == [[1]] and one.weight.tolist() == [[1.0]]
