@@ -162,15 +162,12 @@ __device__ __noinline__ void order_exactly(const MoeScoredParams &p, const T *ro
     if (e >= 0 && place < p.k) out_e[place] = e;
 }
 
-// The groups of a token that stay, where fp32 cannot tell: `stay` by their ranks in fp32, `last` of those that stay and `next` of the others (ranks,
-// and behind them how far each may be off).  Those that lie clear of the other side keep it; the others' ranks are computed in 64 bits.
+// The groups of a token that stay, where fp32 cannot tell: `stay` by their ranks in fp32, of which the `doubtful` may have gone to the wrong side.  Those
+// clear of all of the other side keep theirs; the doubtful ranks are computed in 64 bits, and as many of them stay as did.
 template <typename T>
-__device__ __noinline__ uint32_t groups_exactly(const MoeScoredParams &p, const T *row, const float *ranks, uint32_t stay, int last, int next, int lane) {
+__device__ __noinline__ uint32_t groups_exactly(const MoeScoredParams &p, const T *row, uint32_t stay, uint32_t doubtful, int lane) {
     const RouteScores &q = p.scores;
     const Exact score = exact_scores(p, row, lane);
-    const int mine = min(lane, q.groups - 1), of = stay >> mine & 1 ? next : last;
-    const uint32_t doubtful =
-        __ballot_sync(0xffffffffu, lane < q.groups && ranks[mine] > kNone && fabsf(ranks[mine] - ranks[of]) <= 2.0f * (ranks[q.groups + mine] + ranks[q.groups + of]));
     uint64_t rank = 0;  // of group `lane`
     for (uint32_t left = doubtful; left; left &= left - 1) {
         const int g = __ffs(left) - 1;
@@ -217,6 +214,12 @@ struct Doubt {
     __device__ __forceinline__ float operator()(float c) const { return fmaf(fminf(1.0f, fabsf(c) + bias_max), unit, fmaf(fabsf(c), 1.1920929e-07f, 5.96046448e-08f)); }
 };
 
+// The lower end of a rank that may be off by `off` (anywhere, where both are infinite).
+__device__ __forceinline__ float low_end(float rank, float off) {
+    const float end = rank - off;
+    return end > kNone ? end : kNone;
+}
+
 // The two largest of n values from `at` on (16-byte aligned if n is a multiple of four).
 __device__ __forceinline__ void top2(const float *at, int n, float &t1, float &t2) {
     t1 = t2 = kNone;
@@ -236,6 +239,11 @@ __device__ __forceinline__ void top2(const float *at, int n, float &t1, float &t
 template <int L> __device__ __forceinline__ float max_of_lanes(float v) {
 #pragma unroll
     for (int d = 1; d < L; d <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
+    return v;
+}
+template <int L> __device__ __forceinline__ float min_of_lanes(float v) {
+#pragma unroll
+    for (int d = 1; d < L; d <<= 1) v = fminf(v, __shfl_xor_sync(0xffffffffu, v, d));
     return v;
 }
 template <int L> __device__ __forceinline__ float sum_of_lanes(float v) {
@@ -323,48 +331,50 @@ __device__ __forceinline__ uint32_t select_scored(const MoeScoredParams &p, cons
                 }
             }
             if (bias) off = doubt(t1) + (r.group_best == 2 && t2 > kNone ? doubt(t2) : 0.0f) + fabsf(rank) * 1.1920929e-07f;
-            ranks[g] = rank, offs[g] = off;
+            // (a sum past fp32's largest number may be any such, and a group of them is still one)
+            ranks[g] = t1 > kNone ? fmaxf(rank, -3.40282347e+38f) : kNone, offs[g] = off;
         }
         __syncwarp();
         uint32_t stay = 0;
-        int last = -1, next = -1;  // the last group that stays, the first that does not
+        // who stays, and the intervals that ranks lie in: the least end of those that stay, the greatest of the others
+        const bool inexact = bias || r.group_best == 2;  // (one logit without a bias is exact)
+        float least_in = __int_as_float(0x7f800000), most_out = kNone;
         for (int g = q; g < r.groups; g += L) {
-            const float mine = ranks[g];
+            const float mine = ranks[g], off = 2.0f * offs[g];
             int place = 0;
             for (int o = 0; o < r.groups; ++o) {
                 const float other = ranks[o];
                 place += other > mine || (other == mine && o < g);
             }
             if (mine > kNone) {
-                if (place < r.top_groups) stay |= 1u << g;
-                if (place == r.top_groups - 1) last = g;
-                if (place == r.top_groups) next = g;
+                if (place < r.top_groups) stay |= 1u << g, least_in = fminf(least_in, low_end(mine, off));
+                else most_out = fmaxf(most_out, mine + off);
             }
         }
         stay = any_of_lanes<L>(stay);
-#pragma unroll
-        for (int d = 1; d < L; d <<= 1) {
-            last = max(last, __shfl_xor_sync(0xffffffffu, last, d));
-            next = max(next, __shfl_xor_sync(0xffffffffu, next, d));
-        }
-        bool close = false;
-        if ((bias || r.group_best == 2) && last >= 0 && next >= 0) {  // who lies close to the other side's, and is not its equal, is in doubt
+        least_in = min_of_lanes<L>(least_in), most_out = max_of_lanes<L>(most_out);
+        uint32_t doubtful = 0;  // groups whose interval meets one of the other side
+        if (inexact && least_in <= most_out)
             for (int g = q; g < r.groups; g += L) {
-                const int of = stay >> g & 1 ? next : last;
-                if (ranks[g] > kNone && fabsf(ranks[g] - ranks[of]) <= 2.0f * (offs[g] + offs[of])) {
-                    float a1, a2, b1, b2;
-                    top2(row + g * r.group_size, r.group_size, a1, a2);
-                    top2(row + of * r.group_size, r.group_size, b1, b2);
-                    if (bias || a1 != b1 || (a2 != b2 && r.group_best == 2)) close = true;
-                }
+                const float mine = ranks[g], off = 2.0f * offs[g];
+                if (mine > kNone && (stay >> g & 1 ? low_end(mine, off) <= most_out : mine + off >= least_in)) doubtful |= 1u << g;
             }
+        doubtful = any_of_lanes<L>(doubtful);
+        bool close = doubtful && bias;
+        if (doubtful && !bias) {  // of the same logits they are equal, and the first of them stay
+            float a1, a2, b1, b2;
+            top2(row + (__ffs(doubtful) - 1) * r.group_size, r.group_size, a1, a2);
+            for (int g = q; g < r.groups; g += L)
+                if (doubtful >> g & 1) {
+                    top2(row + g * r.group_size, r.group_size, b1, b2);
+                    if (a1 != b1 || a2 != b2) close = true;
+                }
         }
         for (uint32_t again = __ballot_sync(0xffffffffu, any_of_lanes<L>(close) && q == 0); again; again &= again - 1) {
-            const int l = __ffs(again) - 1, lane = threadIdx.x & 31, t = l / L - lane / L;  // a token of this warp's, from this lane's
+            const int l = __ffs(again) - 1, lane = threadIdx.x & 31;
             const T *x = (const T *)__shfl_sync(0xffffffffu, (unsigned long long)logits, l);
-            const uint32_t exact = groups_exactly<T>(p, x, ranks + t * rank_words(r), __shfl_sync(0xffffffffu, stay, l),
-                                                     __shfl_sync(0xffffffffu, last, l), __shfl_sync(0xffffffffu, next, l), lane);
-            if (t == 0) stay = exact;
+            const uint32_t exact = groups_exactly<T>(p, x, __shfl_sync(0xffffffffu, stay, l), __shfl_sync(0xffffffffu, doubtful, l), lane);
+            if (l / L == lane / L) stay = exact;  // (a token of this warp's)
         }
         __syncwarp();
         for (int g = q; g < r.groups; g += L)

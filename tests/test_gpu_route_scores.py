@@ -291,3 +291,50 @@ def test_a_taken_infinity_takes_all_the_weight(ilw):
     assert w[0].tolist() == [1.0, 0.0, 0.0] and w[1].tolist() == [0.5, 0.5, 0.0] and w[2].tolist() == [1.0, 0.0, 0.0]
     one = ilw.moe_route(torch.tensor([[0.0, -120.0]]).cuda(), 1, True, score="softmax", bias=torch.tensor([0.0, 10.0]).cuda())
     assert one.expert.tolist() == [[1]] and one.weight.tolist() == [[1.0]]
+
+
+def check_groups(ilw, x, bias, k, **how):
+    """The experts of moe_route of x (a GPU tensor) are those of ref_route."""
+    got = ilw.moe_route(x, k, False, bias=bias, **how).expert.cpu().numpy()
+    want = ref_route(x.double().cpu().numpy(), k, False, bias=bias.double().cpu().numpy(), **how)[0]
+    assert np.array_equal(got, want), f"{(got != want).any(1).sum()} of {len(got)} tokens went elsewhere"
+
+
+def test_a_group_of_large_biases_between_two_others(ilw):
+    """Ranks in 64 bits: 1.24267, 1.34267, 1.24266, 1.24265, of which the first is off by some 10^-4 in fp32 and the others by 10^-6."""
+    def logits(rank):  # of two equal scores that add up to rank
+        return [float(np.log(rank / 2 / (1 - rank / 2)))] * 2
+
+    x = torch.tensor([logits(1.24267) + logits(1.34267) + logits(1.24266) + logits(1.24265)] * 40, device="cuda")
+    for B in (100.0, 1e3, 1e4, 1e6):
+        for at in range(4):  # the group of both signs
+            bias = torch.zeros(8, device="cuda")
+            bias[2 * at], bias[2 * at + 1] = B, -B
+            for top_groups in (1, 2, 3):
+                check_groups(ilw, x, bias, 2, score="sigmoid", groups=4, top_groups=top_groups, group_best=2)
+
+
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("B", [1e3, 1e6])
+@pytest.mark.parametrize("T,E,groups,top_groups", [(200, 64, 16, 6), (30000, 6, 3, 1), (20000, 16, 8, 3), (20000, 64, 32, 9)])
+def test_large_biases_that_cancel_within_groups(ilw, T, E, groups, top_groups, B, score):
+    """Some groups have biases +B and -B, so ranks that are off by hundreds of times what their neighbours' are."""
+    rng, size = np.random.default_rng(T + E), E // groups
+    bias = np.zeros(E, np.float32)
+    for g in range(0, groups, 3):
+        bias[g * size], bias[(g + 1) * size - 1] = B, -B
+        bias[g * size + 1: (g + 1) * size - 1] = -2 * B
+    x = rng.standard_normal((T, E)).astype(np.float32) * 0.3
+    check_groups(ilw, torch.from_numpy(x).cuda(), torch.from_numpy(bias).cuda(), 2, score=score, groups=groups, top_groups=top_groups, group_best=2)
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("T", [7, 400])
+def test_ranks_past_the_largest_fp32_number(ilw, T, sign):
+    """Sums of two biases that 64 bits hold and 32 do not; which are the larger is told, and a group of them is one."""
+    bias = sign * torch.tensor([3e38, 2e38, 3e38, 2.5e38, 3.1e38, 2.2e38, 1.5e38, 3.2e38], device="cuda")
+    x = torch.randn((T, 8), generator=torch.Generator("cuda").manual_seed(T), device="cuda")
+    x[T // 2:, 2] = -float("inf")
+    for top_groups in (1, 2, 3):
+        check_groups(ilw, x, bias, 2, score="sigmoid", groups=4, top_groups=top_groups, group_best=2)
+        check_groups(ilw, x, bias, 2, score="softmax", groups=4, top_groups=top_groups, group_best=1)
