@@ -68,7 +68,7 @@ constexpr int kManyLanes = 8, kManyTokens = 64, kFewLanes = 4;
 
 // Few tokens (a multiple of 32 / L, the last ones filled up): all of it by one CTA, L threads a token, as route_one_kernel.
 template <typename T, int S, int L>
-__global__ void __launch_bounds__(L == kManyLanes ? kManyLanes * kManyTokens : kFewLanes * kOneTokens) route_one_scored_kernel(const __grid_constant__ MoeScoredParams p, int wide, int tokens) {
+__global__ void __launch_bounds__(L == kManyLanes ? kManyLanes * kManyTokens : kFewLanes * kOneTokens, 1) route_one_scored_kernel(const __grid_constant__ MoeScoredParams p, int wide, int tokens) {
     extern __shared__ __align__(16) uint32_t dyn[];
     __shared__ int32_t base[kRouteMaxExperts], count[kRouteMaxExperts], all;
     __shared__ float s_bias_max;
