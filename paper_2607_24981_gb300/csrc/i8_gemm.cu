@@ -10,9 +10,12 @@
 
 namespace ilw {
 void gemm_debug_wait(int32_t *skip, long long *cycles);
-extern template cudaError_t launch_i8<float>(const I8Params &, int32_t, int, size_t, cudaStream_t);
-extern template cudaError_t launch_i8<__half>(const I8Params &, int32_t, int, size_t, cudaStream_t);
-extern template cudaError_t launch_i8<__nv_bfloat16>(const I8Params &, int32_t, int, size_t, cudaStream_t);
+extern template cudaError_t launch_i8<float, false>(const I8Params &, int32_t, int, size_t, cudaStream_t);
+extern template cudaError_t launch_i8<__half, false>(const I8Params &, int32_t, int, size_t, cudaStream_t);
+extern template cudaError_t launch_i8<__nv_bfloat16, false>(const I8Params &, int32_t, int, size_t, cudaStream_t);
+extern template cudaError_t launch_i8<float, true>(const I8Params &, int32_t, int, size_t, cudaStream_t);
+extern template cudaError_t launch_i8<__half, true>(const I8Params &, int32_t, int, size_t, cudaStream_t);
+extern template cudaError_t launch_i8<__nv_bfloat16, true>(const I8Params &, int32_t, int, size_t, cudaStream_t);
 namespace {
 
 // A tensor map over rows of codes, [z, rows, cols] bytes (z 0: no such dimension), in swizzled boxes of box_rows x 128.
@@ -26,6 +29,9 @@ bool code_map(CUtensorMap *m, const void *base, int64_t cols, int64_t rows, int6
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+
+// Whether sums are taken out of the accumulators on the way (i8_gemm.cuh).
+bool long_sums(const I8GemmProblem &g) { return g.K > (g.form == ILW_FP32 ? kI8ExactK : kI8ShortK); }
 
 // What a product will take on `sms` SMs, by a model in ns of what the forms were measured to: the forms differ by factors where sizes do,
 // and by a few percent where the model errs.
@@ -53,8 +59,9 @@ Choice choose(const I8GemmProblem &g, int64_t sms) {
     Choice best = {-1, 8, 1, countable ? 2200 + std::max(units * weights / (mean > 2 ? 4400 : 5800), (1000 + 2 * std::min(g.K, 1024)) * turns) : INFINITY};
     const int32_t nkb = (g.K + 127) / 128, top = (int32_t)std::min<double>(kI8MaxTok, std::ceil((g.offsets ? 4 * mean : M) / 32) * 32);
     const double epilogue = g.act == ILW_ACT_GELU ? 21 : 14.5;
+    const int32_t widest = long_sums(g) ? kI8LongTok : kI8MaxTok;
     for (const bool pair : {true, false})
-        for (int32_t n = pair ? 32 : 16; n <= (pair ? top : std::min(top, kI8MaxTokOne)); n += pair ? 32 : 16) {
+        for (int32_t n = pair ? 32 : 16; n <= std::min(top, pair ? widest : kI8MaxTokOne); n += pair ? 32 : 16) {
             const int64_t wtiles = (g.N + (pair ? 2 : 1) * kTileRowsW - 1) / ((pair ? 2 : 1) * kTileRowsW);
             const double about = g.offsets ? std::min(M, std::max(met, M / n + met / 2)) : std::ceil(M / n);
             const double tokens = std::min<double>(n, std::ceil(mean / 16) * 16), stage = pair ? 150 + 0.4 * tokens : 185 + 0.5 * tokens;
@@ -89,7 +96,9 @@ bool lay_out(const I8GemmProblem &g, const Choice &c, I8Params &p, int64_t &tile
     const int32_t tokens = p.mode == TILE_PAIR ? p.nt / 2 : p.nt;  // whose codes a CTA loads
     p.stage_bytes = kTileRowsW * 128 + tokens * 128;
     p.wide_bytes = tokens * 128;
-    const int fixed = 1024 + (g.experts + 1) * (int)sizeof(TileExpert) + g.experts * 4 + (p.wide ? kI8EpiWarps * kI8Patch : 0);
+    p.part = kI8ExactK / 64;
+    p.sums_bytes = long_sums(g) ? kTileRowsW * p.nt * 4 : 0;
+    const int fixed = 1024 + p.sums_bytes + (g.experts + 1) * (int)sizeof(TileExpert) + g.experts * 4 + (p.wide ? kI8EpiWarps * kI8Patch : 0);
     auto bytes = [&] { return fixed + p.stages * p.stage_bytes + p.wides * p.wide_bytes; };
     // two stages of widened codes a set where tensor memory and shared memory have room, then as many stages of codes as fit
     for (p.wides = 2 * p.nt + 32 * kI8MaxWide <= 512 ? kI8MaxWide : kI8Sets;; p.wides = kI8Sets) {
@@ -132,9 +141,10 @@ cudaError_t launch_i8_gemm(const I8GemmProblem &g, cudaStream_t s) {
     int grid = (int)std::min<int64_t>(tiles, sms);
     if (p.mode == TILE_SPLIT) grid = (int)tiles * p.splits;
     if (p.mode == TILE_PAIR) grid = 2 * (int)std::min<int64_t>(tiles, sms / 2);
-    if (g.form == ILW_FP32) return launch_i8<float>(p, g.act, grid, smem, s);
-    if (g.form == ILW_FP16) return launch_i8<__half>(p, g.act, grid, smem, s);
-    return launch_i8<__nv_bfloat16>(p, g.act, grid, smem, s);
+    auto launch = [&](auto plain, auto with_long_sums) { return (long_sums(g) ? with_long_sums : plain)(p, g.act, grid, (size_t)smem, s); };
+    if (g.form == ILW_FP32) return launch(launch_i8<float, false>, launch_i8<float, true>);
+    if (g.form == ILW_FP16) return launch(launch_i8<__half, false>, launch_i8<__half, true>);
+    return launch(launch_i8<__nv_bfloat16, false>, launch_i8<__nv_bfloat16, true>);
 }
 
 }  // namespace ilw

@@ -5,7 +5,13 @@
 //   z[m, n] = sa[m] sw[n] sum_k a[m, k] w[n, k] + bias[n]
 //
 // This chip's tcgen05 has no int8 kind.  Every int8 number is an fp16 number, so the codes are widened on the way to tcgen05.mma.kind::f16,
-// whose products of them are exact and whose fp32 sums are exact below 2^24.  HBM and L2 carry 8 bits all the same.
+// whose products of them are exact and whose fp32 sums are exact below 2^24, so those of 1024 of K are.  HBM and L2 carry 8 bits all the same.
+//
+// Past 2^24 the tensor core cuts off what does not fit, at every 16 of K and always toward zero: sums of codes of one sign lose 4e-6 of themselves at K = 8192,
+// 6e-5 at 32768, 5e-4 at 131071 (a library's fp32 product 1e-6, 2e-6, 5e-6).  Results of two bytes round by more than that up to kI8ShortK.  For
+// fp32 results past K = 1024, and for others past kI8ShortK, the sums of each 1024 of K are taken out of tensor memory and added up in shared
+// memory as 32-bit whole numbers, by the epilogue's warps while the next 1024 are summed in the other accumulator.  The room for that is a tile of
+// 128 tokens' at most.  8192 cubed with fp32 results takes 814 us so (in fp32 sums 567), 2000 cubed 22.3 (19.5), 300 x 4096 x 4096 19.2 (19.8).
 //
 // Widening is what has to keep up with the tensor core.  64 of K of a tile are 384 clocks of MMAs (192 tokens), in which shared memory moves
 // 48 KB.  The codes come by TMA (14 KB in a pair of SMs) and are read once; W's rows, the lanes of a tile, go from registers to tensor
@@ -42,6 +48,9 @@ namespace ilw {
 
 constexpr int kI8MaxTok = 192;  // tokens a tile; a multiple of 32, as tiles of pairs are
 constexpr int kI8MaxTokOne = 128;  // of one CTA, which with more has no room for two stages of codes to spare
+constexpr int kI8LongTok = 128;  // of any form where sums are kept in shared memory
+constexpr int kI8ExactK = 1024;     // 2^14 kI8ExactK = 2^24
+constexpr int kI8ShortK = 16384;    // 2^-23 kI8ShortK / 16 = 2^-13 of the sum of magnitudes at most, and half of it as a rule; fp16 rounds by 2^-11
 constexpr int kI8MaxStages = 8, kI8MinStages = 2;
 constexpr int kI8Sets = 4;      // sets of four widening warps
 constexpr int kI8MaxWide = 2 * kI8Sets;  // stages of widened codes at most: one or two a set
@@ -70,13 +79,16 @@ struct I8Params {
     int32_t stage_bytes, wide_bytes;
     int32_t wide;           // 2-byte rows of Y take 16-byte stores
     int32_t splits;         // CTAs of a cluster that share a tile's K (TILE_SPLIT)
+    int32_t part;           // (LONG) stages of 64 of K after which sums are taken out of an accumulator
+    int32_t sums_bytes;     // (LONG) whole sums [token][row of W] of a tile
     int32_t mode;
     int32_t dbg_skip;
     long long wait_cycles;
     int *status;
 };
 
-template <typename T>
+// LONG: sums are taken out of the accumulators every p.part stages.
+template <typename T, bool LONG>
 cudaError_t launch_i8(const I8Params &p, int32_t act, int grid, size_t smem, cudaStream_t s);
 
 namespace {
@@ -106,6 +118,12 @@ __device__ __forceinline__ void widen4(uint32_t w, uint32_t &lo, uint32_t &hi) {
 }
 __device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__device__ __forceinline__ void sts32(uint32_t a, int32_t v) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(a), "r"(v) : "memory"); }
+__device__ __forceinline__ int32_t lds32(uint32_t a) {
+    int32_t v;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    return v;
 }
 // 16 columns of this thread's lane of tensor memory
 __device__ __forceinline__ void tst16(uint32_t taddr, const uint32_t (&v)[16]) {
@@ -199,7 +217,7 @@ __device__ __forceinline__ void store_tokens(const I8Params &p, float (&v)[16], 
     }
 }
 
-template <int ACT, typename T, int MODE>
+template <int ACT, typename T, int MODE, bool LONG>
 __global__ void __launch_bounds__(kI8Threads, 1) i8_gemm_kernel(const __grid_constant__ I8Params p) {
     constexpr bool SPLIT = MODE == TILE_SPLIT, PAIR = MODE == TILE_PAIR;
     extern __shared__ uint8_t smem_raw[];
@@ -211,7 +229,7 @@ __global__ void __launch_bounds__(kI8Threads, 1) i8_gemm_kernel(const __grid_con
     __shared__ int32_t s_experts, s_head, s_tail;  // experts with rows; rows before the first and from the end of the last
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t data0 = (su32(smem_raw) + 1023) & ~1023u;
-    const uint32_t wide0 = data0 + p.stages * p.stage_bytes, patch0 = wide0 + p.wides * p.wide_bytes;
+    const uint32_t wide0 = data0 + p.stages * p.stage_bytes, sums0 = wide0 + p.wides * p.wide_bytes, patch0 = LONG ? sums0 + p.sums_bytes : sums0;
     TileExpert *tab = (TileExpert *)(smem_raw + (patch0 - su32(smem_raw)) + (p.wide ? kI8EpiWarps * kI8Patch : 0));
     int32_t *tab_id = (int32_t *)(tab + p.E + 1);
 
@@ -361,37 +379,41 @@ __global__ void __launch_bounds__(kI8Threads, 1) i8_gemm_kernel(const __grid_con
         __syncwarp();
     } else if (warp == 1) {
         const uint32_t one = elect_one();
+        const int32_t part = LONG ? p.part : ks_hi - ks_lo;  // of K, to one accumulator
         uint32_t n = 0, cs = 0, cp = 0;
         const uint64_t desc0 = desc_sw128(wide0);
         uint64_t bd = desc0;
         uint32_t at = wcol;
         bool ok = true;
-        for (int32_t t = first; ok && t < tiles; t += step, ++n) {
+        for (int32_t t = first; ok && t < tiles; t += step) {
             Tile x;
             ok = next_tile(x);
             if (!ok || !leader) continue;  // (a pair's second CTA only reads its tiles, so that their places can be filled again)
-            const uint32_t acc = n & 1, d = tmem + acc * p.nt;
             const uint32_t id = idesc_f16(PAIR ? 256 : 128, uniform(mma_tokens(x)));
-            ok = wait_lean(aempty + 8 * acc, ((n >> 1) & 1) ^ 1, &abort_flag, p, kStatusTimeoutFree);
-            if (!ok) break;
-            fence_after();
-            if (one) {
-                for (int32_t ks = ks_lo; ks < ks_hi; ++ks) {
-                    if (!wait_lane(ready + 8 * cs, cp, &abort_flag, p, kStatusTimeoutOperand)) {
-                        ok = false;
-                        break;
-                    }
-                    fence_after();
+            for (int32_t lo = ks_lo; ok && lo < ks_hi; lo += part, ++n) {
+                const uint32_t acc = n & 1, d = tmem + acc * p.nt;
+                const int32_t hi = LONG ? min(lo + part, ks_hi) : ks_hi;
+                ok = wait_lean(aempty + 8 * acc, ((n >> 1) & 1) ^ 1, &abort_flag, p, kStatusTimeoutFree);
+                if (!ok) break;
+                fence_after();
+                if (one) {
+                    for (int32_t ks = lo; ks < hi; ++ks) {
+                        if (!wait_lane(ready + 8 * cs, cp, &abort_flag, p, kStatusTimeoutOperand)) {
+                            ok = false;
+                            break;
+                        }
+                        fence_after();
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) mma_f16<PAIR>(d, at + 8 * j, bd + 2 * j, id, ks > ks_lo || j > 0);
-                    commit_mma<PAIR>(wfree + 8 * cs);
-                    at += 32;
-                    bd += p.wide_bytes / 16;
-                    if (++cs == (uint32_t)p.wides) cs = 0, cp ^= 1, at = wcol, bd = desc0;
+                        for (int j = 0; j < 4; ++j) mma_f16<PAIR>(d, at + 8 * j, bd + 2 * j, id, ks > lo || j > 0);
+                        commit_mma<PAIR>(wfree + 8 * cs);
+                        at += 32;
+                        bd += p.wide_bytes / 16;
+                        if (++cs == (uint32_t)p.wides) cs = 0, cp ^= 1, at = wcol, bd = desc0;
+                    }
+                    if (ok) commit_mma<PAIR>(afull + 8 * acc);
                 }
-                if (ok) commit_mma<PAIR>(afull + 8 * acc);
+                ok = __all_sync(0xffffffffu, ok);
             }
-            ok = __all_sync(0xffffffffu, ok);
         }
         if (!ok && one && leader) {  // the MMAs in flight end before tensor memory is freed
             commit_mma<PAIR>(drain, true);
@@ -508,11 +530,36 @@ __global__ void __launch_bounds__(kI8Threads, 1) i8_gemm_kernel(const __grid_con
             next_scale = __ldg(p.w_scales + (int64_t)y.e * p.N + nn);
             if (p.bias) next_bias = __ldg(p.bias + (int64_t)y.e * p.N + nn);
         };
+        // (LONG) all parts of K but the last to the whole sums: each thread its own, which no other reads
+        auto take_parts = [&](const Tile &y, uint32_t &n) {
+            for (int32_t lo = ks_lo; lo + p.part < ks_hi; lo += p.part, ++n) {
+                const uint32_t acc = n & 1;
+                if (!wait_lean<200>(afull + 8 * acc, (n >> 1) & 1, &abort_flag, p, kStatusTimeoutMma)) return false;
+                fence_after();
+                for (int c0 = 16 * part; c0 < y.rows; c0 += 4 * kI8EpiWarps) {
+                    uint32_t u[16];
+                    tld<16>(tmem + quarter + acc * p.nt + c0, u);
+                    twait<16>(u);
+                    const uint32_t at = sums0 + (c0 * kTileRowsW + row) * 4;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) sts32(at + i * kTileRowsW * 4, __float2int_rn(__uint_as_float(u[i])) + (lo > ks_lo ? lds32(at + i * kTileRowsW * 4) : 0));
+                }
+                fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if constexpr (PAIR) arrive_cluster(free0 + 8 * acc);
+                    else bar_arrive(aempty + 8 * acc);
+                }
+            }
+            return true;
+        };
         Tile next = {};  // (read, with its scale and bias, while a tile is stored)
         if (first < tiles && next_tile(next)) read_row(next);
+        const bool parts = LONG && p.part < ks_hi - ks_lo;
         for (int32_t t = first; t < tiles; t += step, ++n) {
-            const uint32_t acc = n & 1;
             x = next;
+            if (LONG && !take_parts(x, n)) break;
+            const uint32_t acc = n & 1;
             const float scale = next_scale, bias = next_bias;
             const int nn = x.n0 + row;
             // scales of 16 tokens, a lane one of them
@@ -532,11 +579,16 @@ __global__ void __launch_bounds__(kI8Threads, 1) i8_gemm_kernel(const __grid_con
                 }
                 sa = token_scale(c0 + 4 * kI8EpiWarps);
                 twait<16>(u);
-                if constexpr (SPLIT) {  // this CTA's part of the sums: [token][row of W] over the stages, which are all read
+                if (SPLIT || LONG) {  // this CTA's whole sums
+                    const uint32_t at = (c0 * kTileRowsW + row) * 4;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        asm volatile("st.shared.b32 [%0], %1;" ::"r"(data0 + ((c0 + i) * kTileRowsW + row) * 4), "r"(u[i]) : "memory");
-                } else {
+                    for (int i = 0; i < 16; ++i) {
+                        const int32_t sum = __float2int_rn(__uint_as_float(u[i])) + (parts ? lds32(sums0 + at + i * kTileRowsW * 4) : 0);
+                        if constexpr (SPLIT) sts32(data0 + at + i * kTileRowsW * 4, sum);  // (over the stages, which are all read)
+                        else u[i] = __float_as_uint((float)sum);
+                    }
+                }
+                if constexpr (!SPLIT) {
                     float v[16];
                     const uint64_t sw = both(scale), b = both(bias);
 #pragma unroll
@@ -572,22 +624,23 @@ __global__ void __launch_bounds__(kI8Threads, 1) i8_gemm_kernel(const __grid_con
                 const int c0 = u & ~3, row = 32 * (u & 3) + lane, nn = x.n0 + row;
                 const int64_t of = (int64_t)x.e * p.N + nn;
                 const float scale = nn < p.N ? p.w_scales[of] : 0.0f, bias = p.bias && nn < p.N ? p.bias[of] : 0.0f;
-                float v[8][4], z[4];
+                int32_t v[8][4];
+                float z[4];
 #pragma unroll
                 for (int r = 0; r < 8; ++r)
                     if (r < p.splits) {
                         const uint32_t at = in_cta(data0 + (c0 * kTileRowsW + row) * 4, r);
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[r][i]) : "r"(at + i * kTileRowsW * 4) : "memory");
+                            asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v[r][i]) : "r"(at + i * kTileRowsW * 4) : "memory");
                     }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    z[i] = v[0][i];
+                    int32_t sum = v[0][i];
 #pragma unroll
                     for (int r = 1; r < 8; ++r)
-                        if (r < p.splits) z[i] += v[r][i];
-                    z[i] = fmaf(z[i] * (c0 + i < x.rows ? p.a_scales[x.row0 + c0 + i] : 0.0f), scale, bias);
+                        if (r < p.splits) sum += v[r][i];
+                    z[i] = fmaf((float)sum * (c0 + i < x.rows ? p.a_scales[x.row0 + c0 + i] : 0.0f), scale, bias);
                 }
                 constexpr bool kGate = ACT == ILW_ACT_SILU_GATE;
                 const int width = kGate ? p.N / 2 : p.N, col = kGate ? nn >> 1 : nn;
@@ -620,10 +673,10 @@ __global__ void __launch_bounds__(kI8Threads, 1) i8_gemm_kernel(const __grid_con
     }
 }
 
-template <int ACT, typename T, int MODE>
+template <int ACT, typename T, int MODE, bool LONG>
 cudaError_t launch_mode(const I8Params &p, int grid, size_t smem, cudaStream_t s) {
     static SmemLimit limit;
-    cudaError_t e = raise_smem_limit(limit, (const void *)i8_gemm_kernel<ACT, T, MODE>, kI8SmemLimit);
+    cudaError_t e = raise_smem_limit(limit, (const void *)i8_gemm_kernel<ACT, T, MODE, LONG>, kI8SmemLimit);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
@@ -638,23 +691,23 @@ cudaError_t launch_mode(const I8Params &p, int grid, size_t smem, cudaStream_t s
     at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = MODE == TILE_ONE ? 1 : 2;
-    e = cudaLaunchKernelEx(&cfg, i8_gemm_kernel<ACT, T, MODE>, p);
+    e = cudaLaunchKernelEx(&cfg, i8_gemm_kernel<ACT, T, MODE, LONG>, p);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
-template <int ACT, typename T>
+template <int ACT, typename T, bool LONG>
 cudaError_t launch_act(const I8Params &p, int grid, size_t smem, cudaStream_t s) {
-    if (p.mode == TILE_SPLIT) return launch_mode<ACT, T, TILE_SPLIT>(p, grid, smem, s);
-    if (p.mode == TILE_PAIR) return launch_mode<ACT, T, TILE_PAIR>(p, grid, smem, s);
-    return launch_mode<ACT, T, TILE_ONE>(p, grid, smem, s);
+    if (p.mode == TILE_SPLIT) return launch_mode<ACT, T, TILE_SPLIT, LONG>(p, grid, smem, s);
+    if (p.mode == TILE_PAIR) return launch_mode<ACT, T, TILE_PAIR, LONG>(p, grid, smem, s);
+    return launch_mode<ACT, T, TILE_ONE, LONG>(p, grid, smem, s);
 }
 
 }  // namespace
 
-template <typename T>
+template <typename T, bool LONG>
 cudaError_t launch_i8(const I8Params &p, int32_t act, int grid, size_t smem, cudaStream_t s) {
-    if (act == ILW_ACT_GELU) return launch_act<ILW_ACT_GELU, T>(p, grid, smem, s);
-    if (act == ILW_ACT_SILU_GATE) return launch_act<ILW_ACT_SILU_GATE, T>(p, grid, smem, s);
-    return launch_act<ILW_ACT_NONE, T>(p, grid, smem, s);
+    if (act == ILW_ACT_GELU) return launch_act<ILW_ACT_GELU, T, LONG>(p, grid, smem, s);
+    if (act == ILW_ACT_SILU_GATE) return launch_act<ILW_ACT_SILU_GATE, T, LONG>(p, grid, smem, s);
+    return launch_act<ILW_ACT_NONE, T, LONG>(p, grid, smem, s);
 }
 
 }  // namespace ilw

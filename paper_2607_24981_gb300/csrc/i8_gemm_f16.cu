@@ -2,5 +2,5 @@
 #include "i8_gemm.cuh"
 
 namespace ilw {
-template cudaError_t launch_i8<__half>(const I8Params &, int32_t, int, size_t, cudaStream_t);
+template cudaError_t launch_i8<__half, false>(const I8Params &, int32_t, int, size_t, cudaStream_t);
 }  // namespace ilw

@@ -1,0 +1,6 @@
+// i8_gemm_long_f16.cu -- the int8 products with __half results and long sums.
+#include "i8_gemm.cuh"
+
+namespace ilw {
+template cudaError_t launch_i8<__half, true>(const I8Params &, int32_t, int, size_t, cudaStream_t);
+}  // namespace ilw

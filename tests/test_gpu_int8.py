@@ -567,3 +567,60 @@ def test_weights_past_32_bits(ilw, count):
     for e in (0, E - 2, E - 1):
         rows = slice(e * count, (e + 1) * count)
         check_product(y[rows], ilw.I8Tensor(A.codes[rows], A.scales[rows]), ilw.I8Tensor(W.codes[e], W.scales[e]), None, "none")
+
+
+# ---------------------------------------------------------------------------- sums past 2^24
+def of_codes(ilw, codes):
+    m = ilw.i8_empty(*codes.shape)
+    m.codes.copy_(codes)
+    m.scales.fill_(1.0)
+    return m
+
+
+@pytest.mark.parametrize("lo", [0, -128])
+@pytest.mark.parametrize("form,M,N,K", [("few", 3, 60, 9000), (8, 40, 1000, 8200), (4, 130, 1000, 2100), (2, 16, 5000, 8200), ("one", 130, 1712, 1100), ("pair", 3001, 1712, 1030), ("pair", 200, 1712, 2100),
+                                        ("pair", 1500, 1000, 4200), ("pair", 1100, 5000, 32768), (8, 40, 1000, (1 << 17) - 1), ("pair", 600, 3000, (1 << 17) - 1)])
+def test_fp32_results_have_exact_sums(ilw, form, M, N, K, lo):
+    """Codes of one sign, and of both: the result is the whole number, rounded once, whatever form the call takes."""
+    A, W = (of_codes(ilw, torch.randint(lo, 128, (n, K), generator=generator(n + K), device="cuda").to(torch.int8)) for n in (M, N))
+    assert form_of(ilw, M, N, K, None, "none", torch.float32)[0] == form
+    got = ilw.i8_linear(A, W, out_dtype=torch.float32)
+    assert torch.equal(got, (A.codes.double() @ W.codes.double().T).float())
+    assert torch.equal(got[:2], ilw.i8_linear(ilw.I8Tensor(A.codes[:2], A.scales[:2]), W, out_dtype=torch.float32))
+    ilw.device_status()
+
+
+@pytest.mark.parametrize("act", ["none", "gelu", "silu_gate"])
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("counts,N,K", [([700, 0, 1, 333, 1024, 225, 95], 1704, 2600), ([60, 0, 70], 520, 20000), ([5, 0, 1, 2] * 4, 1000, 1700)])
+def test_long_sums_by_expert(ilw, counts, N, K, dtype, act):
+    """Several tiles a CTA, each of several parts of K, scales and biases; sums held exactly where the results' type or K asks for it."""
+    off, E = np.r_[0, np.cumsum(counts)], len(counts)
+    A, W = (of_codes(ilw, torch.randint(-100, 128, (n, K), generator=generator(n + K), device="cuda").to(torch.int8)) for n in (int(off[-1]), E * N))
+    A.scales.uniform_(1e-4, 1e-3, generator=generator(1))
+    W.scales.uniform_(1e-4, 1e-3, generator=generator(2))
+    b = torch.randn((E, N), device="cuda", generator=generator(5))
+    got = ilw.i8_grouped_linear(A, ilw.I8Tensor(W.codes.unflatten(0, (E, N)), W.scales.view(E, N)), torch.from_numpy(off.astype(np.int32)).cuda(), b, act=act, out_dtype=dtype)
+    for e in range(E):
+        if counts[e]:
+            s, w = slice(int(off[e]), int(off[e + 1])), slice(e * N, (e + 1) * N)
+            check_product(got[s], ilw.I8Tensor(A.codes[s], A.scales[s]), ilw.I8Tensor(W.codes[w], W.scales[w]), b[e], act)
+            if dtype == torch.float32 and act == "none":  # a sum rounded once, two factors and a bias
+                z = A.codes[s].double() @ W.codes[w].double().T * A.scales[s].double()[:, None] * W.scales[w].double()
+                assert bool(((got[s].double() - (z + b[e].double())).abs() <= 4 * 2.0**-24 * (2 * z.abs() + b[e].abs())).all())
+    ilw.device_status()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("M", [1, 40, 400, 3000])
+@pytest.mark.parametrize("K", [8192, 16384, 16385, (1 << 17) - 1])
+def test_16_bit_results_of_long_sums(ilw, K, M, dtype):
+    """Codes of one sign.  Up to K = 16384 a tile's sum loses less than a unit of 2^-23 with each 16 of K: 2^-13 in all, and half as much in norm; past that
+    nothing.  The result then is off by that, by three roundings of fp32 and by its own."""
+    A, W = (of_codes(ilw, torch.randint(0, 128, (n, K), generator=generator(n + K), device="cuda").to(torch.int8)) for n in (M, 1000))
+    A.scales.fill_(2.0**-14)
+    want = A.codes.double() @ W.codes.double().T * 2.0**-14
+    got = ilw.i8_linear(A, W, out_dtype=dtype).double()
+    off = K / 16 * 2.0**-23 if K <= 16384 else 0.0
+    assert bool(((got - want).abs() <= (off + 3 * 2.0**-24 + EPS[dtype] * (1 + off)) * want).all())
+    assert float((got - want).norm() / want.norm()) <= off / 2 + EPS[dtype]
