@@ -45,6 +45,12 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
+// sum sa sw + bias of a whole sum, with two roundings: sw first, unless it is above 1.  Then no step overflows, or falls below the normal numbers, where the result
+// does not: |sum| >= 1, so sum sw lies between the normal sw and |sum| <= 2^31, and a sum sa that overflows does so before it grows.
+__device__ __forceinline__ float scaled_sum(float sum, float sa, float sw, float bias) {
+    const bool small = fabsf(sw) <= 1.0f;
+    return fmaf(sum * (small ? sw : sa), small ? sa : sw, bias);
+}
 // z (1 + erf(z / sqrt 2)) / 2 of two values.  With c = |z| / 2 it is z/2 + |z/2| - c erfc(sqrt 2 c), and log2 erfc(sqrt 2 c) is close to a
 // polynomial: this one, of degree 10 without a constant and in -c, was fitted to leave c erfc(sqrt 2 c) an error of at most 1.6e-10 (minimax over
 // c <= 2.9; past that it falls on, and so does the product).  One operation of the special-function unit a value.  Error in fp32:

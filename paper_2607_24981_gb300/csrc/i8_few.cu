@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(32 * kWarps, kCtas) i8_few_kernel(const __grid
             float z = 0.0f;
             if (in) {
                 const int64_t at = (int64_t)x.e * p.N + n;
-                z = fmaf((float)v * p.a_scales[x.row0 + t], p.w_scales[at], p.bias ? p.bias[at] : 0.0f);
+                z = scaled_sum((float)v, p.a_scales[x.row0 + t], p.w_scales[at], p.bias ? p.bias[at] : 0.0f);
             }
             if constexpr (ACT == ILW_ACT_GELU) {
                 float none = 0.0f;

@@ -624,3 +624,34 @@ def test_16_bit_results_of_long_sums(ilw, K, M, dtype):
     off = K / 16 * 2.0**-23 if K <= 16384 else 0.0
     assert bool(((got - want).abs() <= (off + 3 * 2.0**-24 + EPS[dtype] * (1 + off)) * want).all())
     assert float((got - want).norm() / want.norm()) <= off / 2 + EPS[dtype]
+
+
+# ---------------------------------------------------------------------------- scales
+@pytest.mark.parametrize("form,M,N,K", [("few", 12, 40, 256), (4, 130, 1000, 2100), ("one", 130, 1712, 500), ("pair", 700, 1000, 1030)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_scales_of_every_size_meet(ilw, form, M, N, K, dtype):
+    """Neither a large scale of a token nor one of a channel overflows, or a small one loses bits, where the result fits; a scale of 0
+    leaves the bias."""
+    assert form_of(ilw, M, N, K, None, "none", dtype)[0] == form
+    A, W = (of_codes(ilw, torch.randint(-127, 128, (n, K), generator=generator(n), device="cuda").to(torch.int8)) for n in (M, N))
+    sizes = torch.tensor([1.0, 1e36, 2.6e36, 1e30, 1e-30, 2.0**-126, 0.0, 1e10, 1e-10, 3.0])
+    A.scales.copy_(sizes.repeat(M // 10 + 1)[:M])
+    W.scales.copy_(sizes.repeat_interleave(4).repeat(N // 40 + 1)[:N])
+    b = torch.randn(N, device="cuda", generator=generator(5))
+    got = ilw.i8_linear(A, W, b, out_dtype=dtype)
+    sums = A.codes.double() @ W.codes.double().T
+    z = sums * A.scales.double()[:, None] * W.scales.double()
+    want = z + b.double()
+    # (a sum past 2^24 cannot be here; a product of two factors has two roundings, the bias one, the result one; below fp32's normal range they are of
+    # its smallest step; whatever comes within those roundings of the largest number may round past it)
+    lost = torch.where(sums.abs() >= 2.0**24, torch.inf, 0.0)
+    assert not bool(lost.any())
+    top = torch.finfo(dtype).max
+    tol = 4 * 2.0**-24 * (2 * z.abs() + b.abs()) + EPS[dtype] * want.abs() + 1e-44
+    inside, outside = want.abs() < top * (1 - 2.0**-7), want.abs() > top * (1 + 2.0**-7)
+    assert bool(((got.double() - want).abs() <= tol)[inside].all())
+    assert bool((got[outside] == torch.sign(want[outside]) * torch.inf).all()) and bool(outside.any()) and not bool(got.isnan().any())
+    zero = A.scales == 0
+    assert torch.equal(got[zero], b.to(dtype).expand(int(zero.sum()), N))
+    assert torch.equal(got[:, W.scales == 0], b[W.scales == 0].to(dtype).expand(M, int((W.scales == 0).sum())))
+    ilw.device_status()
