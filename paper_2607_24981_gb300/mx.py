@@ -157,10 +157,13 @@ class MxExperts:
 
     ``w1`` [E, F1, d] and ``w2`` [E, d, F] are float CUDA tensors, quantised here once; with ``act`` "silu_gate" F1 = 2 F and
     the rows of w1 alternate (gate_rows), else F1 = F.  Biases are float32 [E, F1] (gated: gate_rows with dim=1) and [E, d].
-    ``routing`` goes to moe_route: score, bias, groups and so on."""
+    What follows ``renormalize`` is as in moe_route, which refuses here what it would refuse in forward."""
 
-    def __init__(self, w1, w2, top: int, act="silu_gate", b1=None, b2=None, renormalize=True, **routing):
-        self.top, self.act, self.b1, self.b2, self.renormalize, self.routing = top, act, b1, b2, renormalize, routing
+    def __init__(self, w1, w2, top: int, act="silu_gate", b1=None, b2=None, renormalize=True, *, score="softmax", bias=None, groups=1,
+                 top_groups=None, group_best=2, scale=1.0):
+        self.top, self.act, self.b1, self.b2, self.renormalize = top, act, b1, b2, renormalize
+        self.routing = dict(score=score, bias=bias, groups=groups, top_groups=top_groups, group_best=group_best, scale=scale)
+        moe_route(w1.new_empty((0, w1.shape[0])), top, renormalize, **self.routing)  # (of no tokens: its checks)
         self.w1, self.w2 = self.pack(w1), self.pack(w2)
         if w1.shape[0] != w2.shape[0] or w2.shape[2] * (2 if act == "silu_gate" else 1) != w1.shape[1] or w1.shape[2] != w2.shape[1]:
             raise IlwError(f"{type(self).__name__}: w1 {tuple(w1.shape)} and w2 {tuple(w2.shape)} do not follow one another")

@@ -655,3 +655,18 @@ def test_scales_of_every_size_meet(ilw, form, M, N, K, dtype):
     assert torch.equal(got[zero], b.to(dtype).expand(int(zero.sum()), N))
     assert torch.equal(got[:, W.scales == 0], b[W.scales == 0].to(dtype).expand(M, int((W.scales == 0).sum())))
     ilw.device_status()
+
+
+@pytest.mark.parametrize("kind", ["MxExperts", "I8Experts"])
+def test_experts_refuse_their_routing_at_once(ilw, kind):
+    """What moe_route would refuse is refused with the weights, not in the first forward."""
+    E, d, F = 8, 64, 96
+    w1, w2 = torch.randn((E, 2 * F, d), generator=generator(1), device="cuda"), torch.randn((E, d, F), generator=generator(2), device="cuda")
+    make = getattr(ilw, kind)
+    for how in (dict(top=9), dict(top=2, bias=torch.zeros(7, device="cuda")), dict(top=2, bias=torch.zeros(8, dtype=torch.float16, device="cuda")), dict(top=2, groups=3),
+                dict(top=2, score="tanh"), dict(top=5, groups=2, top_groups=1), dict(top=2, groups=4, top_groups=5), dict(top=2, scale=float("nan")),
+                dict(top=2, groups=4, top_groups=2, group_best=3)):
+        with pytest.raises(ilw.IlwError):
+            make(w1, w2, **how)
+    x, logits = torch.randn((50, d), generator=generator(3), device="cuda"), torch.randn((50, E), generator=generator(4), device="cuda")
+    assert torch.equal(make(w1, w2, 2).forward(x, logits), make(w1, w2, 2, scale=1.0, groups=2, top_groups=2, score="softmax").forward(x, logits))

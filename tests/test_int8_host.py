@@ -207,3 +207,14 @@ def test_routing_arguments_past_32_bits_are_refused():
         ilw.moe_route(x, 2, score="sigmoid", scale="much")
     with pytest.raises(OverflowError):
         ilw.moe_route(x, 2, score="sigmoid", groups=1 << 70)
+
+
+def test_experts_refuse_unknown_arguments_at_once():
+    pytest.importorskip("torch")
+    import paper_2607_24981_gb300 as ilw
+
+    for experts in (ilw.MxExperts, ilw.I8Experts):
+        with pytest.raises(TypeError, match="renormalise"):
+            experts(None, None, 2, renormalise=False)
+        with pytest.raises(TypeError):
+            experts(None, None, 2, "silu_gate", None, None, True, "sigmoid")
