@@ -670,3 +670,39 @@ def test_experts_refuse_their_routing_at_once(ilw, kind):
             make(w1, w2, **how)
     x, logits = torch.randn((50, d), generator=generator(3), device="cuda"), torch.randn((50, E), generator=generator(4), device="cuda")
     assert torch.equal(make(w1, w2, 2).forward(x, logits), make(w1, w2, 2, scale=1.0, groups=2, top_groups=2, score="softmax").forward(x, logits))
+
+
+def test_offsets_at_the_ends_of_32_bits(ilw):
+    """Whatever the offsets say, nothing outside the result is written, and ranges in order have their products."""
+    A, W = made(ilw, 1, 600, 64), made(ilw, 3, 4 * 34, 64, weights=True)
+    W = ilw.I8Tensor(W.codes.unflatten(0, (4, 34)), W.scales.view(4, 34))
+    top, low = (1 << 31) - 1, -(1 << 31)
+    for offsets in ([0, top, low, 600, 600], [low, low, top, top, top], [top, top, top, top, top], [low, 0, 300, 600, top], [low, top, low, top, low]):
+        wide = torch.full((620, 34), 7.0, device="cuda")
+        ilw.i8_grouped_linear(A, W, torch.tensor(offsets, dtype=torch.int32, device="cuda"), out=wide[10:610])
+        assert bool((wide[:10] == 7).all()) and bool((wide[610:] == 7).all())
+        if offsets == [low, 0, 300, 600, top]:
+            for e in (1, 2):
+                s = slice(300 * (e - 1), 300 * e)
+                check_product(wide[10:610][s], ilw.I8Tensor(A.codes[s], A.scales[s]), ilw.I8Tensor(W.codes[e], W.scales[e]), None, "none")
+    ilw.device_status()
+
+
+def test_weights_past_32_bits_by_form(ilw):
+    """The last of experts with more than 2^31 codes: by the kernel for few tokens, and by tiles."""
+    E, N, K = 36, 8200, 8192
+    x = torch.empty((E * N, K), dtype=torch.bfloat16, device="cuda").normal_(generator=generator(1))
+    q = ilw.i8_quantize(x)
+    del x
+    W = ilw.I8Tensor(q.codes.unflatten(0, (E, N)), q.scales.view(E, N))
+    for form, counts in (("few", {0: 1, E - 2: 1, E - 1: 2}), ("pair", {0: 9, 7: 30, E - 2: 70, E - 1: 33})):
+        off = np.r_[0, np.cumsum([counts.get(e, 0) for e in range(E)])]
+        M = int(off[-1])
+        for dtype in (torch.float32, torch.bfloat16):
+            assert form_of(ilw, M, N, K, E, "none", dtype)[0] == form
+            A = made(ilw, 3, M, K)
+            y = ilw.i8_grouped_linear(A, W, torch.from_numpy(off.astype(np.int32)).cuda(), out_dtype=dtype)
+            for e in counts:
+                s = slice(int(off[e]), int(off[e + 1]))
+                check_product(y[s], ilw.I8Tensor(A.codes[s], A.scales[s]), ilw.I8Tensor(W.codes[e], W.scales[e]), None, "none")
+    ilw.device_status()
