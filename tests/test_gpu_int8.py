@@ -706,3 +706,22 @@ def test_weights_past_32_bits_by_form(ilw):
                 s = slice(int(off[e]), int(off[e + 1]))
                 check_product(y[s], ilw.I8Tensor(A.codes[s], A.scales[s]), ilw.I8Tensor(W.codes[e], W.scales[e]), None, "none")
     ilw.device_status()
+
+
+@pytest.mark.parametrize("form,M,N,K,skipped", [("one", 130, 1712, 1100, 0), (8, 40, 1000, 8200, 0), (2, 16, 5000, 8200, 0), (2, 16, 5000, 8200, 9), ("pair", 3001, 1712, 2600, 0),
+                                                ("pair", 3001, 1712, 2600, 9), ("pair", 3001, 1712, 2600, 30)])
+def test_long_sums_give_up_a_bounded_wait(ilw, form, M, N, K, skipped):
+    """As test_every_form_gives_up_a_bounded_wait, where sums are taken out of tensor memory on the way: a load of the first 1024 of K, of the next
+    ones, of the second tile."""
+    assert form_of(ilw, M, N, K, None, "none", torch.float32)[0] == form
+    A, W = made(ilw, 1, M, K), made(ilw, 3, N, K, weights=True)
+    want = ilw.i8_linear(A, W, out_dtype=torch.float32)
+    assert ilw.lib().ilwdetr_debug_gemm_wait(skipped, 20_000_000) == 0
+    try:
+        ilw.i8_linear(A, W, out_dtype=torch.float32)
+        with pytest.raises(ilw.IlwError, match="wait"):
+            ilw.device_status()
+    finally:
+        assert ilw.lib().ilwdetr_debug_gemm_wait(-1, 0) == 0
+    assert torch.equal(ilw.i8_linear(A, W, out_dtype=torch.float32), want)
+    ilw.device_status()
