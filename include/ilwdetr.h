@@ -550,10 +550,10 @@ int ilwdetr_i8_dequantize(const int8_t *codes, int64_t ldc, const float *scales,
  *   a_scales fp32 [M], w_scales fp32 [experts, N], bias fp32 [experts, N] or NULL; all device
  *   w_codes_stride  bytes between experts (a multiple of 16; ignored for one expert without offsets)
  *   offsets, y_form, Y, ldy, act   as in ilw_mx_gemm_t
- * Products are exact.  Sums are exact too, 32-bit whole numbers, but for 2-byte results of 1024 < K <= 16384: these may be held in
- * fp32 where they pass 2^24 and then be short of the exact sum by up to K / 16 2^-23 (2^-13 at most) of the sum of magnitudes, a fourth of
- * an fp16 rounding, in some calls (few tokens) and not in others.  Scaling (which overflows only where the result does), bias and
- * activation in fp32, the result is rounded once.  1 <= experts <= 1024, K < 2^17, N <= 2^24, M < 2^31 - 1024, (M / 32 + experts) N / 128 < 2^31 - 4096. */
+ * Products are exact.  Sums are exact too, 32-bit whole numbers, but for 2-byte results of 1024 < K <= 16384 and more than a few tokens: those
+ * may be held in fp32 where they pass 2^24 and then be short by up to K / 16 2^-23 (2^-13 at most) of the sum of magnitudes, a fourth of an
+ * fp16 rounding.  Scaling (which overflows only where the result does), bias and activation in fp32, the result is
+ * rounded once.  1 <= experts <= 1024, K < 2^17, N <= 2^24, M < 2^31 - 1024, (M / 32 + experts) N / 128 < 2^31 - 4096. */
 typedef struct {
     uint32_t struct_size;
     const int8_t *a_codes; int64_t a_ldc;
